@@ -1,7 +1,9 @@
-"""MI355X-native expert-parallel MoE token dispatch and combine (one rank's share).
+"""MI355X-native expert-parallel MoE token dispatch and combine (one rank's share), with the
+layer's operators around them.
 
 The work happens in libep.so (HIP kernels for gfx950 plus SDMA host legs; C ABI in
-include/ep.h).  ``paper_2609_40093_amd.api`` is its Python binding; the names below are
+include/ep.h and include/ep_layer.h).  ``paper_2609_40093_amd.api`` is the Python binding of
+the first, ``paper_2609_40093_amd.layer`` of the second; the names below are
 re-exported lazily so that ``paper_2609_40093_amd.synth`` (input generation only) can be
 imported without torch or a GPU.
 """
@@ -13,7 +15,10 @@ _API = ("EPError", "Layout", "Staging", "SimPeers", "dispatch_layout", "layout_v
         "combine_rows", "Dense", "allgather", "reducescatter", "round_advance", "round_read", "dispatch_graph",
         "combine_graph", "graph_legs_sdma")
 
-__all__ = list(_API)
+_LAYER = ("Norm", "rmsnorm", "rmsnorm_grad", "rows8_empty", "rows8_values", "Routing", "route", "route_grad",
+          "combine_grad", "Product", "expert_product", "ProductGrad", "expert_product_grad")
+
+__all__ = list(_API + _LAYER)
 
 
 def __getattr__(name):
@@ -21,5 +26,10 @@ def __getattr__(name):
         from . import api
         value = getattr(api, name)
         globals()[name] = value  # later lookups skip this function
+        return value
+    if name in _LAYER:
+        from . import layer
+        value = getattr(layer, name)
+        globals()[name] = value
         return value
     raise AttributeError(name)

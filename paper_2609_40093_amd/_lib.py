@@ -1,4 +1,4 @@
-"""ctypes declarations of libep.so (include/ep.h and include/ep_sim.h).
+"""ctypes declarations of libep.so (include/ep.h, include/ep_sim.h and include/ep_layer.h).
 
 Loading fails loudly when the library has not been built: there is no fallback path.
 """
@@ -17,8 +17,11 @@ EP_SIM_FLAGS_ONLY, EP_SIM_ECHO = 0, 1
 EP_MODE_PER_SENDER, EP_MODE_DUPLEX, EP_MODE_REMOTE_ONLY, EP_MODE_ACCUMULATE = 1, 2, 4, 8
 ABI_VERSION = 6
 EP_MAX_EXPERTS = 2048
+EP_ROWS_BF16, EP_ROWS_8BIT, EP_ROWS8_EXTRA = 0, 1, 16
+EP_ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "swiglu": 4}
 
 c_i32, c_i64, c_u32, c_size, c_vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_size_t, ctypes.c_void_p
+c_f32 = ctypes.c_float
 c_i32p = ctypes.POINTER(ctypes.c_int32)
 
 
@@ -88,6 +91,22 @@ SIGNATURES = {
                                          c_size, c_vp]),
     "ep_pack": (c_i32, [c_vp, c_i64, c_i32, c_i32, c_vp, c_vp, c_i64, c_vp]),
     "ep_combine_rows": (c_i32, [c_vp, c_i64, c_vp, c_vp, c_i64, c_i32, c_i32, c_vp, c_i32, c_vp]),
+    "ep_rmsnorm": (c_i32, [c_vp, c_vp, c_vp, c_i64, c_i32, c_f32, c_vp, c_vp, c_vp, c_vp]),
+    "ep_rmsnorm_grad_workspace_bytes": (c_i32, [c_i64, c_i32, ctypes.POINTER(c_size)]),
+    "ep_rmsnorm_grad": (c_i32, [c_vp, c_vp, c_vp, c_vp, c_i64, c_i32, c_f32, c_vp, c_vp, c_vp, c_size, c_vp]),
+    "ep_route_workspace_bytes": (c_i32, [c_i64, c_i32, ctypes.POINTER(c_size)]),
+    "ep_route": (c_i32, [c_vp, c_i32, c_vp, c_i64, c_i32, c_i32, c_i32, c_f32, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp,
+                         c_size, c_vp]),
+    "ep_route_grad": (c_i32, [c_vp, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, c_i64, c_i32, c_i32, c_i32, c_f32, c_vp,
+                              c_vp]),
+    "ep_combine_grad": (c_i32, [c_vp, c_vp, c_i64, c_vp, c_vp, c_i64, c_i32, c_i32, c_vp, c_vp, c_vp]),
+    "ep_expert_product_workspace_bytes": (c_i32, [c_i64, c_i32, c_i32, c_i32, c_i32, c_i32, ctypes.POINTER(c_size)]),
+    "ep_expert_product": (c_i32, [c_vp, c_i32, c_i64, c_vp, c_i32, c_vp, c_vp, c_i32, c_i32, c_vp, c_i32, c_vp, c_vp,
+                                  c_vp, c_i32, c_vp, c_size, c_vp]),
+    "ep_expert_product_grad_workspace_bytes": (c_i32, [c_i64, c_i32, c_i32, c_i32, c_i32, c_i32,
+                                                       ctypes.POINTER(c_size)]),
+    "ep_expert_product_grad": (c_i32, [c_vp, c_i64, c_vp, c_i32, c_vp, c_i32, c_i32, c_i32, c_vp, c_vp, c_vp, c_vp,
+                                       c_vp, c_vp, c_size, c_vp]),
     "ep_trace_enable": (c_i32, [c_i32]),
     "ep_trace_read": (c_i32, [ctypes.POINTER(TraceStat), c_i32, ctypes.POINTER(c_i32)]),
     "ep_trace_reset": (c_i32, []),

@@ -1,0 +1,362 @@
+// norm.hip -- RMS norm of the residual stream, forward and backward.
+//
+//   forward   s = x + r;  y = s * rstd * w, rstd = 1 / sqrt(mean(s^2) + eps)
+//   backward  g = d_out * w;  n = s * rstd;  dx = rstd * (g - n mean(g n)) + d_total;
+//             d_weight = sum over tokens of d_out * n
+//
+// Both are HBM-bound: every row is read once and held in registers between its reduction and
+// its results.  The forward reduces sum(s^2) and max|s w| in the same step: the row's largest
+// |y| is max|s w| rstd, so the 8-bit rows need no second reduction; the backward likewise
+// reduces sum(s^2) and sum(g s) together.
+#include "layer.h"
+
+namespace ep {
+namespace {
+
+constexpr float kLeastMax = 0x1p-100f;  // a row's max|y| counts as at least this: its scale stays normal
+constexpr float kF8Max = 448.f;
+
+// Row geometry: WAVES waves hold one row, V vectors of 8 elements per lane; workgroups of
+// 256 threads hold 4 / WAVES rows for WAVES < 4.
+template <int WAVES>
+constexpr int block_threads() {
+    return WAVES < 4 ? 256 : WAVES * 64;
+}
+
+// 1 / sqrt(mean(s^2) + eps) of a row from ss = sum(s^2).  Where the squares leave fp32's range
+// (values above 2^60, or below 2^-40 with next to no eps), the row's sum is taken again of its
+// values times a power of two; `again(f)` gives sum((f s)^2) over the row.  The condition is
+// the same in every lane of a row, and no row of ordinary values takes the branch.
+template <typename F>
+__device__ __forceinline__ float inverse_rms(float ss, int H, float eps, F again) {
+    const bool large = ss > 0x1p120f, small = ss < 0x1p-80f && eps < 0x1p-80f;
+    if (large || small) {
+        const float f = large ? 0x1p-64f : 0x1p64f;
+        return f / sqrtf(again(f) / (float)H + eps * f * f);
+    }
+    return 1.f / sqrtf(ss / (float)H + eps);
+}
+
+// Sum over the waves of a row; every wave of the workgroup calls it.
+template <int WAVES>
+__device__ __forceinline__ float row_sum(float v, float *slot, int tid) {
+    v = wave_sum(v);
+    if (WAVES > 1) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0)
+            slot[tid / 64] = v;
+        __syncthreads();
+        v = 0.f;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i)
+            v += slot[i];
+    }
+    return v;
+}
+
+template <int WAVES, int V>
+__global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_kernel(NormArgs a) {
+    constexpr int kRows = block_threads<WAVES>() / (WAVES * 64);
+    const int tid = (int)threadIdx.x % (WAVES * 64), sub = (int)threadIdx.x / (WAVES * 64);
+    const int vecs = a.H / 8;
+    __shared__ float red[2][WAVES][2], redo[WAVES];
+    u32x4 wv[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int i = v * (WAVES * 64) + tid;
+        wv[v] = u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+        if (a.weight && i < vecs)
+            wv[v] = a.weight[i];
+    }
+    int parity = 0;
+    for (int64_t row = (int64_t)blockIdx.x * kRows + sub; row < a.T; row += (int64_t)gridDim.x * kRows) {
+        const int64_t base = row * vecs;
+        float s[V][8];
+        float ss = 0.f;
+        uint32_t top = 0;  // bits of max|s w|: a NaN's are above every number's
+        u32x4 xv[V], rv[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int i = v * (WAVES * 64) + tid;
+            xv[v] = rv[v] = u32x4{0, 0, 0, 0};
+            if (i < vecs) {
+                xv[v] = a.x[base + i];
+                if (a.residual)
+                    rv[v] = a.residual[base + i];
+            }
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            unpack8(xv[v], s[v]);
+            if (a.residual) {
+                float r[8];
+                unpack8(rv[v], r);
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    s[v][q] += r[q];
+            }
+            float w[8];
+            unpack8(wv[v], w);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                ss = fmaf(s[v][q], s[v][q], ss);
+                const uint32_t m = __float_as_uint(s[v][q] * w[q]) & 0x7fffffffu;
+                top = m > top ? m : top;
+            }
+        }
+        ss = wave_sum(ss);
+        top = wave_max(top);
+        if (WAVES > 1) {
+            if ((threadIdx.x & 63) == 0) {
+                red[parity][tid / 64][0] = ss;
+                red[parity][tid / 64][1] = __uint_as_float(top);
+            }
+            __syncthreads();
+            ss = 0.f;
+            top = 0;
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i) {
+                ss += red[parity][i][0];
+                const uint32_t m = __float_as_uint(red[parity][i][1]);
+                top = m > top ? m : top;
+            }
+            parity ^= 1;  // the next row writes the other half: one barrier per row
+        }
+        const float rstd = inverse_rms(ss, a.H, a.eps, [&](float f) {
+            float q2 = 0.f;
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    q2 = fmaf(s[v][q] * f, s[v][q] * f, q2);
+            return row_sum<WAVES>(q2, redo, tid);
+        });
+        const float most = __uint_as_float(top) * rstd;
+        const float scale = (most < kLeastMax ? kLeastMax : most) / kF8Max;  // a NaN stays one
+        const float inv = 1.f / scale;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int i = v * (WAVES * 64) + tid;
+            if (i >= vecs)
+                continue;
+            if (a.total)
+                a.total[base + i] = pack8(s[v]);
+            float w[8], y[8];
+            unpack8(wv[v], w);
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                y[q] = s[v][q] * rstd * w[q];
+            if (a.out)
+                a.out[base + i] = pack8(y);
+            if (a.rows8) {
+                uint32_t b[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    int p = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * h] * inv, y[4 * h + 1] * inv, 0, false);
+                    b[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * h + 2] * inv, y[4 * h + 3] * inv, p, true);
+                }
+                uint8_t *dst = a.rows8 + row * (a.H + 16);
+                reinterpret_cast<uint2 *>(dst)[i] = uint2{b[0], b[1]};
+            }
+        }
+        if (a.rows8 && tid == 0)
+            *reinterpret_cast<u32x4 *>(a.rows8 + row * (a.H + 16) + a.H) = u32x4{__float_as_uint(scale), 0, 0, 0};
+    }
+}
+
+template <int WAVES, int V>
+__global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_grad_kernel(NormGradArgs a) {
+    constexpr int kRows = block_threads<WAVES>() / (WAVES * 64);
+    const int tid = (int)threadIdx.x % (WAVES * 64), sub = (int)threadIdx.x / (WAVES * 64);
+    const int vecs = a.H / 8;
+    __shared__ float red[2][WAVES][2], redo[WAVES];
+    u32x4 wv[V];
+    float dw[V][8];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int i = v * (WAVES * 64) + tid;
+        wv[v] = u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+        if (a.weight && i < vecs)
+            wv[v] = a.weight[i];
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            dw[v][q] = 0.f;
+    }
+    int parity = 0;
+    for (int64_t row = (int64_t)blockIdx.x * kRows + sub; row < a.T; row += (int64_t)gridDim.x * kRows) {
+        const int64_t base = row * vecs;
+        u32x4 sv[V], dv[V], tv[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int i = v * (WAVES * 64) + tid;
+            sv[v] = dv[v] = tv[v] = u32x4{0, 0, 0, 0};
+            if (i < vecs) {
+                sv[v] = a.total[base + i];
+                dv[v] = a.d_out[base + i];
+                if (a.d_total)
+                    tv[v] = a.d_total[base + i];
+            }
+        }
+        float ss = 0.f, gs = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            float s[8], d[8], w[8];
+            unpack8(sv[v], s);
+            unpack8(dv[v], d);
+            unpack8(wv[v], w);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                ss = fmaf(s[q], s[q], ss);
+                gs = fmaf(d[q] * w[q], s[q], gs);
+            }
+        }
+        ss = wave_sum(ss);
+        gs = wave_sum(gs);
+        if (WAVES > 1) {
+            if ((threadIdx.x & 63) == 0) {
+                red[parity][tid / 64][0] = ss;
+                red[parity][tid / 64][1] = gs;
+            }
+            __syncthreads();
+            ss = gs = 0.f;
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i) {
+                ss += red[parity][i][0];
+                gs += red[parity][i][1];
+            }
+            parity ^= 1;
+        }
+        const float rstd = inverse_rms(ss, a.H, a.eps, [&](float f) {
+            float q2 = 0.f;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                float s[8];
+                unpack8(sv[v], s);
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    q2 = fmaf(s[q] * f, s[q] * f, q2);
+            }
+            return row_sum<WAVES>(q2, redo, tid);
+        });
+        const float c = gs * rstd / (float)a.H;  // mean(g n)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int i = v * (WAVES * 64) + tid;
+            if (i >= vecs)
+                continue;
+            float s[8], d[8], w[8], t[8];
+            unpack8(sv[v], s);
+            unpack8(dv[v], d);
+            unpack8(wv[v], w);
+            unpack8(tv[v], t);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const float n = s[q] * rstd;
+                dw[v][q] = fmaf(d[q], n, dw[v][q]);
+                t[q] = fmaf(rstd, d[q] * w[q] - n * c, t[q]);
+            }
+            a.dx[base + i] = pack8(t);
+        }
+    }
+    if (!a.d_weight)
+        return;
+    // one partial row per row slot of the grid, added up in a fixed order
+    float *dst = a.partial + ((int64_t)blockIdx.x * kRows + sub) * a.H;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int i = v * (WAVES * 64) + tid;
+        if (i < vecs) {
+            reinterpret_cast<float4 *>(dst)[2 * i] = float4{dw[v][0], dw[v][1], dw[v][2], dw[v][3]};
+            reinterpret_cast<float4 *>(dst)[2 * i + 1] = float4{dw[v][4], dw[v][5], dw[v][6], dw[v][7]};
+        }
+    }
+}
+
+// d_weight[h] = sum over the partial rows: 16 columns and 16 row lanes per workgroup.
+__global__ __launch_bounds__(256) void column_sum_kernel(const float *partial, int64_t rows, int32_t H, float *out) {
+    const int c = threadIdx.x & 15, lane = threadIdx.x >> 4;
+    const int64_t h = (int64_t)blockIdx.x * 16 + c;
+    float s = 0.f;
+    if (h < H)
+        for (int64_t r = lane; r < rows; r += 16)
+            s += partial[r * H + h];
+    __shared__ float part[16][17];
+    part[lane][c] = s;
+    __syncthreads();
+    if (lane == 0 && h < H) {
+        s = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            s += part[i][c];
+        out[h] = s;
+    }
+}
+
+// Waves of a row and vectors per lane.
+struct RowGeom {
+    int waves, vecs;
+};
+RowGeom row_geometry(int32_t H) {
+    if (H <= 2048)
+        return {1, H <= 512 ? 1 : H <= 1024 ? 2 : 4};
+    if (H <= 8192)
+        return {4, H <= 4096 ? 2 : 4};
+    return {16, H <= 16384 ? 2 : H <= 32768 ? 4 : 8};
+}
+
+#define EP_ROW_GEOMETRY(g, CALL)                                      \
+    do {                                                              \
+        if (g.waves == 1)                                             \
+            return g.vecs == 1 ? CALL(1, 1) : g.vecs == 2 ? CALL(1, 2) : CALL(1, 4); \
+        if (g.waves == 4)                                             \
+            return g.vecs == 2 ? CALL(4, 2) : CALL(4, 4);             \
+        return g.vecs == 2 ? CALL(16, 2) : g.vecs == 4 ? CALL(16, 4) : CALL(16, 8); \
+    } while (0)
+
+int64_t row_groups(int64_t T, int waves, int64_t most) {
+    const int rows = waves < 4 ? 4 / waves : 1;
+    return std::min<int64_t>((T + rows - 1) / rows, most);
+}
+
+hipError_t launch_grad_rows(const NormGradArgs &a, int64_t groups, hipStream_t stream) {
+    const RowGeom g = row_geometry(a.H);
+#define EP_CALL(W, V) \
+    launch_traced("rmsnorm_grad", rmsnorm_grad_kernel<W, V>, dim3((unsigned)groups), block_threads<W>(), stream, a)
+    EP_ROW_GEOMETRY(g, EP_CALL);
+#undef EP_CALL
+}
+
+}  // namespace
+
+hipError_t launch_rmsnorm(const NormArgs &a, hipStream_t stream) {
+    if (a.T == 0)
+        return hipSuccess;
+    const RowGeom g = row_geometry(a.H);
+    const dim3 grid((unsigned)row_groups(a.T, g.waves, kCus * 32));
+#define EP_CALL(W, V) launch_traced("rmsnorm", rmsnorm_kernel<W, V>, grid, block_threads<W>(), stream, a)
+    EP_ROW_GEOMETRY(g, EP_CALL);
+#undef EP_CALL
+}
+
+// Partial rows of the weight gradient: one per row slot of the grid.
+int64_t rmsnorm_grad_groups(int64_t T, int32_t H) {
+    const RowGeom g = row_geometry(H);
+    const int rows = g.waves < 4 ? 4 / g.waves : 1;
+    return row_groups(T, g.waves, kCus * 2) * rows;
+}
+
+hipError_t launch_rmsnorm_grad(const NormGradArgs &a, hipStream_t stream) {
+    const RowGeom g = row_geometry(a.H);
+    const int64_t partials = a.T ? rmsnorm_grad_groups(a.T, a.H) : 0;
+    if (a.T) {
+        const hipError_t e = launch_grad_rows(a, partials / (g.waves < 4 ? 4 / g.waves : 1), stream);
+        if (e != hipSuccess || !a.d_weight)
+            return e;
+    }
+    if (!a.d_weight)
+        return hipSuccess;
+    return launch_traced("rmsnorm_grad_weight", column_sum_kernel, dim3((unsigned)((a.H + 15) / 16)), 256, stream,
+                         (const float *)a.partial, partials, a.H, a.d_weight);
+}
+
+}  // namespace ep

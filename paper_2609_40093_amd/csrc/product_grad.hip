@@ -1,0 +1,243 @@
+// product_grad.hip -- gradients of the experts' product y = act(x W_e^T + b_e):
+//   dz = d_y act'(pre);  dx = dz W_e;  dw_e = dz^T x;  db_e = column sums of dz.
+//
+// Three kernels: dz and the bias's column sums element by element (HBM-bound; left out where
+// dz is d_y itself and no bias is wanted), then two matrix products on the tile of
+// product_tile.h.  Neither needs a transposed copy: W in dx, and dz and x in dw, are read
+// across the contraction by the transposing LDS load.
+#include "product_tile.h"
+
+namespace ep {
+namespace {
+
+constexpr int kDzRows = 64;   // rows of one dz tile: one expert's, 4 waves of 16 rows
+constexpr int kDzCols = 512;  // columns: 64 lanes of 8
+
+// dz (null: not stored) and the column sums of each row tile (partial, null: not wanted).
+template <bool GATED>
+__global__ __launch_bounds__(256) void product_dz_kernel(const int32_t *offsets, int64_t rows, int32_t E, int32_t N,
+                                                         int32_t act, const uint16_t *pre, const uint16_t *d_y,
+                                                         uint16_t *dz, float *partial) {
+    constexpr int kParts = GATED ? 2 : 1;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const RowTile rt = find_row_tile(offsets, rows, E, kDzRows, (int32_t)blockIdx.x, lane);
+    if (rt.e < 0)
+        return;
+    const int32_t Nw = N * kParts;
+    const int32_t n = (int32_t)blockIdx.y * kDzCols + lane * 8;
+    float sum[kParts][8] = {};
+    if (n < N) {
+        for (int i = wave; i < rt.n; i += 4) {
+            const int64_t r = rt.row0 + i;
+            float d[8], z[kParts][8];
+            unpack8(*reinterpret_cast<const u32x4 *>(d_y + r * N + n), d);
+            if (pre)
+#pragma unroll
+                for (int p = 0; p < kParts; ++p)
+                    unpack8(*reinterpret_cast<const u32x4 *>(pre + r * Nw + p * N + n), z[p]);
+            float o[kParts][8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                if (GATED) {
+                    o[0][q] = d[q] * z[kParts - 1][q] * activation_grad(z[0][q], EP_ACT_SILU);
+                    o[kParts - 1][q] = d[q] * activation(z[0][q], EP_ACT_SILU);
+                } else {
+                    o[0][q] = pre ? d[q] * activation_grad(z[0][q], act) : d[q];
+                }
+#pragma unroll
+                for (int p = 0; p < kParts; ++p)
+                    sum[p][q] += o[p][q];
+            }
+            if (dz)
+#pragma unroll
+                for (int p = 0; p < kParts; ++p)
+                    *reinterpret_cast<u32x4 *>(dz + r * Nw + p * N + n) = pack8(o[p]);
+        }
+    }
+    if (!partial)
+        return;
+    __shared__ float part[4][64][9];
+#pragma unroll
+    for (int p = 0; p < kParts; ++p) {
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            part[wave][lane][q] = sum[p][q];
+        __syncthreads();
+        if (wave == 0 && n < N)
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                partial[(int64_t)blockIdx.x * Nw + p * N + n + q] =
+                    part[0][lane][q] + part[1][lane][q] + part[2][lane][q] + part[3][lane][q];
+    }
+}
+
+// dbias[e][n] = sum over the expert's row tiles, in order.
+__global__ __launch_bounds__(256) void product_dbias_kernel(const int32_t *offsets, int64_t rows, int32_t E, int32_t Nw,
+                                                            const float *partial, float *dbias) {
+    const int lane = threadIdx.x & 63, e = blockIdx.y;
+    const int64_t first = count_row_tiles(offsets, rows, e, kDzRows, lane);
+    int64_t b, t;
+    expert_rows(offsets, rows, e, b, t);
+    const int64_t tiles = (t - b + kDzRows - 1) / kDzRows;
+    const int32_t n = (int32_t)blockIdx.x * 256 + threadIdx.x;
+    if (n >= Nw)
+        return;
+    float s = 0.f;
+    for (int64_t i = 0; i < tiles; ++i)
+        s += partial[(first + i) * Nw + n];
+    dbias[(int64_t)e * Nw + n] = s;
+}
+
+struct GradTileArgs {
+    const int32_t *offsets;
+    int64_t rows;
+    int32_t E, K, Nw;
+    const uint16_t *x, *w, *dz;
+    uint16_t *out;
+};
+
+// dx[r][k] = sum_n dz[r][n] W_e[n][k]: i = k across the contraction, j = rows along it.
+template <class S>
+__global__ __launch_bounds__(S::kThreads) void product_dx_kernel(GradTileArgs a, int32_t col_tiles) {
+    __shared__ __attribute__((aligned(1024))) char lds[2 * S::kStageBytes];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int32_t row_tiles = count_row_tiles(a.offsets, a.rows, a.E, S::kJ, lane);
+    const int64_t t = tile_of_block(blockIdx.x, (int64_t)row_tiles * col_tiles);
+    if (t < 0)
+        return;
+    int32_t tr, tc;
+    tile_order(t, row_tiles, col_tiles, tr, tc);
+    const RowTile rt = find_row_tile(a.offsets, a.rows, a.E, S::kJ, tr, lane);
+    const int32_t k0 = tc * S::kI;
+    AcrossC<S::kI, S::kWaves> w;
+    AlongC<S::kJ, S::kWaves> z;
+    w.init(reinterpret_cast<const char *>(a.w + (int64_t)rt.e * a.Nw * a.K), (int64_t)a.K * 2, a.Nw, k0, wave, lane);
+    const int64_t zs = (int64_t)a.Nw * 2;
+    z.init(reinterpret_cast<const char *>(a.dz) + rt.row0 * zs, (uint32_t)(rt.n * zs), (int32_t)zs, wave, lane,
+           [&](int row) -> uint32_t { return (uint32_t)(row * zs); });
+    f32x4 acc[S::FI][S::FJ] = {};
+    const int64_t steps = (a.Nw + kStepRows - 1) / kStepRows;
+    tile_product<S, Mul::kBf16>(w, z, steps, steps, (char EP_LDS *)lds, wave, lane, acc);
+    const int wi = wave % S::kWavesI, wj = wave / S::kWavesI;
+#pragma unroll
+    for (int j = 0; j < S::FJ; ++j) {
+        const int row = (wj * S::FJ + j) * 16 + lane % 16;
+#pragma unroll
+        for (int i = 0; i < S::FI; ++i) {
+            const int32_t k = k0 + (wi * S::FI + i) * 16 + lane / 16 * 4;
+            if (row < rt.n && k < a.K)
+                *reinterpret_cast<uint2 *>(a.out + (rt.row0 + row) * a.K + k) =
+                    uint2{bf16_pair(acc[i][j][0], acc[i][j][1]), bf16_pair(acc[i][j][2], acc[i][j][3])};
+        }
+    }
+}
+
+// dw_e[n][k] = sum_r dz[r][n] x[r][k]: both operands across the contraction.
+template <class S>
+__global__ __launch_bounds__(S::kThreads) void product_dw_kernel(GradTileArgs a, int32_t n_tiles, int32_t k_tiles) {
+    __shared__ __attribute__((aligned(1024))) char lds[2 * S::kStageBytes];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t per_expert = (int64_t)n_tiles * k_tiles;
+    const int64_t t = tile_of_block(blockIdx.x, per_expert * a.E);
+    if (t < 0)
+        return;
+    const int e = (int)(t / per_expert);
+    int32_t tn, tk;
+    tile_order(t - e * per_expert, n_tiles, k_tiles, tn, tk);
+    int64_t b, end;
+    expert_rows(a.offsets, a.rows, e, b, end);
+    const int32_t k0 = tk * S::kI, n0 = tn * S::kJ;
+    AcrossC<S::kI, S::kWaves> x;
+    AcrossC<S::kJ, S::kWaves> z;
+    x.init(reinterpret_cast<const char *>(a.x + b * a.K), (int64_t)a.K * 2, end - b, k0, wave, lane);
+    z.init(reinterpret_cast<const char *>(a.dz + b * a.Nw), (int64_t)a.Nw * 2, end - b, n0, wave, lane);
+    f32x4 acc[S::FI][S::FJ] = {};
+    const int64_t steps = (end - b + kStepRows - 1) / kStepRows;
+    tile_product<S, Mul::kBf16>(x, z, steps, steps, (char EP_LDS *)lds, wave, lane, acc);
+    const int wi = wave % S::kWavesI, wj = wave / S::kWavesI;
+#pragma unroll
+    for (int j = 0; j < S::FJ; ++j) {
+        const int32_t n = n0 + (wj * S::FJ + j) * 16 + lane % 16;
+#pragma unroll
+        for (int i = 0; i < S::FI; ++i) {
+            const int32_t k = k0 + (wi * S::FI + i) * 16 + lane / 16 * 4;
+            if (n < a.Nw && k < a.K)
+                *reinterpret_cast<uint2 *>(a.out + ((int64_t)e * a.Nw + n) * a.K + k) =
+                    uint2{bf16_pair(acc[i][j][0], acc[i][j][1]), bf16_pair(acc[i][j][2], acc[i][j][3])};
+        }
+    }
+}
+
+typedef TileShape<256, 256, 4, 2> Large;
+typedef TileShape<128, 128, 2, 2> Medium;
+
+template <class S>
+hipError_t launch_dx(const GradTileArgs &a, hipStream_t stream) {
+    const int32_t cols = (a.K + S::kI - 1) / S::kI;
+    const int64_t tiles = row_tiles_most(a.rows, a.E, S::kJ) * cols;
+    if (tiles > kMostTiles)
+        return hipErrorInvalidConfiguration;
+    return launch_traced("expert_product_dx", product_dx_kernel<S>, dim3((unsigned)(tiles + 8)), S::kThreads, stream, a,
+                         cols);
+}
+template <class S>
+hipError_t launch_dw(const GradTileArgs &a, hipStream_t stream) {
+    const int32_t kt = (a.K + S::kI - 1) / S::kI, nt = (a.Nw + S::kJ - 1) / S::kJ;
+    if ((int64_t)kt * nt * a.E > kMostTiles)
+        return hipErrorInvalidConfiguration;
+    return launch_traced("expert_product_dw", product_dw_kernel<S>, dim3((unsigned)((int64_t)kt * nt * a.E + 8)),
+                         S::kThreads, stream, a, nt, kt);
+}
+
+size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+}  // namespace
+
+// dz [rows][Nw] bf16 (with an activation), then the bias's partial sums [row tiles][Nw] fp32.
+size_t product_grad_workspace_bytes(int64_t rows, int32_t E, int32_t, int32_t N, int32_t act, bool bias) {
+    const int64_t Nw = act == EP_ACT_SWIGLU ? 2 * (int64_t)N : N;
+    const size_t dz = act == EP_ACT_NONE ? 0 : align256((size_t)(rows * Nw * 2));
+    return dz + (bias ? (size_t)(row_tiles_most(rows, E, kDzRows) * Nw * 4) : 0);
+}
+
+hipError_t launch_product_grad(const ProductGradArgs &a, hipStream_t stream) {
+    uint16_t *own_dz = a.act == EP_ACT_NONE ? nullptr : static_cast<uint16_t *>(a.workspace);
+    float *partial = nullptr;
+    if (a.dbias)
+        partial = reinterpret_cast<float *>(static_cast<char *>(a.workspace) +
+                                            (own_dz ? align256((size_t)(a.rows * a.Nw * 2)) : 0));
+    if (a.rows > 0 && (own_dz || partial)) {
+        const dim3 grid((unsigned)row_tiles_most(a.rows, a.E, kDzRows), (unsigned)((a.N + kDzCols - 1) / kDzCols));
+        uint16_t *dz = a.dx || a.dw ? own_dz : nullptr;
+#define EP_CALL(GATED)                                                                                              \
+    launch_traced("expert_product_dz", product_dz_kernel<GATED>, grid, 256, stream, a.offsets, a.rows, a.E, a.N, a.act, \
+                  (const uint16_t *)(own_dz ? a.pre : nullptr), (const uint16_t *)a.d_y, dz, partial)
+        const hipError_t e = a.act == EP_ACT_SWIGLU ? EP_CALL(true) : EP_CALL(false);
+#undef EP_CALL
+        if (e != hipSuccess)
+            return e;
+    }
+    if (a.dbias) {
+        const hipError_t e = launch_traced("expert_product_dbias", product_dbias_kernel,
+                                           dim3((unsigned)((a.Nw + 255) / 256), (unsigned)a.E), 256, stream, a.offsets,
+                                           a.rows, a.E, a.Nw, (const float *)partial, a.dbias);
+        if (e != hipSuccess)
+            return e;
+    }
+    GradTileArgs g{a.offsets, a.rows, a.E, a.K, a.Nw, (const uint16_t *)a.x, (const uint16_t *)a.w,
+                   own_dz ? own_dz : (const uint16_t *)a.d_y, nullptr};
+    if (a.dx && a.rows > 0) {
+        g.out = static_cast<uint16_t *>(a.dx);
+        const hipError_t e = a.rows / a.E >= 192 ? launch_dx<Large>(g, stream) : launch_dx<Medium>(g, stream);
+        if (e != hipSuccess)
+            return e;
+    }
+    if (a.dw) {
+        g.out = static_cast<uint16_t *>(a.dw);
+        return a.K >= 512 && a.Nw >= 512 ? launch_dw<Large>(g, stream) : launch_dw<Medium>(g, stream);
+    }
+    return hipSuccess;
+}
+
+}  // namespace ep

@@ -1,0 +1,163 @@
+"""The RMS norm and its gradient against plain implementations in 64 bits.
+
+Bounds, derived from the kernel's arithmetic (fp32): s = x + r has one rounding; the sum of
+squares adds at most 128 terms per lane and 22 partial sums, all positive, so it is within
+2^-16 of itself; with the root, the division and the products y is within 2^-15 of itself
+before its rounding to bf16 (half a step, at most 2^-8 of the value) or e4m3 (half a step, at
+most 2^-4 of the value, or 2^-10 scales below e4m3's smallest normal number).  The gradient's
+terms carry the same 2^-14; the weight's gradient adds T terms one after the other at most.
+"""
+import pytest
+import torch
+
+import layer_ref as ref
+import paper_2609_40093_amd as ep
+from gpu_cases import say
+
+pytestmark = pytest.mark.gpu
+
+# one row length or more for every row geometry, at its ends, and lengths that fill no lane evenly
+LENGTHS = [8, 16, 72, 512, 520, 1024, 1032, 2048, 2056, 2888, 4096, 4104, 7168, 8192, 8200, 16384, 16400, 32768, 40008, 65536]
+
+
+def check(x, r, w, eps, want8=True):
+    T, H = x.shape
+    want8 = want8 and H % 16 == 0
+    got = ep.rmsnorm(x, w, residual=r, eps=eps, total=True, out=True, rows8=want8)
+    s, y = ref.norm(x, r, w, eps)
+    ref.within(got.total, s, s.abs() * ref.BF16, "total")
+    ref.within(got.out, y, y.abs() * (ref.BF16 + 2.0 ** -15), "out")
+    if want8:
+        q, scale = ep.rows8_values(got.rows8)
+        top = y.abs().amax(1, keepdim=True).clamp_min(2.0 ** -100) / 448
+        ref.within(scale, top, top * 2.0 ** -14, "scale")
+        ref.within(q.float().double() * scale.double(), y, torch.maximum(y.abs() * 2.0 ** -4, top * 2.0 ** -10) * (1 + 2.0 ** -8),
+                   "rows8")
+        assert not got.rows8[:, H + 4:].any()
+    return got
+
+
+@pytest.mark.parametrize("H", LENGTHS)
+@pytest.mark.parametrize("T", [1, 3, 37])
+def test_norm(T, H):
+    say(f"rmsnorm T={T} H={H}")
+    g = ref.gen(T * 100003 + H)
+    check(ref.normal((T, H), g), ref.normal((T, H), g, 2.0), ref.normal(H, g), 1e-6)
+
+
+@pytest.mark.parametrize("T", [256, 1023, 9001])
+def test_many_rows(T):
+    say(f"rmsnorm T={T}")
+    g = ref.gen(T)
+    check(ref.normal((T, 1040), g), None, ref.normal(1040, g), 1e-5)
+    check(ref.normal((T, 2064), g, 30.0), ref.normal((T, 2064), g), None, 0.0)
+
+
+def test_no_rows_and_each_output():
+    g = ref.gen(1)
+    x, w = ref.normal((5, 64), g), ref.normal(64, g)
+    empty = ep.rmsnorm(x[:0], w, rows8=True)
+    assert empty.out.shape == (0, 64) and empty.rows8.shape == (0, 80) and empty.total is None
+    whole = ep.rmsnorm(x, w, residual=x, rows8=True)
+    for out, rows8, total in ((True, False, False), (False, True, False), (False, False, True)):
+        one = ep.rmsnorm(x, w, residual=x, out=out, rows8=rows8, total=total)
+        for name in ("total", "out", "rows8"):
+            got = getattr(one, name)
+            assert (got is not None) == {"total": total, "out": out, "rows8": rows8}[name]
+            assert got is None or torch.equal(got.view(torch.uint8), getattr(whole, name).view(torch.uint8))
+
+
+def test_extremes_stay_in_their_rows():
+    """Zeros, the smallest and largest magnitudes, infinities and NaN, each in a row of its own."""
+    say("rmsnorm extremes")
+    H = 2064
+    g = ref.gen(7)
+    x = ref.normal((8, H), g)
+    x[0] = 0
+    x[1] = 1e-38
+    x[2] = 3e18
+    x[3, 5] = float("inf")
+    x[4, 2063] = float("nan")
+    x[5] = 0
+    x[5, 9] = -2.0 ** -130     # a subnormal
+    clean = ep.rmsnorm(x[6:], None, rows8=True)
+    got = check(x[[0, 1, 2, 5, 6, 7]].contiguous(), None, None, 1e-6)
+    q, scale = ep.rows8_values(got.rows8)
+    assert not got.out[0].any() and not q.view(torch.uint8)[0].any() and scale[0] > 0
+    both = ep.rmsnorm(x, None, rows8=True)
+    assert torch.equal(both.out[6:], clean.out) and torch.equal(both.rows8[6:], clean.rows8)
+    assert both.out[3].isnan()[5] and both.out[4].isnan().all()
+    scale = ep.rows8_values(both.rows8)[1]
+    assert scale[3].isnan() and scale[4].isnan() and not scale[[0, 1, 2, 5, 6, 7]].isnan().any()
+
+
+def test_total_in_place_and_side_stream():
+    say("rmsnorm in place, on a stream of its own")
+    g = ref.gen(3)
+    x, r, w = ref.normal((777, 2048), g), ref.normal((777, 2048), g), ref.normal(2048, g)
+    want = ep.rmsnorm(x, w, residual=r)
+    for into in (0, 1):
+        a, b = x.clone(), r.clone()
+        got = ep.rmsnorm(a, w, residual=b, total=(a, b)[into])
+        assert torch.equal(got.total, want.total) and torch.equal(got.out, want.out)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(20):  # fresh outputs of the side stream, freed and allocated again while it works
+        got = ep.rmsnorm(x, w, residual=r, stream=side)
+        torch.empty_like(x).fill_(7.0)
+    side.synchronize()
+    assert torch.equal(got.out, want.out)
+
+
+@pytest.mark.parametrize("H", LENGTHS)
+@pytest.mark.parametrize("T", [1, 38])
+def test_gradient(T, H):
+    say(f"rmsnorm_grad T={T} H={H}")
+    g = ref.gen(T * 7 + H)
+    s, d, w = ref.normal((T, H), g, 3.0), ref.normal((T, H), g), ref.normal(H, g)
+    for dt, wt in ((ref.normal((T, H), g), w), (None, None)):
+        dx, dw = ep.rmsnorm_grad(s, wt, d, d_total=dt, eps=1e-6)
+        want, size, want_w, size_w = ref.norm_grad(s, wt, d, dt, 1e-6)
+        ref.within(dx, want, want.abs() * ref.BF16 + size * 2.0 ** -14, "dx")
+        ref.within(dw, want_w, size_w * (2.0 ** -14 + T * ref.U24), "dw")
+
+
+def test_gradient_over_many_rows_repeats():
+    say("rmsnorm_grad over many rows")
+    T, H = 5003, 1032
+    g = ref.gen(11)
+    s, d, w = ref.normal((T, H), g), ref.normal((T, H), g), ref.normal(H, g)
+    dx, dw = ep.rmsnorm_grad(s, w, d, d_total=d)
+    want, size, want_w, size_w = ref.norm_grad(s, w, d, d, 1e-6)
+    ref.within(dx, want, want.abs() * ref.BF16 + size * 2.0 ** -14, "dx")
+    ref.within(dw, want_w, size_w * (2.0 ** -14 + T * ref.U24), "dw")
+    for _ in range(3):
+        again = ep.rmsnorm_grad(s, w, d, d_total=d)
+        assert torch.equal(again[0], dx) and torch.equal(again[1], dw)
+    only = ep.rmsnorm_grad(s, w, d, d_total=d.clone(), d_weight=False)
+    assert only[1] is None and torch.equal(only[0], dx)
+    a = d.clone()
+    assert torch.equal(ep.rmsnorm_grad(s, w, a, d_total=a, dx=a, d_weight=False)[0], dx)
+    dx0, dw0 = ep.rmsnorm_grad(s[:0], w, d[:0])
+    assert dx0.shape == (0, H) and not dw0.any()
+
+
+def test_gradient_against_differences():
+    """<dx, v> and <dw, u> against central differences of sum(d * y) in 64 bits along v and u:
+    the difference's own error is of third order in a step of 1e-4."""
+    say("rmsnorm_grad against differences")
+    T, H, eps = 9, 264, 1e-3
+    g = ref.gen(5)
+    s, d, w = ref.normal((T, H), g), ref.normal((T, H), g), ref.normal(H, g)
+    v, u = torch.randn((T, H), device="cuda", dtype=torch.float64), torch.randn(H, device="cuda", dtype=torch.float64)
+    dx, dw = ep.rmsnorm_grad(s, w, d, eps=eps)
+
+    def loss(a, b):
+        return (d.double() * ref.norm(a, None, b, eps)[1]).sum()
+
+    h = 1e-4
+    along = (loss(s.double() + h * v, w) - loss(s.double() - h * v, w)) / (2 * h)
+    size = ref.norm_grad(s, w, d, None, eps)
+    assert abs((dx.double() * v).sum() - along) <= (v.abs() * (dx.double().abs() * 2 * ref.BF16 + size[1] * 2.0 ** -14)).sum() + 1e-4
+    along = (loss(s, w.double() + h * u) - loss(s, w.double() - h * u)) / (2 * h)
+    assert abs((dw.double() * u).sum() - along) <= (u.abs() * size[3]).sum() * 2.0 ** -13 + 1e-4
