@@ -4,28 +4,34 @@
 // Tiles of weight rows x packed rows on the matrix cores (product_tile.h).  A workgroup finds
 // its expert and rows from the offsets in device memory, so the host never learns the counts:
 // the grid covers the most tiles that any counts can give, and the rest end at once.  The
-// gated product interleaves 16 gate rows with their 16 up rows of W, so that a lane holds a
-// gate and its up value in neighbouring accumulators.
+// gated product interleaves 8 gate rows with their 8 up rows of W, so that a lane holds a
+// gate and its up value in neighbouring quads of its accumulators.
+//
+// Where the tiles are fewer than the compute units, the contraction is split as well: each
+// part leaves its fp32 sums in the workspace, and a second kernel adds the parts in order and
+// runs the epilogue.
 #include "product_tile.h"
 
 namespace ep {
 namespace {
 
-struct Epilogue {
-    const float *w_scale;    // of the expert, [Nw], or null
-    const uint16_t *bias;    // of the expert, [Nw], or null
+// The rest of a call's arguments that the two kernels share.
+struct Split {
+    int32_t parts;  // of the contraction; 1: the tile kernel runs the epilogue
+    int32_t steps;  // of one part
 };
 
-// Four neighbouring outputs n..n+3 of row r from their sums z (gated: the gates' zg too).
-__device__ __forceinline__ f32x4 scaled(f32x4 z, int32_t col, const Epilogue &ep, float x_scale) {
-    if (ep.w_scale) {
-        const f32x4 s = *reinterpret_cast<const f32x4 *>(ep.w_scale + col);
+// Four neighbouring sums of weight rows col..col+3 of expert e, scaled and with the bias.
+template <bool F8>
+__device__ __forceinline__ f32x4 scaled(const ProductArgs &a, int64_t e, int32_t col, float x_scale, f32x4 z) {
+    if (F8) {
+        const f32x4 s = *reinterpret_cast<const f32x4 *>(a.w_scale + e * a.Nw + col);
 #pragma unroll
         for (int q = 0; q < 4; ++q)
             z[q] *= x_scale * s[q];
     }
-    if (ep.bias) {
-        const uint2 b = *reinterpret_cast<const uint2 *>(ep.bias + col);
+    if (a.bias) {
+        const uint2 b = *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(a.bias) + e * a.Nw + col);
         z[0] += bf16_lo(b.x);
         z[1] += bf16_hi(b.x);
         z[2] += bf16_lo(b.y);
@@ -33,19 +39,21 @@ __device__ __forceinline__ f32x4 scaled(f32x4 z, int32_t col, const Epilogue &ep
     }
     return z;
 }
-__device__ __forceinline__ void store_bf16x4(void *base, int64_t at, f32x4 v) {
-    *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(base) + at) = uint2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+__device__ __forceinline__ float row_scale(const ProductArgs &a, int64_t r) {
+    return *reinterpret_cast<const float *>(static_cast<const char *>(a.x) + r * (a.K + EP_ROWS8_EXTRA) + a.K);
 }
-template <bool GATED>
-__device__ __forceinline__ void finish4(const ProductArgs &a, const Epilogue &ep, int64_t r, int32_t n, float x_scale,
-                                        f32x4 z, f32x4 up) {
-    z = scaled(z, n, ep, x_scale);
+// The results n..n+3 of row r from their sums (gated: z the gates', up the ups').
+template <bool F8, bool GATED>
+__device__ __forceinline__ void finish4(const ProductArgs &a, int64_t e, int64_t r, int32_t n, float x_scale, f32x4 z,
+                                        f32x4 up) {
+    z = scaled<F8>(a, e, n, x_scale, z);
     if (GATED)
-        up = scaled(up, a.N + n, ep, x_scale);
+        up = scaled<F8>(a, e, a.N + n, x_scale, up);
     if (a.pre) {
-        store_bf16x4(a.pre, r * a.Nw + n, z);
+        uint16_t *pre = static_cast<uint16_t *>(a.pre) + r * a.Nw + n;
+        store_bf16x4(pre, z);
         if (GATED)
-            store_bf16x4(a.pre, r * a.Nw + a.N + n, up);
+            store_bf16x4(pre + a.N, up);
     }
     f32x4 y;
 #pragma unroll
@@ -61,18 +69,21 @@ __device__ __forceinline__ void finish4(const ProductArgs &a, const Epilogue &ep
     if (a.f32)
         *reinterpret_cast<f32x4 *>(static_cast<float *>(a.y) + r * a.N + n) = y;
     else
-        store_bf16x4(a.y, r * a.N + n, y);
+        store_bf16x4(static_cast<uint16_t *>(a.y) + r * a.N + n, y);
 }
 
 template <class S, Mul M, bool GATED>
-__global__ __launch_bounds__(S::kThreads) void product_kernel(ProductArgs a, int32_t col_tiles) {
+__global__ __launch_bounds__(S::kThreads) void product_kernel(ProductArgs a, int32_t col_tiles, Split split) {
     constexpr bool F8 = M != Mul::kBf16;
-    __shared__ __attribute__((aligned(1024))) char lds[2 * S::kStageBytes];
+    __shared__ __attribute__((aligned(1024))) char lds[S::kStages * S::kStageBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int32_t row_tiles = count_row_tiles(a.offsets, a.rows, a.E, S::kJ, lane);
-    const int64_t t = tile_of_block(blockIdx.x, (int64_t)row_tiles * col_tiles);
+    const int64_t tiles = (int64_t)row_tiles * col_tiles;
+    int64_t t = tile_of_block(blockIdx.x, tiles * split.parts);
     if (t < 0)
         return;
+    const int32_t part = split.parts == 1 ? 0 : (int32_t)(t / tiles);
+    t -= part * tiles;
     int32_t tr, tc;
     tile_order(t, row_tiles, col_tiles, tr, tc);
     const RowTile rt = find_row_tile(a.offsets, a.rows, a.E, S::kJ, tr, lane);
@@ -83,49 +94,135 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(ProductArgs a, int
     AlongC<S::kJ, S::kWaves> x;
     const char *wbase = static_cast<const char *>(a.w) + rt.e * (a.Nw * kb);
     w.init(wbase, (uint32_t)(a.Nw * kb), (int32_t)kb, wave, lane, [&](int row) -> uint32_t {
-        const int32_t n = GATED ? n0 + (row >> 5) * 16 + (row & 15) : n0 + row;
-        return n < a.N ? (uint32_t)((n + (GATED && (row & 16) ? a.N : 0)) * kb) : kNowhere;
+        const int32_t n = GATED ? n0 + (row >> 4) * 8 + (row & 7) : n0 + row;
+        return n < a.N ? (uint32_t)((n + (GATED && (row & 8) ? a.N : 0)) * kb) : kNowhere;
     });
     x.init(static_cast<const char *>(a.x) + rt.row0 * xs, (uint32_t)(rt.n * xs), (int32_t)kb, wave, lane,
            [&](int row) -> uint32_t { return (uint32_t)(row * xs); });
-    f32x4 acc[S::FI][S::FJ] = {};
-    const int64_t steps = (kb + kStepBytes - 1) / kStepBytes;
-    tile_product<S, M>(w, x, steps, steps, (char EP_LDS *)lds, wave, lane, acc);
+    f32x16 acc[S::FI][S::FJ] = {};
+    int32_t steps = (int32_t)((kb + kStepBytes - 1) / kStepBytes);
+    if (split.parts > 1) {
+        const int32_t first = part * split.steps;
+        steps = steps - first < split.steps ? steps - first : split.steps;
+        w.skip(first);
+        x.skip(first);
+    }
+    tile_product<S, M>(w, x, steps, (char EP_LDS *)lds, wave, lane, acc);
 
-    const Epilogue ep{a.w_scale ? a.w_scale + (int64_t)rt.e * a.Nw : nullptr,
-                      a.bias ? static_cast<const uint16_t *>(a.bias) + (int64_t)rt.e * a.Nw : nullptr};
-    const int wi = wave % S::kWavesI, wj = wave / S::kWavesI;
 #pragma unroll
     for (int j = 0; j < S::FJ; ++j) {
-        const int row = (wj * S::FJ + j) * 16 + lane % 16;
+        const int row = quad_row<S>(wave, j, lane);
         if (row >= rt.n)
             continue;
         const int64_t r = rt.row0 + row;
-        float x_scale = 1.f;
-        if (F8)
-            x_scale = *reinterpret_cast<const float *>(static_cast<const char *>(a.x) + r * xs + a.K);
+        const float x_scale = F8 && split.parts == 1 ? row_scale(a, r) : 1.f;
 #pragma unroll
-        for (int i = 0; i < S::FI; i += GATED ? 2 : 1) {
-            const int frag = wi * S::FI + i;
-            const int32_t n = n0 + (GATED ? frag / 2 : frag) * 16 + lane / 16 * 4;
-            if (n < a.N)
-                finish4<GATED>(a, ep, r, n, x_scale, acc[i][j], GATED ? acc[i + 1][j] : f32x4{});
-        }
+        for (int i = 0; i < S::FI; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; q += GATED ? 2 : 1) {
+                const int col = quad_col<S>(wave, i, q, lane);
+                const int32_t n = n0 + (GATED ? col / 16 * 8 + col % 8 : col);
+                if (n >= a.N)
+                    continue;
+                const f32x4 z = quad(acc[i][j], q), up = GATED ? quad(acc[i][j], q + 1) : f32x4{};
+                if (split.parts == 1) {
+                    finish4<F8, GATED>(a, rt.e, r, n, x_scale, z, up);
+                } else {
+                    float *dst = a.partial + ((int64_t)part * a.rows + r) * a.Nw + n;
+                    *reinterpret_cast<f32x4 *>(dst) = z;
+                    if (GATED)
+                        *reinterpret_cast<f32x4 *>(dst + a.N) = up;
+                }
+            }
     }
 }
 
-typedef TileShape<256, 256, 4, 2> Large;
-typedef TileShape<128, 128, 2, 2> Medium;
+// Adds the parts of a split contraction in order and runs the epilogue: a thread per four
+// results.
+template <bool F8, bool GATED>
+__global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, Split split) {
+    const int32_t quads = a.N / 4;
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t r = at / quads;
+    const int32_t n = (int32_t)(at - r * quads) * 4;
+    if (r >= a.rows)
+        return;
+    int32_t e = 0;
+    if (a.offsets) {  // the last expert that begins at or before r
+        int32_t hi = a.E;
+        while (hi - e > 1) {
+            const int32_t mid = (e + hi) / 2;
+            if (a.offsets[mid] <= r)
+                e = mid;
+            else
+                hi = mid;
+        }
+        if (r < a.offsets[e] || r >= a.offsets[e + 1])
+            return;
+    }
+    f32x4 z{}, up{};
+    const float *src = a.partial + r * a.Nw + n;
+    for (int32_t p = 0; p < split.parts; ++p, src += a.rows * a.Nw) {
+        z += *reinterpret_cast<const f32x4 *>(src);
+        if (GATED)
+            up += *reinterpret_cast<const f32x4 *>(src + a.N);
+    }
+    finish4<F8, GATED>(a, e, r, n, F8 ? row_scale(a, r) : 1.f, z, up);
+}
+
+typedef TileShape<256, 256, 4, 2, 2> Large;
+typedef TileShape<128, 128, 2, 2, 2> Medium;
+typedef TileShape<128, 64, 4, 1, 3> Few;
+typedef TileShape<128, 32, 4, 1, 4> Tiny;
+
+// ---- choice of the tile and of the split, from the sizes the host knows ----------------
+enum class Size { kLarge, kMedium, kFew, kTiny };
+Size tile_size(int64_t rows, int32_t E) {
+    const int64_t mean = rows / E;  // rows per expert
+    return mean >= 192 ? Size::kLarge : mean >= 96 ? Size::kMedium : mean >= 24 ? Size::kFew : Size::kTiny;
+}
+int tile_rows(Size s) { return s == Size::kLarge ? 256 : s == Size::kMedium ? 128 : s == Size::kFew ? 64 : 32; }
+int tile_cols(Size s, bool gated) { return (s == Size::kLarge ? 256 : 128) / (gated ? 2 : 1); }
+
+constexpr int64_t kSplitAim = 2 * kCus;  // workgroups wanted
+constexpr int32_t kSplitSteps = 4;       // fewest steps of a part
+struct Plan {
+    Size size;
+    int64_t tiles;  // at most
+    int32_t cols;
+    Split split;
+};
+Plan make_plan(int64_t rows, int32_t E, int32_t K, int32_t N, bool bits8, bool gated) {
+    Plan p;
+    const int32_t steps = (int32_t)(((int64_t)K * (bits8 ? 1 : 2) + kStepBytes - 1) / kStepBytes);
+    p.size = tile_size(rows, E);
+    for (;;) {
+        p.cols = (N + tile_cols(p.size, gated) - 1) / tile_cols(p.size, gated);
+        p.tiles = row_tiles_most(rows, E, tile_rows(p.size)) * p.cols;
+        // a tile size smaller where the large tiles leave compute units idle
+        if (p.size == Size::kLarge && p.tiles < kCus)
+            p.size = Size::kMedium;
+        else
+            break;
+    }
+    int64_t parts = p.tiles >= kCus ? 1 : std::min<int64_t>(kSplitAim / p.tiles, steps / kSplitSteps);
+    parts = std::max<int64_t>(parts, 1);
+    p.split.steps = (int32_t)((steps + parts - 1) / parts);
+    p.split.parts = (steps + p.split.steps - 1) / p.split.steps;
+    return p;
+}
 
 template <class S, Mul M, bool GATED>
-hipError_t launch_tiles(const ProductArgs &a, hipStream_t stream) {
-    constexpr int kOut = GATED ? S::kI / 2 : S::kI;
-    const int32_t cols = (a.N + kOut - 1) / kOut;
-    const int64_t tiles = row_tiles_most(a.rows, a.E, S::kJ) * cols;
-    if (tiles > kMostTiles)
+hipError_t launch_tiles(const ProductArgs &a, const Plan &p, hipStream_t stream) {
+    if (p.tiles * p.split.parts > kMostTiles)
         return hipErrorInvalidConfiguration;
-    return launch_traced("expert_product", product_kernel<S, M, GATED>, dim3((unsigned)(tiles + 8)), S::kThreads, stream,
-                         a, cols);
+    const hipError_t e = launch_traced("expert_product", product_kernel<S, M, GATED>,
+                                       dim3((unsigned)(p.tiles * p.split.parts + 8)), S::kThreads, stream, a, p.cols, p.split);
+    if (e != hipSuccess || p.split.parts == 1)
+        return e;
+    const int64_t blocks = (a.rows * (a.N / 4) + 255) / 256;
+    return launch_traced("expert_product_join", product_join_kernel<M != Mul::kBf16, GATED>, dim3((unsigned)blocks), 256,
+                         stream, a, p.split);
 }
 // The 8-bit matrix instruction doubles the rate, but it lines its products up to the largest
 // and drops what lies more than 13 bits below (measured: a sum of 7168 products of 8-bit rows
@@ -133,30 +230,36 @@ hipError_t launch_tiles(const ProductArgs &a, hipStream_t stream) {
 // result's own rounding, so long sums that end in bf16 take it; fp32 results and short sums,
 // which the memory bounds anyway, are multiplied as bf16.
 constexpr int32_t kLongSum = 512;
-Mul multiplication(const ProductArgs &a) {
-    return !a.bits8 ? Mul::kBf16 : a.K >= kLongSum && !a.f32 ? Mul::kF8 : Mul::kF8Wide;
-}
 template <class S>
-hipError_t launch_shape(const ProductArgs &a, hipStream_t stream) {
+hipError_t launch_shape(const ProductArgs &a, const Plan &p, hipStream_t stream) {
     const bool gated = a.act == EP_ACT_SWIGLU;
-    switch (multiplication(a)) {
-    case Mul::kBf16:
-        return gated ? launch_tiles<S, Mul::kBf16, true>(a, stream) : launch_tiles<S, Mul::kBf16, false>(a, stream);
-    case Mul::kF8:
-        return gated ? launch_tiles<S, Mul::kF8, true>(a, stream) : launch_tiles<S, Mul::kF8, false>(a, stream);
-    default:
-        return gated ? launch_tiles<S, Mul::kF8Wide, true>(a, stream) : launch_tiles<S, Mul::kF8Wide, false>(a, stream);
-    }
+    if (!a.bits8)
+        return gated ? launch_tiles<S, Mul::kBf16, true>(a, p, stream) : launch_tiles<S, Mul::kBf16, false>(a, p, stream);
+    if (a.K >= kLongSum && !a.f32)
+        return gated ? launch_tiles<S, Mul::kF8, true>(a, p, stream) : launch_tiles<S, Mul::kF8, false>(a, p, stream);
+    return gated ? launch_tiles<S, Mul::kF8Wide, true>(a, p, stream) : launch_tiles<S, Mul::kF8Wide, false>(a, p, stream);
 }
 
 }  // namespace
 
-size_t product_workspace_bytes(int64_t, int32_t, int32_t, int32_t, bool, int32_t) { return 0; }
+size_t product_workspace_bytes(int64_t rows, int32_t E, int32_t K, int32_t N, bool bits8, int32_t act) {
+    if (rows == 0)
+        return 0;
+    const bool gated = act == EP_ACT_SWIGLU;
+    const Plan p = make_plan(rows, E, K, N, bits8, gated);
+    return p.split.parts == 1 ? 0 : (size_t)p.split.parts * rows * N * (gated ? 2 : 1) * sizeof(float);
+}
 
 hipError_t launch_product(const ProductArgs &a, hipStream_t stream) {
     if (a.rows == 0)
         return hipSuccess;
-    return a.rows / a.E >= 192 ? launch_shape<Large>(a, stream) : launch_shape<Medium>(a, stream);
+    const Plan p = make_plan(a.rows, a.E, a.K, a.N, a.bits8, a.act == EP_ACT_SWIGLU);
+    switch (p.size) {
+    case Size::kLarge: return launch_shape<Large>(a, p, stream);
+    case Size::kMedium: return launch_shape<Medium>(a, p, stream);
+    case Size::kFew: return launch_shape<Few>(a, p, stream);
+    default: return launch_shape<Tiny>(a, p, stream);
+    }
 }
 
 }  // namespace ep

@@ -100,7 +100,7 @@ struct GradTileArgs {
 // dx[r][k] = sum_n dz[r][n] W_e[n][k]: i = k across the contraction, j = rows along it.
 template <class S>
 __global__ __launch_bounds__(S::kThreads) void product_dx_kernel(GradTileArgs a, int32_t col_tiles) {
-    __shared__ __attribute__((aligned(1024))) char lds[2 * S::kStageBytes];
+    __shared__ __attribute__((aligned(1024))) char lds[S::kStages * S::kStageBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int32_t row_tiles = count_row_tiles(a.offsets, a.rows, a.E, S::kJ, lane);
     const int64_t t = tile_of_block(blockIdx.x, (int64_t)row_tiles * col_tiles);
@@ -116,27 +116,26 @@ __global__ __launch_bounds__(S::kThreads) void product_dx_kernel(GradTileArgs a,
     const int64_t zs = (int64_t)a.Nw * 2;
     z.init(reinterpret_cast<const char *>(a.dz) + rt.row0 * zs, (uint32_t)(rt.n * zs), (int32_t)zs, wave, lane,
            [&](int row) -> uint32_t { return (uint32_t)(row * zs); });
-    f32x4 acc[S::FI][S::FJ] = {};
-    const int64_t steps = (a.Nw + kStepRows - 1) / kStepRows;
-    tile_product<S, Mul::kBf16>(w, z, steps, steps, (char EP_LDS *)lds, wave, lane, acc);
-    const int wi = wave % S::kWavesI, wj = wave / S::kWavesI;
+    f32x16 acc[S::FI][S::FJ] = {};
+    tile_product<S, Mul::kBf16>(w, z, (a.Nw + kStepRows - 1) / kStepRows, (char EP_LDS *)lds, wave, lane, acc);
 #pragma unroll
     for (int j = 0; j < S::FJ; ++j) {
-        const int row = (wj * S::FJ + j) * 16 + lane % 16;
+        const int row = quad_row<S>(wave, j, lane);
 #pragma unroll
-        for (int i = 0; i < S::FI; ++i) {
-            const int32_t k = k0 + (wi * S::FI + i) * 16 + lane / 16 * 4;
-            if (row < rt.n && k < a.K)
-                *reinterpret_cast<uint2 *>(a.out + (rt.row0 + row) * a.K + k) =
-                    uint2{bf16_pair(acc[i][j][0], acc[i][j][1]), bf16_pair(acc[i][j][2], acc[i][j][3])};
-        }
+        for (int i = 0; i < S::FI; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int32_t k = k0 + quad_col<S>(wave, i, q, lane);
+                if (row < rt.n && k < a.K)
+                    store_bf16x4(a.out + (rt.row0 + row) * a.K + k, quad(acc[i][j], q));
+            }
     }
 }
 
 // dw_e[n][k] = sum_r dz[r][n] x[r][k]: both operands across the contraction.
 template <class S>
 __global__ __launch_bounds__(S::kThreads) void product_dw_kernel(GradTileArgs a, int32_t n_tiles, int32_t k_tiles) {
-    __shared__ __attribute__((aligned(1024))) char lds[2 * S::kStageBytes];
+    __shared__ __attribute__((aligned(1024))) char lds[S::kStages * S::kStageBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t per_expert = (int64_t)n_tiles * k_tiles;
     const int64_t t = tile_of_block(blockIdx.x, per_expert * a.E);
@@ -152,25 +151,24 @@ __global__ __launch_bounds__(S::kThreads) void product_dw_kernel(GradTileArgs a,
     AcrossC<S::kJ, S::kWaves> z;
     x.init(reinterpret_cast<const char *>(a.x + b * a.K), (int64_t)a.K * 2, end - b, k0, wave, lane);
     z.init(reinterpret_cast<const char *>(a.dz + b * a.Nw), (int64_t)a.Nw * 2, end - b, n0, wave, lane);
-    f32x4 acc[S::FI][S::FJ] = {};
-    const int64_t steps = (end - b + kStepRows - 1) / kStepRows;
-    tile_product<S, Mul::kBf16>(x, z, steps, steps, (char EP_LDS *)lds, wave, lane, acc);
-    const int wi = wave % S::kWavesI, wj = wave / S::kWavesI;
+    f32x16 acc[S::FI][S::FJ] = {};
+    tile_product<S, Mul::kBf16>(x, z, (int32_t)((end - b + kStepRows - 1) / kStepRows), (char EP_LDS *)lds, wave, lane, acc);
 #pragma unroll
     for (int j = 0; j < S::FJ; ++j) {
-        const int32_t n = n0 + (wj * S::FJ + j) * 16 + lane % 16;
+        const int32_t n = n0 + quad_row<S>(wave, j, lane);
 #pragma unroll
-        for (int i = 0; i < S::FI; ++i) {
-            const int32_t k = k0 + (wi * S::FI + i) * 16 + lane / 16 * 4;
-            if (n < a.Nw && k < a.K)
-                *reinterpret_cast<uint2 *>(a.out + ((int64_t)e * a.Nw + n) * a.K + k) =
-                    uint2{bf16_pair(acc[i][j][0], acc[i][j][1]), bf16_pair(acc[i][j][2], acc[i][j][3])};
-        }
+        for (int i = 0; i < S::FI; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int32_t k = k0 + quad_col<S>(wave, i, q, lane);
+                if (n < a.Nw && k < a.K)
+                    store_bf16x4(a.out + ((int64_t)e * a.Nw + n) * a.K + k, quad(acc[i][j], q));
+            }
     }
 }
 
-typedef TileShape<256, 256, 4, 2> Large;
-typedef TileShape<128, 128, 2, 2> Medium;
+typedef TileShape<256, 256, 4, 2, 2> Large;
+typedef TileShape<128, 128, 2, 2, 2> Medium;
 
 template <class S>
 hipError_t launch_dx(const GradTileArgs &a, hipStream_t stream) {

@@ -1,10 +1,14 @@
 // product_tile.h -- the MFMA tile shared by the experts' product and its gradients.
 //
 // A workgroup computes a TI x TJ tile of C[j][i] = sum_c A[i][c] B[j][c].  i is the index
-// that is contiguous in C: a lane of the 16x16 matrix instruction holds four consecutive i of
-// one j, so results leave in vectors.  Both operands go from memory to LDS without passing
-// registers (16 bytes per lane, in buffer loads whose range check gives zeros past the last
-// row), 128 bytes of the contraction (64 bf16 or 128 e4m3 values) per step.
+// that is contiguous in C: a lane of the 32x32 matrix instruction holds four consecutive i of
+// one j at a time, so results leave in vectors.  Both operands go from memory to LDS without
+// passing registers (16 bytes per lane, in buffer loads whose range check gives zeros past the
+// last row), 128 bytes of the contraction (64 bf16 or 128 e4m3 values) per step: whole cache
+// lines.  (Measured with the loads alone, 256 x 256 tiles of 16-bit rows out of L2: 128-byte
+// pieces 24.6 TB/s over the chip, 64-byte pieces 15.0, from which the product cannot pass
+// 1100 TFLOP/s.)  A step is multiplied in two halves, and the fragments of a half are read
+// from LDS while the half before it is multiplied.
 //
 // An operand comes in one of two forms:
 //   rows along c      [index][c], c contiguous: LDS rows of 128 bytes, whose 16-byte chunks are
@@ -21,16 +25,19 @@
 
 namespace ep {
 
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 #define EP_LDS __attribute__((address_space(3)))
 
-constexpr int kStepBytes = 128;     // bytes of the contraction per step, rows along c
-constexpr int kStepRows = 64;       // rows of the contraction per step, rows across c
+constexpr int kStepBytes = 128;  // bytes of the contraction per step, rows along c
+constexpr int kStepRows = 64;   // rows of the contraction per step, rows across c
 constexpr uint32_t kNowhere = 0x80000000u;  // an offset past every buffer's range
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const char *base, uint32_t bytes) {
@@ -44,70 +51,80 @@ __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, uint32_t o
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (void EP_LDS *)dst, 16, (int)offset, 0, 0, 0);
 }
 
+// 1 KiB loads of a T-index operand per wave and step.  An operand with fewer of them than
+// there are waves is loaded by several waves alike, so that every wave counts the same.
+template <int T, int W>
+constexpr int loads_per_wave() {
+    return T / 8 > W ? T / 8 / W : 1;
+}
+
 // An operand with rows along c: T rows, loaded by W waves.
 template <int T, int W>
 struct AlongC {
-    static constexpr int kLoads = T / 8 / W;  // 1 KiB loads per wave and step
-    static_assert(T % (8 * W) == 0, "");
+    static constexpr int kLoads = loads_per_wave<T, W>();
+    static constexpr int kReads = 2;  // LDS reads of a fragment
     const char *base;
-    uint32_t left;        // bytes from base to the end of the operand
+    uint32_t left;    // bytes from base to the end of the operand
+    int32_t bytes;    // bytes of the contraction left
     uint32_t offset[kLoads];
-    int32_t tail;         // bytes of the contraction in the last step (1..128)
 
     // The chunk that a row's chunk number `p` holds.
     __device__ __forceinline__ static int swizzle(int row, int p) { return p ^ ((row >> 1) & 7); }
+    __device__ __forceinline__ static int load_number(int wave, int q) { return (wave * kLoads + q) % (T / 8); }
 
     // row_offset(r): the byte offset from base of tile row r, or kNowhere.
     template <typename F>
-    __device__ __forceinline__ void init(const char *b, uint32_t bytes, int32_t contraction_bytes, int wave, int lane,
+    __device__ __forceinline__ void init(const char *b, uint32_t size, int32_t contraction_bytes, int wave, int lane,
                                          F row_offset) {
         base = b;
-        left = bytes;
-        tail = (contraction_bytes - 1) % kStepBytes + 1;
+        left = size;
+        bytes = contraction_bytes;
 #pragma unroll
         for (int q = 0; q < kLoads; ++q) {
-            const int row = (wave * kLoads + q) * 8 + lane / 8;
+            const int row = load_number(wave, q) * 8 + lane / 8;
             offset[q] = row_offset(row) + swizzle(row, lane % 8) * 16;
         }
     }
-    __device__ __forceinline__ void skip(int64_t steps) {
-        base += steps * kStepBytes;
+    __device__ __forceinline__ void skip(int32_t steps) {
+        base += (int64_t)steps * kStepBytes;
         left -= (uint32_t)(steps * kStepBytes);
+        bytes -= steps * kStepBytes;
     }
-    __device__ __forceinline__ void load(char EP_LDS *lds, int wave, int lane, bool last) {
-        const __amdgpu_buffer_rsrc_t r = buffer_of(base, left);
+    // Loads one step (zeros where it is not live).
+    __device__ __forceinline__ void load(char EP_LDS *lds, int wave, int lane, bool live) {
+        const __amdgpu_buffer_rsrc_t r = buffer_of(base, live ? left : 0);
 #pragma unroll
-        for (int q = 0; q < kLoads; ++q) {
-            uint32_t o = offset[q];
-            if (last) {
-                const int row = (wave * kLoads + q) * 8 + lane / 8;
-                o = swizzle(row, lane % 8) * 16 < tail ? o : kNowhere;
-            }
-            load_to_lds(r, o, lds + (wave * kLoads + q) * 1024);
+        for (int q = 0; q < kLoads; ++q) {  // the last step may be shorter: zeros past the contraction's end
+            const int row = load_number(wave, q) * 8 + lane / 8;
+            load_to_lds(r, swizzle(row, lane % 8) * 16 < bytes ? offset[q] : kNowhere, lds + load_number(wave, q) * 1024);
         }
         base += kStepBytes;
         left -= kStepBytes;
+        bytes -= kStepBytes;
     }
-    // The 16 bytes of fragment row `row0 + lane % 16` that half h (0, 1) of the step gives
-    // lane group lane / 16.
+    // The 16 bytes of fragment row `row0 + lane % 32` that quarter h (0..3) of the step gives
+    // lane group lane / 32.
     __device__ __forceinline__ static i32x4 read(const char EP_LDS *lds, int row0, int h, int lane) {
-        const int row = row0 + lane % 16;
-        return *reinterpret_cast<const i32x4 EP_LDS *>(lds + row * 128 + swizzle(row, h * 4 + lane / 16) * 16);
+        const int row = row0 + lane % 32;
+        return *reinterpret_cast<const i32x4 EP_LDS *>(lds + row * 128 + swizzle(row, h * 2 + lane / 32) * 16);
     }
 };
 
 // A bf16 operand with rows across c: T indexes per row, loaded by W waves.
 template <int T, int W>
 struct AcrossC {
-    static constexpr int kLoads = T / 8 / W;
+    static constexpr int kLoads = loads_per_wave<T, W>();
     static constexpr int kChunks = T / 16;  // 32-byte chunks of a row
-    static_assert(T % (8 * W) == 0, "");
+    static constexpr int kReads = 4;
     const char *base;
     int64_t stride;  // bytes of a row
     int64_t rows;    // rows of the contraction left
     uint32_t offset[kLoads];
 
-    __device__ __forceinline__ static int key(int row) { return ((row & 3) | ((row >> 3) & 3) << 2) & (kChunks - 1); }
+    __device__ __forceinline__ static int key(int row) {
+        return kChunks < 8 ? (row >> 1 & 1) << 1 : kChunks < 16 ? (row & 3) << 1 : (row & 3) << 1 | (row >> 3 & 1) << 3;
+    }
+    __device__ __forceinline__ static int load_number(int wave, int q) { return (wave * kLoads + q) % (T / 8); }
 
     __device__ __forceinline__ void init(const char *b, int64_t row_bytes, int64_t n, int64_t index0, int wave, int lane) {
         base = b;
@@ -115,46 +132,47 @@ struct AcrossC {
         rows = n;
 #pragma unroll
         for (int q = 0; q < kLoads; ++q) {
-            const int p = (wave * kLoads + q) * 1024 + lane * 16;
+            const int p = load_number(wave, q) * 1024 + lane * 16;
             const int row = p / (2 * T), chunk = p % (2 * T) / 32, half = p / 16 % 2;
             offset[q] = (uint32_t)(row * stride + index0 * 2 + (chunk ^ key(row)) * 32 + half * 16);
         }
     }
-    __device__ __forceinline__ void load(char EP_LDS *lds, int wave, int, bool) {
-        const int64_t n = rows < kStepRows ? rows : kStepRows;
+    __device__ __forceinline__ void load(char EP_LDS *lds, int wave, int, bool live) {
+        const int64_t n = !live ? 0 : rows < kStepRows ? rows : kStepRows;
         const __amdgpu_buffer_rsrc_t r = buffer_of(base, (uint32_t)(n * stride));
 #pragma unroll
         for (int q = 0; q < kLoads; ++q)
-            load_to_lds(r, offset[q], lds + (wave * kLoads + q) * 1024);
+            load_to_lds(r, offset[q], lds + load_number(wave, q) * 1024);
         base += kStepRows * stride;
         rows -= kStepRows;
     }
-    // As AlongC::read for the indexes row0 + lane % 16: the transposing load gives a lane four
+    // As AlongC::read for the indexes index0 + lane % 32: the transposing load gives a lane four
     // rows of one column, the sixteen lanes of a group addressing those rows in 8-byte pieces.
     __device__ __forceinline__ static i32x4 read(const char EP_LDS *lds, int index0, int h, int lane) {
-        const int g = lane / 16, q = lane % 16;
-        const int row = h * 32 + g * 8 + q / 4;
-        const char EP_LDS *p = lds + row * (2 * T) + ((index0 / 16) ^ key(row)) * 32 + q % 4 * 8;
+        const int q = lane % 16;
+        const int row = h * 16 + lane / 32 * 8 + q / 4;
+        const int chunk = index0 / 16 + lane / 16 % 2;
+        const char EP_LDS *p = lds + row * (2 * T) + (chunk ^ key(row)) * 32 + q % 4 * 8;
         const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 EP_LDS *)p);
-        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 EP_LDS *)(p + 4 * (2 * T)));
-        typedef short s16x8 __attribute__((ext_vector_type(8)));
+        const int row4 = row + 4;  // same key: it looks at the bits 0, 1 and 3 of the row
+        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 EP_LDS *)(p + (row4 - row) * (2 * T)));
         return __builtin_bit_cast(i32x4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };
 
-// TI x TJ tile, WI x WJ waves of FI x FJ fragments each.
-template <int TI, int TJ, int WI, int WJ>
+// TI x TJ tile, WI x WJ waves of FI x FJ fragments each, STAGES steps in LDS.
+template <int TI, int TJ, int WI, int WJ, int STAGES>
 struct TileShape {
     static constexpr int kI = TI, kJ = TJ, kWavesI = WI, kWavesJ = WJ, kWaves = WI * WJ, kThreads = kWaves * 64;
-    static constexpr int FI = TI / WI / 16, FJ = TJ / WJ / 16;
+    static constexpr int FI = TI / WI / 32, FJ = TJ / WJ / 32, kStages = STAGES;
     static constexpr int kStageBytes = (TI + TJ) * kStepBytes;
+    static_assert(FI * WI * 32 == TI && FJ * WJ * 32 == TJ && STAGES >= 2, "");
 };
 
 // What is multiplied: bf16 values; e4m3 values by the 8-bit matrix instruction; or e4m3 values
 // widened to bf16, which holds each of them exactly.
 enum class Mul { kBf16, kF8, kF8Wide };
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ bf16x8 widen(int lo, int hi) {
     const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false);
     const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
@@ -163,77 +181,143 @@ __device__ __forceinline__ bf16x8 widen(int lo, int hi) {
     return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// Runs `steps` steps of the contraction into acc.  Two LDS stages: a step's loads are issued
-// before the step before it is multiplied.
-template <class S, Mul M, class OpA, class OpB>
-__device__ __forceinline__ void tile_product(OpA &a, OpB &b, int64_t steps, int64_t steps_to_end, char EP_LDS *lds,
-                                             int wave, int lane, f32x4 (&acc)[S::FI][S::FJ]) {
-    const int wi = wave % S::kWavesI, wj = wave / S::kWavesI;
-    const int i0 = wi * S::FI * 16, j0 = wj * S::FJ * 16;
-    if (steps <= 0)
-        return;
-    a.load(lds, wave, lane, steps_to_end == 1);
-    b.load(lds + S::kI * kStepBytes, wave, lane, steps_to_end == 1);
-    for (int64_t s = 0; s < steps; ++s) {
-        // this wave's loads of the step have landed, and after the barrier every wave's; the
-        // other stage has been read by every wave
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        char EP_LDS *cur = lds + (s & 1) * S::kStageBytes;
-        if (s + 1 < steps) {
-            char EP_LDS *next = lds + ((s + 1) & 1) * S::kStageBytes;
-            a.load(next, wave, lane, s + 2 == steps_to_end);
-            b.load(next + S::kI * kStepBytes, wave, lane, s + 2 == steps_to_end);
-        }
-        const char EP_LDS *la = cur, *lb = cur + S::kI * kStepBytes;
-        if constexpr (M == Mul::kF8) {
-            i32x8 fa[S::FI], fb[S::FJ];
+// Half a step's fragments of one wave: 32 bytes per lane and 32 indexes.
+template <class S>
+struct Fragments {
+    i32x4 a[S::FI][2], b[S::FJ][2];
+};
+
+template <class S, class OpA, class OpB>
+__device__ __forceinline__ void read_fragments(Fragments<S> &f, const char EP_LDS *stage, int half, int i0, int j0,
+                                               int lane) {
 #pragma unroll
-            for (int f = 0; f < S::FI; ++f)
-                fa[f] = __builtin_shufflevector(OpA::read(la, i0 + f * 16, 0, lane), OpA::read(la, i0 + f * 16, 1, lane),
-                                                0, 1, 2, 3, 4, 5, 6, 7);
+    for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int f = 0; f < S::FJ; ++f)
-                fb[f] = __builtin_shufflevector(OpB::read(lb, j0 + f * 16, 0, lane), OpB::read(lb, j0 + f * 16, 1, lane),
-                                                0, 1, 2, 3, 4, 5, 6, 7);
+        for (int i = 0; i < S::FI; ++i)
+            f.a[i][h] = OpA::read(stage, i0 + i * 32, 2 * half + h, lane);
 #pragma unroll
-            for (int i = 0; i < S::FI; ++i)
+        for (int j = 0; j < S::FJ; ++j)
+            f.b[j][h] = OpB::read(stage + S::kI * kStepBytes, j0 + j * 32, 2 * half + h, lane);
+    }
+}
+
+template <class S, Mul M>
+__device__ __forceinline__ void multiply(const Fragments<S> &f, f32x16 (&acc)[S::FI][S::FJ]) {
+    if constexpr (M == Mul::kF8) {
+#pragma unroll
+        for (int i = 0; i < S::FI; ++i)
+#pragma unroll
+            for (int j = 0; j < S::FJ; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                    __builtin_shufflevector(f.a[i][0], f.a[i][1], 0, 1, 2, 3, 4, 5, 6, 7),
+                    __builtin_shufflevector(f.b[j][0], f.b[j][1], 0, 1, 2, 3, 4, 5, 6, 7), acc[i][j], 0, 0, 0, 0x7f7f7f7f,
+                    0, 0x7f7f7f7f);
+    } else {
+        constexpr int kParts = M == Mul::kF8Wide ? 2 : 1;  // matrix instructions per 16 bytes
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int p = 0; p < kParts; ++p) {
+                bf16x8 a[S::FI], b[S::FJ];
+#pragma unroll
+                for (int i = 0; i < S::FI; ++i)
+                    a[i] = M == Mul::kF8Wide ? widen(f.a[i][h][2 * p], f.a[i][h][2 * p + 1])
+                                             : __builtin_bit_cast(bf16x8, f.a[i][h]);
 #pragma unroll
                 for (int j = 0; j < S::FJ; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa[i], fb[j], acc[i][j], 0, 0, 0,
-                                                                                0x7f7f7f7f, 0, 0x7f7f7f7f);
-        } else {
+                    b[j] = M == Mul::kF8Wide ? widen(f.b[j][h][2 * p], f.b[j][h][2 * p + 1])
+                                             : __builtin_bit_cast(bf16x8, f.b[j][h]);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                i32x4 fa[S::FI], fb[S::FJ];
+                for (int i = 0; i < S::FI; ++i)
 #pragma unroll
-                for (int f = 0; f < S::FI; ++f)
-                    fa[f] = OpA::read(la, i0 + f * 16, h, lane);
-#pragma unroll
-                for (int f = 0; f < S::FJ; ++f)
-                    fb[f] = OpB::read(lb, j0 + f * 16, h, lane);
-                constexpr int kParts = M == Mul::kF8Wide ? 2 : 1;  // matrix instructions per 16 bytes
-#pragma unroll
-                for (int p = 0; p < kParts; ++p) {
-                    bf16x8 va[S::FI], vb[S::FJ];
-#pragma unroll
-                    for (int f = 0; f < S::FI; ++f)
-                        va[f] = M == Mul::kF8Wide ? widen(fa[f][2 * p], fa[f][2 * p + 1]) : __builtin_bit_cast(bf16x8, fa[f]);
-#pragma unroll
-                    for (int f = 0; f < S::FJ; ++f)
-                        vb[f] = M == Mul::kF8Wide ? widen(fb[f][2 * p], fb[f][2 * p + 1]) : __builtin_bit_cast(bf16x8, fb[f]);
-#pragma unroll
-                    for (int i = 0; i < S::FI; ++i)
-#pragma unroll
-                        for (int j = 0; j < S::FJ; ++j)
-                            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[i], vb[j], acc[i][j], 0, 0, 0);
-                }
+                    for (int j = 0; j < S::FJ; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], b[j], acc[i][j], 0, 0, 0);
             }
-        }
-        // every LDS read of this stage is done before the barrier that lets it be overwritten
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
+}
+
+// Waits until at most VM of this wave's loads are in flight, its LDS reads are done, and every
+// wave of the workgroup has come this far.
+template <int VM>
+__device__ __forceinline__ void wait_and_meet() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((VM & 15) | 7 << 4 | VM >> 4 << 14);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Has the compiler issue the LDS reads of the next step between the matrix instructions of
+// this one (left to itself it puts them behind, and the wave waits for them).
+template <class S, Mul M, int READS>
+__device__ __forceinline__ void interleave() {
+    constexpr int kMuls = S::FI * S::FJ * (M == Mul::kF8 ? 1 : M == Mul::kBf16 ? 2 : 4);
+    constexpr int kDs = 0x100, kMfma = 0x8;
+    constexpr int kPerMul = (READS + kMuls - 1) / kMuls;  // reads behind each matrix instruction
+#pragma unroll
+    for (int m = 0; m < kMuls; ++m) {
+        __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+        if (m * kPerMul < READS)
+            __builtin_amdgcn_sched_group_barrier(kDs, kPerMul, 0);
+    }
+}
+
+// Runs `steps` steps of the contraction into acc.  Step t's place in LDS is t % STAGES.  A
+// wave enters step t with its first half in registers; it reads the second half while it
+// multiplies the first.  Once every wave has read the whole step (the barrier), its place
+// takes step t + STAGES, and the first half of step t + 1 is read while the second is
+// multiplied.  Loads past the last step bring zeros, so that the count of loads in flight is
+// the same in every step.
+template <class S, Mul M, class OpA, class OpB>
+__device__ __forceinline__ void tile_product(OpA &a, OpB &b, int32_t steps, char EP_LDS *lds, int wave, int lane,
+                                             f32x16 (&acc)[S::FI][S::FJ]) {
+    constexpr int kLoads = OpA::kLoads + OpB::kLoads;
+    constexpr int kReads = OpA::kReads * S::FI + OpB::kReads * S::FJ;
+    const int i0 = wave % S::kWavesI * S::FI * 32, j0 = wave / S::kWavesI * S::FJ * 32;
+    if (steps <= 0)
+        return;
+#pragma unroll
+    for (int s = 0; s < S::kStages; ++s) {
+        a.load(lds + s * S::kStageBytes, wave, lane, s < steps);
+        b.load(lds + s * S::kStageBytes + S::kI * kStepBytes, wave, lane, s < steps);
+    }
+    Fragments<S> first, second;
+    wait_and_meet<(S::kStages - 1) * kLoads>();
+    read_fragments<S, OpA, OpB>(first, lds, 0, i0, j0, lane);
+    int place = 0;
+    for (int32_t t = 0; t < steps; ++t) {
+        char EP_LDS *here = lds + place * S::kStageBytes;
+        read_fragments<S, OpA, OpB>(second, here, 1, i0, j0, lane);
+        multiply<S, M>(first, acc);
+        interleave<S, M, kReads>();
+        // the own part of step t + 1 has landed, the own reads of step t are done
+        wait_and_meet<(S::kStages - 2) * kLoads>();
+        a.load(here, wave, lane, t + S::kStages < steps);
+        b.load(here + S::kI * kStepBytes, wave, lane, t + S::kStages < steps);
+        place = place + 1 == S::kStages ? 0 : place + 1;
+        read_fragments<S, OpA, OpB>(first, lds + place * S::kStageBytes, 0, i0, j0, lane);
+        multiply<S, M>(second, acc);
+        interleave<S, M, kReads>();
+    }
+    // every load has landed and every read is done before the kernel uses the LDS again
+    wait_and_meet<0>();
+}
+
+// The accumulators' places: quad q (0..3) of fragment (i, j) holds C at row j0 and columns
+// i0 .. i0 + 3 of the tile.
+template <class S>
+__device__ __forceinline__ int quad_row(int wave, int j, int lane) {
+    return (wave / S::kWavesI * S::FJ + j) * 32 + lane % 32;
+}
+template <class S>
+__device__ __forceinline__ int quad_col(int wave, int i, int q, int lane) {
+    return (wave % S::kWavesI * S::FI + i) * 32 + q * 8 + lane / 32 * 4;
+}
+__device__ __forceinline__ f32x4 quad(const f32x16 &v, int q) {
+    return f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+}
+
+__device__ __forceinline__ void store_bf16x4(uint16_t *at, f32x4 v) {
+    *reinterpret_cast<uint2 *>(at) = uint2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
 }
 
 // ---- which rows a tile has --------------------------------------------------------
