@@ -21,55 +21,56 @@ struct Split {
     int32_t steps;  // of one part
 };
 
-// Four neighbouring sums of weight rows col..col+3 of expert e, scaled and with the bias.
+// Eight neighbouring sums of weight rows col..col+7 of expert e, scaled and with the bias.
 template <bool F8>
-__device__ __forceinline__ f32x4 scaled(const ProductArgs &a, int64_t e, int32_t col, float x_scale, f32x4 z) {
+__device__ __forceinline__ void scaled(const ProductArgs &a, int64_t e, int32_t col, float x_scale, float *z) {
     if (F8) {
-        const f32x4 s = *reinterpret_cast<const f32x4 *>(a.w_scale + e * a.Nw + col);
+        const float *s = a.w_scale + e * a.Nw + col;
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
+        for (int q = 0; q < 8; ++q)
             z[q] *= x_scale * s[q];
     }
     if (a.bias) {
-        const uint2 b = *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(a.bias) + e * a.Nw + col);
-        z[0] += bf16_lo(b.x);
-        z[1] += bf16_hi(b.x);
-        z[2] += bf16_lo(b.y);
-        z[3] += bf16_hi(b.y);
+        float b[8];
+        unpack8(*reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(a.bias) + e * a.Nw + col), b);
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            z[q] += b[q];
     }
-    return z;
 }
 __device__ __forceinline__ float row_scale(const ProductArgs &a, int64_t r) {
     return *reinterpret_cast<const float *>(static_cast<const char *>(a.x) + r * (a.K + EP_ROWS8_EXTRA) + a.K);
 }
-// The results n..n+3 of row r from their sums (gated: z the gates', up the ups').
+// The results n..n+7 of row r from their sums (gated: z the gates', up the ups').
 template <bool F8, bool GATED>
-__device__ __forceinline__ void finish4(const ProductArgs &a, int64_t e, int64_t r, int32_t n, float x_scale, f32x4 z,
-                                        f32x4 up) {
-    z = scaled<F8>(a, e, n, x_scale, z);
+__device__ __forceinline__ void finish8(const ProductArgs &a, int64_t e, int64_t r, int32_t n, float x_scale, float *z,
+                                        float *up) {
+    scaled<F8>(a, e, n, x_scale, z);
     if (GATED)
-        up = scaled<F8>(a, e, a.N + n, x_scale, up);
+        scaled<F8>(a, e, a.N + n, x_scale, up);
     if (a.pre) {
         uint16_t *pre = static_cast<uint16_t *>(a.pre) + r * a.Nw + n;
-        store_bf16x4(pre, z);
+        *reinterpret_cast<u32x4 *>(pre) = pack8(z);
         if (GATED)
-            store_bf16x4(pre + a.N, up);
+            *reinterpret_cast<u32x4 *>(pre + a.N) = pack8(up);
     }
-    f32x4 y;
+    float y[8], res[8] = {};
+    if (a.residual)
+        unpack8(*reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(a.residual) + r * a.N + n), res);
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
+    for (int q = 0; q < 8; ++q)
         y[q] = GATED ? activation(z[q], EP_ACT_SILU) * up[q] : activation(z[q], a.act);
-    if (a.residual) {
-        const uint2 v = *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(a.residual) + r * a.N + n);
-        y[0] += bf16_lo(v.x);
-        y[1] += bf16_hi(v.x);
-        y[2] += bf16_lo(v.y);
-        y[3] += bf16_hi(v.y);
+    if (a.residual)
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            y[q] += res[q];
+    if (a.f32) {
+        f32x4 *dst = reinterpret_cast<f32x4 *>(static_cast<float *>(a.y) + r * a.N + n);
+        dst[0] = f32x4{y[0], y[1], y[2], y[3]};
+        dst[1] = f32x4{y[4], y[5], y[6], y[7]};
+    } else {
+        *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.y) + r * a.N + n) = pack8(y);
     }
-    if (a.f32)
-        *reinterpret_cast<f32x4 *>(static_cast<float *>(a.y) + r * a.N + n) = y;
-    else
-        store_bf16x4(static_cast<uint16_t *>(a.y) + r * a.N + n, y);
 }
 
 template <class S, Mul M, bool GATED>
@@ -109,42 +110,41 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(ProductArgs a, int
     }
     tile_product<S, M>(w, x, steps, (char EP_LDS *)lds, wave, lane, acc);
 
-#pragma unroll
-    for (int j = 0; j < S::FJ; ++j) {
-        const int row = quad_row<S>(wave, j, lane);
-        if (row >= rt.n)
-            continue;
-        const int64_t r = rt.row0 + row;
-        const float x_scale = F8 && split.parts == 1 ? row_scale(a, r) : 1.f;
-#pragma unroll
-        for (int i = 0; i < S::FI; ++i)
-#pragma unroll
-            for (int q = 0; q < 4; q += GATED ? 2 : 1) {
-                const int col = quad_col<S>(wave, i, q, lane);
-                const int32_t n = n0 + (GATED ? col / 16 * 8 + col % 8 : col);
-                if (n >= a.N)
-                    continue;
-                const f32x4 z = quad(acc[i][j], q), up = GATED ? quad(acc[i][j], q + 1) : f32x4{};
-                if (split.parts == 1) {
-                    finish4<F8, GATED>(a, rt.e, r, n, x_scale, z, up);
-                } else {
-                    float *dst = a.partial + ((int64_t)part * a.rows + r) * a.Nw + n;
-                    *reinterpret_cast<f32x4 *>(dst) = z;
-                    if (GATED)
-                        *reinterpret_cast<f32x4 *>(dst + a.N) = up;
-                }
-            }
+    if (split.parts > 1) {
+        tile_results<S>(acc, (char EP_LDS *)lds, wave, lane, [&](int row, int col, const float *v) {
+            // gated: the ups' eight columns lie N behind the gates'
+            const int32_t n = n0 + (GATED ? col / 16 * 8 : col);
+            if (row >= rt.n || n >= a.N)
+                return;
+            f32x4 *dst = reinterpret_cast<f32x4 *>(a.partial + ((int64_t)part * a.rows + rt.row0 + row) * a.Nw + n +
+                                                   (GATED && (col & 8) ? a.N : 0));
+            dst[0] = f32x4{v[0], v[1], v[2], v[3]};
+            dst[1] = f32x4{v[4], v[5], v[6], v[7]};
+        });
+        return;
+    }
+    if constexpr (GATED) {
+        tile_pairs<S>(acc, (char EP_LDS *)lds, wave, lane, [&](int row, int col, float *z, float *up) {
+            const int32_t n = n0 + col / 2;
+            if (row < rt.n && n < a.N)
+                finish8<F8, true>(a, rt.e, rt.row0 + row, n, F8 ? row_scale(a, rt.row0 + row) : 1.f, z, up);
+        });
+    } else {
+        tile_results<S>(acc, (char EP_LDS *)lds, wave, lane, [&](int row, int col, float *z) {
+            if (row < rt.n && n0 + col < a.N)
+                finish8<F8, false>(a, rt.e, rt.row0 + row, n0 + col, F8 ? row_scale(a, rt.row0 + row) : 1.f, z, nullptr);
+        });
     }
 }
 
-// Adds the parts of a split contraction in order and runs the epilogue: a thread per four
+// Adds the parts of a split contraction in order and runs the epilogue: a thread per eight
 // results.
 template <bool F8, bool GATED>
 __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, Split split) {
-    const int32_t quads = a.N / 4;
+    const int32_t groups = a.N / 8;
     const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t r = at / quads;
-    const int32_t n = (int32_t)(at - r * quads) * 4;
+    const int64_t r = at / groups;
+    const int32_t n = (int32_t)(at - r * groups) * 8;
     if (r >= a.rows)
         return;
     int32_t e = 0;
@@ -160,14 +160,17 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, Split 
         if (r < a.offsets[e] || r >= a.offsets[e + 1])
             return;
     }
-    f32x4 z{}, up{};
+    float z[8] = {}, up[8] = {};
     const float *src = a.partial + r * a.Nw + n;
     for (int32_t p = 0; p < split.parts; ++p, src += a.rows * a.Nw) {
-        z += *reinterpret_cast<const f32x4 *>(src);
-        if (GATED)
-            up += *reinterpret_cast<const f32x4 *>(src + a.N);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            z[q] += src[q];
+            if (GATED)
+                up[q] += src[a.N + q];
+        }
     }
-    finish4<F8, GATED>(a, e, r, n, F8 ? row_scale(a, r) : 1.f, z, up);
+    finish8<F8, GATED>(a, e, r, n, F8 ? row_scale(a, r) : 1.f, z, up);
 }
 
 typedef TileShape<256, 256, 4, 2, 2> Large;
@@ -220,7 +223,7 @@ hipError_t launch_tiles(const ProductArgs &a, const Plan &p, hipStream_t stream)
                                        dim3((unsigned)(p.tiles * p.split.parts + 8)), S::kThreads, stream, a, p.cols, p.split);
     if (e != hipSuccess || p.split.parts == 1)
         return e;
-    const int64_t blocks = (a.rows * (a.N / 4) + 255) / 256;
+    const int64_t blocks = (a.rows * (a.N / 8) + 255) / 256;
     return launch_traced("expert_product_join", product_join_kernel<M != Mul::kBf16, GATED>, dim3((unsigned)blocks), 256,
                          stream, a, p.split);
 }

@@ -110,7 +110,7 @@ __global__ __launch_bounds__(S::kThreads) void product_dx_kernel(GradTileArgs a,
     tile_order(t, row_tiles, col_tiles, tr, tc);
     const RowTile rt = find_row_tile(a.offsets, a.rows, a.E, S::kJ, tr, lane);
     const int32_t k0 = tc * S::kI;
-    AcrossC<S::kI, S::kWaves> w;
+    AcrossC<S::kI, S::kWaves, S::FI> w;
     AlongC<S::kJ, S::kWaves> z;
     w.init(reinterpret_cast<const char *>(a.w + (int64_t)rt.e * a.Nw * a.K), (int64_t)a.K * 2, a.Nw, k0, wave, lane);
     const int64_t zs = (int64_t)a.Nw * 2;
@@ -118,18 +118,10 @@ __global__ __launch_bounds__(S::kThreads) void product_dx_kernel(GradTileArgs a,
            [&](int row) -> uint32_t { return (uint32_t)(row * zs); });
     f32x16 acc[S::FI][S::FJ] = {};
     tile_product<S, Mul::kBf16>(w, z, (a.Nw + kStepRows - 1) / kStepRows, (char EP_LDS *)lds, wave, lane, acc);
-#pragma unroll
-    for (int j = 0; j < S::FJ; ++j) {
-        const int row = quad_row<S>(wave, j, lane);
-#pragma unroll
-        for (int i = 0; i < S::FI; ++i)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int32_t k = k0 + quad_col<S>(wave, i, q, lane);
-                if (row < rt.n && k < a.K)
-                    store_bf16x4(a.out + (rt.row0 + row) * a.K + k, quad(acc[i][j], q));
-            }
-    }
+    tile_results<S>(acc, (char EP_LDS *)lds, wave, lane, [&](int row, int col, const float *v) {
+        if (row < rt.n && k0 + col < a.K)
+            *reinterpret_cast<u32x4 *>(a.out + (rt.row0 + row) * a.K + k0 + col) = pack8(v);
+    });
 }
 
 // dw_e[n][k] = sum_r dz[r][n] x[r][k]: both operands across the contraction.
@@ -147,24 +139,16 @@ __global__ __launch_bounds__(S::kThreads) void product_dw_kernel(GradTileArgs a,
     int64_t b, end;
     expert_rows(a.offsets, a.rows, e, b, end);
     const int32_t k0 = tk * S::kI, n0 = tn * S::kJ;
-    AcrossC<S::kI, S::kWaves> x;
-    AcrossC<S::kJ, S::kWaves> z;
+    AcrossC<S::kI, S::kWaves, S::FI> x;
+    AcrossC<S::kJ, S::kWaves, S::FJ> z;
     x.init(reinterpret_cast<const char *>(a.x + b * a.K), (int64_t)a.K * 2, end - b, k0, wave, lane);
     z.init(reinterpret_cast<const char *>(a.dz + b * a.Nw), (int64_t)a.Nw * 2, end - b, n0, wave, lane);
     f32x16 acc[S::FI][S::FJ] = {};
     tile_product<S, Mul::kBf16>(x, z, (int32_t)((end - b + kStepRows - 1) / kStepRows), (char EP_LDS *)lds, wave, lane, acc);
-#pragma unroll
-    for (int j = 0; j < S::FJ; ++j) {
-        const int32_t n = n0 + quad_row<S>(wave, j, lane);
-#pragma unroll
-        for (int i = 0; i < S::FI; ++i)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int32_t k = k0 + quad_col<S>(wave, i, q, lane);
-                if (n < a.Nw && k < a.K)
-                    store_bf16x4(a.out + ((int64_t)e * a.Nw + n) * a.K + k, quad(acc[i][j], q));
-            }
-    }
+    tile_results<S>(acc, (char EP_LDS *)lds, wave, lane, [&](int row, int col, const float *v) {
+        if (n0 + row < a.Nw && k0 + col < a.K)
+            *reinterpret_cast<u32x4 *>(a.out + ((int64_t)e * a.Nw + n0 + row) * a.K + k0 + col) = pack8(v);
+    });
 }
 
 typedef TileShape<256, 256, 4, 2, 2> Large;

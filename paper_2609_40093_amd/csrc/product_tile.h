@@ -62,7 +62,6 @@ constexpr int loads_per_wave() {
 template <int T, int W>
 struct AlongC {
     static constexpr int kLoads = loads_per_wave<T, W>();
-    static constexpr int kReads = 2;  // LDS reads of a fragment
     const char *base;
     uint32_t left;    // bytes from base to the end of the operand
     int32_t bytes;    // bytes of the contraction left
@@ -90,32 +89,38 @@ struct AlongC {
         left -= (uint32_t)(steps * kStepBytes);
         bytes -= steps * kStepBytes;
     }
-    // Loads one step (zeros where it is not live).
-    __device__ __forceinline__ void load(char EP_LDS *lds, int wave, int lane, bool live) {
-        const __amdgpu_buffer_rsrc_t r = buffer_of(base, live ? left : 0);
-#pragma unroll
-        for (int q = 0; q < kLoads; ++q) {  // the last step may be shorter: zeros past the contraction's end
-            const int row = load_number(wave, q) * 8 + lane / 8;
-            load_to_lds(r, swizzle(row, lane % 8) * 16 < bytes ? offset[q] : kNowhere, lds + load_number(wave, q) * 1024);
-        }
+    // A step's loads: begin (zeros where it is not live), the kLoads loads, end.
+    __amdgpu_buffer_rsrc_t range;
+    __device__ __forceinline__ void begin(bool live) { range = buffer_of(base, live ? left : 0); }
+    __device__ __forceinline__ void load(int q, char EP_LDS *lds, int wave, int lane) {
+        // the last step may be shorter: zeros past the contraction's end
+        const int row = load_number(wave, q) * 8 + lane / 8;
+        load_to_lds(range, swizzle(row, lane % 8) * 16 < bytes ? offset[q] : kNowhere, lds + load_number(wave, q) * 1024);
+    }
+    __device__ __forceinline__ void end() {
         base += kStepBytes;
         left -= kStepBytes;
         bytes -= kStepBytes;
     }
-    // The 16 bytes of fragment row `row0 + lane % 32` that quarter h (0..3) of the step gives
-    // lane group lane / 32.
-    __device__ __forceinline__ static i32x4 read(const char EP_LDS *lds, int row0, int h, int lane) {
-        const int row = row0 + lane % 32;
-        return *reinterpret_cast<const i32x4 EP_LDS *>(lds + row * 128 + swizzle(row, h * 2 + lane / 32) * 16);
+    // Fragment k of a wave whose first index is index0, quarter h (0..3) of the step: the 16
+    // bytes of row index0 + 32 k + lane % 32 that lane group lane / 32 takes.  The places
+    // within the fragment are the same for every k.
+    uint32_t at[4];
+    __device__ __forceinline__ void aim(int index0, int lane) {
+#pragma unroll
+        for (int h = 0; h < 4; ++h)
+            at[h] = (uint32_t)((index0 + lane % 32) * 128 + swizzle(lane % 32, h * 2 + lane / 32) * 16);
+    }
+    __device__ __forceinline__ i32x4 read(const char EP_LDS *lds, int k, int h) const {
+        return *reinterpret_cast<const i32x4 EP_LDS *>(lds + at[h] + k * 32 * 128);
     }
 };
 
 // A bf16 operand with rows across c: T indexes per row, loaded by W waves.
-template <int T, int W>
+template <int T, int W, int FRAGMENTS>
 struct AcrossC {
     static constexpr int kLoads = loads_per_wave<T, W>();
     static constexpr int kChunks = T / 16;  // 32-byte chunks of a row
-    static constexpr int kReads = 4;
     const char *base;
     int64_t stride;  // bytes of a row
     int64_t rows;    // rows of the contraction left
@@ -137,25 +142,32 @@ struct AcrossC {
             offset[q] = (uint32_t)(row * stride + index0 * 2 + (chunk ^ key(row)) * 32 + half * 16);
         }
     }
-    __device__ __forceinline__ void load(char EP_LDS *lds, int wave, int, bool live) {
+    __amdgpu_buffer_rsrc_t range;
+    __device__ __forceinline__ void begin(bool live) {
         const int64_t n = !live ? 0 : rows < kStepRows ? rows : kStepRows;
-        const __amdgpu_buffer_rsrc_t r = buffer_of(base, (uint32_t)(n * stride));
-#pragma unroll
-        for (int q = 0; q < kLoads; ++q)
-            load_to_lds(r, offset[q], lds + load_number(wave, q) * 1024);
+        range = buffer_of(base, (uint32_t)(n * stride));
+    }
+    __device__ __forceinline__ void load(int q, char EP_LDS *lds, int wave, int) {
+        load_to_lds(range, offset[q], lds + load_number(wave, q) * 1024);
+    }
+    __device__ __forceinline__ void end() {
         base += kStepRows * stride;
         rows -= kStepRows;
     }
-    // As AlongC::read for the indexes index0 + lane % 32: the transposing load gives a lane four
-    // rows of one column, the sixteen lanes of a group addressing those rows in 8-byte pieces.
-    __device__ __forceinline__ static i32x4 read(const char EP_LDS *lds, int index0, int h, int lane) {
-        const int q = lane % 16;
-        const int row = h * 16 + lane / 32 * 8 + q / 4;
-        const int chunk = index0 / 16 + lane / 16 % 2;
-        const char EP_LDS *p = lds + row * (2 * T) + (chunk ^ key(row)) * 32 + q % 4 * 8;
+    // As AlongC's, by the transposing load: it gives a lane four rows of one column, the sixteen
+    // lanes of a group addressing those rows in 8-byte pieces.  The key looks at the bits 0, 1
+    // and 3 of the row, which the quarter (16 rows) and the second four rows leave alone.
+    uint32_t at[FRAGMENTS];
+    __device__ __forceinline__ void aim(int index0, int lane) {
+        const int q = lane % 16, row = lane / 32 * 8 + q / 4;
+#pragma unroll
+        for (int k = 0; k < FRAGMENTS; ++k)
+            at[k] = (uint32_t)(row * (2 * T) + (((index0 + 32 * k) / 16 + lane / 16 % 2) ^ key(row)) * 32 + q % 4 * 8);
+    }
+    __device__ __forceinline__ i32x4 read(const char EP_LDS *lds, int k, int h) const {
+        const char EP_LDS *p = lds + at[k] + h * 16 * (2 * T);
         const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 EP_LDS *)p);
-        const int row4 = row + 4;  // same key: it looks at the bits 0, 1 and 3 of the row
-        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 EP_LDS *)(p + (row4 - row) * (2 * T)));
+        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 EP_LDS *)(p + 4 * (2 * T)));
         return __builtin_bit_cast(i32x4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };
@@ -187,31 +199,38 @@ struct Fragments {
     i32x4 a[S::FI][2], b[S::FJ][2];
 };
 
+// Reads number `r` of the 2 (FI + FJ) fragments of a half.
 template <class S, class OpA, class OpB>
-__device__ __forceinline__ void read_fragments(Fragments<S> &f, const char EP_LDS *stage, int half, int i0, int j0,
-                                               int lane) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-#pragma unroll
-        for (int i = 0; i < S::FI; ++i)
-            f.a[i][h] = OpA::read(stage, i0 + i * 32, 2 * half + h, lane);
-#pragma unroll
-        for (int j = 0; j < S::FJ; ++j)
-            f.b[j][h] = OpB::read(stage + S::kI * kStepBytes, j0 + j * 32, 2 * half + h, lane);
-    }
+__device__ __forceinline__ void read_fragment(Fragments<S> &f, int r, const OpA &a, const OpB &b, const char EP_LDS *stage,
+                                              int half) {
+    const int h = r / (S::FI + S::FJ), k = r % (S::FI + S::FJ);
+    if (k < S::FI)
+        f.a[k][h] = a.read(stage, k, 2 * half + h);
+    else
+        f.b[k - S::FI][h] = b.read(stage + S::kI * kStepBytes, k - S::FI, 2 * half + h);
 }
 
+// Multiplies a half: kMuls matrix instructions, after each of which `behind(m)` runs.  The
+// compiler keeps that order: left to itself it puts the LDS reads and loads that belong
+// between them behind all of them, and the wave waits.
 template <class S, Mul M>
-__device__ __forceinline__ void multiply(const Fragments<S> &f, f32x16 (&acc)[S::FI][S::FJ]) {
+constexpr int muls() {
+    return S::FI * S::FJ * (M == Mul::kF8 ? 1 : M == Mul::kBf16 ? 2 : 4);
+}
+template <class S, Mul M, typename F>
+__device__ __forceinline__ void multiply(const Fragments<S> &f, f32x16 (&acc)[S::FI][S::FJ], F behind) {
     if constexpr (M == Mul::kF8) {
 #pragma unroll
         for (int i = 0; i < S::FI; ++i)
 #pragma unroll
-            for (int j = 0; j < S::FJ; ++j)
+            for (int j = 0; j < S::FJ; ++j) {
                 acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
                     __builtin_shufflevector(f.a[i][0], f.a[i][1], 0, 1, 2, 3, 4, 5, 6, 7),
                     __builtin_shufflevector(f.b[j][0], f.b[j][1], 0, 1, 2, 3, 4, 5, 6, 7), acc[i][j], 0, 0, 0, 0x7f7f7f7f,
                     0, 0x7f7f7f7f);
+                behind(i * S::FJ + j);
+                __builtin_amdgcn_sched_barrier(0);
+            }
     } else {
         constexpr int kParts = M == Mul::kF8Wide ? 2 : 1;  // matrix instructions per 16 bytes
 #pragma unroll
@@ -230,94 +249,148 @@ __device__ __forceinline__ void multiply(const Fragments<S> &f, f32x16 (&acc)[S:
 #pragma unroll
                 for (int i = 0; i < S::FI; ++i)
 #pragma unroll
-                    for (int j = 0; j < S::FJ; ++j)
+                    for (int j = 0; j < S::FJ; ++j) {
                         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], b[j], acc[i][j], 0, 0, 0);
+                        behind(((h * kParts + p) * S::FI + i) * S::FJ + j);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
             }
     }
 }
 
-// Waits until at most VM of this wave's loads are in flight, its LDS reads are done, and every
-// wave of the workgroup has come this far.
-template <int VM>
+// Waits until at most VM of this wave's loads are in flight, with LDS also until its LDS reads
+// are done, and then until every wave of the workgroup has come this far.
+template <int VM, bool LDS>
 __device__ __forceinline__ void wait_and_meet() {
+    static_assert(VM < 64, "");
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt((VM & 15) | 7 << 4 | VM >> 4 << 14);
+    __builtin_amdgcn_s_waitcnt((VM & 15) | 7 << 4 | (LDS ? 0 : 15) << 8 | VM >> 4 << 14);
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
+constexpr int kAnyLoads = 63;  // no wait for loads
 
-// Has the compiler issue the LDS reads of the next step between the matrix instructions of
-// this one (left to itself it puts them behind, and the wave waits for them).
-template <class S, Mul M, int READS>
-__device__ __forceinline__ void interleave() {
-    constexpr int kMuls = S::FI * S::FJ * (M == Mul::kF8 ? 1 : M == Mul::kBf16 ? 2 : 4);
-    constexpr int kDs = 0x100, kMfma = 0x8;
-    constexpr int kPerMul = (READS + kMuls - 1) / kMuls;  // reads behind each matrix instruction
-#pragma unroll
-    for (int m = 0; m < kMuls; ++m) {
-        __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
-        if (m * kPerMul < READS)
-            __builtin_amdgcn_sched_group_barrier(kDs, kPerMul, 0);
-    }
-}
-
-// Runs `steps` steps of the contraction into acc.  Step t's place in LDS is t % STAGES.  A
-// wave enters step t with its first half in registers; it reads the second half while it
-// multiplies the first.  Once every wave has read the whole step (the barrier), its place
-// takes step t + STAGES, and the first half of step t + 1 is read while the second is
-// multiplied.  Loads past the last step bring zeros, so that the count of loads in flight is
-// the same in every step.
+// Runs `steps` steps of the contraction into acc.  Step t's place in LDS is t % STAGES.
+//
+// A wave enters step t with its first half in registers.  Between the matrix instructions of
+// the step it
+//   - reads the second half, early;
+//   - after a barrier (every wave has read the whole step) loads step t + STAGES into the
+//     place of step t, spread over half a step;
+//   - late, after a barrier (every wave's part of step t + 1 has landed), reads the first half
+//     of step t + 1.
+// So with two stages a load has one and a half steps to land.  Loads past the last step bring
+// zeros, so that the count of loads in flight is the same in every step.
 template <class S, Mul M, class OpA, class OpB>
 __device__ __forceinline__ void tile_product(OpA &a, OpB &b, int32_t steps, char EP_LDS *lds, int wave, int lane,
                                              f32x16 (&acc)[S::FI][S::FJ]) {
-    constexpr int kLoads = OpA::kLoads + OpB::kLoads;
-    constexpr int kReads = OpA::kReads * S::FI + OpB::kReads * S::FJ;
-    const int i0 = wave % S::kWavesI * S::FI * 32, j0 = wave / S::kWavesI * S::FJ * 32;
+    constexpr int kLoads = OpA::kLoads + OpB::kLoads, kReads = 2 * (S::FI + S::FJ), kMuls = muls<S, M>();
+    constexpr int kReadSlots = kMuls * 3 / 8 > 0 ? kMuls * 3 / 8 : 1;  // matrix instructions that a half's reads stand behind
+    constexpr int kFree = kMuls / 2;                // behind this one the step's place is free
+    constexpr int kLanded = 2 * kMuls - kReadSlots;  // behind this one the next step is there
     if (steps <= 0)
         return;
+    a.aim(wave % S::kWavesI * S::FI * 32, lane);
+    b.aim(wave / S::kWavesI * S::FJ * 32, lane);
+    const auto load = [&](int q, char EP_LDS *stage) {
+        if (q < OpA::kLoads)
+            a.load(q, stage, wave, lane);
+        else
+            b.load(q - OpA::kLoads, stage + S::kI * kStepBytes, wave, lane);
+    };
 #pragma unroll
     for (int s = 0; s < S::kStages; ++s) {
-        a.load(lds + s * S::kStageBytes, wave, lane, s < steps);
-        b.load(lds + s * S::kStageBytes + S::kI * kStepBytes, wave, lane, s < steps);
+        a.begin(s < steps);
+        b.begin(s < steps);
+#pragma unroll
+        for (int q = 0; q < kLoads; ++q)
+            load(q, lds + s * S::kStageBytes);
+        a.end();
+        b.end();
     }
     Fragments<S> first, second;
-    wait_and_meet<(S::kStages - 1) * kLoads>();
-    read_fragments<S, OpA, OpB>(first, lds, 0, i0, j0, lane);
+    wait_and_meet<(S::kStages - 1) * kLoads, false>();
+#pragma unroll
+    for (int r = 0; r < kReads; ++r)
+        read_fragment<S>(first, r, a, b, lds, 0);
     int place = 0;
     for (int32_t t = 0; t < steps; ++t) {
         char EP_LDS *here = lds + place * S::kStageBytes;
-        read_fragments<S, OpA, OpB>(second, here, 1, i0, j0, lane);
-        multiply<S, M>(first, acc);
-        interleave<S, M, kReads>();
-        // the own part of step t + 1 has landed, the own reads of step t are done
-        wait_and_meet<(S::kStages - 2) * kLoads>();
-        a.load(here, wave, lane, t + S::kStages < steps);
-        b.load(here + S::kI * kStepBytes, wave, lane, t + S::kStages < steps);
         place = place + 1 == S::kStages ? 0 : place + 1;
-        read_fragments<S, OpA, OpB>(first, lds + place * S::kStageBytes, 0, i0, j0, lane);
-        multiply<S, M>(second, acc);
-        interleave<S, M, kReads>();
+        const char EP_LDS *next = lds + place * S::kStageBytes;
+        a.begin(t + S::kStages < steps);
+        b.begin(t + S::kStages < steps);
+        const auto behind = [&](int m) {
+#pragma unroll
+            for (int r = 0; r < kReads; ++r)
+                if (r * kReadSlots / kReads == m)
+                    read_fragment<S>(second, r, a, b, here, 1);
+            if (m == kFree)
+                wait_and_meet<kAnyLoads, true>();
+#pragma unroll
+            for (int q = 0; q < kLoads; ++q)
+                if (kFree + q * kMuls / kLoads == m)
+                    load(q, here);
+            if (m == kLanded)
+                wait_and_meet<(S::kStages - 1) * kLoads, false>();
+#pragma unroll
+            for (int r = 0; r < kReads; ++r)
+                if (kLanded + r * kReadSlots / kReads == m)
+                    read_fragment<S>(first, r, a, b, next, 0);
+        };
+        multiply<S, M>(first, acc, behind);
+        multiply<S, M>(second, acc, [&](int m) { behind(kMuls + m); });
+        a.end();
+        b.end();
     }
     // every load has landed and every read is done before the kernel uses the LDS again
-    wait_and_meet<0>();
+    wait_and_meet<0, true>();
 }
 
-// The accumulators' places: quad q (0..3) of fragment (i, j) holds C at row j0 and columns
-// i0 .. i0 + 3 of the tile.
-template <class S>
-__device__ __forceinline__ int quad_row(int wave, int j, int lane) {
-    return (wave / S::kWavesI * S::FJ + j) * 32 + lane % 32;
+// Hands the tile out in rows: result(row, col, v) gets the eight neighbouring sums C[row][col..],
+// of tile row `row`, from a lane whose neighbours get the columns beside it, so that results
+// leave in whole cache lines.  (The accumulators themselves hold four columns of 32 rows per
+// instruction: stored as they are, 256 x 256 tiles took 57 us each to leave.)  A wave turns its
+// own 32 rows at a time over in its own piece of LDS.
+template <class S, int PER, typename F>
+__device__ __forceinline__ void tile_rows_out(const f32x16 (&acc)[S::FI][S::FJ], char EP_LDS *lds, int wave, int lane, F result) {
+    constexpr int kCols = S::FI * 32, kStride = kCols + 4;    // floats of a row, and with the padding
+    constexpr int kLanes = kCols / PER, kRows = 64 / kLanes;  // lanes of a row, rows at a time
+    static_assert(S::kWaves * 32 * kStride * 4 <= S::kStages * S::kStageBytes, "");
+    float EP_LDS *own = reinterpret_cast<float EP_LDS *>(lds) + wave * 32 * kStride;
+    const int row0 = wave / S::kWavesI * S::FJ * 32, col0 = wave % S::kWavesI * kCols;
+#pragma unroll
+    for (int j = 0; j < S::FJ; ++j) {
+#pragma unroll
+        for (int i = 0; i < S::FI; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<f32x4 EP_LDS *>(own + lane % 32 * kStride + i * 32 + q * 8 + lane / 32 * 4) =
+                    f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int r = 0; r < 32; r += kRows) {
+            const int row = r + lane / kLanes, col = lane % kLanes * PER;
+            float v[PER];
+#pragma unroll
+            for (int q = 0; q < PER; q += 4) {
+                const f32x4 x = *reinterpret_cast<const f32x4 EP_LDS *>(own + row * kStride + col + q);
+                v[q] = x[0], v[q + 1] = x[1], v[q + 2] = x[2], v[q + 3] = x[3];
+            }
+            result(row0 + j * 32 + row, col0 + col, v);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
 }
-template <class S>
-__device__ __forceinline__ int quad_col(int wave, int i, int q, int lane) {
-    return (wave % S::kWavesI * S::FI + i) * 32 + q * 8 + lane / 32 * 4;
+template <class S, typename F>
+__device__ __forceinline__ void tile_results(const f32x16 (&acc)[S::FI][S::FJ], char EP_LDS *lds, int wave, int lane, F result) {
+    tile_rows_out<S, 8>(acc, lds, wave, lane, result);
 }
-__device__ __forceinline__ f32x4 quad(const f32x16 &v, int q) {
-    return f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
-}
-
-__device__ __forceinline__ void store_bf16x4(uint16_t *at, f32x4 v) {
-    *reinterpret_cast<uint2 *>(at) = uint2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+// The same where the columns come in eights by turns: result(row, col, gates, ups) with the
+// gates at col and their ups at col + 8.
+template <class S, typename F>
+__device__ __forceinline__ void tile_pairs(const f32x16 (&acc)[S::FI][S::FJ], char EP_LDS *lds, int wave, int lane, F result) {
+    tile_rows_out<S, 16>(acc, lds, wave, lane, [&](int row, int col, float *v) { result(row, col, v, v + 8); });
 }
 
 // ---- which rows a tile has --------------------------------------------------------
