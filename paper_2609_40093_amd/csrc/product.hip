@@ -21,55 +21,79 @@ struct Split {
     int32_t steps;  // of one part
 };
 
-// Eight neighbouring sums of weight rows col..col+7 of expert e, scaled and with the bias.
+// What eight neighbouring results n..n+7 of every row of expert e share: the scales and the
+// bias of their weight rows (gated: the gates' rows, then the ups').
+template <bool F8, bool GATED>
+struct Columns {
+    float scale[GATED ? 2 : 1][F8 ? 8 : 1], bias[GATED ? 2 : 1][8];
+    __device__ __forceinline__ void load(const ProductArgs &a, int64_t e, int32_t n) {
+#pragma unroll
+        for (int p = 0; p < (GATED ? 2 : 1); ++p) {
+            const int64_t at = e * a.Nw + p * a.N + n;
+            if constexpr (F8)
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    scale[p][q] = a.w_scale[at + q];
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                bias[p][q] = 0.f;
+            if (a.bias)
+                unpack8(*reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(a.bias) + at), bias[p]);
+        }
+    }
+    __device__ __forceinline__ void apply(int p, float x_scale, float *z) const {
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            z[q] = F8 ? fmaf(z[q], x_scale * scale[p][F8 ? q : 0], bias[p][q]) : z[q] + bias[p][q];
+    }
+};
+// What a row brings besides: its eight residuals and its scale.
 template <bool F8>
-__device__ __forceinline__ void scaled(const ProductArgs &a, int64_t e, int32_t col, float x_scale, float *z) {
-    if (F8) {
-        const float *s = a.w_scale + e * a.Nw + col;
-#pragma unroll
-        for (int q = 0; q < 8; ++q)
-            z[q] *= x_scale * s[q];
+struct RowExtra {
+    u32x4 residual;
+    float scale;
+    __device__ __forceinline__ void load(const ProductArgs &a, int64_t r, int32_t n) {
+        residual = u32x4{0, 0, 0, 0};
+        if (a.residual)
+            residual = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(a.residual) + r * a.N + n);
+        scale = 1.f;
+        if (F8)
+            scale = *reinterpret_cast<const float *>(static_cast<const char *>(a.x) + r * (a.K + EP_ROWS8_EXTRA) + a.K);
     }
-    if (a.bias) {
-        float b[8];
-        unpack8(*reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(a.bias) + e * a.Nw + col), b);
-#pragma unroll
-        for (int q = 0; q < 8; ++q)
-            z[q] += b[q];
-    }
-}
-__device__ __forceinline__ float row_scale(const ProductArgs &a, int64_t r) {
-    return *reinterpret_cast<const float *>(static_cast<const char *>(a.x) + r * (a.K + EP_ROWS8_EXTRA) + a.K);
-}
+};
 // The results n..n+7 of row r from their sums (gated: z the gates', up the ups').
 template <bool F8, bool GATED>
-__device__ __forceinline__ void finish8(const ProductArgs &a, int64_t e, int64_t r, int32_t n, float x_scale, float *z,
-                                        float *up) {
-    scaled<F8>(a, e, n, x_scale, z);
-    if (GATED)
-        scaled<F8>(a, e, a.N + n, x_scale, up);
+__device__ __forceinline__ void finish8(const ProductArgs &a, const Columns<F8, GATED> &c, const RowExtra<F8> &x, int64_t r,
+                                        int32_t n, float *z, float *up) {
+    c.apply(0, x.scale, z);
+    if constexpr (GATED)
+        c.apply(1, x.scale, up);
     if (a.pre) {
         uint16_t *pre = static_cast<uint16_t *>(a.pre) + r * a.Nw + n;
         *reinterpret_cast<u32x4 *>(pre) = pack8(z);
         if (GATED)
             *reinterpret_cast<u32x4 *>(pre + a.N) = pack8(up);
     }
-    float y[8], res[8] = {};
-    if (a.residual)
-        unpack8(*reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(a.residual) + r * a.N + n), res);
-#pragma unroll
-    for (int q = 0; q < 8; ++q)
-        y[q] = GATED ? activation(z[q], EP_ACT_SILU) * up[q] : activation(z[q], a.act);
-    if (a.residual)
+    if (GATED) {
 #pragma unroll
         for (int q = 0; q < 8; ++q)
-            y[q] += res[q];
+            z[q] = z[q] * sigmoid(z[q]) * up[q];
+    } else {
+        activate8(z, a.act);
+    }
+    if (a.residual) {
+        float res[8];
+        unpack8(x.residual, res);
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            z[q] += res[q];
+    }
     if (a.f32) {
         f32x4 *dst = reinterpret_cast<f32x4 *>(static_cast<float *>(a.y) + r * a.N + n);
-        dst[0] = f32x4{y[0], y[1], y[2], y[3]};
-        dst[1] = f32x4{y[4], y[5], y[6], y[7]};
+        dst[0] = f32x4{z[0], z[1], z[2], z[3]};
+        dst[1] = f32x4{z[4], z[5], z[6], z[7]};
     } else {
-        *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.y) + r * a.N + n) = pack8(y);
+        *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.y) + r * a.N + n) = pack8(z);
     }
 }
 
@@ -123,18 +147,24 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(ProductArgs a, int
         });
         return;
     }
-    if constexpr (GATED) {
-        tile_pairs<S>(acc, (char EP_LDS *)lds, wave, lane, [&](int row, int col, float *z, float *up) {
-            const int32_t n = n0 + col / 2;
+    // a lane's columns: eight results, gated from the eight gates and the eight ups behind them
+    constexpr int kPer = GATED ? 16 : 8;
+    const int32_t n = n0 + first_col<S, kPer>(wave, lane) / (kPer / 8);
+    Columns<F8, GATED> columns;
+    if (n < a.N)
+        columns.load(a, rt.e, n);
+    tile_rows_out<S, kPer>(
+        acc, (char EP_LDS *)lds, wave, lane,
+        [&](int row) {
+            RowExtra<F8> x;
             if (row < rt.n && n < a.N)
-                finish8<F8, true>(a, rt.e, rt.row0 + row, n, F8 ? row_scale(a, rt.row0 + row) : 1.f, z, up);
+                x.load(a, rt.row0 + row, n);
+            return x;
+        },
+        [&](int row, int, float *v, const RowExtra<F8> &x) {
+            if (row < rt.n && n < a.N)
+                finish8<F8, GATED>(a, columns, x, rt.row0 + row, n, v, v + kPer / 2);
         });
-    } else {
-        tile_results<S>(acc, (char EP_LDS *)lds, wave, lane, [&](int row, int col, float *z) {
-            if (row < rt.n && n0 + col < a.N)
-                finish8<F8, false>(a, rt.e, rt.row0 + row, n0 + col, F8 ? row_scale(a, rt.row0 + row) : 1.f, z, nullptr);
-        });
-    }
 }
 
 // Adds the parts of a split contraction in order and runs the epilogue: a thread per eight
@@ -170,7 +200,11 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, Split 
                 up[q] += src[a.N + q];
         }
     }
-    finish8<F8, GATED>(a, e, r, n, F8 ? row_scale(a, r) : 1.f, z, up);
+    Columns<F8, GATED> columns;
+    columns.load(a, e, n);
+    RowExtra<F8> x;
+    x.load(a, r, n);
+    finish8<F8, GATED>(a, columns, x, r, n, z, up);
 }
 
 typedef TileShape<256, 256, 4, 2, 2> Large;

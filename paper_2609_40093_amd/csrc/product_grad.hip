@@ -36,18 +36,28 @@ __global__ __launch_bounds__(256) void product_dz_kernel(const int32_t *offsets,
                 for (int p = 0; p < kParts; ++p)
                     unpack8(*reinterpret_cast<const u32x4 *>(pre + r * Nw + p * N + n), z[p]);
             float o[kParts][8];
+            if (GATED) {
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                if (GATED) {
-                    o[0][q] = d[q] * z[kParts - 1][q] * activation_grad(z[0][q], EP_ACT_SILU);
-                    o[kParts - 1][q] = d[q] * activation(z[0][q], EP_ACT_SILU);
-                } else {
-                    o[0][q] = pre ? d[q] * activation_grad(z[0][q], act) : d[q];
+                for (int q = 0; q < 8; ++q) {
+                    const float s = sigmoid(z[0][q]);
+                    o[0][q] = d[q] * z[kParts - 1][q] * s * (1.f + z[0][q] * (1.f - s));
+                    o[kParts - 1][q] = d[q] * z[0][q] * s;
                 }
+            } else if (pre) {
+                activation_grad8(z[0], act);
 #pragma unroll
-                for (int p = 0; p < kParts; ++p)
-                    sum[p][q] += o[p][q];
+                for (int q = 0; q < 8; ++q)
+                    o[0][q] = d[q] * z[0][q];
+            } else {
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    o[0][q] = d[q];
             }
+#pragma unroll
+            for (int p = 0; p < kParts; ++p)
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    sum[p][q] += o[p][q];
             if (dz)
 #pragma unroll
                 for (int p = 0; p < kParts; ++p)

@@ -347,20 +347,35 @@ __device__ __forceinline__ void tile_product(OpA &a, OpB &b, int32_t steps, char
     wait_and_meet<0, true>();
 }
 
-// Hands the tile out in rows: result(row, col, v) gets the eight neighbouring sums C[row][col..],
-// of tile row `row`, from a lane whose neighbours get the columns beside it, so that results
+// Hands the tile out in rows: result(row, col, v, f) gets the PER neighbouring sums C[row][col..]
+// of tile row `row` from a lane whose neighbours get the columns beside them, so that results
 // leave in whole cache lines.  (The accumulators themselves hold four columns of 32 rows per
-// instruction: stored as they are, 256 x 256 tiles took 57 us each to leave.)  A wave turns its
-// own 32 rows at a time over in its own piece of LDS.
-template <class S, int PER, typename F>
-__device__ __forceinline__ void tile_rows_out(const f32x16 (&acc)[S::FI][S::FJ], char EP_LDS *lds, int wave, int lane, F result) {
+// instruction.)  A wave turns its own 32 rows at a time over in its own piece of LDS; a lane
+// always gets the same columns, first_col(...) + 0 .. PER-1.  What a row needs from memory
+// besides, f = fetch(row), is on its way a turn earlier.
+template <class S, int PER>
+__device__ __forceinline__ int first_col(int wave, int lane) {
+    return wave % S::kWavesI * S::FI * 32 + lane % (S::FI * 32 / PER) * PER;
+}
+template <class S, int PER, typename G, typename F>
+__device__ __forceinline__ void tile_rows_out(const f32x16 (&acc)[S::FI][S::FJ], char EP_LDS *lds, int wave, int lane, G fetch,
+                                              F result) {
     constexpr int kCols = S::FI * 32, kStride = kCols + 4;    // floats of a row, and with the padding
     constexpr int kLanes = kCols / PER, kRows = 64 / kLanes;  // lanes of a row, rows at a time
+    constexpr int kTurns = 32 / kRows;
     static_assert(S::kWaves * 32 * kStride * 4 <= S::kStages * S::kStageBytes, "");
     float EP_LDS *own = reinterpret_cast<float EP_LDS *>(lds) + wave * 32 * kStride;
-    const int row0 = wave / S::kWavesI * S::FJ * 32, col0 = wave % S::kWavesI * kCols;
+    const int row0 = wave / S::kWavesI * S::FJ * 32, col = lane % kLanes * PER;
+    decltype(fetch(0)) got[2][kTurns];
+#pragma unroll
+    for (int r = 0; r < kTurns; ++r)
+        got[0][r] = fetch(row0 + r * kRows + lane / kLanes);
 #pragma unroll
     for (int j = 0; j < S::FJ; ++j) {
+        if (j + 1 < S::FJ)
+#pragma unroll
+            for (int r = 0; r < kTurns; ++r)
+                got[(j + 1) % 2][r] = fetch(row0 + (j + 1) * 32 + r * kRows + lane / kLanes);
 #pragma unroll
         for (int i = 0; i < S::FI; ++i)
 #pragma unroll
@@ -369,28 +384,25 @@ __device__ __forceinline__ void tile_rows_out(const f32x16 (&acc)[S::FI][S::FJ],
                     f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (int r = 0; r < 32; r += kRows) {
-            const int row = r + lane / kLanes, col = lane % kLanes * PER;
+        for (int r = 0; r < kTurns; ++r) {
+            const int row = r * kRows + lane / kLanes;
             float v[PER];
 #pragma unroll
             for (int q = 0; q < PER; q += 4) {
                 const f32x4 x = *reinterpret_cast<const f32x4 EP_LDS *>(own + row * kStride + col + q);
                 v[q] = x[0], v[q + 1] = x[1], v[q + 2] = x[2], v[q + 3] = x[3];
             }
-            result(row0 + j * 32 + row, col0 + col, v);
+            result(row0 + j * 32 + row, first_col<S, PER>(wave, lane), v, got[j % 2][r]);
         }
         __builtin_amdgcn_wave_barrier();
     }
 }
+struct Nothing {};
 template <class S, typename F>
 __device__ __forceinline__ void tile_results(const f32x16 (&acc)[S::FI][S::FJ], char EP_LDS *lds, int wave, int lane, F result) {
-    tile_rows_out<S, 8>(acc, lds, wave, lane, result);
-}
-// The same where the columns come in eights by turns: result(row, col, gates, ups) with the
-// gates at col and their ups at col + 8.
-template <class S, typename F>
-__device__ __forceinline__ void tile_pairs(const f32x16 (&acc)[S::FI][S::FJ], char EP_LDS *lds, int wave, int lane, F result) {
-    tile_rows_out<S, 16>(acc, lds, wave, lane, [&](int row, int col, float *v) { result(row, col, v, v + 8); });
+    tile_rows_out<S, 8>(
+        acc, lds, wave, lane, [](int) { return Nothing{}; },
+        [&](int row, int col, float *v, Nothing) { result(row, col, v); });
 }
 
 // ---- which rows a tile has --------------------------------------------------------
@@ -474,27 +486,40 @@ __device__ __forceinline__ void tile_order(int64_t t, int32_t row_tiles, int32_t
 constexpr int64_t kMostTiles = 1 << 30;  // of a grid (launch_traced refuses the ones too large for their workgroups)
 inline int64_t row_tiles_most(int64_t rows, int32_t E, int per) { return rows / per + std::min<int64_t>(E, rows); }
 
-// Activation of one value, and its derivative.
-__device__ __forceinline__ float sigmoid(float z) { return 1.f / (1.f + expf(-z)); }
-__device__ __forceinline__ float activation(float z, int act) {
-    switch (act) {
-    case 1: return z < 0.f ? 0.f : z;  // a NaN stays one
-    case 2: return z * sigmoid(z);
-    case 3: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-    default: return z;
-    }
+// Activations, and their derivatives.
+// exp by the hardware's base-2 exponential: z log2(e) is rounded once, so the result is within
+// (|z| + 2) 2^-24 of itself.
+__device__ __forceinline__ float quick_exp(float z) { return __builtin_amdgcn_exp2f(z * 1.44269504f); }
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + quick_exp(-z)); }
+__device__ __forceinline__ float normal_cdf(float z) { return 0.5f * (1.f + erff(z * 0.70710678118654752f)); }
+__device__ __forceinline__ float silu_grad(float z) {
+    const float s = sigmoid(z);
+    return s * (1.f + z * (1.f - s));
 }
-__device__ __forceinline__ float activation_grad(float z, int act) {
-    switch (act) {
-    case 1: return z > 0.f ? 1.f : z != z ? z : 0.f;
-    case 2: {
-        const float s = sigmoid(z);
-        return s * (1.f + z * (1.f - s));
-    }
-    case 3:
-        return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.3989422804014327f;
-    default: return 1.f;
-    }
+// Eight values at a time: one branch on the activation for all of them.
+template <typename F>
+__device__ __forceinline__ void each8(float *v, F f) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+        v[q] = f(v[q]);
+}
+__device__ __forceinline__ void activate8(float *z, int act) {
+    if (act == EP_ACT_RELU)
+        each8(z, [](float v) { return v < 0.f ? 0.f : v; });  // a NaN stays one
+    else if (act == EP_ACT_SILU)
+        each8(z, [](float v) { return v * sigmoid(v); });
+    else if (act == EP_ACT_GELU)
+        each8(z, [](float v) { return v * normal_cdf(v); });
+}
+__device__ __forceinline__ void activation_grad8(float *z, int act) {
+    if (act == EP_ACT_RELU)
+        each8(z, [](float v) { return v > 0.f ? 1.f : v != v ? v : 0.f; });
+    else if (act == EP_ACT_SILU)
+        each8(z, silu_grad);
+    else if (act == EP_ACT_GELU)
+        each8(z, [](float v) { return normal_cdf(v) + v * quick_exp(-0.5f * v * v) * 0.3989422804014327f; });
+    else
+        each8(z, [](float) { return 1.f; });
 }
 
 }  // namespace ep
