@@ -61,6 +61,40 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
     return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 
+// Sum over rows [begin, end) of column h of an fp32 matrix, in a fixed order: workgroups of
+// 1024 threads, 32 neighbouring columns (h = base + threadIdx.x % 32) by 32 rows at a time.
+// The sum is valid in the first 32 threads.
+__device__ __forceinline__ float column_sum(const float *matrix, int64_t begin, int64_t end, int64_t width, int64_t h) {
+    __shared__ float part[32][33];
+    const int c = threadIdx.x & 31, lane = threadIdx.x >> 5;
+    float s = 0.f;
+    if (h < width) {
+        constexpr int kAhead = 8;
+        for (int64_t r = begin + lane; r < end; r += 32 * kAhead) {
+            float v[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                v[i] = r + i * 32 < end ? matrix[(r + i * 32) * width + h] : 0.f;
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                s += v[i];
+        }
+    }
+    part[lane][c] = s;
+    __syncthreads();
+    if (lane == 0) {
+        s = 0.f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            s += part[i][c];
+    }
+    return s;
+}
+
+// exp by the hardware's base-2 exponential: z log2(e) is rounded once, so the result is within
+// (|z| + 2) 2^-24 of itself.
+__device__ __forceinline__ float quick_exp(float z) { return __builtin_amdgcn_exp2f(z * 1.44269504f); }
+
 // ---- launches ---------------------------------------------------------------------
 // One kernel launch, timed under `name` while tracing is on.  A grid of 2^32 threads or more
 // along x is an error (the hardware counts them in 32 bits).

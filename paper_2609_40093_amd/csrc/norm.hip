@@ -272,24 +272,12 @@ __global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_grad_kernel(No
     }
 }
 
-// d_weight[h] = sum over the partial rows: 16 columns and 16 row lanes per workgroup.
-__global__ __launch_bounds__(256) void column_sum_kernel(const float *partial, int64_t rows, int32_t H, float *out) {
-    const int c = threadIdx.x & 15, lane = threadIdx.x >> 4;
-    const int64_t h = (int64_t)blockIdx.x * 16 + c;
-    float s = 0.f;
-    if (h < H)
-        for (int64_t r = lane; r < rows; r += 16)
-            s += partial[r * H + h];
-    __shared__ float part[16][17];
-    part[lane][c] = s;
-    __syncthreads();
-    if (lane == 0 && h < H) {
-        s = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            s += part[i][c];
+// d_weight[h] = sum over the partial rows.
+__global__ __launch_bounds__(1024) void norm_weight_kernel(const float *partial, int64_t rows, int32_t H, float *out) {
+    const int64_t h = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31);
+    const float s = column_sum(partial, 0, rows, H, h);
+    if (threadIdx.x < 32 && h < H)
         out[h] = s;
-    }
 }
 
 // Waves of a row and vectors per lane.
@@ -355,7 +343,7 @@ hipError_t launch_rmsnorm_grad(const NormGradArgs &a, hipStream_t stream) {
     }
     if (!a.d_weight)
         return hipSuccess;
-    return launch_traced("rmsnorm_grad_weight", column_sum_kernel, dim3((unsigned)((a.H + 15) / 16)), 256, stream,
+    return launch_traced("rmsnorm_grad_weight", norm_weight_kernel, dim3((unsigned)((a.H + 31) / 32)), 1024, stream,
                          (const float *)a.partial, partials, a.H, a.d_weight);
 }
 

@@ -167,18 +167,19 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(ProductArgs a, int
         });
 }
 
-// Adds the parts of a split contraction in order and runs the epilogue: a thread per eight
-// results.
+// Adds the parts of a split contraction and runs the epilogue.  A wave takes eight groups of
+// eight neighbouring results; its eight lanes per group add every eighth part each, in order,
+// and are added up in a fixed order.
 template <bool F8, bool GATED>
 __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, Split split) {
     const int32_t groups = a.N / 8;
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int lane = threadIdx.x & 63, first = lane / 8;
+    const int64_t at = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * 8 + lane % 8;
     const int64_t r = at / groups;
     const int32_t n = (int32_t)(at - r * groups) * 8;
-    if (r >= a.rows)
-        return;
+    bool mine = r < a.rows;
     int32_t e = 0;
-    if (a.offsets) {  // the last expert that begins at or before r
+    if (mine && a.offsets) {  // the last expert that begins at or before r
         int32_t hi = a.E;
         while (hi - e > 1) {
             const int32_t mid = (e + hi) / 2;
@@ -187,19 +188,43 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, Split 
             else
                 hi = mid;
         }
-        if (r < a.offsets[e] || r >= a.offsets[e + 1])
-            return;
+        mine = r >= a.offsets[e] && r < a.offsets[e + 1];
     }
     float z[8] = {}, up[8] = {};
-    const float *src = a.partial + r * a.Nw + n;
-    for (int32_t p = 0; p < split.parts; ++p, src += a.rows * a.Nw) {
+    if (mine) {
+        constexpr int kAhead = 4;
+        const int64_t part = a.rows * a.Nw;
+        const float *src = a.partial + r * a.Nw + n;
+        for (int32_t p0 = first; p0 < split.parts; p0 += 8 * kAhead) {
+            f32x4 v[kAhead][GATED ? 4 : 2];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            z[q] += src[q];
-            if (GATED)
-                up[q] += src[a.N + q];
+            for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+                for (int h = 0; h < (GATED ? 4 : 2); ++h) {
+                    v[i][h] = f32x4{};
+                    if (p0 + 8 * i < split.parts)
+                        v[i][h] = *reinterpret_cast<const f32x4 *>(src + (p0 + 8 * i) * part + (h / 2) * a.N + (h & 1) * 4);
+                }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    z[q] += v[i][q / 4][q % 4];
+                    if (GATED)
+                        up[q] += v[i][(GATED ? 2 : 0) + q / 4][q % 4];
+                }
         }
     }
+#pragma unroll
+    for (int d = 8; d < 64; d *= 2)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            z[q] += __shfl_xor(z[q], d);
+            if (GATED)
+                up[q] += __shfl_xor(up[q], d);
+        }
+    if (!mine || first != 0)
+        return;
     Columns<F8, GATED> columns;
     columns.load(a, e, n);
     RowExtra<F8> x;
@@ -207,19 +232,33 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, Split 
     finish8<F8, GATED>(a, columns, x, r, n, z, up);
 }
 
-typedef TileShape<256, 256, 4, 2, 2> Large;
-typedef TileShape<128, 128, 2, 2, 2> Medium;
-typedef TileShape<128, 64, 4, 1, 3> Few;
-typedef TileShape<128, 32, 4, 1, 4> Tiny;
+typedef TileShape<256, 256, 4, 2, 2> Large;  // one workgroup per compute unit (128 KiB of LDS)
+typedef TileShape<256, 128, 4, 2, 2> Wide;   // one (96 KiB)
+typedef TileShape<256, 64, 4, 2, 3> Few;     // one (120 KiB)
+typedef TileShape<128, 128, 2, 2, 2> Medium; // two (64 KiB)
+typedef TileShape<128, 32, 4, 1, 4> Tiny;    // two (80 KiB)
 
 // ---- choice of the tile and of the split, from the sizes the host knows ----------------
-enum class Size { kLarge, kMedium, kFew, kTiny };
+// By the mean rows per expert.  Measured, us (bf16 gated, 32 experts, K 7168, N 2048; then 128
+// experts, K 2048, N 768), Large / Wide / Few / Medium:
+//   mean  24  363 / 338 / 398 / 355    178 / 180 / 180 / 162
+//   mean  64  389 / 427 / 394 / 421    183 / 195 / 203 / 187
+//   mean  96  507 / 431 / 534 / 464    218 / 194 / 221 / 207
+//   mean 160  538 / 548 / 738 / 600    248 / 246 / 287 / 250
+//   mean 256  609 / 721 / 991 / 820
+// Below 80 rows the weights' bytes bound it, and what differs is how evenly the tiles fill the
+// compute units.  With less than 16 rows Tiny gains up to a tenth on Medium (16 experts, K 4096,
+// N 1536, mean 8: 84 / 93).  Where the larger tiles are fewer than the compute units, Medium takes over
+// (4096 rows of 8 experts, K 2048, N 1024: Large 64, Medium 32).
+enum class Size { kLarge, kWide, kFew, kMedium, kTiny };
 Size tile_size(int64_t rows, int32_t E) {
-    const int64_t mean = rows / E;  // rows per expert
-    return mean >= 192 ? Size::kLarge : mean >= 96 ? Size::kMedium : mean >= 24 ? Size::kFew : Size::kTiny;
+    const int64_t mean = rows / E;
+    return mean >= 160 ? Size::kLarge : mean >= 80 ? Size::kWide : mean >= 40 ? Size::kFew : mean >= 16 ? Size::kMedium : Size::kTiny;
 }
-int tile_rows(Size s) { return s == Size::kLarge ? 256 : s == Size::kMedium ? 128 : s == Size::kFew ? 64 : 32; }
-int tile_cols(Size s, bool gated) { return (s == Size::kLarge ? 256 : 128) / (gated ? 2 : 1); }
+int tile_rows(Size s) {
+    return s == Size::kLarge ? Large::kJ : s == Size::kWide ? Wide::kJ : s == Size::kFew ? Few::kJ : s == Size::kMedium ? Medium::kJ : Tiny::kJ;
+}
+int tile_cols(Size s, bool gated) { return (s >= Size::kMedium ? Medium::kI : Large::kI) / (gated ? 2 : 1); }
 
 constexpr int64_t kSplitAim = 2 * kCus;  // workgroups wanted
 constexpr int32_t kSplitSteps = 4;       // fewest steps of a part
@@ -232,16 +271,14 @@ struct Plan {
 Plan make_plan(int64_t rows, int32_t E, int32_t K, int32_t N, bool bits8, bool gated) {
     Plan p;
     const int32_t steps = (int32_t)(((int64_t)K * (bits8 ? 1 : 2) + kStepBytes - 1) / kStepBytes);
-    p.size = tile_size(rows, E);
-    for (;;) {
-        p.cols = (N + tile_cols(p.size, gated) - 1) / tile_cols(p.size, gated);
-        p.tiles = row_tiles_most(rows, E, tile_rows(p.size)) * p.cols;
-        // a tile size smaller where the large tiles leave compute units idle
-        if (p.size == Size::kLarge && p.tiles < kCus)
-            p.size = Size::kMedium;
-        else
-            break;
-    }
+    const auto take = [&](Size size) {
+        p.size = size;
+        p.cols = (N + tile_cols(size, gated) - 1) / tile_cols(size, gated);
+        p.tiles = row_tiles_most(rows, E, tile_rows(size)) * p.cols;
+    };
+    take(tile_size(rows, E));
+    if (p.size < Size::kMedium && p.tiles < kCus)
+        take(Size::kMedium);
     int64_t parts = p.tiles >= kCus ? 1 : std::min<int64_t>(kSplitAim / p.tiles, steps / kSplitSteps);
     parts = std::max<int64_t>(parts, 1);
     p.split.steps = (int32_t)((steps + parts - 1) / parts);
@@ -257,7 +294,7 @@ hipError_t launch_tiles(const ProductArgs &a, const Plan &p, hipStream_t stream)
                                        dim3((unsigned)(p.tiles * p.split.parts + 8)), S::kThreads, stream, a, p.cols, p.split);
     if (e != hipSuccess || p.split.parts == 1)
         return e;
-    const int64_t blocks = (a.rows * (a.N / 8) + 255) / 256;
+    const int64_t blocks = (a.rows * (a.N / 8) + 31) / 32;
     return launch_traced("expert_product_join", product_join_kernel<M != Mul::kBf16, GATED>, dim3((unsigned)blocks), 256,
                          stream, a, p.split);
 }
@@ -294,6 +331,7 @@ hipError_t launch_product(const ProductArgs &a, hipStream_t stream) {
     switch (p.size) {
     case Size::kLarge: return launch_shape<Large>(a, p, stream);
     case Size::kMedium: return launch_shape<Medium>(a, p, stream);
+    case Size::kWide: return launch_shape<Wide>(a, p, stream);
     case Size::kFew: return launch_shape<Few>(a, p, stream);
     default: return launch_shape<Tiny>(a, p, stream);
     }

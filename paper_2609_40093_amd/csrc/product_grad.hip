@@ -27,41 +27,57 @@ __global__ __launch_bounds__(256) void product_dz_kernel(const int32_t *offsets,
     const int32_t n = (int32_t)blockIdx.y * kDzCols + lane * 8;
     float sum[kParts][8] = {};
     if (n < N) {
-        for (int i = wave; i < rt.n; i += 4) {
-            const int64_t r = rt.row0 + i;
-            float d[8], z[kParts][8];
-            unpack8(*reinterpret_cast<const u32x4 *>(d_y + r * N + n), d);
-            if (pre)
+        // kAhead rows on their way at a time
+        constexpr int kAhead = GATED ? 2 : 4;
+        for (int i0 = wave; i0 < rt.n; i0 += 4 * kAhead) {
+            u32x4 dv[kAhead], zv[kAhead][kParts];
 #pragma unroll
-                for (int p = 0; p < kParts; ++p)
-                    unpack8(*reinterpret_cast<const u32x4 *>(pre + r * Nw + p * N + n), z[p]);
-            float o[kParts][8];
-            if (GATED) {
+            for (int u = 0; u < kAhead; ++u) {
+                const int64_t r = rt.row0 + (i0 + 4 * u < rt.n ? i0 + 4 * u : i0);
+                dv[u] = *reinterpret_cast<const u32x4 *>(d_y + r * N + n);
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    const float s = sigmoid(z[0][q]);
-                    o[0][q] = d[q] * z[kParts - 1][q] * s * (1.f + z[0][q] * (1.f - s));
-                    o[kParts - 1][q] = d[q] * z[0][q] * s;
+                for (int p = 0; p < kParts; ++p) {
+                    zv[u][p] = u32x4{0, 0, 0, 0};
+                    if (pre)
+                        zv[u][p] = *reinterpret_cast<const u32x4 *>(pre + r * Nw + p * N + n);
                 }
-            } else if (pre) {
-                activation_grad8(z[0], act);
-#pragma unroll
-                for (int q = 0; q < 8; ++q)
-                    o[0][q] = d[q] * z[0][q];
-            } else {
-#pragma unroll
-                for (int q = 0; q < 8; ++q)
-                    o[0][q] = d[q];
             }
 #pragma unroll
-            for (int p = 0; p < kParts; ++p)
-#pragma unroll
-                for (int q = 0; q < 8; ++q)
-                    sum[p][q] += o[p][q];
-            if (dz)
+            for (int u = 0; u < kAhead; ++u) {
+                if (i0 + 4 * u >= rt.n)
+                    break;
+                const int64_t r = rt.row0 + i0 + 4 * u;
+                float d[8], z[kParts][8], o[kParts][8];
+                unpack8(dv[u], d);
 #pragma unroll
                 for (int p = 0; p < kParts; ++p)
-                    *reinterpret_cast<u32x4 *>(dz + r * Nw + p * N + n) = pack8(o[p]);
+                    unpack8(zv[u][p], z[p]);
+                if (GATED) {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        const float s = sigmoid(z[0][q]);
+                        o[0][q] = d[q] * z[kParts - 1][q] * s * (1.f + z[0][q] * (1.f - s));
+                        o[kParts - 1][q] = d[q] * z[0][q] * s;
+                    }
+                } else if (pre) {
+                    activation_grad8(z[0], act);
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        o[0][q] = d[q] * z[0][q];
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        o[0][q] = d[q];
+                }
+#pragma unroll
+                for (int p = 0; p < kParts; ++p) {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        sum[p][q] += o[p][q];
+                    if (dz)
+                        *reinterpret_cast<u32x4 *>(dz + r * Nw + p * N + n) = pack8(o[p]);
+                }
+            }
         }
     }
     if (!partial)
@@ -82,21 +98,17 @@ __global__ __launch_bounds__(256) void product_dz_kernel(const int32_t *offsets,
     }
 }
 
-// dbias[e][n] = sum over the expert's row tiles, in order.
-__global__ __launch_bounds__(256) void product_dbias_kernel(const int32_t *offsets, int64_t rows, int32_t E, int32_t Nw,
-                                                            const float *partial, float *dbias) {
-    const int lane = threadIdx.x & 63, e = blockIdx.y;
-    const int64_t first = count_row_tiles(offsets, rows, e, kDzRows, lane);
+// dbias[e][n] = sum over the expert's row tiles.
+__global__ __launch_bounds__(1024) void product_dbias_kernel(const int32_t *offsets, int64_t rows, int32_t E, int32_t Nw,
+                                                             const float *partial, float *dbias) {
+    const int e = blockIdx.y;
+    const int64_t first = count_row_tiles(offsets, rows, e, kDzRows, threadIdx.x & 63);
     int64_t b, t;
     expert_rows(offsets, rows, e, b, t);
-    const int64_t tiles = (t - b + kDzRows - 1) / kDzRows;
-    const int32_t n = (int32_t)blockIdx.x * 256 + threadIdx.x;
-    if (n >= Nw)
-        return;
-    float s = 0.f;
-    for (int64_t i = 0; i < tiles; ++i)
-        s += partial[(first + i) * Nw + n];
-    dbias[(int64_t)e * Nw + n] = s;
+    const int64_t n = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31);
+    const float s = column_sum(partial, first, first + (t - b + kDzRows - 1) / kDzRows, Nw, n);
+    if (threadIdx.x < 32 && n < Nw)
+        dbias[(int64_t)e * Nw + n] = s;
 }
 
 struct GradTileArgs {
@@ -212,7 +224,7 @@ hipError_t launch_product_grad(const ProductGradArgs &a, hipStream_t stream) {
     }
     if (a.dbias) {
         const hipError_t e = launch_traced("expert_product_dbias", product_dbias_kernel,
-                                           dim3((unsigned)((a.Nw + 255) / 256), (unsigned)a.E), 256, stream, a.offsets,
+                                           dim3((unsigned)((a.Nw + 31) / 32), (unsigned)a.E), 1024, stream, a.offsets,
                                            a.rows, a.E, a.Nw, (const float *)partial, a.dbias);
         if (e != hipSuccess)
             return e;

@@ -6,13 +6,19 @@
 //   d z_i = w_i (dw_i - sum_j w_j dw_j) on the chosen (normalized gates), or the same through
 //           p (gates p), plus p_i (g_i - sum_e p_e g_e), g_e = d_loss balance E c_e / (N k N)
 //
-// A wave holds one token, lane l the NV experts [l NV, (l + 1) NV).  The k largest are picked
-// one after the other: each lane's best key, the wave's best by DPP, and the lowest lane that
-// has it gives its expert up (the lowest index among equals, since lanes hold ascending
-// ranges).  Keys are the logits' bits in integer order, so the choice is exact.  Counts go to
-// LDS integers; a lane keeps the probability sums of its own experts in registers over all
-// its tokens, and they are added up in a fixed order: over the waves in LDS, over the
+// A wave holds one token, lane l the NV experts [l NV, (l + 1) NV).  Each lane sorts its few
+// experts once; the k largest are then picked one after the other: the best of the lanes'
+// heads by DPP, the lowest lane that has it (the lowest index among equals, since lanes hold
+// ascending ranges), and that lane moves on to its next.  Keys are the logits' bits in integer
+// order, so the choice is exact.  What a pick leaves to do (the gate's exponential, the count,
+// the stores) waits for the last pick and is done by k lanes at once.  Lanes with more than 4
+// experts search them at every pick instead of sorting.
+//
+// Counts go to LDS integers; a lane keeps the probability sums of its own experts in registers
+// over all its tokens, and they are added up in a fixed order: over the waves in LDS, over the
 // workgroups by a second kernel, which also computes the loss.
+//
+// Bound by its instructions: 32768 tokens of 256 experts, top-8, are 34 MB of logits.
 #include "layer.h"
 
 namespace ep {
@@ -29,32 +35,130 @@ __device__ __forceinline__ float key_logit(uint32_t key) {
     return __uint_as_float((key >> 31) ? key ^ 0x80000000u : ~key);
 }
 
-// The logits of this lane's experts; -inf past the last expert.
-template <int NV, typename L>
+// The logits of this lane's experts; -inf past the last expert.  VEC: every lane's experts all
+// exist or all do not, and lie on a vector's boundary.
+template <int NV, bool VEC, typename L>
 __device__ __forceinline__ void load_logits(const L *row, int e0, int E, float *z) {
+    struct __attribute__((aligned(sizeof(L) * NV))) Vec {
+        L v[NV];
+    };
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        z[i] = -__builtin_inff();
+    Vec raw;
+    if (VEC) {
+        if (e0 >= E)
+            return;
+        raw = *reinterpret_cast<const Vec *>(row + e0);
+    }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        z[i] = -__builtin_inff();
-        if (e0 + i < E) {
-            if constexpr (sizeof(L) == 2)
-                z[i] = bf16_lo(row[e0 + i]);
-            else
-                z[i] = row[e0 + i];
+        if (!VEC) {
+            if (e0 + i >= E)
+                continue;
+            raw.v[i] = row[e0 + i];
         }
+        if constexpr (sizeof(L) == 2)
+            z[i] = bf16_lo(raw.v[i]);
+        else
+            z[i] = raw.v[i];
     }
+}
+template <typename L>
+__device__ __forceinline__ float one_logit(const L *row, int e) {
+    if constexpr (sizeof(L) == 2)
+        return bf16_lo(row[e]);
+    else
+        return row[e];
 }
 
 // exp(z - top) with a row of -inf alone giving zeros.
 __device__ __forceinline__ float exp_below(float z, float top) {
-    return top == -__builtin_inff() ? 0.f : expf(z - top);
+    return top == -__builtin_inff() && z == z ? 0.f : quick_exp(z - top);
 }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp_fmax(float v) {
+    const int o = __builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), CTRL, ROWS, 0xf, false);
+    return fmaxf(v, __int_as_float(o));
+}
+// Largest over the wave; NaN only where every lane has one.
+__device__ __forceinline__ float wave_fmax(float v) {
+    v = dpp_fmax<0x111, 0xf>(v);
+    v = dpp_fmax<0x112, 0xf>(v);
+    v = dpp_fmax<0x114, 0xf>(v);
+    v = dpp_fmax<0x118, 0xf>(v);
+    v = dpp_fmax<0x142, 0xa>(v);
+    v = dpp_fmax<0x143, 0xc>(v);
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
+// A lane's experts for the picks: the best one's key and number.
+template <int NV>
+struct Heads {
+    static constexpr bool kSorted = NV <= 4;
+    uint32_t key[NV];
+    int at[kSorted ? NV : 1];
+    __device__ __forceinline__ void order(int i, int j) {  // key[i] >= key[j], the lower number first among equals
+        const bool swap = key[j] > key[i];
+        const uint32_t k = swap ? key[j] : key[i];
+        const int n = swap ? at[j] : at[i];
+        key[j] = swap ? key[i] : key[j];
+        at[j] = swap ? at[i] : at[j];
+        key[i] = k;
+        at[i] = n;
+    }
+    __device__ __forceinline__ void prepare() {
+        if constexpr (kSorted) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                at[i] = i;
+            // neighbours only: a stable exchange sort keeps equals in their order
+#pragma unroll
+            for (int round = 0; round < NV; ++round)
+#pragma unroll
+                for (int i = round % 2; i + 1 < NV; i += 2)
+                    order(i, i + 1);
+        }
+    }
+    __device__ __forceinline__ uint32_t best(int &number) const {
+        if constexpr (kSorted) {
+            number = at[0];
+            return key[0];
+        } else {
+            uint32_t b = key[0];
+            number = 0;
+#pragma unroll
+            for (int i = 1; i < NV; ++i)
+                if (key[i] > b) {
+                    b = key[i];
+                    number = i;
+                }
+            return b;
+        }
+    }
+    __device__ __forceinline__ void take(bool mine, int number) {
+        if constexpr (kSorted) {
+#pragma unroll
+            for (int i = 0; i + 1 < NV; ++i) {
+                key[i] = mine ? key[i + 1] : key[i];
+                at[i] = mine ? at[i + 1] : at[i];
+            }
+            key[NV - 1] = mine ? 0u : key[NV - 1];
+        } else {
+            const int gone = mine ? number : -1;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                key[i] = i == gone ? 0u : key[i];
+        }
+    }
+};
 
 template <int NV>
 constexpr int route_waves() {
     return NV <= 8 ? 16 : 4;
 }
 
-template <int NV, typename L>
+template <int NV, bool VEC, typename L>
 __global__ __launch_bounds__(route_waves<NV>() * 64) void route_kernel(RouteArgs a) {
     constexpr int W = route_waves<NV>();
     __shared__ int counts[64 * NV];
@@ -68,7 +172,18 @@ __global__ __launch_bounds__(route_waves<NV>() * 64) void route_kernel(RouteArgs
 #pragma unroll
     for (int i = 0; i < NV; ++i)
         psum[i] = 0.f;
-    for (int64_t t = (int64_t)blockIdx.x * W + wave; t < a.T; t += (int64_t)gridDim.x * W) {
+    const int64_t stride = (int64_t)gridDim.x * W;
+    int64_t t = (int64_t)blockIdx.x * W + wave;
+    float ahead[NV];  // the next token's logits
+    if (t < a.T)
+        load_logits<NV, VEC>(static_cast<const L *>(a.logits) + t * a.E, e0, a.E, ahead);
+    for (; t < a.T; t += stride) {
+        float z[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            z[i] = ahead[i];
+        if (t + stride < a.T)
+            load_logits<NV, VEC>(static_cast<const L *>(a.logits) + (t + stride) * a.E, e0, a.E, ahead);
         const bool live = !a.mask || a.mask[t];
         int32_t *ids = a.topk_idx + t * a.k;
         float *gates = a.topk_w + t * a.k;
@@ -79,42 +194,39 @@ __global__ __launch_bounds__(route_waves<NV>() * 64) void route_kernel(RouteArgs
             }
             continue;
         }
-        float z[NV];
-        uint32_t key[NV];
-        load_logits<NV>(static_cast<const L *>(a.logits) + t * a.E, e0, a.E, z);
+        Heads<NV> heads;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-            key[i] = e0 + i < a.E ? order_key(z[i]) : 0u;
-        float top = 0.f, chosen_sum = 0.f, mine = 0.f;
-        for (int j = 0; j < a.k; ++j) {
-            uint32_t best = key[0];
-            int at = 0;
-#pragma unroll
-            for (int i = 1; i < NV; ++i)
-                if (key[i] > best) {
-                    best = key[i];
-                    at = i;
-                }
-            const uint32_t m = wave_max(best);
-            const int owner = __builtin_ctzll(__ballot(best == m));
-            const float zj = m == 1u ? __builtin_nanf("") : key_logit(m);
-            if (j == 0)
-                top = zj;
-            chosen_sum += exp_below(zj, top);
-            if (lane == owner) {
-                ids[j] = e0 + at;
-                if (a.counts)
-                    atomicAdd(&counts[e0 + at], 1);
+            heads.key[i] = e0 + i < a.E ? order_key(z[i]) : 0u;
+        heads.prepare();
+        // 64 picks at a time: lane j holds pick j's key and expert
+        float top = 0.f, chosen_sum = 0.f, gate = 0.f;
+        for (int j0 = 0; j0 < a.k; j0 += 64) {
+            const int picks = a.k - j0 < 64 ? a.k - j0 : 64;
+            uint32_t key = 0;
+            int expert = 0;
+            for (int j = 0; j < picks; ++j) {
+                int number;
+                const uint32_t b = heads.best(number);
+                const uint32_t m = wave_max(b);
+                const int owner = __builtin_ctzll(__ballot(b == m));
+                const int e = __builtin_amdgcn_readlane(e0 + number, owner);
+                key = lane == j ? m : key;
+                expert = lane == j ? e : expert;
+                heads.take(lane == owner, number);
             }
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (lane == owner && i == at)
-                    key[i] = 0;
-            if (lane == (j & 63)) {
+            float zj = key == 1u ? __builtin_nanf("") : key_logit(key);
+            if (j0 == 0)
+                top = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(zj), 0));
+            if (lane < picks) {
+                zj = exp_below(zj, top);
+                chosen_sum += zj;
+                ids[j0 + lane] = expert;
+                gate = zj;
                 if (a.k > 64)
-                    gates[j] = zj;  // the same lane reads it back below
-                else
-                    mine = zj;
+                    gates[j0 + lane] = zj;  // the same lane scales it below
+                if (a.counts)
+                    atomicAdd(&counts[expert], 1);
             }
         }
         float sum = 0.f;
@@ -124,13 +236,17 @@ __global__ __launch_bounds__(route_waves<NV>() * 64) void route_kernel(RouteArgs
             sum += z[i];
         }
         sum = wave_sum(sum);
+        chosen_sum = wave_sum(chosen_sum);
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-            psum[i] += z[i] * inv;
+            psum[i] = fmaf(z[i], inv, psum[i]);
         const float scale = !a.normalize ? inv : chosen_sum == 0.f ? 0.f : 1.f / chosen_sum;
-        for (int j = lane; j < a.k; j += 64)
-            gates[j] = exp_below(a.k > 64 ? gates[j] : mine, top) * scale;
+        if (a.k > 64)
+            for (int j = lane; j < a.k; j += 64)
+                gates[j] *= scale;
+        else if (lane < a.k)
+            gates[lane] = gate * scale;
     }
     if (!a.counts)
         return;
@@ -150,39 +266,67 @@ __global__ __launch_bounds__(route_waves<NV>() * 64) void route_kernel(RouteArgs
     }
 }
 
-// Counts and sums over the groups, then the loss.  One workgroup; L lanes share a column.
+// Counts and sums over the groups, then the loss: one workgroup.  A thread adds 4 neighbouring
+// experts' (PER; 1 where E is no multiple of 4) of every lanes-th group, kAhead groups on their
+// way at a time.
+template <int PER>
 __global__ __launch_bounds__(1024) void route_finish_kernel(const int32_t *workspace, int64_t groups, int32_t E,
                                                             int32_t k, float balance, int32_t *counts,
                                                             float *prob_sums, float *loss) {
-    __shared__ int part_n[1024];
-    __shared__ float part_s[1024];
+    struct __attribute__((aligned(4 * PER))) Vec {
+        uint32_t v[PER];
+    };
+    __shared__ int part_n[1024 * PER];
+    __shared__ float part_s[1024 * PER];
     __shared__ float wave_loss[16];
     __shared__ int wave_n[16];
+    constexpr int kAhead = 8;
     float dot = 0.f;
     int total = 0;
-    const int cols = E < 1024 ? E : 1024;
+    const int all = E / PER, cols = all < 1024 ? all : 1024;
     const int lanes = 1024 / cols, col = threadIdx.x % cols, part = threadIdx.x / cols;
-    for (int base = 0; base < E; base += cols) {
+    const Vec *table = reinterpret_cast<const Vec *>(workspace);
+    for (int base = 0; base < all; base += cols) {
         const int e = base + col;
-        int n = 0;
-        float s = 0.f;
-        if (part < lanes && e < E)
-            for (int64_t g = part; g < groups; g += lanes) {
-                n += workspace[g * 2 * E + e];
-                s += reinterpret_cast<const float *>(workspace)[g * 2 * E + E + e];
+        int n[PER] = {};
+        float s[PER] = {};
+        if (part < lanes && e < all)
+            for (int64_t g0 = part; g0 < groups; g0 += lanes * kAhead) {
+                Vec vn[kAhead], vs[kAhead];
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    const int64_t g = g0 + i * lanes;
+                    vn[i] = vs[i] = Vec{};
+                    if (g < groups) {
+                        vn[i] = table[g * 2 * all + e];
+                        vs[i] = table[g * 2 * all + all + e];
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+                    for (int q = 0; q < PER; ++q) {
+                        n[q] += (int)vn[i].v[q];
+                        s[q] += __uint_as_float(vs[i].v[q]);
+                    }
             }
-        part_n[threadIdx.x] = n;
-        part_s[threadIdx.x] = s;
+#pragma unroll
+        for (int q = 0; q < PER; ++q) {
+            part_n[q * 1024 + threadIdx.x] = n[q];
+            part_s[q * 1024 + threadIdx.x] = s[q];
+        }
         __syncthreads();
-        if (part == 0 && e < E) {
-            for (int p = 1; p < lanes; ++p) {
-                n += part_n[p * cols + col];
-                s += part_s[p * cols + col];
+        for (int c = threadIdx.x; c < cols * PER && base * PER + c < E; c += 1024) {
+            int cn = 0;
+            float cs = 0.f;
+            for (int p = 0; p < lanes; ++p) {
+                cn += part_n[c % PER * 1024 + p * cols + c / PER];
+                cs += part_s[c % PER * 1024 + p * cols + c / PER];
             }
-            counts[e] = n;
-            prob_sums[e] = s;
-            dot = fmaf((float)n, s, dot);
-            total += n;
+            counts[base * PER + c] = cn;
+            prob_sums[base * PER + c] = cs;
+            dot = fmaf((float)cn, cs, dot);
+            total += cn;
         }
         __syncthreads();
     }
@@ -207,7 +351,7 @@ __global__ __launch_bounds__(1024) void route_finish_kernel(const int32_t *works
     }
 }
 
-template <int NV, typename L>
+template <int NV, bool VEC, typename L>
 __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradArgs a) {
     __shared__ float chosen[4][64 * NV];  // per wave: the gates' gradient by expert, zero elsewhere
     __shared__ int wave_n[4];
@@ -237,108 +381,121 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradArgs a) {
             if (e0 + i < a.E)
                 g[i] = c * (float)a.counts[e0 + i];
     }
-    for (int64_t t = (int64_t)blockIdx.x * 4 + wave; t < a.T; t += (int64_t)gridDim.x * 4) {
+    const int64_t stride = (int64_t)gridDim.x * 4;
+    for (int64_t t = (int64_t)blockIdx.x * 4 + wave; t < a.T; t += stride) {
         const L *row = static_cast<const L *>(a.logits) + t * a.E;
         L *out = static_cast<L *>(a.d_logits) + t * a.E;
         const bool live = !a.mask || a.mask[t];
         float z[NV];
-        load_logits<NV>(row, e0, a.E, z);
-        uint32_t best = 0;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const uint32_t key = e0 + i < a.E ? order_key(z[i]) : 0u;
-            best = key > best ? key : best;
+        load_logits<NV, VEC>(row, e0, a.E, z);
+        // the chosen experts: lane j (and j + 64, ...) takes the j-th
+        int expert = -1;
+        float zc = 0.f, dc = 0.f;
+        if (a.d_topk_w && lane < a.k) {
+            expert = a.topk_idx[t * a.k + lane];
+            dc = a.d_topk_w[t * a.k + lane];
+            expert = expert < a.E ? expert : -1;
+            if (expert >= 0)
+                zc = one_logit(row, expert);
         }
-        const uint32_t m = wave_max(best);
-        const float top = m == 1u ? __builtin_nanf("") : key_logit(m);
+        float top = -__builtin_inff();
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            top = fmaxf(top, z[i]);
+        top = wave_fmax(top);
         float sum = 0.f, pg = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             z[i] = exp_below(z[i], top);
             sum += z[i];
+            pg = fmaf(z[i], g[i], pg);
         }
         sum = wave_sum(sum);
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            z[i] *= inv;
-            pg = fmaf(z[i], g[i], pg);
-        }
-        if (a.d_loss)
-            pg = wave_sum(pg);
+        pg = a.d_loss ? wave_sum(pg) * inv : 0.f;
         if (a.d_topk_w && live) {
             // the chosen experts' exponentials; their sum normalizes the gates
-            float es = 0.f, ed = 0.f;
-            for (int j = lane; j < a.k; j += 64) {
+            const float v = expert >= 0 ? exp_below(zc, top) : 0.f;
+            float es = v, ed = v * dc;
+            for (int j = lane + 64; j < a.k; j += 64) {
                 const int e = a.topk_idx[t * a.k + j];
                 if (e < 0 || e >= a.E)
                     continue;
-                float v;
-                if constexpr (sizeof(L) == 2)
-                    v = exp_below(bf16_lo(row[e]), top);
-                else
-                    v = exp_below(row[e], top);
-                es += v;
-                ed = fmaf(v, a.d_topk_w[t * a.k + j], ed);
+                const float u = exp_below(one_logit(row, e), top);
+                es += u;
+                ed = fmaf(u, a.d_topk_w[t * a.k + j], ed);
             }
-            es = wave_sum(es);
             ed = wave_sum(ed);
+            if (a.normalize)
+                es = wave_sum(es);
             const float scale = !a.normalize ? inv : es == 0.f ? 0.f : 1.f / es;
-            const float mean = ed * scale;
-            for (int j = lane; j < a.k; j += 64) {
+            const float mean = ed * scale, less = a.normalize ? mean : 0.f;
+            if (expert >= 0)
+                chosen[wave][expert] = v * scale * (dc - less);
+            for (int j = lane + 64; j < a.k; j += 64) {
                 const int e = a.topk_idx[t * a.k + j];
-                if (e < 0 || e >= a.E)
-                    continue;
-                float v;
-                if constexpr (sizeof(L) == 2)
-                    v = exp_below(bf16_lo(row[e]), top);
-                else
-                    v = exp_below(row[e], top);
-                chosen[wave][e] = v * scale * (a.d_topk_w[t * a.k + j] - (a.normalize ? mean : 0.f));
+                if (e >= 0 && e < a.E)
+                    chosen[wave][e] = exp_below(one_logit(row, e), top) * scale * (a.d_topk_w[t * a.k + j] - less);
             }
             if (!a.normalize)
                 pg += mean;
             __builtin_amdgcn_wave_barrier();
         }
-        float d[NV];
+        struct __attribute__((aligned(sizeof(L) * NV))) Vec {
+            L v[NV];
+        } vec;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            d[i] = fmaf(z[i], g[i] - pg, chosen[wave][e0 + i]);
+            const float d = live ? fmaf(z[i] * inv, g[i] - pg, chosen[wave][e0 + i]) : 0.f;
             chosen[wave][e0 + i] = 0.f;
-            if (!live)
-                d[i] = 0.f;
-            if (e0 + i < a.E) {
-                if constexpr (sizeof(L) == 2)
-                    out[e0 + i] = (uint16_t)bf16_pair(d[i], 0.f);
-                else
-                    out[e0 + i] = d[i];
-            }
+            if constexpr (sizeof(L) == 2)
+                vec.v[i] = (L)bf16_pair(d, 0.f);
+            else
+                vec.v[i] = d;
+        }
+        if (VEC) {
+            if (e0 < a.E)
+                *reinterpret_cast<Vec *>(out + e0) = vec;
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (e0 + i < a.E)
+                    out[e0 + i] = vec.v[i];
         }
         __builtin_amdgcn_wave_barrier();
     }
 }
 
-template <int NV, typename L>
+template <int NV, bool VEC, typename L>
 hipError_t launch_one(const RouteArgs &a, hipStream_t stream) {
     constexpr int W = route_waves<NV>();
-    return launch_traced("route", route_kernel<NV, L>, dim3((unsigned)route_groups(a.T, a.E)), W * 64, stream, a);
+    return launch_traced("route", route_kernel<NV, VEC, L>, dim3((unsigned)route_groups(a.T, a.E)), W * 64, stream, a);
 }
-template <int NV, typename L>
+template <int NV, bool VEC, typename L>
 hipError_t launch_one(const RouteGradArgs &a, hipStream_t stream) {
     const int64_t groups = std::min<int64_t>((a.T + 3) / 4, kCus * 8);
-    return launch_traced("route_grad", route_grad_kernel<NV, L>, dim3((unsigned)groups), 256, stream, a);
+    return launch_traced("route_grad", route_grad_kernel<NV, VEC, L>, dim3((unsigned)groups), 256, stream, a);
+}
+// Vector loads where a lane's NV experts end with the row and begin on a vector's boundary
+// (logits are 16-byte aligned; wider vectors than 16 bytes would need more).
+template <int NV, typename L, typename A>
+hipError_t launch_lanes(const A &a, hipStream_t stream) {
+    if constexpr (NV > 1 && NV * sizeof(L) <= 16)
+        if (a.E % NV == 0)
+            return launch_one<NV, true, L>(a, stream);
+    return launch_one<NV, false, L>(a, stream);
 }
 template <typename L, typename A>
 hipError_t launch_experts(const A &a, hipStream_t stream) {
     if (a.E <= 64)
-        return launch_one<1, L>(a, stream);
+        return launch_lanes<1, L>(a, stream);
     if (a.E <= 128)
-        return launch_one<2, L>(a, stream);
+        return launch_lanes<2, L>(a, stream);
     if (a.E <= 256)
-        return launch_one<4, L>(a, stream);
+        return launch_lanes<4, L>(a, stream);
     if (a.E <= 512)
-        return launch_one<8, L>(a, stream);
-    return a.E <= 1024 ? launch_one<16, L>(a, stream) : launch_one<32, L>(a, stream);
+        return launch_lanes<8, L>(a, stream);
+    return a.E <= 1024 ? launch_lanes<16, L>(a, stream) : launch_lanes<32, L>(a, stream);
 }
 
 }  // namespace
@@ -356,9 +513,12 @@ hipError_t launch_route(const RouteArgs &a, hipStream_t stream) {
     }
     if (!a.counts)
         return hipSuccess;
-    return launch_traced("route_finish", route_finish_kernel, dim3(1), 1024, stream, (const int32_t *)a.workspace,
-                         a.T ? route_groups(a.T, a.E) : (int64_t)0, a.E, a.k, a.balance, a.counts, a.prob_sums,
-                         a.loss);
+    const int64_t groups = a.T ? route_groups(a.T, a.E) : 0;
+#define EP_CALL(PER)                                                                                                  \
+    launch_traced("route_finish", route_finish_kernel<PER>, dim3(1), 1024, stream, (const int32_t *)a.workspace, groups, \
+                  a.E, a.k, a.balance, a.counts, a.prob_sums, a.loss)
+    return a.E % 4 == 0 ? EP_CALL(4) : EP_CALL(1);
+#undef EP_CALL
 }
 
 hipError_t launch_route_grad(const RouteGradArgs &a, hipStream_t stream) {
