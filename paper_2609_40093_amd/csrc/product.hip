@@ -236,6 +236,7 @@ typedef TileShape<256, 256, 4, 2, 2> Large;  // one workgroup per compute unit (
 typedef TileShape<256, 128, 4, 2, 2> Wide;   // one (96 KiB)
 typedef TileShape<256, 64, 4, 2, 3> Few;     // one (120 KiB)
 typedef TileShape<128, 128, 2, 2, 2> Medium; // two (64 KiB)
+typedef TileShape<64, 64, 2, 2, 4> Small;    // two (64 KiB)
 typedef TileShape<128, 32, 4, 1, 4> Tiny;    // two (80 KiB)
 
 // ---- choice of the tile and of the split, from the sizes the host knows ----------------
@@ -248,42 +249,77 @@ typedef TileShape<128, 32, 4, 1, 4> Tiny;    // two (80 KiB)
 //   mean 256  609 / 721 / 991 / 820
 // Below 80 rows the weights' bytes bound it, and what differs is how evenly the tiles fill the
 // compute units.  With less than 16 rows Tiny gains up to a tenth on Medium (16 experts, K 4096,
-// N 1536, mean 8: 84 / 93).  Where the larger tiles are fewer than the compute units, Medium takes over
-// (4096 rows of 8 experts, K 2048, N 1024: Large 64, Medium 32).
-enum class Size { kLarge, kWide, kFew, kMedium, kTiny };
+// N 1536, mean 8: 84 / 93).
+//
+// Where that tile gives fewer tiles than compute units (the dense products of a decode step,
+// few experts), the smaller tiles and the parts of the contraction are weighed by an estimate of the time: turns of the
+// workgroups, steps of a part, and for more than one part a second kernel and the fp32 sums
+// written and read again.  Measured, us, estimate's choice against the larger tile split to
+// fill the chip: 256 rows K 7168 N 256 12 / 15, 500 rows 4096 x 4096 30 / 40, 256 rows 2048 x 2048
+// 12 / 22.
+enum class Size { kLarge, kWide, kFew, kMedium, kSmall, kTiny };
 Size tile_size(int64_t rows, int32_t E) {
     const int64_t mean = rows / E;
     return mean >= 160 ? Size::kLarge : mean >= 80 ? Size::kWide : mean >= 40 ? Size::kFew : mean >= 16 ? Size::kMedium : Size::kTiny;
 }
 int tile_rows(Size s) {
-    return s == Size::kLarge ? Large::kJ : s == Size::kWide ? Wide::kJ : s == Size::kFew ? Few::kJ : s == Size::kMedium ? Medium::kJ : Tiny::kJ;
+    switch (s) {
+    case Size::kLarge: return Large::kJ;
+    case Size::kWide: return Wide::kJ;
+    case Size::kFew: return Few::kJ;
+    case Size::kMedium: return Medium::kJ;
+    case Size::kSmall: return Small::kJ;
+    default: return Tiny::kJ;
+    }
 }
-int tile_cols(Size s, bool gated) { return (s >= Size::kMedium ? Medium::kI : Large::kI) / (gated ? 2 : 1); }
+int tile_cols(Size s, bool gated) {
+    return (s < Size::kMedium ? Large::kI : s == Size::kSmall ? Small::kI : Medium::kI) / (gated ? 2 : 1);
+}
 
-constexpr int64_t kSplitAim = 2 * kCus;  // workgroups wanted
-constexpr int32_t kSplitSteps = 4;       // fewest steps of a part
 struct Plan {
     Size size;
     int64_t tiles;  // at most
     int32_t cols;
     Split split;
 };
+// Estimated us of a plan with a small tile: a step takes `one` with a workgroup per compute
+// unit and `two` with two of them, which is the most.
+double estimate(const Plan &p, int64_t rows, int64_t Nw) {
+    const double one = p.size == Size::kMedium ? 0.55 : p.size == Size::kSmall ? 0.28 : 0.30;
+    const double two = p.size == Size::kMedium ? 0.90 : p.size == Size::kSmall ? 0.43 : 0.50;
+    const int64_t groups = p.tiles * p.split.parts;
+    const double turns = groups <= kCus ? one : two * (double)((groups + 2 * kCus - 1) / (2 * kCus));
+    const double join = p.split.parts > 1 ? 3.0 + (double)p.split.parts * (double)(rows * Nw) * 8 / 3e6 : 0.0;
+    return turns * p.split.steps + join;
+}
+constexpr int32_t kSplitSteps = 4;  // fewest steps of a part
 Plan make_plan(int64_t rows, int32_t E, int32_t K, int32_t N, bool bits8, bool gated) {
-    Plan p;
     const int32_t steps = (int32_t)(((int64_t)K * (bits8 ? 1 : 2) + kStepBytes - 1) / kStepBytes);
-    const auto take = [&](Size size) {
+    const auto plan = [&](Size size, int32_t parts) {
+        Plan p;
         p.size = size;
         p.cols = (N + tile_cols(size, gated) - 1) / tile_cols(size, gated);
         p.tiles = row_tiles_most(rows, E, tile_rows(size)) * p.cols;
+        p.split.steps = (steps + parts - 1) / parts;
+        p.split.parts = (steps + p.split.steps - 1) / p.split.steps;
+        return p;
     };
-    take(tile_size(rows, E));
-    if (p.size < Size::kMedium && p.tiles < kCus)
-        take(Size::kMedium);
-    int64_t parts = p.tiles >= kCus ? 1 : std::min<int64_t>(kSplitAim / p.tiles, steps / kSplitSteps);
-    parts = std::max<int64_t>(parts, 1);
-    p.split.steps = (int32_t)((steps + parts - 1) / parts);
-    p.split.parts = (steps + p.split.steps - 1) / p.split.steps;
-    return p;
+    Plan best = plan(tile_size(rows, E), 1);
+    if (best.tiles >= kCus)
+        return best;
+    double least = 0;
+    bool any = false;
+    for (Size size : {Size::kMedium, Size::kSmall, Size::kTiny})
+        for (int32_t parts = 1; parts == 1 || steps / parts >= kSplitSteps; parts *= 2) {
+            const Plan p = plan(size, parts);
+            const double t = estimate(p, rows, (int64_t)N * (gated ? 2 : 1));
+            if (!any || t < least) {
+                any = true;
+                least = t;
+                best = p;
+            }
+        }
+    return best;
 }
 
 template <class S, Mul M, bool GATED>
@@ -331,6 +367,7 @@ hipError_t launch_product(const ProductArgs &a, hipStream_t stream) {
     switch (p.size) {
     case Size::kLarge: return launch_shape<Large>(a, p, stream);
     case Size::kMedium: return launch_shape<Medium>(a, p, stream);
+    case Size::kSmall: return launch_shape<Small>(a, p, stream);
     case Size::kWide: return launch_shape<Wide>(a, p, stream);
     case Size::kFew: return launch_shape<Few>(a, p, stream);
     default: return launch_shape<Tiny>(a, p, stream);

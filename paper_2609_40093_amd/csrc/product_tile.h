@@ -352,7 +352,8 @@ __device__ __forceinline__ void tile_product(OpA &a, OpB &b, int32_t steps, char
 // leave in whole cache lines.  (The accumulators themselves hold four columns of 32 rows per
 // instruction.)  A wave turns its own 32 rows at a time over in its own piece of LDS; a lane
 // always gets the same columns, first_col(...) + 0 .. PER-1.  What a row needs from memory
-// besides, f = fetch(row), is on its way a turn earlier.
+// besides, f = fetch(row), is on its way four turns earlier (rows past the wave's own may be
+// fetched in vain).
 template <class S, int PER>
 __device__ __forceinline__ int first_col(int wave, int lane) {
     return wave % S::kWavesI * S::FI * 32 + lane % (S::FI * 32 / PER) * PER;
@@ -362,20 +363,17 @@ __device__ __forceinline__ void tile_rows_out(const f32x16 (&acc)[S::FI][S::FJ],
                                               F result) {
     constexpr int kCols = S::FI * 32, kStride = kCols + 4;    // floats of a row, and with the padding
     constexpr int kLanes = kCols / PER, kRows = 64 / kLanes;  // lanes of a row, rows at a time
-    constexpr int kTurns = 32 / kRows;
+    constexpr int kTurns = 32 / kRows, kAhead = 4;
     static_assert(S::kWaves * 32 * kStride * 4 <= S::kStages * S::kStageBytes, "");
     float EP_LDS *own = reinterpret_cast<float EP_LDS *>(lds) + wave * 32 * kStride;
-    const int row0 = wave / S::kWavesI * S::FJ * 32, col = lane % kLanes * PER;
-    decltype(fetch(0)) got[2][kTurns];
+    const float EP_LDS *from = own + lane / kLanes * kStride + lane % kLanes * PER;
+    int row = wave / S::kWavesI * S::FJ * 32 + lane / kLanes;
+    decltype(fetch(0)) got[kAhead];
 #pragma unroll
-    for (int r = 0; r < kTurns; ++r)
-        got[0][r] = fetch(row0 + r * kRows + lane / kLanes);
+    for (int i = 0; i < kAhead; ++i)
+        got[i] = fetch(row + i * kRows);
 #pragma unroll
     for (int j = 0; j < S::FJ; ++j) {
-        if (j + 1 < S::FJ)
-#pragma unroll
-            for (int r = 0; r < kTurns; ++r)
-                got[(j + 1) % 2][r] = fetch(row0 + (j + 1) * 32 + r * kRows + lane / kLanes);
 #pragma unroll
         for (int i = 0; i < S::FI; ++i)
 #pragma unroll
@@ -383,16 +381,22 @@ __device__ __forceinline__ void tile_rows_out(const f32x16 (&acc)[S::FI][S::FJ],
                 *reinterpret_cast<f32x4 EP_LDS *>(own + lane % 32 * kStride + i * 32 + q * 8 + lane / 32 * 4) =
                     f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
         __builtin_amdgcn_wave_barrier();
-#pragma unroll
+        // not unrolled: the epilogue's code, once per turn, would not stay in the instruction cache
+#pragma unroll 1
         for (int r = 0; r < kTurns; ++r) {
-            const int row = r * kRows + lane / kLanes;
             float v[PER];
 #pragma unroll
             for (int q = 0; q < PER; q += 4) {
-                const f32x4 x = *reinterpret_cast<const f32x4 EP_LDS *>(own + row * kStride + col + q);
+                const f32x4 x = *reinterpret_cast<const f32x4 EP_LDS *>(from + r * kRows * kStride + q);
                 v[q] = x[0], v[q + 1] = x[1], v[q + 2] = x[2], v[q + 3] = x[3];
             }
-            result(row0 + j * 32 + row, first_col<S, PER>(wave, lane), v, got[j % 2][r]);
+            const auto now = got[0];
+#pragma unroll
+            for (int i = 0; i + 1 < kAhead; ++i)
+                got[i] = got[i + 1];
+            got[kAhead - 1] = fetch(row + kAhead * kRows);
+            result(row, first_col<S, PER>(wave, lane), v, now);
+            row += kRows;
         }
         __builtin_amdgcn_wave_barrier();
     }
