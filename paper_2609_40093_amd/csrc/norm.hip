@@ -54,7 +54,19 @@ __device__ __forceinline__ float row_sum(float v, float *slot, int tid) {
     return v;
 }
 
-template <int WAVES, int V>
+template <typename T>
+__device__ __forceinline__ T load_row(const T *p, bool nt) {
+    return nt ? __builtin_nontemporal_load(p) : *p;
+}
+template <typename T>
+__device__ __forceinline__ void store_row(T v, T *p, bool nt) {
+    if (nt)
+        __builtin_nontemporal_store(v, p);
+    else
+        *p = v;
+}
+
+template <int WAVES, int V, bool NT>
 __global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_kernel(NormArgs a) {
     constexpr int kRows = block_threads<WAVES>() / (WAVES * 64);
     const int tid = (int)threadIdx.x % (WAVES * 64), sub = (int)threadIdx.x / (WAVES * 64);
@@ -80,9 +92,9 @@ __global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_kernel(NormArg
             const int i = v * (WAVES * 64) + tid;
             xv[v] = rv[v] = u32x4{0, 0, 0, 0};
             if (i < vecs) {
-                xv[v] = a.x[base + i];
+                xv[v] = load_row(a.x + base + i, NT);
                 if (a.residual)
-                    rv[v] = a.residual[base + i];
+                    rv[v] = load_row(a.residual + base + i, NT);
             }
         }
 #pragma unroll
@@ -140,14 +152,14 @@ __global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_kernel(NormArg
             if (i >= vecs)
                 continue;
             if (a.total)
-                a.total[base + i] = pack8(s[v]);
+                store_row(pack8(s[v]), a.total + base + i, NT);
             float w[8], y[8];
             unpack8(wv[v], w);
 #pragma unroll
             for (int q = 0; q < 8; ++q)
                 y[q] = s[v][q] * rstd * w[q];
             if (a.out)
-                a.out[base + i] = pack8(y);
+                store_row(pack8(y), a.out + base + i, NT);
             if (a.rows8) {
                 uint32_t b[2];
 #pragma unroll
@@ -156,7 +168,7 @@ __global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_kernel(NormArg
                     b[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * h + 2] * inv, y[4 * h + 3] * inv, p, true);
                 }
                 uint8_t *dst = a.rows8 + row * (a.H + 16);
-                reinterpret_cast<uint2 *>(dst)[i] = uint2{b[0], b[1]};
+                store_row((uint64_t)b[1] << 32 | b[0], reinterpret_cast<uint64_t *>(dst) + i, NT);
             }
         }
         if (a.rows8 && tid == 0)
@@ -164,7 +176,11 @@ __global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_kernel(NormArg
     }
 }
 
-template <int WAVES, int V>
+// The rows of a workgroup follow each other, with few workgroups, so that the partial weight
+// gradients stay few.  The next row is on its way while one is reduced where a lane has two
+// vectors of it (5003 rows of 2888: 28.9 / 27.5 us); with four, the registers this takes cost more than it gives
+// (20000 rows of 7168: 196 / 215 us).
+template <int WAVES, int V, bool NT>
 __global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_grad_kernel(NormGradArgs a) {
     constexpr int kRows = block_threads<WAVES>() / (WAVES * 64);
     const int tid = (int)threadIdx.x % (WAVES * 64), sub = (int)threadIdx.x / (WAVES * 64);
@@ -183,20 +199,38 @@ __global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_grad_kernel(No
             dw[v][q] = 0.f;
     }
     int parity = 0;
-    for (int64_t row = (int64_t)blockIdx.x * kRows + sub; row < a.T; row += (int64_t)gridDim.x * kRows) {
-        const int64_t base = row * vecs;
-        u32x4 sv[V], dv[V], tv[V];
+    const int64_t stride = (int64_t)gridDim.x * kRows;
+    u32x4 sn[V], dn[V], tn[V];
+    const auto load = [&](int64_t row) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int i = v * (WAVES * 64) + tid;
-            sv[v] = dv[v] = tv[v] = u32x4{0, 0, 0, 0};
-            if (i < vecs) {
-                sv[v] = a.total[base + i];
-                dv[v] = a.d_out[base + i];
+            sn[v] = dn[v] = tn[v] = u32x4{0, 0, 0, 0};
+            if (row < a.T && i < vecs) {
+                sn[v] = load_row(a.total + row * vecs + i, NT);
+                dn[v] = load_row(a.d_out + row * vecs + i, NT);
                 if (a.d_total)
-                    tv[v] = a.d_total[base + i];
+                    tn[v] = load_row(a.d_total + row * vecs + i, NT);
             }
         }
+    };
+    constexpr bool kNextRow = V <= 2 && WAVES <= 4;
+    int64_t row = (int64_t)blockIdx.x * kRows + sub;
+    if (kNextRow)
+        load(row);
+    for (; row < a.T; row += stride) {
+        const int64_t base = row * vecs;
+        u32x4 sv[V], dv[V], tv[V];
+        if (!kNextRow)
+            load(row);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            sv[v] = sn[v];
+            dv[v] = dn[v];
+            tv[v] = tn[v];
+        }
+        if (kNextRow)
+            load(row + stride);
         float ss = 0.f, gs = 0.f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -255,13 +289,25 @@ __global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_grad_kernel(No
                 dw[v][q] = fmaf(d[q], n, dw[v][q]);
                 t[q] = fmaf(rstd, d[q] * w[q] - n * c, t[q]);
             }
-            a.dx[base + i] = pack8(t);
+            store_row(pack8(t), a.dx + base + i, NT);
         }
     }
     if (!a.d_weight)
         return;
-    // one partial row per row slot of the grid, added up in a fixed order
-    float *dst = a.partial + ((int64_t)blockIdx.x * kRows + sub) * a.H;
+    // one partial row per workgroup, added up in a fixed order
+    float *dst = a.partial + (int64_t)blockIdx.x * a.H;
+    if constexpr (kRows > 1) {
+        __shared__ float fold[kRows][V * 64 * 8];
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                fold[sub][(v * 64 + tid) * 8 + q] = dw[v][q];
+        __syncthreads();
+        for (int h = threadIdx.x; h < a.H; h += block_threads<WAVES>())
+            dst[h] = (fold[0][h] + fold[1][h]) + (fold[2][h] + fold[3][h]);
+        return;
+    }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const int i = v * (WAVES * 64) + tid;
@@ -306,45 +352,58 @@ int64_t row_groups(int64_t T, int waves, int64_t most) {
     return std::min<int64_t>((T + rows - 1) / rows, most);
 }
 
+// Rows past what the memory-side cache holds are loaded and stored non-temporally.  Measured, us:
+// rmsnorm_grad of 20000 rows of 7168 (1.1 GB) 219 / 196; the forward's at its launcher.
+constexpr int64_t kNormStreamBytes = 256ll << 20;
+
 hipError_t launch_grad_rows(const NormGradArgs &a, int64_t groups, hipStream_t stream) {
     const RowGeom g = row_geometry(a.H);
-#define EP_CALL(W, V) \
-    launch_traced("rmsnorm_grad", rmsnorm_grad_kernel<W, V>, dim3((unsigned)groups), block_threads<W>(), stream, a)
+    const bool nt = a.T * a.H * (a.d_total ? 8 : 6) >= kNormStreamBytes;
+#define EP_CALL(W, V)                                                                                              \
+    (nt ? launch_traced("rmsnorm_grad", rmsnorm_grad_kernel<W, V, true>, dim3((unsigned)groups), block_threads<W>(), \
+                        stream, a)                                                                                 \
+        : launch_traced("rmsnorm_grad", rmsnorm_grad_kernel<W, V, false>, dim3((unsigned)groups), block_threads<W>(), \
+                        stream, a))
     EP_ROW_GEOMETRY(g, EP_CALL);
 #undef EP_CALL
 }
 
 }  // namespace
 
+// A workgroup per row (or four short ones).  Rows past what the memory-side cache holds are
+// loaded and stored non-temporally.  Measured at 32768 rows of 7168 with every output (2.1 GB), us:
+// 32 workgroups per compute unit that loop over the rows 402, one per row 382, non-temporal 372; 8
+// per compute unit 415.
 hipError_t launch_rmsnorm(const NormArgs &a, hipStream_t stream) {
     if (a.T == 0)
         return hipSuccess;
     const RowGeom g = row_geometry(a.H);
-    const dim3 grid((unsigned)row_groups(a.T, g.waves, kCus * 32));
-#define EP_CALL(W, V) launch_traced("rmsnorm", rmsnorm_kernel<W, V>, grid, block_threads<W>(), stream, a)
+    const dim3 grid((unsigned)row_groups(a.T, g.waves, 1 << 21));
+    const int64_t per = 2 + (a.residual ? 2 : 0) + (a.total ? 2 : 0) + (a.out ? 2 : 0) + (a.rows8 ? 1 : 0);
+    const bool nt = a.T * a.H * per >= kNormStreamBytes;
+#define EP_CALL(W, V)                                                                                        \
+    (nt ? launch_traced("rmsnorm", rmsnorm_kernel<W, V, true>, grid, block_threads<W>(), stream, a)          \
+        : launch_traced("rmsnorm", rmsnorm_kernel<W, V, false>, grid, block_threads<W>(), stream, a))
     EP_ROW_GEOMETRY(g, EP_CALL);
 #undef EP_CALL
 }
 
-// Partial rows of the weight gradient: one per row slot of the grid.
-int64_t rmsnorm_grad_groups(int64_t T, int32_t H) {
-    const RowGeom g = row_geometry(H);
-    const int rows = g.waves < 4 ? 4 / g.waves : 1;
-    return row_groups(T, g.waves, kCus * 2) * rows;
-}
+// Workgroups, and partial rows of the weight gradient.  Two per compute unit: with one, 5003 rows
+// of 2888 take 37 us instead of 29, with four, 8192 rows of 2048 46 instead of 36 (their partials
+// grow).
+int64_t rmsnorm_grad_groups(int64_t T, int32_t H) { return row_groups(T, row_geometry(H).waves, kCus * 2); }
 
 hipError_t launch_rmsnorm_grad(const NormGradArgs &a, hipStream_t stream) {
-    const RowGeom g = row_geometry(a.H);
-    const int64_t partials = a.T ? rmsnorm_grad_groups(a.T, a.H) : 0;
+    const int64_t groups = a.T ? rmsnorm_grad_groups(a.T, a.H) : 0;
     if (a.T) {
-        const hipError_t e = launch_grad_rows(a, partials / (g.waves < 4 ? 4 / g.waves : 1), stream);
+        const hipError_t e = launch_grad_rows(a, groups, stream);
         if (e != hipSuccess || !a.d_weight)
             return e;
     }
     if (!a.d_weight)
         return hipSuccess;
     return launch_traced("rmsnorm_grad_weight", norm_weight_kernel, dim3((unsigned)((a.H + 31) / 32)), 1024, stream,
-                         (const float *)a.partial, partials, a.H, a.d_weight);
+                         (const float *)a.partial, groups, a.H, a.d_weight);
 }
 
 }  // namespace ep

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 from dataclasses import dataclass
 from typing import Optional, Tuple, Union
 
@@ -59,9 +60,11 @@ def _workspace(n: int, device) -> Optional[torch.Tensor]:
     return torch.empty(n, dtype=torch.uint8, device=device) if n else None
 
 
-def _bytes(call, name: str, *args) -> int:
+@functools.lru_cache(maxsize=4096)
+def _bytes(name: str, *args) -> int:
+    """Workspace bytes of a call: a pure function of the sizes."""
     n = ctypes.c_size_t()
-    _check(call(*args, ctypes.byref(n)), name)
+    _check(getattr(_lib_handle(), name)(*args, ctypes.byref(n)), name)
     return n.value
 
 
@@ -122,7 +125,7 @@ def rmsnorm_grad(total: torch.Tensor, weight: Optional[torch.Tensor], d_out: tor
     with _on(stream):
         dx = _output(True if dx is None else dx, "dx", torch.bfloat16, total.shape, total.device)
         d_weight = _output(d_weight, "d_weight", torch.float32, (H,), total.device)
-        n = _bytes(lib.ep_rmsnorm_grad_workspace_bytes, "ep_rmsnorm_grad_workspace_bytes", T, H) if d_weight is not None else 0
+        n = _bytes("ep_rmsnorm_grad_workspace_bytes", T, H) if d_weight is not None else 0
         ws = _workspace(n, total.device)
     _check(lib.ep_rmsnorm_grad(_ptr(total), _ptr(weight), _ptr(d_out), _ptr(d_total), T, H, eps, _ptr(dx),
                                _ptr(d_weight), _ptr(ws), n, _current_stream(stream)), "ep_rmsnorm_grad")
@@ -170,7 +173,7 @@ def route(logits: torch.Tensor, k: int, *, mask: Optional[torch.Tensor] = None, 
             _optional(out.loss, "out.loss", _F32, (1,))
         n = 0
         if out.expert_counts is not None:
-            n = _bytes(lib.ep_route_workspace_bytes, "ep_route_workspace_bytes", T, E)
+            n = _bytes("ep_route_workspace_bytes", T, E)
         ws = _workspace(n, dev)
     _check(lib.ep_route(_ptr(logits), logits.dtype == torch.bfloat16, _ptr(mask), T, E, k, normalize, balance,
                         _ptr(out.topk_idx), _ptr(out.topk_w), _ptr(out.expert_counts), _ptr(out.prob_sums),
@@ -290,7 +293,7 @@ def expert_product(x: torch.Tensor, w: torch.Tensor, offsets: Optional[torch.Ten
     with _on(stream):
         got = Product(_output(True if out is None else out, "out", out_dtype, (rows, N), x.device),
                       _output(keep_pre, "pre", torch.bfloat16, (rows, wide), x.device))
-        n = _bytes(lib.ep_expert_product_workspace_bytes, "ep_expert_product_workspace_bytes", rows, E, K, N, kind, code)
+        n = _bytes("ep_expert_product_workspace_bytes", rows, E, K, N, kind, code)
         ws = _workspace(n, x.device)
     _check(lib.ep_expert_product(
         _ptr(x), kind, rows, _ptr(offsets), E, _ptr(w), _ptr(w_scale), K, N, _ptr(bias), code, _ptr(residual),
@@ -329,7 +332,7 @@ def expert_product_grad(x: torch.Tensor, w: torch.Tensor, d_y: torch.Tensor, off
         got = ProductGrad(_output(dx, "dx", torch.bfloat16, (rows, K), x.device),
                           _output(dw, "dw", torch.bfloat16, (E, wide, K), x.device),
                           _output(dbias if dbias is not None else with_bias, "dbias", torch.float32, (E, wide), x.device))
-        n = _bytes(lib.ep_expert_product_grad_workspace_bytes, "ep_expert_product_grad_workspace_bytes", rows, E, K, N,
+        n = _bytes("ep_expert_product_grad_workspace_bytes", rows, E, K, N,
                    code, got.dbias is not None)
         ws = _workspace(n, x.device)
     _check(lib.ep_expert_product_grad(
