@@ -232,7 +232,7 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, Split 
     finish8<F8, GATED>(a, columns, x, r, n, z, up);
 }
 
-typedef TileShape<256, 256, 4, 2, 2> Large;  // one workgroup per compute unit (128 KiB of LDS)
+// Large and Broad (product_tile.h): one workgroup per compute unit (128 and 112 KiB of LDS)
 typedef TileShape<256, 128, 4, 2, 2> Wide;   // one (96 KiB)
 typedef TileShape<256, 64, 4, 2, 3> Few;     // one (120 KiB)
 typedef TileShape<128, 128, 2, 2, 2> Medium; // two (64 KiB)
@@ -257,7 +257,7 @@ typedef TileShape<128, 32, 4, 1, 4> Tiny;    // two (80 KiB)
 // written and read again.  Measured, us, estimate's choice against the larger tile split to
 // fill the chip: 256 rows K 7168 N 256 12 / 15, 500 rows 4096 x 4096 30 / 40, 256 rows 2048 x 2048
 // 12 / 22.
-enum class Size { kLarge, kWide, kFew, kMedium, kSmall, kTiny };
+enum class Size { kLarge, kBroad, kWide, kFew, kMedium, kSmall, kTiny };
 Size tile_size(int64_t rows, int32_t E) {
     const int64_t mean = rows / E;
     return mean >= 160 ? Size::kLarge : mean >= 80 ? Size::kWide : mean >= 40 ? Size::kFew : mean >= 16 ? Size::kMedium : Size::kTiny;
@@ -265,6 +265,7 @@ Size tile_size(int64_t rows, int32_t E) {
 int tile_rows(Size s) {
     switch (s) {
     case Size::kLarge: return Large::kJ;
+    case Size::kBroad: return Broad::kJ;
     case Size::kWide: return Wide::kJ;
     case Size::kFew: return Few::kJ;
     case Size::kMedium: return Medium::kJ;
@@ -305,6 +306,8 @@ Plan make_plan(int64_t rows, int32_t E, int32_t K, int32_t N, bool bits8, bool g
         return p;
     };
     Plan best = plan(tile_size(rows, E), 1);
+    if (best.size == Size::kLarge && broad_rows(rows, E, best.cols))
+        best = plan(Size::kBroad, 1);
     if (best.tiles >= kCus)
         return best;
     double least = 0;
@@ -366,6 +369,7 @@ hipError_t launch_product(const ProductArgs &a, hipStream_t stream) {
     const Plan p = make_plan(a.rows, a.E, a.K, a.N, a.bits8, a.act == EP_ACT_SWIGLU);
     switch (p.size) {
     case Size::kLarge: return launch_shape<Large>(a, p, stream);
+    case Size::kBroad: return launch_shape<Broad>(a, p, stream);
     case Size::kMedium: return launch_shape<Medium>(a, p, stream);
     case Size::kSmall: return launch_shape<Small>(a, p, stream);
     case Size::kWide: return launch_shape<Wide>(a, p, stream);

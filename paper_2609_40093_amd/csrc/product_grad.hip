@@ -151,13 +151,17 @@ template <class S>
 __global__ __launch_bounds__(S::kThreads) void product_dw_kernel(GradTileArgs a, int32_t n_tiles, int32_t k_tiles) {
     __shared__ __attribute__((aligned(1024))) char lds[S::kStages * S::kStageBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t per_expert = (int64_t)n_tiles * k_tiles;
-    const int64_t t = tile_of_block(blockIdx.x, per_expert * a.E);
-    if (t < 0)
+    // Every XCD takes a contiguous eighth of each expert's tiles, expert after expert: an expert's
+    // tiles cost as many steps as it has rows.  (With a contiguous eighth of all tiles, 8192 rows
+    // split 1520 / 6672 over two 4096 x 4096 experts took 347 us, split evenly 244.)
+    const int64_t per_expert = (int64_t)n_tiles * k_tiles, per_xcd = (per_expert + 7) / 8;
+    const int64_t turn = blockIdx.x / 8;
+    const int e = (int)(turn / per_xcd);
+    const int64_t t = blockIdx.x % 8 * per_xcd + turn % per_xcd;
+    if (t >= per_expert)
         return;
-    const int e = (int)(t / per_expert);
     int32_t tn, tk;
-    tile_order(t - e * per_expert, n_tiles, k_tiles, tn, tk);
+    tile_order(t, n_tiles, k_tiles, tn, tk);
     int64_t b, end;
     expert_rows(a.offsets, a.rows, e, b, end);
     const int32_t k0 = tk * S::kI, n0 = tn * S::kJ;
@@ -173,7 +177,6 @@ __global__ __launch_bounds__(S::kThreads) void product_dw_kernel(GradTileArgs a,
     });
 }
 
-typedef TileShape<256, 256, 4, 2, 2> Large;
 typedef TileShape<128, 128, 2, 2, 2> Medium;
 
 template <class S>
@@ -188,10 +191,15 @@ hipError_t launch_dx(const GradTileArgs &a, hipStream_t stream) {
 template <class S>
 hipError_t launch_dw(const GradTileArgs &a, hipStream_t stream) {
     const int32_t kt = (a.K + S::kI - 1) / S::kI, nt = (a.Nw + S::kJ - 1) / S::kJ;
-    if ((int64_t)kt * nt * a.E > kMostTiles)
+    const int64_t groups = ((int64_t)kt * nt + 7) / 8 * 8 * a.E;
+    if (groups > kMostTiles)
         return hipErrorInvalidConfiguration;
-    return launch_traced("expert_product_dw", product_dw_kernel<S>, dim3((unsigned)((int64_t)kt * nt * a.E + 8)),
-                         S::kThreads, stream, a, nt, kt);
+    return launch_traced("expert_product_dw", product_dw_kernel<S>, dim3((unsigned)groups), S::kThreads, stream, a, nt, kt);
+}
+
+// The large tiles where the experts fill them and there is one for every compute unit.
+bool large_rows(int64_t rows, int32_t E, int64_t cols) {
+    return rows / E >= 160 && row_tiles_most(rows, E, Large::kJ) * cols >= kCus;
 }
 
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -233,13 +241,21 @@ hipError_t launch_product_grad(const ProductGradArgs &a, hipStream_t stream) {
                    own_dz ? own_dz : (const uint16_t *)a.d_y, nullptr};
     if (a.dx && a.rows > 0) {
         g.out = static_cast<uint16_t *>(a.dx);
-        const hipError_t e = a.rows / a.E >= 192 ? launch_dx<Large>(g, stream) : launch_dx<Medium>(g, stream);
+        const int64_t cols = (a.K + Large::kI - 1) / Large::kI;
+        const hipError_t e = !large_rows(a.rows, a.E, cols)     ? launch_dx<Medium>(g, stream)
+                             : broad_rows(a.rows, a.E, cols) ? launch_dx<Broad>(g, stream)
+                                                             : launch_dx<Large>(g, stream);
         if (e != hipSuccess)
             return e;
     }
     if (a.dw) {
         g.out = static_cast<uint16_t *>(a.dw);
-        return a.K >= 512 && a.Nw >= 512 ? launch_dw<Large>(g, stream) : launch_dw<Medium>(g, stream);
+        const int64_t k = (int64_t)a.E * ((a.K + Large::kI - 1) / Large::kI);
+        const int64_t tiles = k * ((a.Nw + Large::kJ - 1) / Large::kJ);
+        if (tiles < kCus)
+            return launch_dw<Medium>(g, stream);
+        return broad_wins((double)tiles, (double)(k * ((a.Nw + Broad::kJ - 1) / Broad::kJ))) ? launch_dw<Broad>(g, stream)
+                                                                                           : launch_dw<Large>(g, stream);
     }
     return hipSuccess;
 }

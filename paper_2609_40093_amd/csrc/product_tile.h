@@ -126,8 +126,11 @@ struct AcrossC {
     int64_t rows;    // rows of the contraction left
     uint32_t offset[kLoads];
 
+    // What a row's chunk numbers are exchanged with.  It stays within the row's chunks: 4, 8 or
+    // 16 of them, or 12, where only neighbouring pairs change places.
+    static_assert(kChunks == 4 || kChunks == 8 || kChunks == 12 || kChunks == 16, "");
     __device__ __forceinline__ static int key(int row) {
-        return kChunks < 8 ? (row >> 1 & 1) << 1 : kChunks < 16 ? (row & 3) << 1 : (row & 3) << 1 | (row >> 3 & 1) << 3;
+        return kChunks % 8 ? (row >> 1 & 1) << 1 : kChunks == 8 ? (row & 3) << 1 : (row & 3) << 1 | (row >> 3 & 1) << 3;
     }
     __device__ __forceinline__ static int load_number(int wave, int q) { return (wave * kLoads + q) % (T / 8); }
 
@@ -492,6 +495,24 @@ constexpr int64_t kMostTiles = 1 << 30;  // of a grid (launch_traced refuses the
 inline int64_t row_tiles_most(int64_t rows, int32_t E, int per) {
     const int64_t some = std::min<int64_t>(E, rows);
     return some + (rows - some) / per;
+}
+
+// The two large tiles, one workgroup of 8 waves per compute unit each.  A tile of Broad takes
+// 0.78 of the time of one of Large (measured), a little more than its share; it wins where Large
+// leaves a last turn of the chip nearly empty (8192 rows of two 4096 x 4096 experts: 528 tiles of
+// Large in three turns 306 us, 699 of Broad in three turns 266 us).
+typedef TileShape<256, 256, 4, 2, 2> Large;
+typedef TileShape<256, 192, 4, 2, 2> Broad;
+inline bool broad_wins(double tiles_large, double tiles_broad) {
+    const auto turns = [](double tiles) { return (double)(int64_t)((tiles + kCus - 1) / kCus); };
+    return turns(tiles_broad) * 0.78 < turns(tiles_large);
+}
+// Row tiles to expect: half a tile more than the rows fill for every expert.
+inline double row_tiles_likely(int64_t rows, int32_t E, int per) {
+    return E == 1 ? (double)((rows + per - 1) / per) : (double)rows / per + 0.5 * E;
+}
+inline bool broad_rows(int64_t rows, int32_t E, int64_t cols) {
+    return broad_wins(row_tiles_likely(rows, E, Large::kJ) * cols, row_tiles_likely(rows, E, Broad::kJ) * cols);
 }
 
 // Activations, and their derivatives.

@@ -110,6 +110,27 @@ def test_few_rows_and_long_sums(rows, K, N):
     check(make([rows], K, N, "swiglu", rows + K, bias=True, residual=True))
 
 
+# Enough columns that every tile size has a tile for each compute unit: which size runs goes by
+# the mean rows per expert, and between the two largest by how they fill the chip.
+MANY = [[3, 0, 9], [20, 40], [37, 70, 60, 0], [100, 90, 140], [300, 190], [700, 513], [193, 1, 600], [1024], [2049]]
+
+
+@pytest.mark.parametrize("bits8", [False, True])
+@pytest.mark.parametrize("counts", MANY, ids=str)
+def test_many_columns(counts, bits8):
+    for K, N, act in ((144, 16392, "none"), (528, 8200, "swiglu")):
+        say(f"expert_product many columns rows={counts} K={K} N={N} {act} 8-bit={bits8}")
+        check(make(counts, K, N, act, K, bits8=bits8, bias=True, residual=act == "none"), f32=K == 144)
+
+
+@pytest.mark.parametrize("act", ACTS)
+def test_large_tiles_epilogues(act):
+    for counts in ([300, 190], [90, 100, 81], [45, 60, 50]):
+        say(f"expert_product many columns rows={counts} {act}")
+        for bias, residual in ((False, True), (True, False)):
+            check(make(counts, 72, 16392 if act != "swiglu" else 8200, act, 7, first=3, past=5, bias=bias, residual=residual))
+
+
 def test_rows_of_no_expert_stay():
     for rows in ([0, 0], [5, 0], [200, 90]):
         say(f"expert_product inside a larger buffer: {rows}")
@@ -281,6 +302,14 @@ def test_gradient_lengths(K, N):
         say(f"expert_product_grad rows={counts} K={K} N={N}")
         check_grad(counts, K, N, "none", N, bias=False)
         check_grad(counts, K, N, "swiglu", N)
+
+
+@pytest.mark.parametrize("counts", [[300, 190], [700, 513], [193, 1, 600], [1024], [2049], [0, 321, 0, 400]], ids=str)
+def test_gradient_many_columns(counts):
+    """dx over long rows and dw over many tiles: both large tiles."""
+    for K, N in ((16392, 72), (4104, 1032)):
+        say(f"expert_product_grad many columns rows={counts} K={K} N={N}")
+        check_grad(counts, K, N, "none", K, bias=False)
 
 
 def test_gradient_parts_and_empty():
