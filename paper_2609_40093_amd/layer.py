@@ -16,7 +16,7 @@ import torch
 
 from . import _lib
 from ._lib import EP_OUT_BF16, EP_OUT_F32, EP_ROWS8_EXTRA, EP_ROWS_8BIT, EP_ROWS_BF16
-from .api import _check, _current_stream, _lib_handle, _need, _ptr
+from .api import _check, _current_stream, _get_device, _lib_handle, _need, _ptr
 
 __all__ = ["Norm", "rmsnorm", "rmsnorm_grad", "rows8_empty", "rows8_values", "Routing", "route", "route_grad",
            "combine_grad", "Product", "expert_product", "ProductGrad", "expert_product_grad"]
@@ -42,18 +42,28 @@ def _shape(t: torch.Tensor, name: str, shape):
 
 
 def _optional(t: Optional[torch.Tensor], name: str, dtypes, shape):
-    if t is not None:
-        _need(t, name, dtypes)
-        _shape(t, name, shape)
+    """Checks an argument that may be None.  One expression for a tensor that fits."""
+    if t is None or (t.is_cuda and t.dtype in dtypes and t.shape == shape and t.is_contiguous()
+                     and t.get_device() == _get_device()):
+        return
+    _need(t, name, dtypes)
+    _shape(t, name, shape)
+
+
+def _given(t: Optional[torch.Tensor], name: str) -> torch.Tensor:
+    if t is None:
+        raise ValueError(f"{name} is required")
+    return t
 
 
 def _output(want: Union[bool, torch.Tensor, None], name: str, dtype, shape, device) -> Optional[torch.Tensor]:
     """An output to write: the tensor given, a new one for True, none for False or None."""
-    if isinstance(want, torch.Tensor):
-        _need(want, name, (dtype,))
-        _shape(want, name, shape)
-        return want
-    return torch.empty(shape, dtype=dtype, device=device) if want else None
+    if want is True:
+        return torch.empty(*shape, dtype=dtype, device=device)
+    if want is False or want is None:
+        return None
+    _optional(want, name, (dtype,), shape)
+    return want
 
 
 def _workspace(n: int, device) -> Optional[torch.Tensor]:
@@ -117,8 +127,7 @@ def rmsnorm_grad(total: torch.Tensor, weight: Optional[torch.Tensor], d_out: tor
     """ep_rmsnorm_grad: (dx bf16 [T, H], d_weight fp32 [H] or None) at the norm's `total`."""
     _need(total, "total", _BF16, 2)
     T, H = total.shape
-    _need(d_out, "d_out", _BF16)
-    _shape(d_out, "d_out", total.shape)
+    _optional(_given(d_out, "d_out"), "d_out", _BF16, total.shape)
     _optional(d_total, "d_total", _BF16, total.shape)
     _optional(weight, "weight", _BF16, (H,))
     lib = _lib_handle()
@@ -161,10 +170,10 @@ def route(logits: torch.Tensor, k: int, *, mask: Optional[torch.Tensor] = None, 
     lib, dev = _lib_handle(), logits.device
     with _on(stream):
         if out is None:
-            out = Routing(torch.empty((T, k), dtype=torch.int32, device=dev),
-                          torch.empty((T, k), dtype=torch.float32, device=dev),
-                          *((torch.empty(E, dtype=torch.int32, device=dev), torch.empty(E, device=dev),
-                             torch.empty(1, device=dev)) if counts else (None, None, None)), None, True, 0.0)
+            f32 = torch.float32
+            out = Routing(torch.empty(T, k, dtype=torch.int32, device=dev), torch.empty(T, k, dtype=f32, device=dev),
+                          *((torch.empty(E, dtype=torch.int32, device=dev), torch.empty(E, dtype=f32, device=dev),
+                             torch.empty(1, dtype=f32, device=dev)) if counts else (None, None, None)), None, True, 0.0)
         else:
             _optional(out.topk_idx, "out.topk_idx", _I32, (T, k))
             _optional(out.topk_w, "out.topk_w", _F32, (T, k))
@@ -212,15 +221,12 @@ def combine_grad(d_out: torch.Tensor, y: torch.Tensor, slot_pos: torch.Tensor, t
     """ep_combine_grad of combine_rows(y, slot_pos, topk_w): (dy bf16 like y, d_topk_w fp32
     [T, k]).  A new dy is zero where no slot names a row only if every row is named: give a
     zeroed `dy` for layouts with unnamed rows."""
-    _need(d_out, "d_out", _BF16, 2)
     _need(topk_w, "topk_w", _F32, 2)
-    T, k = topk_w.shape
-    H = d_out.shape[1]
-    _shape(d_out, "d_out", (T, H))
-    _need(slot_pos, "slot_pos", _I32, 1)
-    _shape(slot_pos, "slot_pos", (T * k,))
     _need(y, "y", _BF16, 2)
-    _shape(y, "y", (y.shape[0], H))
+    T, k = topk_w.shape
+    H = y.shape[1]
+    _optional(_given(d_out, "d_out"), "d_out", _BF16, (T, H))
+    _optional(_given(slot_pos, "slot_pos"), "slot_pos", _I32, (T * k,))
     with _on(stream):
         dy = _output(dy, "dy", torch.bfloat16, y.shape, y.device)
         d_topk_w = _output(d_topk_w, "d_topk_w", torch.float32, (T, k), y.device)
@@ -257,8 +263,7 @@ def _offsets(offsets: Optional[torch.Tensor], E: int):
         if E != 1:
             raise ValueError("more than one expert needs offsets")
     else:
-        _need(offsets, "offsets", _I32, 1)
-        _shape(offsets, "offsets", (E + 1,))
+        _optional(offsets, "offsets", _I32, (E + 1,))
 
 
 def expert_product(x: torch.Tensor, w: torch.Tensor, offsets: Optional[torch.Tensor] = None, *,
@@ -321,8 +326,7 @@ def expert_product_grad(x: torch.Tensor, w: torch.Tensor, d_y: torch.Tensor, off
     rows = x.shape[0]
     _shape(x, "x", (rows, K))
     _offsets(offsets, E)
-    _need(d_y, "d_y", _BF16, 2)
-    _shape(d_y, "d_y", (rows, N))
+    _optional(_given(d_y, "d_y"), "d_y", _BF16, (rows, N))
     code = _act(act)
     if act != "none" and pre is None:
         raise ValueError("an activation's gradient needs pre")

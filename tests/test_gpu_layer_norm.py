@@ -161,3 +161,30 @@ def test_gradient_against_differences():
     assert abs((dx.double() * v).sum() - along) <= (v.abs() * (dx.double().abs() * 2 * ref.BF16 + size[1] * 2.0 ** -14)).sum() + 1e-4
     along = (loss(s, w.double() + h * u) - loss(s, w.double() - h * u)) / (2 * h)
     assert abs((dw.double() * u).sum() - along) <= (u.abs() * size[3]).sum() * 2.0 ** -13 + 1e-4
+
+
+def test_binding_refusals():
+    """Wrong devices, types, layouts and shapes raise before anything is enqueued."""
+    say("rmsnorm: refusals of the binding")
+    g = ref.gen(1)
+    x, w = ref.normal((6, 64), g), ref.normal(64, g)
+    for bad in (x.cpu(), x.float(), x.t(), x[:, ::2], x[0], x[:, 8:]):
+        with pytest.raises(ValueError):
+            ep.rmsnorm(bad, None)
+    for bad in (w[:32], w.float(), w.cpu()):
+        with pytest.raises(ValueError):
+            ep.rmsnorm(x, bad)
+    with pytest.raises(ValueError):
+        ep.rmsnorm(x, w, residual=x[:5])
+    with pytest.raises(ValueError):
+        ep.rmsnorm(x, w, out=x.float())
+    with pytest.raises(ep.EPError):
+        ep.rmsnorm(x, w, out=False)
+    with pytest.raises(ep.EPError):
+        ep.rmsnorm(ref.normal((6, 72), g), rows8=True)
+    with pytest.raises(ValueError):
+        ep.rmsnorm_grad(x, w, None)
+    with pytest.raises(ValueError):
+        ep.rmsnorm_grad(x, w, x[:3])
+    with pytest.raises(ValueError):
+        ep.rmsnorm_grad(x, w, x, d_weight=torch.zeros(64, device="cuda", dtype=torch.bfloat16))

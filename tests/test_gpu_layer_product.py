@@ -349,3 +349,33 @@ def test_gradient_against_differences():
             along = (loss(*up) - loss(*down)) / (2 * h)
             # pre is bf16: the slope is taken up to 2^-8 |z| beside z, and dz and the result are rounded
             assert abs((grad.double() * v).sum() - along) <= 0.02 * float((grad.double() * v).abs().sum()), (act, i)
+
+
+def test_binding_refusals():
+    """Wrong devices, types, layouts and shapes raise before anything is enqueued."""
+    say("expert_product: refusals of the binding")
+    s = make([3, 2], 64, 32, "none", 1)
+    x, w, off = s["x"], s["w"], s["offsets"]
+    for bad in (x.cpu(), x.float(), x.t(), x[:, :48], x[0]):
+        with pytest.raises(ValueError):
+            ep.expert_product(bad, w, off)
+    for bad in (w.float(), w.transpose(1, 2), w[0], w.cpu()):
+        with pytest.raises(ValueError):
+            ep.expert_product(x, bad, off)
+    for bad in (None, off[:2], off.long(), off.cpu()):
+        with pytest.raises(ValueError):
+            ep.expert_product(x, w, bad)
+    for more in (dict(act="tanh"), dict(bias=w[0]), dict(residual=x), dict(out=x), dict(out_dtype=torch.float16),
+                 dict(w_scale=torch.ones((2, 31), device="cuda")), dict(keep_pre=x)):
+        with pytest.raises(ValueError):
+            ep.expert_product(x, w, off, **more)
+    with pytest.raises(ep.EPError):
+        ep.expert_product(x, w, off, w_scale=torch.ones((2, 32), device="cuda"))   # scales go with 8-bit rows
+    with pytest.raises(ValueError):
+        ep.expert_product(ep.rows8_empty(5, 64), w.to(torch.float8_e4m3fn), off)
+    d_y = torch.zeros((5, 32), dtype=torch.bfloat16, device="cuda")
+    for bad in (None, d_y[:4], d_y.float()):
+        with pytest.raises(ValueError):
+            ep.expert_product_grad(x, w, bad, off)
+    with pytest.raises(ValueError):
+        ep.expert_product_grad(x, w, d_y, off, act="silu")

@@ -197,3 +197,25 @@ def test_gradient_against_differences(normalize):
     h = 1e-4
     along = (loss(z.cpu().double() + h * v) - loss(z.cpu().double() - h * v)) / (2 * h)
     assert abs((dz.cpu().double() * v).sum() - along) <= 1e-4 * (1 + float(d.abs().sum()) * 1e-2)
+
+
+def test_binding_refusals():
+    """Wrong devices, types, layouts and shapes raise before anything is enqueued."""
+    say("route: refusals of the binding")
+    z = torch.randn((6, 16), device="cuda")
+    got = ep.route(z, 2)
+    for bad in (z.cpu(), z.double(), z.t(), z[:, ::2], z[0]):
+        with pytest.raises(ValueError):
+            ep.route(bad, 2)
+    for k in (0, 17):
+        with pytest.raises((ep.EPError, RuntimeError)):
+            ep.route(z, k)
+    with pytest.raises(ValueError):
+        ep.route(z, 2, mask=torch.ones(5, dtype=torch.bool, device="cuda"))
+    with pytest.raises(ValueError):
+        ep.route(z, 3, out=got)
+    for bad in (torch.zeros((6, 3), device="cuda"), torch.zeros((6, 2), device="cuda", dtype=torch.float64), torch.zeros((6, 2))):
+        with pytest.raises(ValueError):
+            ep.route_grad(z, got, bad)
+    with pytest.raises(ValueError):
+        ep.route_grad(z, got, None, torch.zeros((), device="cuda"))
