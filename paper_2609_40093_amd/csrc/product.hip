@@ -232,12 +232,9 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, Split 
     finish8<F8, GATED>(a, columns, x, r, n, z, up);
 }
 
-// Large and Broad (product_tile.h): one workgroup per compute unit (128 and 112 KiB of LDS)
-typedef TileShape<256, 128, 4, 2, 2> Wide;   // one (96 KiB)
+// Besides the sizes of product_tile.h, for many experts of few rows:
+typedef TileShape<256, 128, 4, 2, 2> Wide;   // one workgroup per compute unit (96 KiB of LDS)
 typedef TileShape<256, 64, 4, 2, 3> Few;     // one (120 KiB)
-typedef TileShape<128, 128, 2, 2, 2> Medium; // two (64 KiB)
-typedef TileShape<64, 64, 2, 2, 4> Small;    // two (64 KiB)
-typedef TileShape<128, 32, 4, 1, 4> Tiny;    // two (80 KiB)
 
 // ---- choice of the tile and of the split, from the sizes the host knows ----------------
 // By the mean rows per expert.  Measured, us (bf16 gated, 32 experts, K 7168, N 2048; then 128
@@ -252,9 +249,8 @@ typedef TileShape<128, 32, 4, 1, 4> Tiny;    // two (80 KiB)
 // N 1536, mean 8: 84 / 93).
 //
 // Where that tile gives fewer tiles than compute units (the dense products of a decode step,
-// few experts), the smaller tiles and the parts of the contraction are weighed by an estimate of the time: turns of the
-// workgroups, steps of a part, and for more than one part a second kernel and the fp32 sums
-// written and read again.  Measured, us, estimate's choice against the larger tile split to
+// few experts), the smaller tiles and the parts of the contraction are weighed by an estimate of the time
+// (product_tile.h).  Measured, us, estimate's choice against the larger tile split to
 // fill the chip: 256 rows K 7168 N 256 12 / 15, 500 rows 4096 x 4096 30 / 40, 256 rows 2048 x 2048
 // 12 / 22.
 enum class Size { kLarge, kBroad, kWide, kFew, kMedium, kSmall, kTiny };
@@ -283,17 +279,6 @@ struct Plan {
     int32_t cols;
     Split split;
 };
-// Estimated us of a plan with a small tile: a step takes `one` with a workgroup per compute
-// unit and `two` with two of them, which is the most.
-double estimate(const Plan &p, int64_t rows, int64_t Nw) {
-    const double one = p.size == Size::kMedium ? 0.55 : p.size == Size::kSmall ? 0.28 : 0.30;
-    const double two = p.size == Size::kMedium ? 0.90 : p.size == Size::kSmall ? 0.43 : 0.50;
-    const int64_t groups = p.tiles * p.split.parts;
-    const double turns = groups <= kCus ? one : two * (double)((groups + 2 * kCus - 1) / (2 * kCus));
-    const double join = p.split.parts > 1 ? 3.0 + (double)p.split.parts * (double)(rows * Nw) * 8 / 3e6 : 0.0;
-    return turns * p.split.steps + join;
-}
-constexpr int32_t kSplitSteps = 4;  // fewest steps of a part
 Plan make_plan(int64_t rows, int32_t E, int32_t K, int32_t N, bool bits8, bool gated) {
     const int32_t steps = (int32_t)(((int64_t)K * (bits8 ? 1 : 2) + kStepBytes - 1) / kStepBytes);
     const auto plan = [&](Size size, int32_t parts) {
@@ -315,7 +300,8 @@ Plan make_plan(int64_t rows, int32_t E, int32_t K, int32_t N, bool bits8, bool g
     for (Size size : {Size::kMedium, Size::kSmall, Size::kTiny})
         for (int32_t parts = 1; parts == 1 || steps / parts >= kSplitSteps; parts *= 2) {
             const Plan p = plan(size, parts);
-            const double t = estimate(p, rows, (int64_t)N * (gated ? 2 : 1));
+            const StepCost cost = size == Size::kMedium ? kMediumCost : size == Size::kSmall ? kSmallCost : kTinyCost;
+            const double t = estimate(cost, p.tiles, p.split.parts, p.split.steps, rows * N * (gated ? 2 : 1));
             if (!any || t < least) {
                 any = true;
                 least = t;

@@ -117,6 +117,8 @@ struct GradTileArgs {
     int32_t E, K, Nw;
     const uint16_t *x, *w, *dz;
     uint16_t *out;
+    float *partial;  // dw in parts: [parts][E][Nw][K]
+    int32_t parts;
 };
 
 // dx[r][k] = sum_n dz[r][n] W_e[n][k]: i = k across the contraction, j = rows along it.
@@ -156,7 +158,8 @@ __global__ __launch_bounds__(S::kThreads) void product_dw_kernel(GradTileArgs a,
     // split 1520 / 6672 over two 4096 x 4096 experts took 347 us, split evenly 244.)
     const int64_t per_expert = (int64_t)n_tiles * k_tiles, per_xcd = (per_expert + 7) / 8;
     const int64_t turn = blockIdx.x / 8;
-    const int e = (int)(turn / per_xcd);
+    const int32_t part = (int32_t)(turn / per_xcd % a.parts);
+    const int e = (int)(turn / per_xcd / a.parts);
     const int64_t t = blockIdx.x % 8 * per_xcd + turn % per_xcd;
     if (t >= per_expert)
         return;
@@ -170,14 +173,51 @@ __global__ __launch_bounds__(S::kThreads) void product_dw_kernel(GradTileArgs a,
     x.init(reinterpret_cast<const char *>(a.x + b * a.K), (int64_t)a.K * 2, end - b, k0, wave, lane);
     z.init(reinterpret_cast<const char *>(a.dz + b * a.Nw), (int64_t)a.Nw * 2, end - b, n0, wave, lane);
     f32x16 acc[S::FI][S::FJ] = {};
-    tile_product<S, Mul::kBf16>(x, z, (int32_t)((end - b + kStepRows - 1) / kStepRows), (char EP_LDS *)lds, wave, lane, acc);
+    const int32_t all = (int32_t)((end - b + kStepRows - 1) / kStepRows), per = (all + a.parts - 1) / a.parts;
+    const int32_t first = part * per, steps = all - first < per ? all - first : per;  // of this part; 0 or less: none
+    x.skip(first);
+    z.skip(first);
+    tile_product<S, Mul::kBf16>(x, z, steps, (char EP_LDS *)lds, wave, lane, acc);
     tile_results<S>(acc, (char EP_LDS *)lds, wave, lane, [&](int row, int col, const float *v) {
-        if (n0 + row < a.Nw && k0 + col < a.K)
+        if (n0 + row >= a.Nw || k0 + col >= a.K)
+            return;
+        if (a.parts == 1) {
             *reinterpret_cast<u32x4 *>(a.out + ((int64_t)e * a.Nw + n0 + row) * a.K + k0 + col) = pack8(v);
+        } else {
+            f32x4 *dst = reinterpret_cast<f32x4 *>(a.partial + (((int64_t)part * a.E + e) * a.Nw + n0 + row) * a.K + k0 + col);
+            dst[0] = f32x4{v[0], v[1], v[2], v[3]};
+            dst[1] = f32x4{v[4], v[5], v[6], v[7]};
+        }
     });
 }
 
-typedef TileShape<128, 128, 2, 2, 2> Medium;
+// dw from its parts, added in order: eight values per thread.
+__global__ __launch_bounds__(256) void product_dw_join_kernel(const float *partial, int32_t parts, int64_t groups,
+                                                              uint16_t *dw) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= groups)
+        return;
+    float s[8] = {};
+    const f32x4 *src = reinterpret_cast<const f32x4 *>(partial) + i * 2;
+    constexpr int kAhead = 4;
+    for (int32_t p0 = 0; p0 < parts; p0 += kAhead) {
+        f32x4 v[kAhead][2];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                v[u][h] = f32x4{};
+                if (p0 + u < parts)
+                    v[u][h] = src[(p0 + u) * groups * 2 + h];
+            }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                s[q] += v[u][q / 4][q % 4];
+    }
+    reinterpret_cast<u32x4 *>(dw)[i] = pack8(s);
+}
 
 template <class S>
 hipError_t launch_dx(const GradTileArgs &a, hipStream_t stream) {
@@ -188,10 +228,20 @@ hipError_t launch_dx(const GradTileArgs &a, hipStream_t stream) {
     return launch_traced("expert_product_dx", product_dx_kernel<S>, dim3((unsigned)(tiles + 8)), S::kThreads, stream, a,
                          cols);
 }
+// The smaller of the tiles by the estimate of their time (300 rows 2048 x 2048: 28 us with
+// Medium, 13 with Small).
+hipError_t launch_dx_small(const GradTileArgs &a, hipStream_t stream) {
+    const int32_t steps = (a.Nw + kStepRows - 1) / kStepRows;
+    const auto cost = [&](StepCost c, int i, int j) {
+        return estimate(c, row_tiles_most(a.rows, a.E, j) * ((a.K + i - 1) / i), 1, steps, 0);
+    };
+    return cost(kSmallCost, Small::kI, Small::kJ) < cost(kMediumCost, Medium::kI, Medium::kJ) ? launch_dx<Small>(a, stream)
+                                                                                             : launch_dx<Medium>(a, stream);
+}
 template <class S>
 hipError_t launch_dw(const GradTileArgs &a, hipStream_t stream) {
     const int32_t kt = (a.K + S::kI - 1) / S::kI, nt = (a.Nw + S::kJ - 1) / S::kJ;
-    const int64_t groups = ((int64_t)kt * nt + 7) / 8 * 8 * a.E;
+    const int64_t groups = ((int64_t)kt * nt + 7) / 8 * 8 * a.E * a.parts;
     if (groups > kMostTiles)
         return hipErrorInvalidConfiguration;
     return launch_traced("expert_product_dw", product_dw_kernel<S>, dim3((unsigned)groups), S::kThreads, stream, a, nt, kt);
@@ -202,23 +252,62 @@ bool large_rows(int64_t rows, int32_t E, int64_t cols) {
     return rows / E >= 160 && row_tiles_most(rows, E, Large::kJ) * cols >= kCus;
 }
 
+// The tile and the parts of dw, from the rows per expert to expect.  Small tiles and parts where
+// the large tiles are fewer than the compute units: dw of 11253 rows, one 2432 x 512 expert.
+enum class DwSize { kLarge, kBroad, kMedium, kSmall };
+struct DwPlan {
+    DwSize size;
+    int32_t parts;
+};
+DwPlan plan_dw(int64_t rows, int32_t E, int32_t K, int64_t Nw) {
+    const auto tiles = [&](int i, int j) { return (int64_t)E * ((K + i - 1) / i) * ((Nw + j - 1) / j); };
+    const int64_t large = tiles(Large::kI, Large::kJ);
+    if (large >= kCus)
+        return {broad_wins((double)large, (double)tiles(Broad::kI, Broad::kJ)) ? DwSize::kBroad : DwSize::kLarge, 1};
+    const int32_t steps = (int32_t)std::max<int64_t>(1, (rows / E + kStepRows - 1) / kStepRows);
+    DwPlan best{DwSize::kMedium, 1};
+    double least = 0;
+    for (DwSize size : {DwSize::kMedium, DwSize::kSmall})
+        for (int32_t parts = 1; parts == 1 || steps / parts >= kSplitSteps; parts *= 2) {
+            const bool medium = size == DwSize::kMedium;
+            const double t = estimate(medium ? kMediumCost : kSmallCost,
+                                      medium ? tiles(Medium::kI, Medium::kJ) : tiles(Small::kI, Small::kJ), parts,
+                                      (steps + parts - 1) / parts, E * Nw * K);
+            if (least == 0 || t < least) {
+                least = t;
+                best = {size, parts};
+            }
+        }
+    return best;
+}
+
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// dz [rows][Nw] bf16 (with an activation), then the bias's partial sums [row tiles][Nw] fp32, then
+// dw's parts [parts][E][Nw][K] fp32 (more than one).
+struct GradWorkspace {
+    size_t bias = 0, parts = 0, bytes = 0;  // offsets, and the size
+    GradWorkspace(int64_t rows, int32_t E, int32_t K, int64_t Nw, int32_t act, bool with_bias, int32_t dw_parts) {
+        bias = act == EP_ACT_NONE ? 0 : align256((size_t)(rows * Nw * 2));
+        parts = bias + (with_bias ? align256((size_t)(row_tiles_most(rows, E, kDzRows) * Nw * 4)) : 0);
+        bytes = parts + (dw_parts > 1 ? (size_t)dw_parts * E * Nw * K * 4 : 0);
+    }
+};
 
 }  // namespace
 
-// dz [rows][Nw] bf16 (with an activation), then the bias's partial sums [row tiles][Nw] fp32.
-size_t product_grad_workspace_bytes(int64_t rows, int32_t E, int32_t, int32_t N, int32_t act, bool bias) {
+size_t product_grad_workspace_bytes(int64_t rows, int32_t E, int32_t K, int32_t N, int32_t act, bool bias) {
     const int64_t Nw = act == EP_ACT_SWIGLU ? 2 * (int64_t)N : N;
-    const size_t dz = act == EP_ACT_NONE ? 0 : align256((size_t)(rows * Nw * 2));
-    return dz + (bias ? (size_t)(row_tiles_most(rows, E, kDzRows) * Nw * 4) : 0);
+    return GradWorkspace(rows, E, K, Nw, act, bias, plan_dw(rows, E, K, Nw).parts).bytes;
 }
 
 hipError_t launch_product_grad(const ProductGradArgs &a, hipStream_t stream) {
     uint16_t *own_dz = a.act == EP_ACT_NONE ? nullptr : static_cast<uint16_t *>(a.workspace);
+    const DwPlan dw = plan_dw(a.rows, a.E, a.K, a.Nw);
+    const GradWorkspace ws(a.rows, a.E, a.K, a.Nw, a.act, a.dbias != nullptr, dw.parts);
     float *partial = nullptr;
     if (a.dbias)
-        partial = reinterpret_cast<float *>(static_cast<char *>(a.workspace) +
-                                            (own_dz ? align256((size_t)(a.rows * a.Nw * 2)) : 0));
+        partial = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + ws.bias);
     if (a.rows > 0 && (own_dz || partial)) {
         const dim3 grid((unsigned)row_tiles_most(a.rows, a.E, kDzRows), (unsigned)((a.N + kDzCols - 1) / kDzCols));
         uint16_t *dz = a.dx || a.dw ? own_dz : nullptr;
@@ -238,11 +327,11 @@ hipError_t launch_product_grad(const ProductGradArgs &a, hipStream_t stream) {
             return e;
     }
     GradTileArgs g{a.offsets, a.rows, a.E, a.K, a.Nw, (const uint16_t *)a.x, (const uint16_t *)a.w,
-                   own_dz ? own_dz : (const uint16_t *)a.d_y, nullptr};
+                   own_dz ? own_dz : (const uint16_t *)a.d_y, nullptr, nullptr, 1};
     if (a.dx && a.rows > 0) {
         g.out = static_cast<uint16_t *>(a.dx);
         const int64_t cols = (a.K + Large::kI - 1) / Large::kI;
-        const hipError_t e = !large_rows(a.rows, a.E, cols)     ? launch_dx<Medium>(g, stream)
+        const hipError_t e = !large_rows(a.rows, a.E, cols) ? launch_dx_small(g, stream)
                              : broad_rows(a.rows, a.E, cols) ? launch_dx<Broad>(g, stream)
                                                              : launch_dx<Large>(g, stream);
         if (e != hipSuccess)
@@ -250,12 +339,17 @@ hipError_t launch_product_grad(const ProductGradArgs &a, hipStream_t stream) {
     }
     if (a.dw) {
         g.out = static_cast<uint16_t *>(a.dw);
-        const int64_t k = (int64_t)a.E * ((a.K + Large::kI - 1) / Large::kI);
-        const int64_t tiles = k * ((a.Nw + Large::kJ - 1) / Large::kJ);
-        if (tiles < kCus)
-            return launch_dw<Medium>(g, stream);
-        return broad_wins((double)tiles, (double)(k * ((a.Nw + Broad::kJ - 1) / Broad::kJ))) ? launch_dw<Broad>(g, stream)
-                                                                                           : launch_dw<Large>(g, stream);
+        g.parts = dw.parts;
+        g.partial = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + ws.parts);
+        const hipError_t e = dw.size == DwSize::kLarge    ? launch_dw<Large>(g, stream)
+                             : dw.size == DwSize::kBroad  ? launch_dw<Broad>(g, stream)
+                             : dw.size == DwSize::kMedium ? launch_dw<Medium>(g, stream)
+                                                          : launch_dw<Small>(g, stream);
+        if (e != hipSuccess || dw.parts == 1)
+            return e;
+        const int64_t groups = (int64_t)a.E * a.Nw * a.K / 8;
+        return launch_traced("expert_product_dw_join", product_dw_join_kernel, dim3((unsigned)((groups + 255) / 256)), 256,
+                             stream, (const float *)g.partial, dw.parts, groups, g.out);
     }
     return hipSuccess;
 }

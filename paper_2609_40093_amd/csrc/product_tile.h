@@ -145,6 +145,10 @@ struct AcrossC {
             offset[q] = (uint32_t)(row * stride + index0 * 2 + (chunk ^ key(row)) * 32 + half * 16);
         }
     }
+    __device__ __forceinline__ void skip(int32_t steps) {
+        base += (int64_t)steps * kStepRows * stride;
+        rows -= (int64_t)steps * kStepRows;
+    }
     __amdgpu_buffer_rsrc_t range;
     __device__ __forceinline__ void begin(bool live) {
         const int64_t n = !live ? 0 : rows < kStepRows ? rows : kStepRows;
@@ -514,6 +518,25 @@ inline double row_tiles_likely(int64_t rows, int32_t E, int per) {
 inline bool broad_rows(int64_t rows, int32_t E, int64_t cols) {
     return broad_wins(row_tiles_likely(rows, E, Large::kJ) * cols, row_tiles_likely(rows, E, Broad::kJ) * cols);
 }
+
+// Small tiles, for sizes with fewer large tiles than compute units.  What a step takes with a
+// workgroup per compute unit (`one`) and with two (`two`), in us, measured; two are the most.
+typedef TileShape<128, 128, 2, 2, 2> Medium;  // two workgroups per compute unit (64 KiB of LDS)
+typedef TileShape<64, 64, 2, 2, 4> Small;     // two (64 KiB)
+typedef TileShape<128, 32, 4, 1, 4> Tiny;     // two (80 KiB)
+struct StepCost {
+    double one, two;
+};
+constexpr StepCost kMediumCost{0.55, 0.90}, kSmallCost{0.28, 0.43}, kTinyCost{0.30, 0.50};
+// Estimated us of `tiles` tiles whose contraction is cut into `parts` of `steps` steps: the
+// turns of the workgroups, and for more than one part a second kernel and the fp32 sums
+// written and read again.
+inline double estimate(StepCost cost, int64_t tiles, int32_t parts, int32_t steps, int64_t outputs) {
+    const int64_t groups = tiles * parts;
+    const double turns = groups <= kCus ? cost.one : cost.two * (double)((groups + 2 * kCus - 1) / (2 * kCus));
+    return turns * steps + (parts > 1 ? 3.0 + (double)parts * (double)outputs * 8 / 3e6 : 0.0);
+}
+constexpr int32_t kSplitSteps = 4;  // fewest steps of a part
 
 // Activations, and their derivatives.
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + quick_exp(-z)); }

@@ -312,6 +312,16 @@ def test_gradient_many_columns(counts):
         check_grad(counts, K, N, "none", K, bias=False)
 
 
+@pytest.mark.parametrize("counts", [[5000], [3000, 0, 100], [1, 2500], [700] * 5], ids=str)
+def test_gradient_of_many_rows(counts):
+    """dw of few tiles, whose rows are split into parts, and the same bits at every call."""
+    for K, N, act in ((72, 40, "none"), (520, 264, "gelu"), (136, 72, "swiglu")):
+        say(f"expert_product_grad rows={counts} K={K} N={N} {act}")
+        s, d_y, pre, got = check_grad(counts, K, N, act, K)
+        again = ep.expert_product_grad(s["x"], s["w"], d_y, s["offsets"], pre=pre, act=act, with_bias=True)
+        assert torch.equal(again.dw, got.dw) and torch.equal(again.dx, got.dx) and torch.equal(again.dbias, got.dbias)
+
+
 def test_gradient_parts_and_empty():
     say("expert_product_grad: parts, rows of no expert, no rows")
     s, d_y, pre, whole = check_grad([90, 0, 200], 264, 136, "gelu", 3, first=5, past=70)
