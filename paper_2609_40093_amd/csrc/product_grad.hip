@@ -5,6 +5,11 @@
 // dz is d_y itself and no bias is wanted), then two matrix products on the tile of
 // product_tile.h.  Neither needs a transposed copy: W in dx, and dz and x in dw, are read
 // across the contraction by the transposing LDS load.
+//
+// 8192 rows of two 4096 x 4096 experts through gelu, with a bias: dz 46 us, dbias 5, dx 259 (1060
+// TFLOP/s), dw 222 (1240).  dx is the slower since the two experts' rows fill no whole number of
+// tiles nor of the chip's turns; both products are bound by the matrix cores and the LDS reads
+// that feed them.
 #include "product_tile.h"
 
 namespace ep {
@@ -133,6 +138,8 @@ __global__ __launch_bounds__(S::kThreads) void product_dx_kernel(GradTileArgs a,
     int32_t tr, tc;
     tile_order(t, row_tiles, col_tiles, tr, tc);
     const RowTile rt = find_row_tile(a.offsets, a.rows, a.E, S::kJ, tr, lane);
+    if (rt.e < 0)
+        return;
     const int32_t k0 = tc * S::kI;
     AcrossC<S::kI, S::kWaves, S::FI> w;
     AlongC<S::kJ, S::kWaves> z;
@@ -228,8 +235,8 @@ hipError_t launch_dx(const GradTileArgs &a, hipStream_t stream) {
     return launch_traced("expert_product_dx", product_dx_kernel<S>, dim3((unsigned)(tiles + 8)), S::kThreads, stream, a,
                          cols);
 }
-// The smaller of the tiles by the estimate of their time (300 rows 2048 x 2048: 28 us with
-// Medium, 13 with Small).
+// The smaller of the tiles by the estimate of their time (300 rows 2048 x 2048, a call's dx and
+// dw: 28 us with Medium alone, 21).
 hipError_t launch_dx_small(const GradTileArgs &a, hipStream_t stream) {
     const int32_t steps = (a.Nw + kStepRows - 1) / kStepRows;
     const auto cost = [&](StepCost c, int i, int j) {

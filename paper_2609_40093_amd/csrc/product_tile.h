@@ -421,7 +421,6 @@ struct RowTile {
     int32_t e;     // expert, -1: no such tile
     int64_t row0;  // first row
     int32_t n;     // rows of the expert from row0 on, at most `per`
-    int64_t tiles; // row tiles in all
 };
 
 __device__ __forceinline__ int64_t clamp_row(int64_t r, int64_t rows) { return r < 0 ? 0 : r > rows ? rows : r; }
@@ -466,11 +465,11 @@ __device__ __forceinline__ RowTile find_row_tile(const int32_t *offsets, int64_t
             const int64_t end = (int64_t)__builtin_amdgcn_readlane((int32_t)t, at);
             const int64_t row0 = begin + (int64_t)tile * per;
             const int64_t left = end - row0;
-            return {e0 + at, row0, (int32_t)(left < per ? left : per), 0};
+            return {e0 + at, row0, (int32_t)(left < per ? left : per)};
         }
         before += __builtin_amdgcn_readlane(incl, 63);
     }
-    return {-1, 0, 0, 0};
+    return {-1, 0, 0};
 }
 
 // ---- order of the tiles -----------------------------------------------------------

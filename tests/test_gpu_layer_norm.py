@@ -91,6 +91,60 @@ def test_extremes_stay_in_their_rows():
     assert scale[3].isnan() and scale[4].isnan() and not scale[[0, 1, 2, 5, 6, 7]].isnan().any()
 
 
+def test_rows_past_4_gib():
+    """Rows whose byte offsets pass 32 bits, and the traffic that goes non-temporally."""
+    say("rmsnorm past 4 GiB")
+    H = 7168
+    T = (1 << 32) // (2 * H) + 400
+    g = ref.gen(21)
+    x = torch.zeros((T, H), dtype=torch.bfloat16, device="cuda")
+    w = ref.normal(H, g)
+    x[:200], x[-200:] = ref.normal((200, H), g), ref.normal((200, H), g)
+    ends = torch.cat([torch.arange(200), torch.arange(T - 200, T)]).cuda()
+    got = ep.rmsnorm(x, w, residual=x, rows8=True)
+    want = ep.rmsnorm(x[ends], w, residual=x[ends], rows8=True)
+    for name in ("total", "out", "rows8"):
+        assert torch.equal(getattr(got, name)[ends], getattr(want, name))
+    assert not got.out[200:-200].any()
+    dx, dw = ep.rmsnorm_grad(got.total, w, got.out, d_total=x)
+    dx2, dw2 = ep.rmsnorm_grad(want.total, w, want.out, d_total=x[ends])
+    assert torch.equal(dx[ends], dx2)
+    size = ref.norm_grad(want.total, w, want.out, x[ends], 1e-6)[3]
+    ref.within(dw, dw2.double(), size * (2.0 ** -13 + T * ref.U24), "dw")   # rows of zeros add nothing
+
+
+def test_graph():
+    """The norm, its gradient, the router's and the combine's in one captured graph, replayed with
+    new inputs against eager calls."""
+    say("layer operators in a graph")
+    T, H, E, k = 300, 1040, 24, 3
+    g = ref.gen(17)
+    x, w, d = ref.normal((T, H), g), ref.normal(H, g), ref.normal((T, H), g)
+    z, dg = torch.randn((T, E), device="cuda", generator=g), torch.randn((T, k), device="cuda", generator=g)
+    y, pos = ref.normal((T * k, H), g), torch.randperm(T * k, device="cuda", generator=g).int()
+    one = torch.ones(1, device="cuda")
+
+    def step():
+        n = ep.rmsnorm(x, w, residual=d, rows8=True)
+        r = ep.route(z, k, balance=0.5)
+        dy, dw = ep.combine_grad(d, y, pos, r.topk_w)
+        return [n.total, n.out, n.rows8, *ep.rmsnorm_grad(n.total, w, d, d_total=x), r.topk_idx, r.topk_w, r.expert_counts,
+                r.prob_sums, r.loss, ep.route_grad(z, r, dg, one), dy, dw]
+
+    step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for i in range(4):
+        x.mul_(-1.5), z.mul_(0.5).add_(0.1), y.neg_()
+        want = step()
+        for t in held:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a.view(torch.uint8) if a.dtype == torch.uint8 else a, b) for a, b in zip(held, want)), i
+
+
 def test_total_in_place_and_side_stream():
     say("rmsnorm in place, on a stream of its own")
     g = ref.gen(3)
