@@ -148,9 +148,9 @@ struct RouteArgs {
     float *topk_w;
     int32_t *counts;  // null: no counts, sums and loss
     float *prob_sums, *loss;
-    void *workspace;  // per group: int32 [E] counts, fp32 [E] sums
+    void *workspace;  // of route_workspace_bytes; per group: int32 counts, fp32 sums, E rounded up to 4 of each
 };
-int64_t route_groups(int64_t T, int32_t E);
+size_t route_workspace_bytes(int64_t T, int32_t E);
 hipError_t launch_route(const RouteArgs &a, hipStream_t stream);
 
 struct RouteGradArgs {

@@ -113,17 +113,13 @@ extern "C" ep_status ep_rmsnorm_grad(const void *total_dev, const void *weight_d
     return EP_OK;
 }
 
-namespace {
-size_t route_workspace(int64_t T, int32_t E) { return (size_t)ep::route_groups(T, E) * E * 8; }
-}  // namespace
-
 extern "C" ep_status ep_route_workspace_bytes(int64_t num_tokens, int32_t num_experts, size_t *bytes) {
     const ep_status st = check_route("ep_route_workspace_bytes", num_tokens, num_experts, 1);
     if (st != EP_OK)
         return st;
     if (!bytes)
         return fail(EP_ERR_INVALID_ARG, "ep_route_workspace_bytes: bytes is NULL");
-    *bytes = route_workspace(num_tokens, num_experts);
+    *bytes = ep::route_workspace_bytes(num_tokens, num_experts);
     return EP_OK;
 }
 
@@ -141,7 +137,7 @@ extern "C" ep_status ep_route(const void *logits_dev, int32_t logits_bf16, const
         return fail(EP_ERR_INVALID_ARG, "ep_route: counts, prob_sums and loss come together");
     if (!aligned(counts, 4) || !aligned(prob_sums, 4) || !aligned(loss, 4))
         return fail(EP_ERR_INVALID_ARG, "ep_route: counts, prob_sums and loss are not 4-byte aligned");
-    const size_t need = counts ? route_workspace(num_tokens, num_experts) : 0;
+    const size_t need = counts ? ep::route_workspace_bytes(num_tokens, num_experts) : 0;
     if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need))
         return fail(EP_ERR_INVALID_ARG, "ep_route: workspace of %zu bytes, need %zu, 16-byte aligned",
                     workspace ? workspace_bytes : (size_t)0, need);

@@ -94,6 +94,19 @@ __device__ __forceinline__ float wave_fmax(float v) {
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_add(int v) {
+    return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, true);
+}
+__device__ __forceinline__ int wave_sum_int(int v) {
+    v = dpp_add<0x111, 0xf>(v);
+    v = dpp_add<0x112, 0xf>(v);
+    v = dpp_add<0x114, 0xf>(v);
+    v = dpp_add<0x118, 0xf>(v);
+    v = dpp_add<0x142, 0xa>(v);
+    v = dpp_add<0x143, 0xc>(v);
+    return __builtin_amdgcn_readlane(v, 63);
+}
 // A lane's experts for the picks: the best one's key and number.
 template <int NV>
 struct Heads {
@@ -154,6 +167,9 @@ struct Heads {
         }
     }
 };
+
+// Experts of a group's counts, and of its sums, in the workspace: whole vectors.
+__host__ __device__ constexpr int group_experts(int E) { return (E + 3) / 4 * 4; }
 
 template <int NV>
 constexpr int route_waves() {
@@ -256,8 +272,9 @@ __global__ __launch_bounds__(route_waves<NV>() * 64) void route_kernel(RouteArgs
     for (int i = 0; i < NV; ++i)
         sums[wave][e0 + i] = psum[i];
     __syncthreads();
-    int32_t *group_counts = static_cast<int32_t *>(a.workspace) + (int64_t)blockIdx.x * 2 * a.E;
-    float *group_sums = reinterpret_cast<float *>(group_counts + a.E);
+    const int half = group_experts(a.E);
+    int32_t *group_counts = static_cast<int32_t *>(a.workspace) + (int64_t)blockIdx.x * 2 * half;
+    float *group_sums = reinterpret_cast<float *>(group_counts + half);
     for (int e = threadIdx.x; e < a.E; e += W * 64) {
         float s = 0.f;
 #pragma unroll
@@ -269,93 +286,82 @@ __global__ __launch_bounds__(route_waves<NV>() * 64) void route_kernel(RouteArgs
 }
 
 // Counts and sums over the groups, then the loss: one workgroup.  A thread adds 4 neighbouring
-// experts' (PER; 1 where E is no multiple of 4) of every lanes-th group, kAhead groups on their
-// way at a time.
-template <int PER>
-__global__ __launch_bounds__(1024) void route_finish_kernel(const int32_t *workspace, int64_t groups, int32_t E,
-                                                            int32_t k, float balance, int32_t *counts,
+// experts of every lanes-th group, kAhead groups on their way at a time; the buffer's range gives
+// zeros past the last group.  2^shift threads lie side by side over the experts, and `lanes` of
+// those rows of threads share the groups.  The code is kept short: it runs once, out of a cold
+// instruction cache.
+__global__ __launch_bounds__(1024) void route_finish_kernel(void *workspace, int32_t groups, int32_t E, int32_t shift,
+                                                            int32_t lanes, int32_t k, float balance, int32_t *counts,
                                                             float *prob_sums, float *loss) {
-    struct __attribute__((aligned(4 * PER))) Vec {
-        uint32_t v[PER];
-    };
-    __shared__ int part_n[1024 * PER];
-    __shared__ float part_s[1024 * PER];
+    __shared__ u32x4 part_n[1024], part_s[1024];
     __shared__ float wave_loss[16];
     __shared__ int wave_n[16];
     constexpr int kAhead = 8;
+    constexpr uint32_t kNowhere = 0x80000000u;
+    const int cols = 1 << shift, col = threadIdx.x & (cols - 1), part = threadIdx.x >> shift;
+    const uint32_t half = (uint32_t)group_experts(E) * 4, row = 2 * half;  // bytes of a group: counts, then sums
+    const __amdgpu_buffer_rsrc_t table = __builtin_amdgcn_make_buffer_rsrc(workspace, 0, groups * (int32_t)row, 0x00020000);
     float dot = 0.f;
     int total = 0;
-    const int all = E / PER, cols = all < 1024 ? all : 1024;
-    const int lanes = 1024 / cols, col = threadIdx.x % cols, part = threadIdx.x / cols;
-    const Vec *table = reinterpret_cast<const Vec *>(workspace);
-    for (int base = 0; base < all; base += cols) {
-        const int e = base + col;
-        int n[PER] = {};
-        float s[PER] = {};
-        if (part < lanes && e < all)
-            for (int64_t g0 = part; g0 < groups; g0 += lanes * kAhead) {
-                Vec vn[kAhead], vs[kAhead];
+    for (int base = 0; base < E; base += cols * 4) {
+        const int e = base + col * 4;
+        uint32_t at = e < E && part < lanes ? part * row + e * 4 : kNowhere;
+        u32x4 n = {0, 0, 0, 0};
+        float s[4] = {};
+        for (int g = 0; g < groups; g += lanes * kAhead) {
+            u32x4 vn[kAhead], vs[kAhead];
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i) {
-                    const int64_t g = g0 + i * lanes;
-                    vn[i] = vs[i] = Vec{};
-                    if (g < groups) {
-                        vn[i] = table[g * 2 * all + e];
-                        vs[i] = table[g * 2 * all + all + e];
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < kAhead; ++i)
-#pragma unroll
-                    for (int q = 0; q < PER; ++q) {
-                        n[q] += (int)vn[i].v[q];
-                        s[q] += __uint_as_float(vs[i].v[q]);
-                    }
+            for (int i = 0; i < kAhead; ++i) {
+                vn[i] = __builtin_amdgcn_raw_buffer_load_b128(table, at, 0, 0);
+                vs[i] = __builtin_amdgcn_raw_buffer_load_b128(table, at + half, 0, 0);
+                at += lanes * row;
             }
 #pragma unroll
-        for (int q = 0; q < PER; ++q) {
-            part_n[q * 1024 + threadIdx.x] = n[q];
-            part_s[q * 1024 + threadIdx.x] = s[q];
+            for (int i = 0; i < kAhead; ++i) {
+                n += vn[i];
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    s[q] += __uint_as_float(vs[i][q]);
+            }
         }
+        part_n[threadIdx.x] = n;
+        part_s[threadIdx.x] = u32x4{__float_as_uint(s[0]), __float_as_uint(s[1]), __float_as_uint(s[2]), __float_as_uint(s[3])};
         __syncthreads();
-        for (int c = threadIdx.x; c < cols * PER && base * PER + c < E; c += 1024) {
+        for (int c = threadIdx.x; c < cols * 4 && base + c < E; c += 1024) {
             int cn = 0;
             float cs = 0.f;
+#pragma unroll 4
             for (int p = 0; p < lanes; ++p) {
-                cn += part_n[c % PER * 1024 + p * cols + c / PER];
-                cs += part_s[c % PER * 1024 + p * cols + c / PER];
+                cn += reinterpret_cast<const int *>(part_n)[p * cols * 4 + c];
+                cs += reinterpret_cast<const float *>(part_s)[p * cols * 4 + c];
             }
-            counts[base * PER + c] = cn;
-            prob_sums[base * PER + c] = cs;
+            counts[base + c] = cn;
+            prob_sums[base + c] = cs;
             dot = fmaf((float)cn, cs, dot);
             total += cn;
         }
         __syncthreads();
     }
     dot = wave_sum(dot);
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1)
-        total += __shfl_xor(total, d);
+    total = wave_sum_int(total);
     if ((threadIdx.x & 63) == 0) {
         wave_loss[threadIdx.x >> 6] = dot;
         wave_n[threadIdx.x >> 6] = total;
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
-        dot = 0.f;
-        total = 0;
-        for (int w = 0; w < 16; ++w) {
-            dot += wave_loss[w];
-            total += wave_n[w];
-        }
+    if (threadIdx.x < 64) {
+        dot = wave_sum(threadIdx.x < 16 ? wave_loss[threadIdx.x & 15] : 0.f);
+        total = wave_sum_int(threadIdx.x < 16 ? wave_n[threadIdx.x & 15] : 0);
         const float n = (float)(total / k);
-        *loss = total == 0 ? 0.f : balance * (float)E * dot / (n * (float)k * n);
+        if (threadIdx.x == 0)
+            *loss = total == 0 ? 0.f : balance * (float)E * dot / (n * (float)k * n);
     }
 }
 
 template <int NV, bool VEC, typename L>
 __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradArgs a) {
     __shared__ float chosen[4][64 * NV];  // per wave: the gates' gradient by expert, zero elsewhere
+    const auto place = [](int e) { return e % NV * 64 + e / NV; };  // lanes side by side: no bank conflicts
     __shared__ int wave_n[4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int e0 = lane * NV;
@@ -363,7 +369,7 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradArgs a) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         g[i] = 0.f;
-        chosen[wave][e0 + i] = 0.f;
+        chosen[wave][i * 64 + lane] = 0.f;
     }
     if (a.d_loss) {
         int n = 0;
@@ -433,11 +439,11 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradArgs a) {
             const float scale = !a.normalize ? inv : es == 0.f ? 0.f : 1.f / es;
             const float mean = ed * scale, less = a.normalize ? mean : 0.f;
             if (expert >= 0)
-                chosen[wave][expert] = v * scale * (dc - less);
+                chosen[wave][place(expert)] = v * scale * (dc - less);
             for (int j = lane + 64; j < a.k; j += 64) {
                 const int e = a.topk_idx[t * a.k + j];
                 if (e >= 0 && e < a.E)
-                    chosen[wave][e] = exp_below(one_logit(row, e), top) * scale * (a.d_topk_w[t * a.k + j] - less);
+                    chosen[wave][place(e)] = exp_below(one_logit(row, e), top) * scale * (a.d_topk_w[t * a.k + j] - less);
             }
             if (!a.normalize)
                 pg += mean;
@@ -448,8 +454,8 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradArgs a) {
         } vec;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const float d = live ? fmaf(z[i] * inv, g[i] - pg, chosen[wave][e0 + i]) : 0.f;
-            chosen[wave][e0 + i] = 0.f;
+            const float d = live ? fmaf(z[i] * inv, g[i] - pg, chosen[wave][i * 64 + lane]) : 0.f;
+            chosen[wave][i * 64 + lane] = 0.f;
             if constexpr (sizeof(L) == 2)
                 vec.v[i] = (L)bf16_pair(d, 0.f);
             else
@@ -468,6 +474,10 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradArgs a) {
     }
 }
 
+int64_t route_groups(int64_t T, int32_t E) {
+    const int waves = E <= 512 ? route_waves<8>() : route_waves<16>();
+    return std::min<int64_t>((T + waves - 1) / waves, kCus);
+}
 template <int NV, bool VEC, typename L>
 hipError_t launch_one(const RouteArgs &a, hipStream_t stream) {
     constexpr int W = route_waves<NV>();
@@ -502,10 +512,7 @@ hipError_t launch_experts(const A &a, hipStream_t stream) {
 
 }  // namespace
 
-int64_t route_groups(int64_t T, int32_t E) {
-    const int waves = E <= 512 ? 16 : 4;
-    return std::min<int64_t>((T + waves - 1) / waves, kCus);
-}
+size_t route_workspace_bytes(int64_t T, int32_t E) { return (size_t)route_groups(T, E) * group_experts(E) * 8; }
 
 hipError_t launch_route(const RouteArgs &a, hipStream_t stream) {
     if (a.T > 0) {
@@ -516,11 +523,12 @@ hipError_t launch_route(const RouteArgs &a, hipStream_t stream) {
     if (!a.counts)
         return hipSuccess;
     const int64_t groups = a.T ? route_groups(a.T, a.E) : 0;
-#define EP_CALL(PER)                                                                                                  \
-    launch_traced("route_finish", route_finish_kernel<PER>, dim3(1), 1024, stream, (const int32_t *)a.workspace, groups, \
-                  a.E, a.k, a.balance, a.counts, a.prob_sums, a.loss)
-    return a.E % 4 == 0 ? EP_CALL(4) : EP_CALL(1);
-#undef EP_CALL
+    int32_t shift = 0;
+    while (shift < 10 && (4 << shift) < a.E)
+        ++shift;
+    // with 32 rows of threads every group is on its way at once
+    return launch_traced("route_finish", route_finish_kernel, dim3(1), 1024, stream, a.workspace, (int32_t)groups, a.E, shift,
+                         std::min(1024 >> shift, 32), a.k, a.balance, a.counts, a.prob_sums, a.loss);
 }
 
 hipError_t launch_route_grad(const RouteGradArgs &a, hipStream_t stream) {
