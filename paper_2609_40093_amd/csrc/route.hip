@@ -19,8 +19,8 @@
 // workgroups by a second kernel, which also computes the loss.
 //
 // Bound by its instructions: 32768 tokens of 256 experts, top-8, are 34 MB of logits, 6 us of HBM;
-// the forward takes 28 us, its second kernel 6 to 9, the gradient 18 (67 MB, 12 us of HBM).  256
-// tokens: 5.4 and 3.9 us, latency.
+// the forward takes 28 us, its second kernel 5, the gradient 17 (67 MB, 12 us of HBM).  256 tokens:
+// 5.4 and 4.2 us, latency.
 #include "layer.h"
 
 namespace ep {
@@ -37,33 +37,37 @@ __device__ __forceinline__ float key_logit(uint32_t key) {
     return __uint_as_float((key >> 31) ? key ^ 0x80000000u : ~key);
 }
 
-// The logits of this lane's experts; -inf past the last expert.  VEC: every lane's experts all
-// exist or all do not, and lie on a vector's boundary.
-template <int NV, bool VEC, typename L>
-__device__ __forceinline__ void load_logits(const L *row, int e0, int E, float *z) {
-    struct __attribute__((aligned(sizeof(L) * NV))) Vec {
-        L v[NV];
-    };
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-        z[i] = -__builtin_inff();
-    Vec raw;
-    if (VEC) {
-        if (e0 >= E)
-            return;
-        raw = *reinterpret_cast<const Vec *>(row + e0);
-    }
+// A lane's experts.  Lane l has [l NV, (l + 1) NV), and loads and stores them as one vector; where
+// the experts end within it (EVEN: in no lane), the vector is moved down to [E - NV, E), and its
+// first ones, which the lane before has, do not count.  (E >= NV: a launch takes the smallest NV
+// that holds E.)  Before the vectors were moved, lanes loaded and stored such experts one by one:
+// 32768 tokens of 511 experts forward and backward 129 us, now 91.
+template <int NV, bool EVEN>
+struct Lane {
+    int first, e0;  // first expert of its own; first of its vector
+    bool some;      // it has one
+    __device__ __forceinline__ Lane(int lane, int E)
+        : first(lane * NV), e0(first < E - NV ? first : E - NV), some(first < E) {}
+    __device__ __forceinline__ bool has(int i) const { return EVEN ? some : e0 + i >= first; }
+};
+// NV elements at any element's alignment
+template <int NV, typename L>
+struct __attribute__((packed, aligned(sizeof(L)))) Elements {
+    L v[NV];
+};
+
+// The logits of the lane's experts; -inf for those that do not count.
+template <int NV, bool EVEN, typename L>
+__device__ __forceinline__ void load_logits(const L *row, const Lane<NV, EVEN> &l, float *z) {
+    const Elements<NV, L> raw = *reinterpret_cast<const Elements<NV, L> *>(row + l.e0);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        if (!VEC) {
-            if (e0 + i >= E)
-                continue;
-            raw.v[i] = row[e0 + i];
-        }
+        float v;
         if constexpr (sizeof(L) == 2)
-            z[i] = bf16_lo(raw.v[i]);
+            v = bf16_lo(raw.v[i]);
         else
-            z[i] = raw.v[i];
+            v = raw.v[i];
+        z[i] = l.has(i) ? v : -__builtin_inff();
     }
 }
 template <typename L>
@@ -176,13 +180,13 @@ constexpr int route_waves() {
     return NV <= 8 ? 16 : 4;
 }
 
-template <int NV, bool VEC, typename L>
+template <int NV, bool EVEN, typename L>
 __global__ __launch_bounds__(route_waves<NV>() * 64) void route_kernel(RouteArgs a) {
     constexpr int W = route_waves<NV>();
     __shared__ int counts[64 * NV];
     __shared__ float sums[W][64 * NV];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int e0 = lane * NV;
+    const Lane<NV, EVEN> own(lane, a.E);
     for (int i = threadIdx.x; i < 64 * NV; i += W * 64)
         counts[i] = 0;
     __syncthreads();
@@ -194,14 +198,14 @@ __global__ __launch_bounds__(route_waves<NV>() * 64) void route_kernel(RouteArgs
     int64_t t = (int64_t)blockIdx.x * W + wave;
     float ahead[NV];  // the next token's logits
     if (t < a.T)
-        load_logits<NV, VEC>(static_cast<const L *>(a.logits) + t * a.E, e0, a.E, ahead);
+        load_logits(static_cast<const L *>(a.logits) + t * a.E, own, ahead);
     for (; t < a.T; t += stride) {
         float z[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             z[i] = ahead[i];
         if (t + stride < a.T)
-            load_logits<NV, VEC>(static_cast<const L *>(a.logits) + (t + stride) * a.E, e0, a.E, ahead);
+            load_logits(static_cast<const L *>(a.logits) + (t + stride) * a.E, own, ahead);
         const bool live = !a.mask || a.mask[t];
         int32_t *ids = a.topk_idx + t * a.k;
         float *gates = a.topk_w + t * a.k;
@@ -215,7 +219,7 @@ __global__ __launch_bounds__(route_waves<NV>() * 64) void route_kernel(RouteArgs
         Heads<NV> heads;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-            heads.key[i] = e0 + i < a.E ? order_key(z[i]) : 0u;
+            heads.key[i] = own.has(i) ? order_key(z[i]) : 0u;
         heads.prepare();
         // 64 picks at a time: lane j holds pick j's key and expert
         float top = 0.f, chosen_sum = 0.f, gate = 0.f;
@@ -228,7 +232,7 @@ __global__ __launch_bounds__(route_waves<NV>() * 64) void route_kernel(RouteArgs
                 const uint32_t b = heads.best(number);
                 const uint32_t m = wave_max(b);
                 const int owner = __builtin_ctzll(__ballot(b == m));
-                const int e = __builtin_amdgcn_readlane(e0 + number, owner);
+                const int e = __builtin_amdgcn_readlane(own.e0 + number, owner);
                 key = lane == j ? m : key;
                 expert = lane == j ? e : expert;
                 heads.take(lane == owner, number);
@@ -270,7 +274,8 @@ __global__ __launch_bounds__(route_waves<NV>() * 64) void route_kernel(RouteArgs
         return;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
-        sums[wave][e0 + i] = psum[i];
+        if (own.has(i))
+            sums[wave][own.e0 + i] = psum[i];
     __syncthreads();
     const int half = group_experts(a.E);
     int32_t *group_counts = static_cast<int32_t *>(a.workspace) + (int64_t)blockIdx.x * 2 * half;
@@ -358,19 +363,23 @@ __global__ __launch_bounds__(1024) void route_finish_kernel(void *workspace, int
     }
 }
 
-template <int NV, bool VEC, typename L>
+template <int NV, bool EVEN, typename L>
 __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradArgs a) {
     __shared__ float chosen[4][64 * NV];  // per wave: the gates' gradient by expert, zero elsewhere
-    const auto place = [](int e) { return e % NV * 64 + e / NV; };  // lanes side by side: no bank conflicts
     __shared__ int wave_n[4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int e0 = lane * NV;
+    const Lane<NV, EVEN> own(lane, a.E);
     float g[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         g[i] = 0.f;
         chosen[wave][i * 64 + lane] = 0.f;
     }
+    // an expert's place: its lane's element, lanes side by side, so that no banks conflict
+    const auto place = [&](uint32_t e) {
+        const Lane<NV, EVEN> l(e / NV, a.E);
+        return (EVEN ? e % NV : e - l.e0) * 64 + e / NV;
+    };
     if (a.d_loss) {
         int n = 0;
         for (int e = threadIdx.x; e < a.E; e += 256)
@@ -386,8 +395,8 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradArgs a) {
         const float c = total == 0 ? 0.f : *a.d_loss * a.balance * (float)a.E / (tokens * (float)a.k * tokens);
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-            if (e0 + i < a.E)
-                g[i] = c * (float)a.counts[e0 + i];
+            if (own.has(i))
+                g[i] = c * (float)a.counts[own.e0 + i];
     }
     const int64_t stride = (int64_t)gridDim.x * 4;
     for (int64_t t = (int64_t)blockIdx.x * 4 + wave; t < a.T; t += stride) {
@@ -395,7 +404,7 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradArgs a) {
         L *out = static_cast<L *>(a.d_logits) + t * a.E;
         const bool live = !a.mask || a.mask[t];
         float z[NV];
-        load_logits<NV, VEC>(row, e0, a.E, z);
+        load_logits(row, own, z);
         // the chosen experts: lane j (and j + 64, ...) takes the j-th
         int expert = -1;
         float zc = 0.f, dc = 0.f;
@@ -449,9 +458,7 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradArgs a) {
                 pg += mean;
             __builtin_amdgcn_wave_barrier();
         }
-        struct __attribute__((aligned(sizeof(L) * NV))) Vec {
-            L v[NV];
-        } vec;
+        Elements<NV, L> vec;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const float d = live ? fmaf(z[i] * inv, g[i] - pg, chosen[wave][i * 64 + lane]) : 0.f;
@@ -461,14 +468,13 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradArgs a) {
             else
                 vec.v[i] = d;
         }
-        if (VEC) {
-            if (e0 < a.E)
-                *reinterpret_cast<Vec *>(out + e0) = vec;
-        } else {
+        if (EVEN ? own.some : own.e0 == own.first) {
+            *reinterpret_cast<Elements<NV, L> *>(out + own.e0) = vec;
+        } else if (!EVEN) {
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if (e0 + i < a.E)
-                    out[e0 + i] = vec.v[i];
+                if (own.has(i))
+                    out[own.e0 + i] = vec.v[i];
         }
         __builtin_amdgcn_wave_barrier();
     }
@@ -478,36 +484,34 @@ int64_t route_groups(int64_t T, int32_t E) {
     const int waves = E <= 512 ? route_waves<8>() : route_waves<16>();
     return std::min<int64_t>((T + waves - 1) / waves, kCus);
 }
-template <int NV, bool VEC, typename L>
-hipError_t launch_one(const RouteArgs &a, hipStream_t stream) {
+template <int NV, bool EVEN, typename L>
+hipError_t launch_lanes(const RouteArgs &a, hipStream_t stream) {
     constexpr int W = route_waves<NV>();
-    return launch_traced("route", route_kernel<NV, VEC, L>, dim3((unsigned)route_groups(a.T, a.E)), W * 64, stream, a);
+    return launch_traced("route", route_kernel<NV, EVEN, L>, dim3((unsigned)route_groups(a.T, a.E)), W * 64, stream, a);
 }
-template <int NV, bool VEC, typename L>
-hipError_t launch_one(const RouteGradArgs &a, hipStream_t stream) {
+template <int NV, bool EVEN, typename L>
+hipError_t launch_lanes(const RouteGradArgs &a, hipStream_t stream) {
     const int64_t groups = std::min<int64_t>((a.T + 3) / 4, kCus * 8);
-    return launch_traced("route_grad", route_grad_kernel<NV, VEC, L>, dim3((unsigned)groups), 256, stream, a);
+    return launch_traced("route_grad", route_grad_kernel<NV, EVEN, L>, dim3((unsigned)groups), 256, stream, a);
 }
-// Vector loads where a lane's NV experts end with the row and begin on a vector's boundary
-// (logits are 16-byte aligned; wider vectors than 16 bytes would need more).
 template <int NV, typename L, typename A>
-hipError_t launch_lanes(const A &a, hipStream_t stream) {
-    if constexpr (NV > 1 && NV * sizeof(L) <= 16)
-        if (a.E % NV == 0)
-            return launch_one<NV, true, L>(a, stream);
-    return launch_one<NV, false, L>(a, stream);
+hipError_t launch_one(const A &a, hipStream_t stream) {
+    if constexpr (NV > 1)
+        if (a.E % NV)
+            return launch_lanes<NV, false, L>(a, stream);
+    return launch_lanes<NV, true, L>(a, stream);
 }
 template <typename L, typename A>
 hipError_t launch_experts(const A &a, hipStream_t stream) {
     if (a.E <= 64)
-        return launch_lanes<1, L>(a, stream);
+        return launch_one<1, L>(a, stream);
     if (a.E <= 128)
-        return launch_lanes<2, L>(a, stream);
+        return launch_one<2, L>(a, stream);
     if (a.E <= 256)
-        return launch_lanes<4, L>(a, stream);
+        return launch_one<4, L>(a, stream);
     if (a.E <= 512)
-        return launch_lanes<8, L>(a, stream);
-    return a.E <= 1024 ? launch_lanes<16, L>(a, stream) : launch_lanes<32, L>(a, stream);
+        return launch_one<8, L>(a, stream);
+    return a.E <= 1024 ? launch_one<16, L>(a, stream) : launch_one<32, L>(a, stream);
 }
 
 }  // namespace
