@@ -4,6 +4,8 @@
 
 #include "ep_internal.h"
 
+#include <algorithm>
+#include <cmath>
 #include <utility>
 
 namespace ep {

@@ -255,10 +255,10 @@ typedef TileShape<256, 64, 4, 2, 3> Few;     // one (120 KiB)
 // N 1536, mean 8: 84 / 93).
 //
 // Where that tile gives fewer tiles than compute units (the dense products of a decode step,
-// few experts), the smaller tiles and the parts of the contraction are weighed by an estimate of the time
+// few experts), the tiles and the parts of the contraction are weighed by an estimate of the time
 // (product_tile.h).  Measured, us, estimate's choice against the larger tile split to
 // fill the chip: 256 rows K 7168 N 256 12 / 15, 500 rows 4096 x 4096 30 / 40, 256 rows 2048 x 2048
-// 12 / 22.
+// 12 / 22; against the small tiles alone: 3190 rows of 15 experts 4176 x 1984 120 / 193.
 enum class Size { kLarge, kBroad, kWide, kFew, kMedium, kSmall, kTiny };
 Size tile_size(int64_t rows, int32_t E) {
     const int64_t mean = rows / E;
@@ -303,11 +303,16 @@ Plan make_plan(int64_t rows, int32_t E, int32_t K, int32_t N, bool bits8, bool g
         return best;
     double least = 0;
     bool any = false;
-    for (Size size : {Size::kMedium, Size::kSmall, Size::kTiny})
+    for (Size size : {Size::kLarge, Size::kBroad, Size::kMedium, Size::kSmall, Size::kTiny})
         for (int32_t parts = 1; parts == 1 || steps / parts >= kSplitSteps; parts *= 2) {
             const Plan p = plan(size, parts);
-            const StepCost cost = size == Size::kMedium ? kMediumCost : size == Size::kSmall ? kSmallCost : kTinyCost;
-            const double t = estimate(cost, p.tiles, p.split.parts, p.split.steps, rows * N * (gated ? 2 : 1));
+            const StepCost cost = size == Size::kLarge    ? kLargeCost
+                                  : size == Size::kBroad  ? kBroadCost
+                                  : size == Size::kMedium ? kMediumCost
+                                  : size == Size::kSmall  ? kSmallCost
+                                                          : kTinyCost;
+            const double t = estimate(cost, row_tiles_likely(rows, E, tile_rows(size)) * p.cols, p.split.parts, p.split.steps,
+                                      rows * N * (gated ? 2 : 1));
             if (!any || t < least) {
                 any = true;
                 least = t;

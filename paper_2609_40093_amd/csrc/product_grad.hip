@@ -235,16 +235,6 @@ hipError_t launch_dx(const GradTileArgs &a, hipStream_t stream) {
     return launch_traced("expert_product_dx", product_dx_kernel<S>, dim3((unsigned)(tiles + 8)), S::kThreads, stream, a,
                          cols);
 }
-// The smaller of the tiles by the estimate of their time (300 rows 2048 x 2048, a call's dx and
-// dw: 28 us with Medium alone, 21).
-hipError_t launch_dx_small(const GradTileArgs &a, hipStream_t stream) {
-    const int32_t steps = (a.Nw + kStepRows - 1) / kStepRows;
-    const auto cost = [&](StepCost c, int i, int j) {
-        return estimate(c, row_tiles_most(a.rows, a.E, j) * ((a.K + i - 1) / i), 1, steps, 0);
-    };
-    return cost(kSmallCost, Small::kI, Small::kJ) < cost(kMediumCost, Medium::kI, Medium::kJ) ? launch_dx<Small>(a, stream)
-                                                                                             : launch_dx<Medium>(a, stream);
-}
 template <class S>
 hipError_t launch_dw(const GradTileArgs &a, hipStream_t stream) {
     const int32_t kt = (a.K + S::kI - 1) / S::kI, nt = (a.Nw + S::kJ - 1) / S::kJ;
@@ -254,35 +244,62 @@ hipError_t launch_dw(const GradTileArgs &a, hipStream_t stream) {
     return launch_traced("expert_product_dw", product_dw_kernel<S>, dim3((unsigned)groups), S::kThreads, stream, a, nt, kt);
 }
 
-// The large tiles where the experts fill them and there is one for every compute unit.
-bool large_rows(int64_t rows, int32_t E, int64_t cols) {
-    return rows / E >= 160 && row_tiles_most(rows, E, Large::kJ) * cols >= kCus;
+enum class GradSize { kLarge, kBroad, kMedium, kSmall };
+struct GradTile {
+    GradSize size;
+    int i, j;
+    StepCost cost;
+};
+constexpr GradTile kGradTiles[] = {{GradSize::kLarge, Large::kI, Large::kJ, kLargeCost},
+                                   {GradSize::kBroad, Broad::kI, Broad::kJ, kBroadCost},
+                                   {GradSize::kMedium, Medium::kI, Medium::kJ, kMediumCost},
+                                   {GradSize::kSmall, Small::kI, Small::kJ, kSmallCost}};
+
+// The tile of dx: the large ones where the experts fill them and there is one for every compute
+// unit, else by the estimate of the time.  Measured, us: 300 rows 2048 x 2048, a call's dx and dw,
+// 28 with Medium alone, 21; dx of 4096 rows of four 2048 x 1408 experts 33 with Broad, 46 with
+// Medium; of 574 rows of eight 3168 x 3056 experts 58 with Medium, 88 with Small.
+GradSize plan_dx(int64_t rows, int32_t E, int32_t K, int32_t Nw) {
+    const int64_t large = (K + Large::kI - 1) / Large::kI;
+    if (rows / E >= 160 && row_tiles_most(rows, E, Large::kJ) * large >= kCus)
+        return broad_rows(rows, E, large) ? GradSize::kBroad : GradSize::kLarge;
+    const int32_t steps = (Nw + kStepRows - 1) / kStepRows;
+    GradSize best = GradSize::kMedium;
+    double least = 0;
+    for (const GradTile &g : kGradTiles) {
+        const double t = estimate(g.cost, row_tiles_likely(rows, E, g.j) * ((K + g.i - 1) / g.i), 1, steps, 0);
+        if (least == 0 || t < least) {
+            least = t;
+            best = g.size;
+        }
+    }
+    return best;
 }
 
-// The tile and the parts of dw, from the rows per expert to expect.  Small tiles and parts where
-// the large tiles are fewer than the compute units: dw of 11253 rows, one 2432 x 512 expert.
-enum class DwSize { kLarge, kBroad, kMedium, kSmall };
+// The tile and the parts of dw, from the rows per expert to expect: by the estimate where the large
+// tiles are fewer than the compute units (dw of 11253 rows, one 2432 x 512 expert).  A large tile
+// waits for the expert with the most rows: with several, its time counts a fifth more (measured,
+// us: 13124 rows of 15 skewed 1536 x 512 experts 44 with Large, 38 with Medium; 4096 rows of four
+// 2048 x 1408 experts 33 with Broad, 39 with Medium).
 struct DwPlan {
-    DwSize size;
+    GradSize size;
     int32_t parts;
 };
 DwPlan plan_dw(int64_t rows, int32_t E, int32_t K, int64_t Nw) {
-    const auto tiles = [&](int i, int j) { return (int64_t)E * ((K + i - 1) / i) * ((Nw + j - 1) / j); };
-    const int64_t large = tiles(Large::kI, Large::kJ);
+    const auto tiles = [&](int i, int j) { return (double)E * ((K + i - 1) / i) * ((Nw + j - 1) / j); };
+    const double large = tiles(Large::kI, Large::kJ);
     if (large >= kCus)
-        return {broad_wins((double)large, (double)tiles(Broad::kI, Broad::kJ)) ? DwSize::kBroad : DwSize::kLarge, 1};
+        return {broad_wins(large, tiles(Broad::kI, Broad::kJ)) ? GradSize::kBroad : GradSize::kLarge, 1};
     const int32_t steps = (int32_t)std::max<int64_t>(1, (rows / E + kStepRows - 1) / kStepRows);
-    DwPlan best{DwSize::kMedium, 1};
+    DwPlan best{GradSize::kMedium, 1};
     double least = 0;
-    for (DwSize size : {DwSize::kMedium, DwSize::kSmall})
+    for (const GradTile &g : kGradTiles)
         for (int32_t parts = 1; parts == 1 || steps / parts >= kSplitSteps; parts *= 2) {
-            const bool medium = size == DwSize::kMedium;
-            const double t = estimate(medium ? kMediumCost : kSmallCost,
-                                      medium ? tiles(Medium::kI, Medium::kJ) : tiles(Small::kI, Small::kJ), parts,
-                                      (steps + parts - 1) / parts, E * Nw * K);
+            const double t = estimate(g.cost, tiles(g.i, g.j), parts, (steps + parts - 1) / parts, E * Nw * K) *
+                             (E > 1 && !g.cost.two ? 1.2 : 1.0);
             if (least == 0 || t < least) {
                 least = t;
-                best = {size, parts};
+                best = {g.size, parts};
             }
         }
     return best;
@@ -337,10 +354,11 @@ hipError_t launch_product_grad(const ProductGradArgs &a, hipStream_t stream) {
                    own_dz ? own_dz : (const uint16_t *)a.d_y, nullptr, nullptr, 1};
     if (a.dx && a.rows > 0) {
         g.out = static_cast<uint16_t *>(a.dx);
-        const int64_t cols = (a.K + Large::kI - 1) / Large::kI;
-        const hipError_t e = !large_rows(a.rows, a.E, cols) ? launch_dx_small(g, stream)
-                             : broad_rows(a.rows, a.E, cols) ? launch_dx<Broad>(g, stream)
-                                                             : launch_dx<Large>(g, stream);
+        const GradSize size = plan_dx(a.rows, a.E, a.K, a.Nw);
+        const hipError_t e = size == GradSize::kLarge    ? launch_dx<Large>(g, stream)
+                             : size == GradSize::kBroad  ? launch_dx<Broad>(g, stream)
+                             : size == GradSize::kMedium ? launch_dx<Medium>(g, stream)
+                                                         : launch_dx<Small>(g, stream);
         if (e != hipSuccess)
             return e;
     }
@@ -348,9 +366,9 @@ hipError_t launch_product_grad(const ProductGradArgs &a, hipStream_t stream) {
         g.out = static_cast<uint16_t *>(a.dw);
         g.parts = dw.parts;
         g.partial = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + ws.parts);
-        const hipError_t e = dw.size == DwSize::kLarge    ? launch_dw<Large>(g, stream)
-                             : dw.size == DwSize::kBroad  ? launch_dw<Broad>(g, stream)
-                             : dw.size == DwSize::kMedium ? launch_dw<Medium>(g, stream)
+        const hipError_t e = dw.size == GradSize::kLarge    ? launch_dw<Large>(g, stream)
+                             : dw.size == GradSize::kBroad  ? launch_dw<Broad>(g, stream)
+                             : dw.size == GradSize::kMedium ? launch_dw<Medium>(g, stream)
                                                           : launch_dw<Small>(g, stream);
         if (e != hipSuccess || dw.parts == 1)
             return e;

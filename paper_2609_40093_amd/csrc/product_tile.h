@@ -510,29 +510,40 @@ inline bool broad_wins(double tiles_large, double tiles_broad) {
     const auto turns = [](double tiles) { return (double)(int64_t)((tiles + kCus - 1) / kCus); };
     return turns(tiles_broad) * 0.78 < turns(tiles_large);
 }
-// Row tiles to expect: half a tile more than the rows fill for every expert.
+// Row tiles to expect: half a tile more than the rows fill for every expert, one at least.
 inline double row_tiles_likely(int64_t rows, int32_t E, int per) {
-    return E == 1 ? (double)((rows + per - 1) / per) : (double)rows / per + 0.5 * E;
+    return E == 1 ? (double)((rows + per - 1) / per)
+                  : std::max((double)std::min<int64_t>(E, rows), (double)rows / per + 0.5 * E);
 }
 inline bool broad_rows(int64_t rows, int32_t E, int64_t cols) {
     return broad_wins(row_tiles_likely(rows, E, Large::kJ) * cols, row_tiles_likely(rows, E, Broad::kJ) * cols);
 }
 
-// Small tiles, for sizes with fewer large tiles than compute units.  What a step takes with a
-// workgroup per compute unit (`one`) and with two (`two`), in us, measured; two are the most.
+// Small tiles, for sizes with fewer large tiles than compute units.
 typedef TileShape<128, 128, 2, 2, 2> Medium;  // two workgroups per compute unit (64 KiB of LDS)
 typedef TileShape<64, 64, 2, 2, 4> Small;     // two (64 KiB)
 typedef TileShape<128, 32, 4, 1, 4> Tiny;     // two (80 KiB)
+// What a step takes, in us, measured.  Small tiles: with a workgroup per compute unit (`less`) and
+// with two, the most there are (`full`).  Large ones: with next to no compute unit busy and with
+// all, in between by the share that is.
 struct StepCost {
-    double one, two;
+    bool two;
+    double less, full;
 };
-constexpr StepCost kMediumCost{0.55, 0.90}, kSmallCost{0.28, 0.43}, kTinyCost{0.30, 0.50};
+constexpr StepCost kLargeCost{false, 1.10, 1.85}, kBroadCost{false, 0.86, 1.44}, kMediumCost{true, 0.55, 0.90},
+    kSmallCost{true, 0.28, 0.43}, kTinyCost{true, 0.30, 0.50};
 // Estimated us of `tiles` tiles whose contraction is cut into `parts` of `steps` steps: the
 // turns of the workgroups, and for more than one part a second kernel and the fp32 sums
 // written and read again.
-inline double estimate(StepCost cost, int64_t tiles, int32_t parts, int32_t steps, int64_t outputs) {
-    const int64_t groups = tiles * parts;
-    const double turns = groups <= kCus ? cost.one : cost.two * (double)((groups + 2 * kCus - 1) / (2 * kCus));
+inline double estimate(StepCost cost, double tiles, int32_t parts, int32_t steps, int64_t outputs) {
+    const double groups = tiles * parts;
+    double turns;
+    if (cost.two) {
+        turns = groups <= kCus ? cost.less : cost.full * std::ceil(groups / (2 * kCus));
+    } else {
+        const double whole = std::floor(groups / kCus), rest = groups / kCus - whole;
+        turns = whole * cost.full + (rest > 0 ? cost.less + rest * (cost.full - cost.less) : 0.0);
+    }
     return turns * steps + (parts > 1 ? 3.0 + (double)parts * (double)outputs * 8 / 3e6 : 0.0);
 }
 constexpr int32_t kSplitSteps = 4;  // fewest steps of a part
