@@ -250,10 +250,11 @@ struct GradTile {
     int i, j;
     StepCost cost;
 };
-constexpr GradTile kGradTiles[] = {{GradSize::kLarge, Large::kI, Large::kJ, kLargeCost},
-                                   {GradSize::kBroad, Broad::kI, Broad::kJ, kBroadCost},
-                                   {GradSize::kMedium, Medium::kI, Medium::kJ, kMediumCost},
-                                   {GradSize::kSmall, Small::kI, Small::kJ, kSmallCost}};
+// An operand read across the contraction makes a step longer, the smaller the tile the more.
+constexpr GradTile kGradTiles[] = {{GradSize::kLarge, Large::kI, Large::kJ, {false, 1.15, 1.90}},
+                                   {GradSize::kBroad, Broad::kI, Broad::kJ, {false, 1.00, 1.48}},
+                                   {GradSize::kMedium, Medium::kI, Medium::kJ, {true, 0.75, 1.10}},
+                                   {GradSize::kSmall, Small::kI, Small::kJ, {true, 0.50, 0.65}}};
 
 // The tile of dx: the large ones where the experts fill them and there is one for every compute
 // unit, else by the estimate of the time.  Measured, us: 300 rows 2048 x 2048, a call's dx and dw,
@@ -277,10 +278,9 @@ GradSize plan_dx(int64_t rows, int32_t E, int32_t K, int32_t Nw) {
 }
 
 // The tile and the parts of dw, from the rows per expert to expect: by the estimate where the large
-// tiles are fewer than the compute units (dw of 11253 rows, one 2432 x 512 expert).  A large tile
-// waits for the expert with the most rows: with several, its time counts a fifth more (measured,
-// us: 13124 rows of 15 skewed 1536 x 512 experts 44 with Large, 38 with Medium; 4096 rows of four
-// 2048 x 1408 experts 33 with Broad, 39 with Medium).
+// tiles are fewer than the compute units.  The expert with the most rows has the longest tiles: of
+// E experts about the fourth root of E times the mean's (routing with a normal bias of 0.5 or a
+// Zipf one of 0.7 gives 1.2 to 1.3 at 2 experts, 2.1 to 3.2 at 16).
 struct DwPlan {
     GradSize size;
     int32_t parts;
@@ -295,8 +295,8 @@ DwPlan plan_dw(int64_t rows, int32_t E, int32_t K, int64_t Nw) {
     double least = 0;
     for (const GradTile &g : kGradTiles)
         for (int32_t parts = 1; parts == 1 || steps / parts >= kSplitSteps; parts *= 2) {
-            const double t = estimate(g.cost, tiles(g.i, g.j), parts, (steps + parts - 1) / parts, E * Nw * K) *
-                             (E > 1 && !g.cost.two ? 1.2 : 1.0);
+            const double t = estimate(g.cost, tiles(g.i, g.j), parts, (steps + parts - 1) / parts, E * Nw * K,
+                                      std::sqrt(std::sqrt((double)E)));
             if (least == 0 || t < least) {
                 least = t;
                 best = {g.size, parts};

@@ -534,17 +534,19 @@ constexpr StepCost kLargeCost{false, 1.10, 1.85}, kBroadCost{false, 0.86, 1.44},
     kSmallCost{true, 0.28, 0.43}, kTinyCost{true, 0.30, 0.50};
 // Estimated us of `tiles` tiles whose contraction is cut into `parts` of `steps` steps: the
 // turns of the workgroups, and for more than one part a second kernel and the fp32 sums
-// written and read again.
-inline double estimate(StepCost cost, double tiles, int32_t parts, int32_t steps, int64_t outputs) {
+// written and read again (6 MB a us: most of them stay in the memory-side cache).  The longest tile
+// has `longest` times as many steps as the mean one.
+inline double estimate(StepCost cost, double tiles, int32_t parts, int32_t steps, int64_t outputs, double longest = 1.0) {
     const double groups = tiles * parts;
     double turns;
     if (cost.two) {
-        turns = groups <= kCus ? cost.less : cost.full * std::ceil(groups / (2 * kCus));
+        turns = groups <= kCus ? cost.less * longest : cost.full * std::max(std::ceil(groups / (2 * kCus)), longest);
     } else {
         const double whole = std::floor(groups / kCus), rest = groups / kCus - whole;
         turns = whole * cost.full + (rest > 0 ? cost.less + rest * (cost.full - cost.less) : 0.0);
+        turns = whole < 1 ? turns * longest : std::max(turns, cost.full * longest);
     }
-    return turns * steps + (parts > 1 ? 3.0 + (double)parts * (double)outputs * 8 / 3e6 : 0.0);
+    return turns * steps + (parts > 1 ? 3.0 + (double)parts * (double)outputs * 8 / 6e6 : 0.0);
 }
 constexpr int32_t kSplitSteps = 4;  // fewest steps of a part
 
