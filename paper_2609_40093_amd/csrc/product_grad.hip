@@ -15,17 +15,22 @@
 namespace ep {
 namespace {
 
-constexpr int kDzRows = 64;   // rows of one dz tile: one expert's, 4 waves of 16 rows
-constexpr int kDzCols = 512;  // columns: 64 lanes of 8
+constexpr int kDzCols = 512;  // columns of one dz tile: 64 lanes of 8
+// Rows of one dz tile, one expert's: 4 waves of 16 rows (the longer tiles leave fewer sums for the
+// bias), or of 4 where that gives fewer than two workgroups per compute unit.  Measured, us: 4725
+// rows of 352 15.8 / 8.7, 7574 rows of 512 gated 19.9 / 11.7.
+int dz_rows(int64_t rows, int32_t E, int32_t N) {
+    return row_tiles_most(rows, E, 64) * ((N + kDzCols - 1) / kDzCols) < 2 * kCus ? 16 : 64;
+}
 
 // dz (null: not stored) and the column sums of each row tile (partial, null: not wanted).
 template <bool GATED>
-__global__ __launch_bounds__(256) void product_dz_kernel(const int32_t *offsets, int64_t rows, int32_t E, int32_t N,
+__global__ __launch_bounds__(256) void product_dz_kernel(const int32_t *offsets, int64_t rows, int32_t E, int per, int32_t N,
                                                          int32_t act, const uint16_t *pre, const uint16_t *d_y,
                                                          uint16_t *dz, float *partial) {
     constexpr int kParts = GATED ? 2 : 1;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const RowTile rt = find_row_tile(offsets, rows, E, kDzRows, (int32_t)blockIdx.x, lane);
+    const RowTile rt = find_row_tile(offsets, rows, E, per, (int32_t)blockIdx.x, lane);
     if (rt.e < 0)
         return;
     const int32_t Nw = N * kParts;
@@ -104,14 +109,14 @@ __global__ __launch_bounds__(256) void product_dz_kernel(const int32_t *offsets,
 }
 
 // dbias[e][n] = sum over the expert's row tiles.
-__global__ __launch_bounds__(1024) void product_dbias_kernel(const int32_t *offsets, int64_t rows, int32_t E, int32_t Nw,
+__global__ __launch_bounds__(1024) void product_dbias_kernel(const int32_t *offsets, int64_t rows, int32_t E, int per, int32_t Nw,
                                                              const float *partial, float *dbias) {
     const int e = blockIdx.y;
-    const int64_t first = count_row_tiles(offsets, rows, e, kDzRows, threadIdx.x & 63);
+    const int64_t first = count_row_tiles(offsets, rows, e, per, threadIdx.x & 63);
     int64_t b, t;
     expert_rows(offsets, rows, e, b, t);
     const int64_t n = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31);
-    const float s = column_sum(partial, first, first + (t - b + kDzRows - 1) / kDzRows, Nw, n);
+    const float s = column_sum(partial, first, first + (t - b + per - 1) / per, Nw, n);
     if (threadIdx.x < 32 && n < Nw)
         dbias[(int64_t)e * Nw + n] = s;
 }
@@ -311,9 +316,9 @@ size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 // dw's parts [parts][E][Nw][K] fp32 (more than one).
 struct GradWorkspace {
     size_t bias = 0, parts = 0, bytes = 0;  // offsets, and the size
-    GradWorkspace(int64_t rows, int32_t E, int32_t K, int64_t Nw, int32_t act, bool with_bias, int32_t dw_parts) {
+    GradWorkspace(int64_t rows, int32_t E, int32_t K, int32_t N, int64_t Nw, int32_t act, bool with_bias, int32_t dw_parts) {
         bias = act == EP_ACT_NONE ? 0 : align256((size_t)(rows * Nw * 2));
-        parts = bias + (with_bias ? align256((size_t)(row_tiles_most(rows, E, kDzRows) * Nw * 4)) : 0);
+        parts = bias + (with_bias ? align256((size_t)(row_tiles_most(rows, E, dz_rows(rows, E, N)) * Nw * 4)) : 0);
         bytes = parts + (dw_parts > 1 ? (size_t)dw_parts * E * Nw * K * 4 : 0);
     }
 };
@@ -322,21 +327,22 @@ struct GradWorkspace {
 
 size_t product_grad_workspace_bytes(int64_t rows, int32_t E, int32_t K, int32_t N, int32_t act, bool bias) {
     const int64_t Nw = act == EP_ACT_SWIGLU ? 2 * (int64_t)N : N;
-    return GradWorkspace(rows, E, K, Nw, act, bias, plan_dw(rows, E, K, Nw).parts).bytes;
+    return GradWorkspace(rows, E, K, N, Nw, act, bias, plan_dw(rows, E, K, Nw).parts).bytes;
 }
 
 hipError_t launch_product_grad(const ProductGradArgs &a, hipStream_t stream) {
     uint16_t *own_dz = a.act == EP_ACT_NONE ? nullptr : static_cast<uint16_t *>(a.workspace);
     const DwPlan dw = plan_dw(a.rows, a.E, a.K, a.Nw);
-    const GradWorkspace ws(a.rows, a.E, a.K, a.Nw, a.act, a.dbias != nullptr, dw.parts);
+    const GradWorkspace ws(a.rows, a.E, a.K, a.N, a.Nw, a.act, a.dbias != nullptr, dw.parts);
+    const int per = dz_rows(a.rows, a.E, a.N);
     float *partial = nullptr;
     if (a.dbias)
         partial = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + ws.bias);
     if (a.rows > 0 && (own_dz || partial)) {
-        const dim3 grid((unsigned)row_tiles_most(a.rows, a.E, kDzRows), (unsigned)((a.N + kDzCols - 1) / kDzCols));
+        const dim3 grid((unsigned)row_tiles_most(a.rows, a.E, per), (unsigned)((a.N + kDzCols - 1) / kDzCols));
         uint16_t *dz = a.dx || a.dw ? own_dz : nullptr;
 #define EP_CALL(GATED)                                                                                              \
-    launch_traced("expert_product_dz", product_dz_kernel<GATED>, grid, 256, stream, a.offsets, a.rows, a.E, a.N, a.act, \
+    launch_traced("expert_product_dz", product_dz_kernel<GATED>, grid, 256, stream, a.offsets, a.rows, a.E, per, a.N, a.act, \
                   (const uint16_t *)(own_dz ? a.pre : nullptr), (const uint16_t *)a.d_y, dz, partial)
         const hipError_t e = a.act == EP_ACT_SWIGLU ? EP_CALL(true) : EP_CALL(false);
 #undef EP_CALL
@@ -346,7 +352,7 @@ hipError_t launch_product_grad(const ProductGradArgs &a, hipStream_t stream) {
     if (a.dbias) {
         const hipError_t e = launch_traced("expert_product_dbias", product_dbias_kernel,
                                            dim3((unsigned)((a.Nw + 31) / 32), (unsigned)a.E), 1024, stream, a.offsets,
-                                           a.rows, a.E, a.Nw, (const float *)partial, a.dbias);
+                                           a.rows, a.E, per, a.Nw, (const float *)partial, a.dbias);
         if (e != hipSuccess)
             return e;
     }
