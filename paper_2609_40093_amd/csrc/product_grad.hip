@@ -108,15 +108,16 @@ __global__ __launch_bounds__(256) void product_dz_kernel(const int32_t *offsets,
     }
 }
 
-// dbias[e][n] = sum over the expert's row tiles.
+// dbias[e][n] = sum over the expert's row tiles, of which `partial` holds `most` (offsets that
+// decrease would make more).
 __global__ __launch_bounds__(1024) void product_dbias_kernel(const int32_t *offsets, int64_t rows, int32_t E, int per, int32_t Nw,
-                                                             const float *partial, float *dbias) {
+                                                             const float *partial, int64_t most, float *dbias) {
     const int e = blockIdx.y;
-    const int64_t first = count_row_tiles(offsets, rows, e, per, threadIdx.x & 63);
+    const int64_t first = clamp_row(count_row_tiles(offsets, rows, e, per, threadIdx.x & 63), most);
     int64_t b, t;
     expert_rows(offsets, rows, e, b, t);
     const int64_t n = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31);
-    const float s = column_sum(partial, first, first + (t - b + per - 1) / per, Nw, n);
+    const float s = column_sum(partial, first, clamp_row(first + (t - b + per - 1) / per, most), Nw, n);
     if (threadIdx.x < 32 && n < Nw)
         dbias[(int64_t)e * Nw + n] = s;
 }
@@ -352,7 +353,8 @@ hipError_t launch_product_grad(const ProductGradArgs &a, hipStream_t stream) {
     if (a.dbias) {
         const hipError_t e = launch_traced("expert_product_dbias", product_dbias_kernel,
                                            dim3((unsigned)((a.Nw + 31) / 32), (unsigned)a.E), 1024, stream, a.offsets,
-                                           a.rows, a.E, per, a.Nw, (const float *)partial, a.dbias);
+                                           a.rows, a.E, per, a.Nw, (const float *)partial, row_tiles_most(a.rows, a.E, per),
+                                           a.dbias);
         if (e != hipSuccess)
             return e;
     }

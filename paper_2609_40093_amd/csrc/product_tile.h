@@ -465,6 +465,8 @@ __device__ __forceinline__ RowTile find_row_tile(const int32_t *offsets, int64_t
             const int64_t end = (int64_t)__builtin_amdgcn_readlane((int32_t)t, at);
             const int64_t row0 = begin + (int64_t)tile * per;
             const int64_t left = end - row0;
+            if (left <= 0)  // more tiles than 32 bits count: only where offsets decrease
+                return {-1, 0, 0};
             return {e0 + at, row0, (int32_t)(left < per ? left : per)};
         }
         before += __builtin_amdgcn_readlane(incl, 63);

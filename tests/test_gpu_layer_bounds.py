@@ -132,3 +132,20 @@ def test_product_of_8bit_rows(counts, K, N, streamed):
         got = run(streamed, lambda s: ep.expert_product(x, w, off, w_scale=scale, out=at((rows, N), dtype), stream=s))
         at.check()
         assert torch.equal(got.out, ep.expert_product(x, w, off, w_scale=scale, out_dtype=dtype).out)
+
+
+@pytest.mark.parametrize("offsets", [[0, 300, 0, 300], [300, 0, 300, 0], [-5, 1000, -7, 2000], [0, 0, 0, 0]])
+@pytest.mark.parametrize("act", ["none", "silu", "swiglu"])
+def test_decreasing_offsets_stay_in_bounds(offsets, act):
+    """What such offsets give is not defined; nothing beside the outputs is touched."""
+    say(f"decreasing offsets {offsets} {act}")
+    rows, E, K, N = 300, 3, 136, 72
+    wide = 2 * N if act == "swiglu" else N
+    g, at = ref.gen(5), Guarded()
+    x, w, d = ref.normal((rows, K), g), ref.normal((E, wide, K), g), ref.normal((rows, N), g)
+    pre = ref.normal((rows, wide), g)
+    off = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+    ep.expert_product(x, w, off, act=act, keep_pre=at((rows, wide)), out=at((rows, N)))
+    ep.expert_product_grad(x, w, d, off, pre=pre, act=act, dx=at((rows, K)), dw=at((E, wide, K)),
+                           dbias=at((E, wide), torch.float32))
+    at.check()
