@@ -25,18 +25,24 @@ constexpr int block_threads() {
     return WAVES < 4 ? 256 : WAVES * 64;
 }
 
-// 1 / sqrt(mean(s^2) + eps) of a row from ss = sum(s^2).  Where the squares leave fp32's range
-// (values above 2^60, or below 2^-40 with next to no eps), the row's sum is taken again of its
-// values times a power of two; `again(f)` gives sum((f s)^2) over the row.  The condition is
-// the same in every lane of a row, and no row of ordinary values takes the branch.
+// 1 / sqrt(mean(s^2) + eps) of a row from ss = sum(s^2), as the factors of s f r: f a power of two.
+// Where the squares leave fp32's range (values above 2^52, or below 2^-40 with next to no eps), the
+// row's sum is taken again of its values times f, which puts every row of finite values within the
+// range: the values of the first kind, below 2^128, come to less than 2^32, and those of the second,
+// bf16's subnormals among them, to 2^-37 .. 2^56.  `again(f)` gives sum((f s)^2) over the row.  r alone
+// stays a normal number, where f r need not.  The condition is the same in every lane of a row; f is 1
+// in rows of ordinary values.
+struct InverseRms {
+    float f, r;
+};
 template <typename F>
-__device__ __forceinline__ float inverse_rms(float ss, int H, float eps, F again) {
+__device__ __forceinline__ InverseRms inverse_rms(float ss, int H, float eps, F again) {
     const bool large = ss > 0x1p120f, small = ss < 0x1p-80f && eps < 0x1p-80f;
     if (large || small) {
-        const float f = large ? 0x1p-64f : 0x1p64f;
-        return f / sqrtf(again(f) / (float)H + eps * f * f);
+        const float f = large ? 0x1p-96f : 0x1p96f;
+        return {f, 1.f / sqrtf(again(f) / (float)H + eps * f * f)};
     }
-    return 1.f / sqrtf(ss / (float)H + eps);
+    return {1.f, 1.f / sqrtf(ss / (float)H + eps)};
 }
 
 // Sum over the waves of a row; every wave of the workgroup calls it.
@@ -136,7 +142,7 @@ __global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_kernel(NormArg
             }
             parity ^= 1;  // the next row writes the other half: one barrier per row
         }
-        const float rstd = inverse_rms(ss, a.H, a.eps, [&](float f) {
+        const InverseRms rms = inverse_rms(ss, a.H, a.eps, [&](float f) {
             float q2 = 0.f;
 #pragma unroll
             for (int v = 0; v < V; ++v)
@@ -145,7 +151,7 @@ __global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_kernel(NormArg
                     q2 = fmaf(s[v][q] * f, s[v][q] * f, q2);
             return row_sum<WAVES>(q2, redo, tid);
         });
-        const float most = __uint_as_float(top) * rstd;
+        const float most = __uint_as_float(top) * rms.f * rms.r;
         const float scale = (most < kLeastMax ? kLeastMax : most) / kF8Max;  // a NaN stays one
         const float inv = 1.f / scale;
 #pragma unroll
@@ -159,7 +165,7 @@ __global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_kernel(NormArg
             unpack8(wv[v], w);
 #pragma unroll
             for (int q = 0; q < 8; ++q)
-                y[q] = s[v][q] * rstd * w[q];
+                y[q] = s[v][q] * rms.f * rms.r * w[q];
             if (a.out)
                 store_row(pack8(y), a.out + base + i, NT);
             if (a.rows8) {
@@ -262,7 +268,7 @@ __global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_grad_kernel(No
             }
             parity ^= 1;
         }
-        const float rstd = inverse_rms(ss, a.H, a.eps, [&](float f) {
+        const InverseRms rms = inverse_rms(ss, a.H, a.eps, [&](float f) {
             float q2 = 0.f;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
@@ -274,7 +280,7 @@ __global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_grad_kernel(No
             }
             return row_sum<WAVES>(q2, redo, tid);
         });
-        const float c = gs * rstd / (float)a.H;  // mean(g n)
+        const float c = gs * rms.f * rms.r / (float)a.H;  // mean(g n)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int i = v * (WAVES * 64) + tid;
@@ -287,9 +293,9 @@ __global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_grad_kernel(No
             unpack8(tv[v], t);
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
-                const float n = s[q] * rstd;
+                const float n = s[q] * rms.f * rms.r;
                 dw[v][q] = fmaf(d[q], n, dw[v][q]);
-                t[q] = fmaf(rstd, d[q] * w[q] - n * c, t[q]);
+                t[q] = fmaf(rms.r, (d[q] * w[q] - n * c) * rms.f, t[q]);
             }
             store_row(pack8(t), a.dx + base + i, NT);
         }

@@ -242,3 +242,38 @@ def test_binding_refusals():
         ep.rmsnorm_grad(x, w, x[:3])
     with pytest.raises(ValueError):
         ep.rmsnorm_grad(x, w, x, d_weight=torch.zeros(64, device="cuda", dtype=torch.bfloat16))
+
+
+# Row lengths of every number of waves per row.
+WAVES = [80, 1040, 2064, 7168, 16400, 65536]
+
+
+def rows_at(exponents, H, seed):
+    """Rows of values of random sign in [1/2, 1) 2^e, one for each e."""
+    g = ref.gen(seed)
+    x = (torch.rand((len(exponents), H), device="cuda", generator=g, dtype=torch.float64) * 0.5 + 0.5)
+    x = x * torch.where(torch.rand(x.shape, device="cuda", generator=g) < 0.5, -1.0, 1.0)
+    return (x * 2.0 ** torch.tensor(exponents, device="cuda", dtype=torch.float64)[:, None]).clamp(-3.3e38, 3.3e38).bfloat16()
+
+
+@pytest.mark.parametrize("H", WAVES)
+def test_largest_values(H):
+    """Rows whose squares, and sums of squares, leave fp32 at the top: y is of the size of the weight."""
+    say(f"rmsnorm of the largest values H={H}")
+    exponents = [59, 60, 61, 64, 100, 116, 120, 122, 123, 124, 125, 126, 127, 128]
+    x = rows_at(exponents, H, H)
+    x[-1] = 3.3895313892515355e38                   # bf16's largest
+    for eps in (0.0, 1e-6):
+        check(x, None, None, eps)
+    check(x[:-2], x[:-2], None, 1e-6)               # sums of them, up to 2^127
+    one = torch.full((1, H), 5e36, dtype=torch.bfloat16, device="cuda")
+    assert (ep.rmsnorm(one, None).out == 1).all()
+
+
+@pytest.mark.parametrize("H", WAVES)
+def test_smallest_values(H):
+    """The same at the bottom, without eps, down to the subnormals."""
+    say(f"rmsnorm of the smallest values H={H}")
+    x = rows_at([-39, -40, -41, -44, -64, -100, -120, -126, -128, -130, -132], H, H)
+    check(x, None, None, 0.0)
+    check(x[:8], x[:8], None, 0.0)
