@@ -6,7 +6,7 @@
 //
 // Both are HBM-bound: every row is read once and held in registers between its reduction and
 // its results.  The forward reduces sum(s^2) and max|s w| in the same step: the row's largest
-// |y| is max|s w| rstd, so the 8-bit rows need no second reduction; the backward likewise
+// |y| is max|s w| rstd, so the 8-bit rows of ordinary values need no second reduction; the backward likewise
 // reduces sum(s^2) and sum(g s) together.  32768 rows of 7168 with a residual, the sum, bf16 and
 // 8-bit rows: 2.1 GB in 372 us, 5.7 TB/s; the gradient of 5003 rows of 2888: 116 MB in 27 us, 4.3
 // TB/s; 256 rows of 7168 into 8-bit rows: 5 us, of which 2 are bytes.
@@ -38,7 +38,7 @@ struct InverseRms {
 template <typename F>
 __device__ __forceinline__ InverseRms inverse_rms(float ss, int H, float eps, F again) {
     const bool large = ss > 0x1p120f, small = ss < 0x1p-80f && eps < 0x1p-80f;
-    if (large || small) {
+    if (__builtin_expect(large || small, false)) {
         const float f = large ? 0x1p-96f : 0x1p96f;
         return {f, 1.f / sqrtf(again(f) / (float)H + eps * f * f)};
     }
@@ -58,6 +58,25 @@ __device__ __forceinline__ float row_sum(float v, float *slot, int tid) {
 #pragma unroll
         for (int i = 0; i < WAVES; ++i)
             v += slot[i];
+    }
+    return v;
+}
+
+// The same of the largest.
+template <int WAVES>
+__device__ __forceinline__ uint32_t row_max(uint32_t v, float *slot, int tid) {
+    v = wave_max(v);
+    if (WAVES > 1) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0)
+            slot[tid / 64] = __uint_as_float(v);
+        __syncthreads();
+        v = 0;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) {
+            const uint32_t m = __float_as_uint(slot[i]);
+            v = m > v ? m : v;
+        }
     }
     return v;
 }
@@ -151,7 +170,23 @@ __global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_kernel(NormArg
                     q2 = fmaf(s[v][q] * f, s[v][q] * f, q2);
             return row_sum<WAVES>(q2, redo, tid);
         });
-        const float most = __uint_as_float(top) * rms.f * rms.r;
+        float most = __uint_as_float(top) * rms.r;
+        // The largest |y| itself where s w may have left fp32 and y not.  (A product below fp32's normal
+        // numbers lacks digits, which counts where 1 / rms brings it above kLeastMax.)
+        if (__builtin_expect(a.rows8 && (rms.f != 1.f || top == 0x7f800000u || (top < 0x00800000u && rms.r > 0x1p26f)), false)) {
+            top = 0;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                float w[8];
+                unpack8(wv[v], w);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const uint32_t m = __float_as_uint(s[v][q] * rms.f * rms.r * w[q]) & 0x7fffffffu;
+                    top = m > top ? m : top;
+                }
+            }
+            most = __uint_as_float(row_max<WAVES>(top, redo, tid));
+        }
         const float scale = (most < kLeastMax ? kLeastMax : most) / kF8Max;  // a NaN stays one
         const float inv = 1.f / scale;
 #pragma unroll

@@ -277,3 +277,18 @@ def test_smallest_values(H):
     x = rows_at([-39, -40, -41, -44, -64, -100, -120, -126, -128, -130, -132], H, H)
     check(x, None, None, 0.0)
     check(x[:8], x[:8], None, 0.0)
+
+
+@pytest.mark.parametrize("H", WAVES)
+def test_8bit_scale_of_large_and_small_products(H):
+    """Values times weights that leave fp32 where y, their product over the row's size, does not."""
+    say(f"rmsnorm, 8-bit rows of large and small products H={H}")
+    for value, weight, eps in ((50, 100, 1e-6), (100, 30, 1e-6), (3, 126, 1e-6), (126, 60, 0.0), (-100, -40, 0.0), (-40, -95, 0.0),
+                               (-120, -20, 0.0), (-60, 120, 0.0), (-10, -115, 0.0)):
+        x = rows_at([value - 1, value, value + 1], H, H + value + 200)
+        check(x, None, rows_at([weight], H, H)[0].contiguous(), eps)
+    x = rows_at([3, 3], H, 1)
+    x[0] = 0                                        # zeros beside ordinary rows, whatever the weight
+    for weight in (120, -120):
+        got = check(x, None, rows_at([weight], H, H)[0].contiguous(), 1e-6)
+        assert not ep.rows8_values(got.rows8)[0][0].float().any()    # a zero times a negative weight is -0
