@@ -315,7 +315,24 @@ __global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_grad_kernel(No
             }
             return row_sum<WAVES>(q2, redo, tid);
         });
-        const float c = gs * rms.f * rms.r / (float)a.H;  // mean(g n)
+        // sum(g n); from its own terms where those of sum(g s) may have left fp32 (what they lose below its
+        // normal numbers counts where 1 / rms is large)
+        float gn = gs * rms.r;
+        if (__builtin_expect(rms.f != 1.f || !(fabsf(gs) < INFINITY) || (fabsf(gs) < 0x1p-100f && rms.r > 16.f), false)) {
+            gn = 0.f;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                float s[8], d[8], w[8];
+                unpack8(sv[v], s);
+                unpack8(dv[v], d);
+                unpack8(wv[v], w);
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    gn = fmaf(d[q] * w[q], s[q] * rms.f * rms.r, gn);
+            }
+            gn = row_sum<WAVES>(gn, redo, tid);
+        }
+        const float c = gn / (float)a.H;  // mean(g n)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int i = v * (WAVES * 64) + tid;

@@ -292,3 +292,35 @@ def test_8bit_scale_of_large_and_small_products(H):
     for weight in (120, -120):
         got = check(x, None, rows_at([weight], H, H)[0].contiguous(), 1e-6)
         assert not ep.rows8_values(got.rows8)[0][0].float().any()    # a zero times a negative weight is -0
+
+
+@pytest.mark.parametrize("H", WAVES)
+def test_gradient_of_large_and_small_values(H):
+    """The gradient where the row's values, the rows' gradients or their products are near the ends
+    of fp32.  bf16's subnormals are 2^-133 apart, so that a result that small is half of that off."""
+    say(f"rmsnorm_grad of large and small values H={H}")
+    for value, slope, weight, eps in ((64, 0, 0, 1e-6), (100, 0, 0, 1e-6), (122, 0, 0, 0.0), (127, 0, 0, 0.0), (60, 80, 10, 0.0),
+                                      (100, 60, 40, 0.0), (20, 110, 5, 1e-6), (-64, 0, 0, 0.0), (-100, -20, -10, 0.0),
+                                      (-126, -6, 0, 0.0), (-130, -12, 0, 0.0), (-20, -90, -20, 0.0), (-38, -60, -40, 0.0)):
+        s = rows_at([value - 1, value, value - 2], H, H + value + 300)
+        d, w = rows_at([slope, slope, slope - 3], H, H + slope + 700), rows_at([weight], H, H)[0].contiguous()
+        for dt in (None, rows_at([0, 3, -20], H, H + 5)):
+            dx, dw = ep.rmsnorm_grad(s, w, d, d_total=dt, eps=eps)
+            want, size, want_w, size_w = ref.norm_grad(s, w, d, dt, eps)
+            ref.within(dx, want, want.abs() * ref.BF16 + size * 2.0 ** -14 + 2.0 ** -133, "dx")
+            ref.within(dw, want_w, size_w * (2.0 ** -14 + 3 * ref.U24) + 2.0 ** -147, "dw")
+
+
+def test_gradient_of_zeros_nan_and_infinity_stays_in_their_rows():
+    say("rmsnorm_grad: zeros, NaN and infinities")
+    for H in (1032, 7168):
+        g = ref.gen(H)
+        s, d, w = ref.normal((9, H), g), ref.normal((9, H), g), ref.normal(H, g)
+        d[1] = 0
+        clean, _ = ep.rmsnorm_grad(s, w, d, d_total=d)
+        s[3, 7], d[5, 9] = float("nan"), float("inf")
+        d[6, 4] = float("nan")
+        dx, _ = ep.rmsnorm_grad(s, w, d, d_total=d)
+        keep = [0, 1, 2, 4, 7, 8]
+        assert torch.equal(dx[keep], clean[keep]) and not dx[1].any()
+        assert dx[3].isnan().all() and dx[6].isnan().all() and not torch.isfinite(dx[5]).any()
