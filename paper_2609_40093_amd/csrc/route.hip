@@ -398,6 +398,8 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradArgs a) {
             if (own.has(i))
                 g[i] = c * (float)a.counts[own.e0 + i];
     }
+    // normalized gates alone do not look at the others' p: a NaN there is none of theirs
+    const bool through_p = a.d_loss || !a.normalize;
     const int64_t stride = (int64_t)gridDim.x * 4;
     for (int64_t t = (int64_t)blockIdx.x * 4 + wave; t < a.T; t += stride) {
         const L *row = static_cast<const L *>(a.logits) + t * a.E;
@@ -461,7 +463,8 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradArgs a) {
         Elements<NV, L> vec;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const float d = live ? fmaf(z[i] * inv, g[i] - pg, chosen[wave][i * 64 + lane]) : 0.f;
+            const float c = chosen[wave][i * 64 + lane];
+            const float d = !live ? 0.f : through_p ? fmaf(z[i] * inv, g[i] - pg, c) : c;
             chosen[wave][i * 64 + lane] = 0.f;
             if constexpr (sizeof(L) == 2)
                 vec.v[i] = (L)bf16_pair(d, 0.f);

@@ -219,3 +219,31 @@ def test_binding_refusals():
             ep.route_grad(z, got, bad)
     with pytest.raises(ValueError):
         ep.route_grad(z, got, None, torch.zeros((), device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gradient_of_normalized_gates_looks_at_the_chosen_alone(dtype):
+    """Without the loss's gradient a NaN that was not chosen is no part of the gates: the row's gradient
+    is the one without it.  A NaN or +inf among the chosen is their gradient's, and no other expert's."""
+    say(f"route_grad: NaN beside the chosen {dtype}")
+    for E, k in ((40, 4), (7, 3), (130, 3), (700, 5), (300, 70)):
+        T = 12
+        g = ref.gen(E)
+        z = ref.normal((T, E), g, 1.0, dtype)
+        low = z.float().argmin(1)                   # never among the k largest
+        z[3, low[3]] = float("nan")
+        z[8, low[8]] = float("nan")
+        z[10, 2] = math.inf
+        d = torch.randn((T, k), device="cuda", generator=g)
+        got = ep.route(z, k)
+        assert low[3] not in got.topk_idx[3] and torch.isfinite(got.topk_w[[3, 8]]).all()
+        dz = ep.route_grad(z, got, d)
+        rest = [t for t in range(T) if t != 10]
+        want, size = ref.route_grad(z[rest], got.topk_idx[rest].cpu().long(), k, None, True, 0.0, d[rest], None, None)
+        step = ref.BF16 if dtype == torch.bfloat16 else 2.0 ** -20
+        ref.within(dz[rest].cpu(), want, want.abs() * step + size * 2.0 ** -14 + 1e-36, "d_logits")
+        chosen = torch.zeros(E, dtype=torch.bool, device="cuda")
+        chosen[got.topk_idx[10].long()] = True
+        assert dz[10][chosen].isnan().all() and not dz[10][~chosen].any()
+        whole = ep.route_grad(z, got, d, torch.ones(1, device="cuda"))     # the loss's goes through every p
+        assert whole[[3, 8, 10]].isnan().all()
