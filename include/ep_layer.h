@@ -124,7 +124,7 @@ ep_status ep_route(const void *logits_dev, int32_t logits_bf16, const uint8_t *m
  *   d_loss    device fp32 [1] or NULL: the balance loss's gradient
  *   topk_idx  as ep_route wrote it;  counts  int32 [E] as ep_route wrote it (only with d_loss):
  *             a group of ranks that balances over all its tokens sums the counts and gives the
- *             sum; N is then the sum's number of tokens
+ *             sum; N is then the sum's number of tokens (the counts together may pass 2^31)
  *   d_logits  [T][E] in the logits' type; may be the logits themselves
  * The counts are constants of the loss, as usual.  A token that is not live gets zeros. */
 ep_status ep_route_grad(const void *logits_dev, int32_t logits_bf16, const uint8_t *mask, const int32_t *topk_idx,

@@ -366,7 +366,7 @@ __global__ __launch_bounds__(1024) void route_finish_kernel(void *workspace, int
 template <int NV, bool EVEN, typename L>
 __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradArgs a) {
     __shared__ float chosen[4][64 * NV];  // per wave: the gates' gradient by expert, zero elsewhere
-    __shared__ int wave_n[4];
+    __shared__ long long wave_n[4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Lane<NV, EVEN> own(lane, a.E);
     float g[NV];
@@ -381,7 +381,7 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradArgs a) {
         return (EVEN ? e % NV : e - l.e0) * 64 + e / NV;
     };
     if (a.d_loss) {
-        int n = 0;
+        long long n = 0;  // a group's counts may pass 32 bits together
         for (int e = threadIdx.x; e < a.E; e += 256)
             n += a.counts[e];
 #pragma unroll
@@ -390,8 +390,8 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteGradArgs a) {
         if (lane == 0)
             wave_n[wave] = n;
         __syncthreads();
-        const int total = wave_n[0] + wave_n[1] + wave_n[2] + wave_n[3];
-        const float tokens = (float)(total / a.k);
+        const long long total = wave_n[0] + wave_n[1] + wave_n[2] + wave_n[3];
+        const float tokens = (float)((double)total / a.k);
         const float c = total == 0 ? 0.f : *a.d_loss * a.balance * (float)a.E / (tokens * (float)a.k * tokens);
 #pragma unroll
         for (int i = 0; i < NV; ++i)

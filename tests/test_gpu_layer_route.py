@@ -247,3 +247,19 @@ def test_gradient_of_normalized_gates_looks_at_the_chosen_alone(dtype):
         assert dz[10][chosen].isnan().all() and not dz[10][~chosen].any()
         whole = ep.route_grad(z, got, d, torch.ones(1, device="cuda"))     # the loss's goes through every p
         assert whole[[3, 8, 10]].isnan().all()
+
+
+def test_counts_of_a_large_group():
+    """A group's counts may add up to more than 32 bits hold."""
+    say("route_grad with a large group's counts")
+    k, balance, d_loss = 2, 0.5, 3e9
+    for E, counts in ((4, [2 ** 31 - 8, 2 ** 31 - 100, 2 ** 30, 2 ** 31 - 2]), (600, [2 ** 24 + 3 * e for e in range(600)])):
+        z = ref.normal((20, E), ref.gen(E), 1.0, torch.float32)
+        total = torch.tensor(counts, dtype=torch.int32, device="cuda")
+        got = ep.route(z, k, balance=balance)
+        dz = ep.route_grad(z, got, None, torch.tensor([d_loss], device="cuda"), counts=total)
+        n = sum(counts) // k
+        g = torch.tensor([d_loss * balance * E * c / (n * k * n) for c in counts], dtype=torch.float64)
+        p = torch.softmax(z.double().cpu(), 1)
+        want, size = p * (g - (p @ g)[:, None]), p * (g + (p @ g)[:, None])
+        ref.within(dz.cpu(), want, want.abs() * 2.0 ** -20 + size * 2.0 ** -14 + 1e-36, "d_logits")
