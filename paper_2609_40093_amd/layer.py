@@ -219,8 +219,10 @@ def combine_grad(d_out: torch.Tensor, y: torch.Tensor, slot_pos: torch.Tensor, t
                  dy: Union[bool, torch.Tensor] = True, d_topk_w: Union[bool, torch.Tensor] = True,
                  stream=None) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
     """ep_combine_grad of combine_rows(y, slot_pos, topk_w): (dy bf16 like y, d_topk_w fp32
-    [T, k]).  A new dy is zero where no slot names a row only if every row is named: give a
-    zeroed `dy` for layouts with unnamed rows."""
+    [T, k]).  Rows that no slot names keep what dy holds.  A new dy holds zeros there if y has
+    more rows than there are slots; with as many or fewer its memory is not cleared, so where
+    slots are without a row (a slot_pos outside y) and the rows left over are read, give a
+    zeroed `dy`."""
     _need(topk_w, "topk_w", _F32, 2)
     _need(y, "y", _BF16, 2)
     T, k = topk_w.shape
@@ -228,7 +230,10 @@ def combine_grad(d_out: torch.Tensor, y: torch.Tensor, slot_pos: torch.Tensor, t
     _optional(_given(d_out, "d_out"), "d_out", _BF16, (T, H))
     _optional(_given(slot_pos, "slot_pos"), "slot_pos", _I32, (T * k,))
     with _on(stream):
-        dy = _output(dy, "dy", torch.bfloat16, y.shape, y.device)
+        if dy is True and y.shape[0] > T * k:
+            dy = torch.zeros_like(y)
+        else:
+            dy = _output(dy, "dy", torch.bfloat16, y.shape, y.device)
         d_topk_w = _output(d_topk_w, "d_topk_w", torch.float32, (T, k), y.device)
     _check(_lib_handle().ep_combine_grad(_ptr(d_out), _ptr(y), y.shape[0], _ptr(slot_pos), _ptr(topk_w), T, H, k,
                                          _ptr(dy), _ptr(d_topk_w), _current_stream(stream)), "ep_combine_grad")

@@ -106,3 +106,21 @@ def test_rows_past_4_gib():
     ref.within(dy[pos.long()], want, want.abs() * (ref.BF16 + 2.0 ** -20), "dy")
     terms = y[pos.long()].double() * d.double().repeat_interleave(2, 0)
     ref.within(dw.view(-1), terms.sum(1), terms.abs().sum(1) * (H / 64 + 8) * ref.U24, "d_topk_w")
+
+
+def test_new_dy_of_a_buffer_with_more_rows_than_slots():
+    """Rows behind the last slot's are zeros in a new dy, whatever its memory held."""
+    say("combine_grad: a new dy with rows that no slot names")
+    T, k, H, more = 50, 3, 264, 37
+    g = ref.gen(4)
+    d, y, w = ref.normal((T, H), g), ref.normal((T * k + more, H), g), torch.rand((T, k), device="cuda", generator=g)
+    pos = torch.randperm(T * k + more, device="cuda", generator=g)[:T * k].int()
+    want, _ = ep.combine_grad(d, y, pos, w, dy=torch.zeros_like(y))
+    for stream in (None, torch.cuda.Stream()):
+        for _ in range(3):
+            held = torch.full_like(y, float("nan"))
+            torch.cuda.synchronize()
+            del held                                # a new tensor of this size is likely to get its memory
+            dy, _ = ep.combine_grad(d, y, pos, w, stream=stream)
+            torch.cuda.synchronize()
+            assert torch.equal(dy, want)
