@@ -6,6 +6,8 @@ for the bias, the two scales, the residual and the join of partial sums).  An ac
 stretches that by at most 1.2 (layer_ref.act_error) and is itself within 2^-18.  The
 gradient's dz is rounded to bf16 before the two products (2^-8 of each term) and its
 activation's slope is within 2^-17."""
+import math
+
 import pytest
 import torch
 
@@ -389,3 +391,27 @@ def test_binding_refusals():
             ep.expert_product_grad(x, w, bad, off)
     with pytest.raises(ValueError):
         ep.expert_product_grad(x, w, d_y, off, act="silu")
+
+
+def test_gelu_of_negative_values_keeps_its_digits():
+    """z Phi(z) over the range of its tail, through an identity: the exponent -z^2 / 2 and its
+    exponential are off by 1.25 z^2 2^-24, the polynomial and its arithmetic by 24 2^-24; below 2^-120
+    the exponential may come out as zero."""
+    say("expert_product: gelu's tail")
+    g = ref.gen(12)
+    K = 64
+    x = (torch.rand((400, K), device="cuda", generator=g) * 26 - 13).bfloat16()
+    eye = torch.eye(K, device="cuda", dtype=torch.bfloat16)[None].contiguous()
+    z = x.double()
+    y = z * torch.exp(torch.special.log_ndtr(z))
+    off = y.abs() * (1.25 * z.square() + 32) * ref.U24 + 2.0 ** -120
+    wide = ep.expert_product(x, eye, act="gelu", out_dtype=torch.float32).out
+    ref.within(wide, y, off, "fp32")
+    ref.within(ep.expert_product(x, eye, act="gelu").out, y, (y.abs() + off) * ref.BF16 + off, "bf16")
+    # the slope Phi(z) + z phi(z), through d_y of ones; its terms cancel near -0.75
+    cdf, density = torch.exp(torch.special.log_ndtr(z)), z * torch.exp(-z * z / 2) / math.sqrt(2 * math.pi)
+    grad = ep.expert_product_grad(x, eye, torch.ones_like(x), pre=x, act="gelu", dw=False)
+    size = (cdf + density.abs()) * (1.25 * z.square() + 32) * ref.U24 + 2.0 ** -118
+    want = cdf + density
+    # dz is rounded to bf16, which the product with the identity keeps
+    ref.within(grad.dx, want, (want.abs() + size) * ref.BF16 + size, "slope")
