@@ -487,3 +487,38 @@ def test_gradient_against_differences_along_itself(act):
             along = (loss(*up) - loss(*down)) / (2 * h)
             whole = float(grad.double().abs().sum())
             assert abs(whole - float(along)) <= 0.004 * whole, (act, i)
+
+
+# ------------------------------------------------------------------- long sums of 8-bit rows
+
+# sums of 4000 terms and more are cut into more than four parts where rows are few
+@pytest.mark.parametrize("K", [512, 528, 1040, 2048, 4096, 7168])
+@pytest.mark.parametrize("counts", [[1], [8], [5, 0, 30], [70, 200], [300]], ids=str)
+def test_long_sums_of_8bit_rows(counts, K):
+    """fp32 results are sums of exact products: at 7168 terms of random signs, 16 to an addition, each
+    addition truncated to 2^-23 of the sum so far, their 2-norm is off by at most 2^-23 sqrt(448) / 2 =
+    1.3e-6 of the result's, so 2e-6 with the scales; twice that for a gate times an up.  bf16
+    results go through the 8-bit instruction, off by less than 2^-15 in the 2-norm, before their own
+    rounding of at most 2^-9."""
+    for N, act in ((72, "none"), (40, "swiglu")):
+        say(f"expert_product 8-bit rows={counts} K={K} N={N} {act}")
+        s = make(counts, K, N, act, K + N, bits8=True)
+        z, _ = ref.product_z(s["xd"], s["wd"], s["offsets"])
+        y = ref.act(z, act)
+        check(s, f32=True, pre=False)
+        check(s)
+        more = dict(w_scale=s["w_scale"], act=act)
+        wide = ep.expert_product(s["x"], s["w"], s["offsets"], out_dtype=torch.float32, **more).out.double()
+        assert float((wide - y).norm() / y.norm()) <= (2e-6 if act == "none" else 4e-6)
+        pre = ep.expert_product(s["x"], s["w"], s["offsets"], keep_pre=True, **more).pre.double()
+        assert float((pre - z).norm() / z.norm()) <= 2.0 ** -9 + 2.0 ** -15
+
+
+@pytest.mark.parametrize("rows,K,N", [(1, 7168, 256), (256, 7168, 256), (4, 2048, 4096), (100, 8192, 64)])
+def test_few_rows_keep_fp32_sums(rows, K, N):
+    """As test_few_rows_and_long_sums, in the 2-norm: sums cut into parts stay in fp32 to the end."""
+    say(f"expert_product dense rows={rows} K={K} N={N} in the 2-norm")
+    s = make([rows], K, N, "none", rows + K)
+    got = ep.expert_product(s["x"], s["w"], s["offsets"], out_dtype=torch.float32).out.double()
+    want = s["xd"] @ s["wd"][0].t()
+    assert float((got - want).norm() / want.norm()) <= 2e-6
