@@ -3,6 +3,10 @@
 Norm, router, experts' products and the gradients run in the library's HIP kernels; outputs
 and workspaces are torch tensors of the current device.  Without a tensor to write to, a call
 allocates its outputs; with `stream`, allocations belong to that stream.
+
+No call takes part in torch's autograd: outputs come detached, also of inputs that require grad,
+and the ..._grad calls are what a backward pass is made of (examples/moe_layer.py, or the
+backward of a torch.autograd.Function of the caller's).
 """
 from __future__ import annotations
 
