@@ -174,9 +174,13 @@ ep_status ep_expert_product(const void *x_dev, ep_rows_kind kind, int64_t rows, 
                             void *pre_dev, void *y_dev, ep_out_dtype out_dtype, void *workspace,
                             size_t workspace_bytes, hipStream_t stream);
 
-/* Bytes of workspace ep_expert_product_grad needs. */
+/* Bytes of workspace ep_expert_product_grad needs for the results named: EP_GRAD_DBIAS or 0, and
+ * what is not wanted.  (1 and 0, with a bias and without, stand for a call for dx and dw.) */
+#define EP_GRAD_DBIAS 1
+#define EP_GRAD_WITHOUT_DX 2
+#define EP_GRAD_WITHOUT_DW 4
 ep_status ep_expert_product_grad_workspace_bytes(int64_t rows, int32_t num_experts, int32_t in_length,
-                                                 int32_t out_length, ep_activation act, int32_t with_bias,
+                                                 int32_t out_length, ep_activation act, int32_t results,
                                                  size_t *bytes /* host out */);
 
 /* Gradient of ep_expert_product with bf16 rows:

@@ -18,6 +18,7 @@ EP_MODE_PER_SENDER, EP_MODE_DUPLEX, EP_MODE_REMOTE_ONLY, EP_MODE_ACCUMULATE = 1,
 ABI_VERSION = 6
 EP_MAX_EXPERTS = 2048
 EP_ROWS_BF16, EP_ROWS_8BIT, EP_ROWS8_EXTRA = 0, 1, 16
+EP_GRAD_DBIAS, EP_GRAD_WITHOUT_DX, EP_GRAD_WITHOUT_DW = 1, 2, 4
 EP_ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "swiglu": 4}
 
 c_i32, c_i64, c_u32, c_size, c_vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_size_t, ctypes.c_void_p

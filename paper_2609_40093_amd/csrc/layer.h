@@ -205,7 +205,7 @@ struct ProductGradArgs {
     float *dbias;
     void *workspace;  // of product_grad_workspace_bytes
 };
-size_t product_grad_workspace_bytes(int64_t rows, int32_t E, int32_t K, int32_t N, int32_t act, bool bias);
+size_t product_grad_workspace_bytes(int64_t rows, int32_t E, int32_t K, int32_t N, int32_t act, bool dx, bool dw, bool bias);
 hipError_t launch_product_grad(const ProductGradArgs &a, hipStream_t stream);
 
 }  // namespace ep

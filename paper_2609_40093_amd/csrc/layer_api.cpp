@@ -267,7 +267,7 @@ extern "C" ep_status ep_expert_product(const void *x_dev, ep_rows_kind kind, int
 }
 
 extern "C" ep_status ep_expert_product_grad_workspace_bytes(int64_t rows, int32_t num_experts, int32_t in_length,
-                                                            int32_t out_length, ep_activation act, int32_t with_bias,
+                                                            int32_t out_length, ep_activation act, int32_t results,
                                                             size_t *bytes) {
     const ep_status st = check_product("ep_expert_product_grad_workspace_bytes", rows, num_experts, in_length, out_length,
                                        EP_ROWS_BF16, act);
@@ -275,7 +275,10 @@ extern "C" ep_status ep_expert_product_grad_workspace_bytes(int64_t rows, int32_
         return st;
     if (!bytes)
         return fail(EP_ERR_INVALID_ARG, "ep_expert_product_grad_workspace_bytes: bytes is NULL");
-    *bytes = ep::product_grad_workspace_bytes(rows, num_experts, in_length, out_length, act, with_bias != 0);
+    if (results < 0 || results > (EP_GRAD_DBIAS | EP_GRAD_WITHOUT_DX | EP_GRAD_WITHOUT_DW))
+        return fail(EP_ERR_INVALID_ARG, "ep_expert_product_grad_workspace_bytes: unknown results %d", results);
+    *bytes = ep::product_grad_workspace_bytes(rows, num_experts, in_length, out_length, act, !(results & EP_GRAD_WITHOUT_DX),
+                                              !(results & EP_GRAD_WITHOUT_DW), (results & EP_GRAD_DBIAS) != 0);
     return EP_OK;
 }
 
@@ -296,7 +299,8 @@ extern "C" ep_status ep_expert_product_grad(const void *x_dev, int64_t rows, con
                                         "are required, every array 16-byte aligned");
     if (!aligned16(dx_dev) || !aligned16(dw_dev) || !aligned16(dbias) || !aligned(offsets, 4))
         return fail(EP_ERR_INVALID_ARG, "ep_expert_product_grad: an output is not 16-byte aligned");
-    const size_t need = ep::product_grad_workspace_bytes(rows, num_experts, in_length, out_length, act, dbias != nullptr);
+    const size_t need = ep::product_grad_workspace_bytes(rows, num_experts, in_length, out_length, act, dx_dev != nullptr,
+                                                         dw_dev != nullptr, dbias != nullptr);
     if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need))
         return fail(EP_ERR_INVALID_ARG, "ep_expert_product_grad: workspace of %zu bytes, need %zu, 16-byte aligned",
                     workspace ? workspace_bytes : (size_t)0, need);

@@ -313,12 +313,12 @@ DwPlan plan_dw(int64_t rows, int32_t E, int32_t K, int64_t Nw) {
 
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// dz [rows][Nw] bf16 (with an activation), then the bias's partial sums [row tiles][Nw] fp32, then
-// dw's parts [parts][E][Nw][K] fp32 (more than one).
+// dz [rows][Nw] bf16 (with an activation, for the products), then the bias's partial sums [row tiles][Nw]
+// fp32, then dw's parts [parts][E][Nw][K] fp32 (more than one).
 struct GradWorkspace {
     size_t bias = 0, parts = 0, bytes = 0;  // offsets, and the size
-    GradWorkspace(int64_t rows, int32_t E, int32_t K, int32_t N, int64_t Nw, int32_t act, bool with_bias, int32_t dw_parts) {
-        bias = act == EP_ACT_NONE ? 0 : align256((size_t)(rows * Nw * 2));
+    GradWorkspace(int64_t rows, int32_t E, int32_t K, int32_t N, int64_t Nw, bool with_dz, bool with_bias, int32_t dw_parts) {
+        bias = with_dz ? align256((size_t)(rows * Nw * 2)) : 0;
         parts = bias + (with_bias ? align256((size_t)(row_tiles_most(rows, E, dz_rows(rows, E, N)) * Nw * 4)) : 0);
         bytes = parts + (dw_parts > 1 ? (size_t)dw_parts * E * Nw * K * 4 : 0);
     }
@@ -326,25 +326,25 @@ struct GradWorkspace {
 
 }  // namespace
 
-size_t product_grad_workspace_bytes(int64_t rows, int32_t E, int32_t K, int32_t N, int32_t act, bool bias) {
+size_t product_grad_workspace_bytes(int64_t rows, int32_t E, int32_t K, int32_t N, int32_t act, bool dx, bool dw, bool bias) {
     const int64_t Nw = act == EP_ACT_SWIGLU ? 2 * (int64_t)N : N;
-    return GradWorkspace(rows, E, K, N, Nw, act, bias, plan_dw(rows, E, K, Nw).parts).bytes;
+    return GradWorkspace(rows, E, K, N, Nw, act != EP_ACT_NONE && (dx || dw), bias, dw ? plan_dw(rows, E, K, Nw).parts : 1).bytes;
 }
 
 hipError_t launch_product_grad(const ProductGradArgs &a, hipStream_t stream) {
-    uint16_t *own_dz = a.act == EP_ACT_NONE ? nullptr : static_cast<uint16_t *>(a.workspace);
-    const DwPlan dw = plan_dw(a.rows, a.E, a.K, a.Nw);
-    const GradWorkspace ws(a.rows, a.E, a.K, a.N, a.Nw, a.act, a.dbias != nullptr, dw.parts);
+    const bool activated = a.act != EP_ACT_NONE, with_dz = activated && (a.dx || a.dw);
+    uint16_t *own_dz = with_dz ? static_cast<uint16_t *>(a.workspace) : nullptr;
+    const DwPlan dw = a.dw ? plan_dw(a.rows, a.E, a.K, a.Nw) : DwPlan{GradSize::kMedium, 1};
+    const GradWorkspace ws(a.rows, a.E, a.K, a.N, a.Nw, with_dz, a.dbias != nullptr, dw.parts);
     const int per = dz_rows(a.rows, a.E, a.N);
     float *partial = nullptr;
     if (a.dbias)
         partial = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + ws.bias);
     if (a.rows > 0 && (own_dz || partial)) {
         const dim3 grid((unsigned)row_tiles_most(a.rows, a.E, per), (unsigned)((a.N + kDzCols - 1) / kDzCols));
-        uint16_t *dz = a.dx || a.dw ? own_dz : nullptr;
 #define EP_CALL(GATED)                                                                                              \
     launch_traced("expert_product_dz", product_dz_kernel<GATED>, grid, 256, stream, a.offsets, a.rows, a.E, per, a.N, a.act, \
-                  (const uint16_t *)(own_dz ? a.pre : nullptr), (const uint16_t *)a.d_y, dz, partial)
+                  (const uint16_t *)(activated ? a.pre : nullptr), (const uint16_t *)a.d_y, own_dz, partial)
         const hipError_t e = a.act == EP_ACT_SWIGLU ? EP_CALL(true) : EP_CALL(false);
 #undef EP_CALL
         if (e != hipSuccess)

@@ -345,8 +345,9 @@ def expert_product_grad(x: torch.Tensor, w: torch.Tensor, d_y: torch.Tensor, off
         got = ProductGrad(_output(dx, "dx", torch.bfloat16, (rows, K), x.device),
                           _output(dw, "dw", torch.bfloat16, (E, wide, K), x.device),
                           _output(dbias if dbias is not None else with_bias, "dbias", torch.float32, (E, wide), x.device))
-        n = _bytes("ep_expert_product_grad_workspace_bytes", rows, E, K, N,
-                   code, got.dbias is not None)
+        n = _bytes("ep_expert_product_grad_workspace_bytes", rows, E, K, N, code,
+                   (_lib.EP_GRAD_DBIAS if got.dbias is not None else 0) | (_lib.EP_GRAD_WITHOUT_DX if got.dx is None else 0)
+                   | (_lib.EP_GRAD_WITHOUT_DW if got.dw is None else 0))
         ws = _workspace(n, x.device)
     _check(lib.ep_expert_product_grad(
         _ptr(x), rows, _ptr(offsets), E, _ptr(w), K, N, code, _ptr(pre), _ptr(d_y), _ptr(got.dx), _ptr(got.dw),

@@ -1,10 +1,13 @@
 """The layer operators write what is theirs and nothing beside it, on a stream of the caller's."""
+import ctypes
+
 import pytest
 import torch
 
 import layer_ref as ref
 import paper_2609_40093_amd as ep
 from gpu_cases import say
+from paper_2609_40093_amd import _lib
 
 pytestmark = pytest.mark.gpu
 
@@ -149,3 +152,33 @@ def test_decreasing_offsets_stay_in_bounds(offsets, act):
     ep.expert_product_grad(x, w, d, off, pre=pre, act=act, dx=at((rows, K)), dw=at((E, wide, K)),
                            dbias=at((E, wide), torch.float32))
     at.check()
+
+
+@pytest.mark.parametrize("counts,K,N", [([70, 130], 520, 264), ([3000, 0, 100], 136, 72), ([5], 16, 16)])
+@pytest.mark.parametrize("act", ["none", "gelu", "swiglu"])
+def test_product_gradient_within_the_workspace_of_its_results(counts, K, N, act):
+    """Every choice of results, in a workspace of just the bytes that the query names for it."""
+    say(f"product gradient in its own workspace {counts} {K} {N} {act}")
+    lib, code = _lib.load(), _lib.EP_ACTIVATIONS[act]
+    E, rows, wide = len(counts), sum(counts), 2 * N if act == "swiglu" else N
+    g = ref.gen(rows + K)
+    x, w, d = ref.normal((rows, K), g), ref.normal((E, wide, K), g), ref.normal((rows, N), g)
+    pre = None if act == "none" else ref.normal((rows, wide), g)
+    off = torch.tensor([0] + counts, device="cuda").cumsum(0).int()
+    want = ep.expert_product_grad(x, w, d, off, pre=pre, act=act, with_bias=True)
+    need = {}
+    for dx, dw, db in ((1, 1, 1), (1, 1, 0), (1, 0, 1), (0, 1, 1), (1, 0, 0), (0, 1, 0), (0, 0, 1)):
+        at, n = Guarded(), ctypes.c_size_t()
+        flags = db * _lib.EP_GRAD_DBIAS | (not dx) * _lib.EP_GRAD_WITHOUT_DX | (not dw) * _lib.EP_GRAD_WITHOUT_DW
+        assert lib.ep_expert_product_grad_workspace_bytes(rows, E, K, N, code, flags, ctypes.byref(n)) == _lib.EP_OK
+        need[dx, dw, db] = n.value
+        outs = [at((rows, K)) if dx else None, at((E, wide, K)) if dw else None, at((E, wide), torch.float32) if db else None]
+        work = at((n.value,), torch.uint8)
+        ptr = [t.data_ptr() if t is not None else None for t in (x, off, w, pre, d, *outs, work)]
+        assert lib.ep_expert_product_grad(ptr[0], rows, ptr[1], E, ptr[2], K, N, code, ptr[3], ptr[4], ptr[5], ptr[6], ptr[7],
+                                          ptr[8], n.value, torch.cuda.current_stream().cuda_stream) == _lib.EP_OK
+        at.check()
+        for got, name in zip(outs, ("dx", "dw", "dbias")):
+            assert got is None or torch.equal(got, getattr(want, name)), (dx, dw, db, name)
+    assert need[1, 0, 0] == (0 if act == "none" else -(-rows * wide * 2 // 256) * 256)     # dz and nothing else
+    assert need[0, 0, 1] == need[1, 0, 1] - need[1, 0, 0]                                   # no dz

@@ -126,3 +126,23 @@ def test_nothing_to_do_is_no_error(lib):
     assert combine_grad(lib, T=0, d=None, y=None, pos=None, w=None) == _lib.EP_OK
     assert product(lib, rows=0, x=None, w=None, y=None) == _lib.EP_OK
     assert product_grad(lib, rows=0, x=None, w=None, dy=None, pre=None, dw=None, db=None) == _lib.EP_OK
+
+
+def test_gradient_workspace_goes_by_the_results(lib):
+    """dx alone needs no parts of dw, the bias alone no dz; results that do not exist are refused."""
+    n = ctypes.c_size_t()
+
+    def need(results, rows=9000, E=2, K=520, N=264, act=3):
+        assert lib.ep_expert_product_grad_workspace_bytes(rows, E, K, N, act, results, ctypes.byref(n)) == _lib.EP_OK
+        return n.value
+
+    dz = 9000 * 264 * 2
+    everything, no_dx, no_dw = need(1), need(1 | _lib.EP_GRAD_WITHOUT_DX), need(1 | _lib.EP_GRAD_WITHOUT_DW)
+    bias = need(1 | _lib.EP_GRAD_WITHOUT_DX | _lib.EP_GRAD_WITHOUT_DW)
+    assert everything == no_dx and dz <= need(_lib.EP_GRAD_WITHOUT_DW) < dz + 256
+    assert everything - no_dw >= 2 * 2 * 264 * 520 * 4      # dw's parts, two or more
+    assert no_dw - bias == need(_lib.EP_GRAD_WITHOUT_DW) and 0 < bias < dz
+    assert need(1, act=0) - need(1 | _lib.EP_GRAD_WITHOUT_DW, act=0) == everything - no_dw
+    for bad in (-1, 8):
+        refused(lib, lib.ep_expert_product_grad_workspace_bytes(9000, 2, 520, 264, 3, bad, ctypes.byref(n)),
+                "ep_expert_product_grad_workspace_bytes", b"results")
