@@ -1,15 +1,16 @@
 // norm.hip -- RMS norm of the residual stream, forward and backward.
 //
-//   forward   s = x + r;  y = s * rstd * w, rstd = 1 / sqrt(mean(s^2) + eps)
+//   forward   s = x + r;  y = s * rstd * w,  rstd = 1 / sqrt(mean(s^2) + eps)
 //   backward  g = d_out * w;  n = s * rstd;  dx = rstd * (g - n mean(g n)) + d_total;
 //             d_weight = sum over tokens of d_out * n
 //
 // Both are HBM-bound: every row is read once and held in registers between its reduction and
 // its results.  The forward reduces sum(s^2) and max|s w| in the same step: the row's largest
-// |y| is max|s w| rstd, so the 8-bit rows of ordinary values need no second reduction; the backward likewise
-// reduces sum(s^2) and sum(g s) together.  32768 rows of 7168 with a residual, the sum, bf16 and
-// 8-bit rows: 2.1 GB in 372 us, 5.7 TB/s; the gradient of 5003 rows of 2888: 116 MB in 27 us, 4.3
-// TB/s; 256 rows of 7168 into 8-bit rows: 5 us, of which 2 are bytes.
+// |y| is max|s w| rstd, so the 8-bit rows need no second reduction; the backward likewise reduces
+// sum(s^2) and sum(g s) together.  Only rows whose sums leave fp32 are reduced again.  32768 rows of
+// 7168 with a residual, the sum, bf16 and 8-bit rows: 2.1 GB in 376 us, 5.6 TB/s; the gradient of
+// 5003 rows of 2888: 116 MB in 27 us, 4.3 TB/s; 256 rows of 7168 into 8-bit rows: 5 us, of which 2 are
+// bytes.
 #include "layer.h"
 
 namespace ep {

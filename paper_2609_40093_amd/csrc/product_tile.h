@@ -560,7 +560,7 @@ __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf
 // largest, until that was even (1.7e-7).  So the tail keeps its digits however small it is: with
 // the arithmetic in fp32 it is within 16 2^-24 of itself, plus what e is off (1.2 z^2 2^-24).  The library's
 // erf takes three times as long, which made the gradient of the gelu's product wait for it
-// (62 us for 8192 x 4096 values, 46 with this one and four rows on their way at a time).
+// (62 us for 8192 x 4096 values, 49 with this one and four rows on their way at a time).
 __device__ __forceinline__ float normal_cdf(float z, float e) {
     const float t = __builtin_amdgcn_rcpf(fmaf(0.3f, fabsf(z), 1.f));
     float p = fmaf(0.0354237221f, t, -0.156158388f);
