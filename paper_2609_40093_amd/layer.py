@@ -285,7 +285,8 @@ def expert_product(x: torch.Tensor, w: torch.Tensor, offsets: Optional[torch.Ten
     x: bf16 [rows, K] with bf16 w [E, N, K], or 8-bit rows (uint8 [rows, K + 16]) with
     float8_e4m3fn w and w_scale fp32 [E, N].  offsets: int32 [E + 1] of a layout, none for one
     expert.  act: none, relu, silu, gelu, or swiglu (w [E, 2N, K]: gates, then ups).  keep_pre:
-    also the values before the activation, as the gradient reads them."""
+    also the values before the activation, as the gradient reads them.  Rows outside the offsets
+    keep what the outputs hold (new ones are not cleared)."""
     bits8 = x.dtype == torch.uint8
     _need(x, "x", (torch.uint8,) if bits8 else _BF16, 2)
     E, wide, N, K = _weights(w, act, _F8 if bits8 else _BF16)
@@ -329,7 +330,7 @@ def expert_product_grad(x: torch.Tensor, w: torch.Tensor, d_y: torch.Tensor, off
                         dbias: Optional[torch.Tensor] = None, stream=None) -> ProductGrad:
     """ep_expert_product_grad of a bf16 product: dx [rows, K], dw [E, N, K], and with_bias dbias
     fp32 [E, N].  pre: what the forward kept, needed with an activation.  Rows outside the
-    offsets keep what dx holds."""
+    offsets keep what dx holds (a new one is not cleared)."""
     _need(x, "x", _BF16, 2)
     E, wide, N, K = _weights(w, act, _BF16)
     rows = x.shape[0]
