@@ -8,6 +8,8 @@
  *   ep_route            top-k experts, gates, counts per expert, balance loss
  *   ep_expert_product   y = act(x W_e^T + b_e) + residual over the rows packed by expert
  *   ep_combine_grad     the gradient of the gate-weighted combine
+ *   ep_adapter_product  a projection shared by all rows beside low-rank adapters, one per request
+ *   ep_dropout, ep_dropout_rmsnorm  dropout of what joins the residual stream, alone and in the norm
  *   ..._grad            their backward passes
  *
  * A training step's forward is: ep_rmsnorm, ep_expert_product (one expert: the router's
@@ -45,6 +47,8 @@ extern "C" {
 #define EP_ROWS8_EXTRA 16       /* bytes of an 8-bit row behind its values */
 #define EP_NORM_MAX_HIDDEN 65536 /* longest row of the norm */
 #define EP_PRODUCT_MAX_LENGTH 262144 /* largest K and largest number of weight rows */
+#define EP_ADAPTER_MAX 2047     /* most adapters of a call */
+#define EP_ADAPTER_MAX_RANK 256
 
 typedef enum {
     EP_ROWS_BF16 = 0,
@@ -195,6 +199,109 @@ ep_status ep_expert_product_grad(const void *x_dev, int64_t rows, const int32_t 
                                  const void *w_dev, int32_t in_length, int32_t out_length, ep_activation act,
                                  const void *pre_dev, const void *d_y_dev, void *dx_dev, void *dw_dev, float *dbias,
                                  void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------ low-rank adapters */
+
+/* The rows of a batch by their adapter, for the two calls below; made once for all of a batch's
+ * projections:
+ *   row_adapter  device int32 [rows]: the adapter of each row; an id outside [0, A): none
+ *   order        int32 [rows]: the rows sorted by adapter, stably, those of none last
+ *   offsets      int32 [A+1]: adapter a's rows are order[offsets[a]] .. order[offsets[a+1] - 1]
+ * Requires 0 <= rows < 2^31, 1 <= A <= EP_ADAPTER_MAX. */
+ep_status ep_adapter_rows(const int32_t *row_adapter, int64_t rows, int32_t num_adapters, int32_t *order,
+                          int32_t *offsets, hipStream_t stream);
+
+/* Bytes of workspace ep_adapter_product needs: with_w and keep_low say whether w and low are given. */
+ep_status ep_adapter_product_workspace_bytes(int64_t rows, int32_t num_adapters, int32_t rank, int32_t in_length,
+                                             int32_t out_length, int32_t with_w, ep_activation act, int32_t keep_low,
+                                             size_t *bytes /* host out */);
+
+/* A projection with the low-rank adapters of its rows.  Place i of the adapters' order is row
+ * r = order[i], of adapter a if offsets[a] <= i < offsets[a+1]:
+ *   low[i] = bf16(scale[a] * x[r] A_a^T), zeros without an adapter
+ *   z = x[r] W^T + low[i] B_a^T (+ bias);  y[r] = act(z) (+ residual[r])
+ *   x        bf16 [rows][K]
+ *   order    device int32 [rows], a permutation of the rows; NULL: the rows come in the adapters' order
+ *            (an entry outside [0, rows) is no row)
+ *   offsets  device int32 [A+1], not decreasing, within [0, rows]; NULL with A = 1: all rows.
+ *            Offsets outside [0, rows] are taken as the nearest of the two
+ *   a        bf16 [A][R][K];  b  bf16 [A][Nw][R], Nw = N (2N with EP_ACT_SWIGLU)
+ *   scale    device fp32 [A] or NULL for ones
+ *   w        bf16 [Nw][K]; NULL: the adapters alone, beside a product made elsewhere (of 8-bit rows, or
+ *            of rows before their dropout) that comes as the residual
+ *   bias     bf16 [Nw] or NULL;  residual  bf16 [rows][N] or NULL, may be y itself
+ *   pre      bf16 [rows][Nw] or NULL: z, which the gradient of an activation needs
+ *   low      bf16 [rows][R] or NULL (kept in the workspace then), in the adapters' order, as the
+ *            gradient reads it
+ *   y        bf16 [rows][N]
+ * An adapter's infinities and NaN reach its own rows only.
+ * Requires 0 <= rows < 2^31, 1 <= A <= EP_ADAPTER_MAX, R a multiple of 8 up to EP_ADAPTER_MAX_RANK, K and N
+ * positive multiples of 8, K and Nw <= EP_PRODUCT_MAX_LENGTH; w, a and b, and x with an order and w,
+ * smaller than 2^31 bytes. */
+ep_status ep_adapter_product(const void *x_dev, int64_t rows, const int32_t *order, const int32_t *offsets,
+                             int32_t num_adapters, int32_t rank, const void *a_dev, const void *b_dev, const float *scale,
+                             const void *w_dev, int32_t in_length, int32_t out_length, const void *bias_dev,
+                             ep_activation act, const void *residual_dev, void *pre_dev, void *low_dev, void *y_dev,
+                             void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Bytes of workspace ep_adapter_product_grad needs for the results named (EP_ADAPTER_DX, _DA, _DB). */
+#define EP_ADAPTER_DX 1
+#define EP_ADAPTER_DA 2
+#define EP_ADAPTER_DB 4
+ep_status ep_adapter_product_grad_workspace_bytes(int64_t rows, int32_t num_adapters, int32_t rank, int32_t in_length,
+                                                  int32_t out_length, ep_activation act, int32_t with_order,
+                                                  int32_t results, size_t *bytes /* host out */);
+
+/* Gradient of ep_adapter_product with w held fast:
+ *   dz = d_y * act'(pre);  v[i] = bf16(scale[a] * dz[r] B_a)
+ *   dx[r] = dz[r] W + v[i] A_a;  da_a = sum v[i]^T x[r];  db_a = sum dz[r]^T low[i]
+ * (the residual's gradient is d_y itself; w's, where it is trained too, ep_expert_product_grad's of one expert)
+ *   x, order, offsets, a, b, scale, w  as in the forward (w NULL: dx of the adapters alone)
+ *   low     bf16 [rows][R] as the forward wrote it (for db)
+ *   pre     bf16 [rows][Nw] as the forward wrote it; NULL with EP_ACT_NONE
+ *   d_y     bf16 [rows][N]
+ *   dx      bf16 [rows][K] or NULL;  da  bf16 [A][R][K] or NULL;  db  bf16 [A][Nw][R] or NULL
+ * dz and v are rounded to bf16 for the products.  An adapter without rows gets zeros in da and db.
+ * Requires what the forward requires, but that x may have any size. */
+ep_status ep_adapter_product_grad(const void *x_dev, int64_t rows, const int32_t *order, const int32_t *offsets,
+                                  int32_t num_adapters, int32_t rank, const void *a_dev, const void *b_dev,
+                                  const float *scale, const void *w_dev, int32_t in_length, int32_t out_length,
+                                  const void *low_dev, ep_activation act, const void *pre_dev, const void *d_y_dev,
+                                  void *dx_dev, void *da_dev, void *db_dev, void *workspace, size_t workspace_bytes,
+                                  hipStream_t stream);
+
+/* ------------------------------------------------------------------------- dropout */
+
+/* Dropout, with a residual that what is left is added to:
+ *   out[i] = keep(i) ? x[i] / (1 - q) : 0  (+ residual[i])
+ *   q = cut / 65536, cut = round(65536 p) (ties to even); keep(i): 16 random bits of value i >= cut
+ *   x, residual, out  bf16 [count]; residual may be NULL; out may be x or residual itself
+ *   rng      device int64 [2]: the seed and the step
+ *   site     which of a program's dropouts this is
+ * The bits: Philox4x32-10 with the seed as key (low word first) of the counter (g, g >> 32, step
+ * mod 2^32, site) gives the values 8g .. 8g+7, two to a word, the low half first.  Nothing is stored: the
+ * gradient is the same call (d_x = ep_dropout of d_out with the same rng, site and no residual; the
+ * residual's gradient is d_out).  rng is read on the device, so a captured graph draws new masks where the
+ * program advances the step between replays.
+ * Sum and product are fp32, rounded once.  Requires count a multiple of 8, 0 <= p <= 1. */
+ep_status ep_dropout(const void *x_dev, const void *residual_dev, int64_t count, double p, const int64_t *rng,
+                     uint32_t site, void *out_dev, hipStream_t stream);
+
+/* ep_rmsnorm of s = dropout(x) + residual, x's values numbered t * H + h.  Requires what ep_rmsnorm and
+ * ep_dropout require. */
+ep_status ep_dropout_rmsnorm(const void *x_dev, const void *residual_dev, const void *weight_dev, int64_t num_tokens,
+                             int32_t hidden, float eps, double p, const int64_t *rng, uint32_t site, void *total_dev,
+                             void *out_dev, void *rows8_dev, hipStream_t stream);
+
+/* Gradient of ep_dropout_rmsnorm: ep_rmsnorm_grad's dx is the residual's gradient, and its dropout x's.
+ *   dx          bf16 [T][H] or NULL: keep ? d_residual / (1 - q) : 0, from the unrounded d_residual
+ *   d_residual  bf16 [T][H] or NULL
+ * (at least one of the two; each may be d_out or d_total, not both the same).  The rest, and the workspace, as
+ * ep_rmsnorm_grad. */
+ep_status ep_dropout_rmsnorm_grad(const void *total_dev, const void *weight_dev, const void *d_out_dev,
+                                  const void *d_total_dev, int64_t num_tokens, int32_t hidden, float eps, double p,
+                                  const int64_t *rng, uint32_t site, void *dx_dev, void *d_residual_dev, float *d_weight,
+                                  void *workspace, size_t workspace_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

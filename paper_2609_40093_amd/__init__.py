@@ -16,7 +16,9 @@ _API = ("EPError", "Layout", "Staging", "SimPeers", "dispatch_layout", "layout_v
         "combine_graph", "graph_legs_sdma")
 
 _LAYER = ("Norm", "rmsnorm", "rmsnorm_grad", "rows8_empty", "rows8_values", "Routing", "route", "route_grad",
-          "combine_grad", "Product", "expert_product", "ProductGrad", "expert_product_grad")
+          "combine_grad", "Product", "expert_product", "ProductGrad", "expert_product_grad",
+          "AdapterRows", "adapter_rows", "AdapterProduct", "adapter_product", "AdapterGrad", "adapter_product_grad",
+          "dropout", "dropout_rmsnorm", "dropout_rmsnorm_grad")
 
 __all__ = list(_API + _LAYER)
 

@@ -19,10 +19,12 @@ ABI_VERSION = 6
 EP_MAX_EXPERTS = 2048
 EP_ROWS_BF16, EP_ROWS_8BIT, EP_ROWS8_EXTRA = 0, 1, 16
 EP_GRAD_DBIAS, EP_GRAD_WITHOUT_DX, EP_GRAD_WITHOUT_DW = 1, 2, 4
+EP_ADAPTER_MAX, EP_ADAPTER_MAX_RANK = 2047, 256
+EP_ADAPTER_DX, EP_ADAPTER_DA, EP_ADAPTER_DB = 1, 2, 4
 EP_ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "swiglu": 4}
 
 c_i32, c_i64, c_u32, c_size, c_vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_size_t, ctypes.c_void_p
-c_f32 = ctypes.c_float
+c_f32, c_f64 = ctypes.c_float, ctypes.c_double
 c_i32p = ctypes.POINTER(ctypes.c_int32)
 
 
@@ -108,6 +110,19 @@ SIGNATURES = {
                                                        ctypes.POINTER(c_size)]),
     "ep_expert_product_grad": (c_i32, [c_vp, c_i64, c_vp, c_i32, c_vp, c_i32, c_i32, c_i32, c_vp, c_vp, c_vp, c_vp,
                                        c_vp, c_vp, c_size, c_vp]),
+    "ep_adapter_rows": (c_i32, [c_vp, c_i64, c_i32, c_vp, c_vp, c_vp]),
+    "ep_adapter_product_workspace_bytes": (c_i32, [c_i64, c_i32, c_i32, c_i32, c_i32, c_i32, c_i32, c_i32,
+                                                   ctypes.POINTER(c_size)]),
+    "ep_adapter_product": (c_i32, [c_vp, c_i64, c_vp, c_vp, c_i32, c_i32, c_vp, c_vp, c_vp, c_vp, c_i32, c_i32, c_vp,
+                                   c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, c_size, c_vp]),
+    "ep_adapter_product_grad_workspace_bytes": (c_i32, [c_i64, c_i32, c_i32, c_i32, c_i32, c_i32, c_i32, c_i32,
+                                                        ctypes.POINTER(c_size)]),
+    "ep_adapter_product_grad": (c_i32, [c_vp, c_i64, c_vp, c_vp, c_i32, c_i32, c_vp, c_vp, c_vp, c_vp, c_i32, c_i32, c_vp,
+                                        c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_size, c_vp]),
+    "ep_dropout": (c_i32, [c_vp, c_vp, c_i64, c_f64, c_vp, c_u32, c_vp, c_vp]),
+    "ep_dropout_rmsnorm": (c_i32, [c_vp, c_vp, c_vp, c_i64, c_i32, c_f32, c_f64, c_vp, c_u32, c_vp, c_vp, c_vp, c_vp]),
+    "ep_dropout_rmsnorm_grad": (c_i32, [c_vp, c_vp, c_vp, c_vp, c_i64, c_i32, c_f32, c_f64, c_vp, c_u32, c_vp, c_vp, c_vp,
+                                        c_vp, c_size, c_vp]),
     "ep_trace_enable": (c_i32, [c_i32]),
     "ep_trace_read": (c_i32, [ctypes.POINTER(TraceStat), c_i32, ctypes.POINTER(c_i32)]),
     "ep_trace_reset": (c_i32, []),

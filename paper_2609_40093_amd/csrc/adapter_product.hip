@@ -1,0 +1,284 @@
+// adapter_product.hip -- a shared projection with the low-rank adapters of its rows:
+//   z = x[r] W^T + low[r] b_a^T;  y[r] = act(z + bias) + residual[r],  a the adapter of row r.
+//
+// The low-rank values low = scale_a x a_a^T come from adapter_low.hip.  Rows go in the adapters'
+// order: a tile gathers its rows of x through it and leaves its results through it.  The
+// contraction over K goes on over the ranks of the adapters that the tile's rows have
+// (adapter_tile.h), so the adapters cost the tile (segments * R) / 64 steps, and y is written
+// once.  Without W the contraction begins with the ranks.
+#include "adapter_tile.h"
+#include "product_finish.h"
+#include "product_plan.h"
+
+namespace ep {
+namespace {
+
+// The sums of place i (row r), columns n..n+7, of their own terms alone.
+__device__ __forceinline__ void redo8(const ProductArgs &a, const AdapterSide &s, int64_t i, int64_t r, int32_t n, float *z) {
+    const int32_t e = adapter_of(s, a.rows, i);
+#pragma unroll 1
+    for (int q = 0; q < 8; ++q) {
+        float sum = 0.f;
+        const auto dot = [&](const uint16_t *u, const uint16_t *v, int32_t length) {
+#pragma unroll 1
+            for (int32_t k = 0; k < length; k += 8) {
+                float f[8], g[8];
+                unpack8(*reinterpret_cast<const u32x4 *>(u + k), f);
+                unpack8(*reinterpret_cast<const u32x4 *>(v + k), g);
+#pragma unroll
+                for (int p = 0; p < 8; ++p)
+                    sum = fmaf(f[p], g[p], sum);
+            }
+        };
+        if (a.w)
+            dot(static_cast<const uint16_t *>(a.x) + r * a.K, static_cast<const uint16_t *>(a.w) + (int64_t)(n + q) * a.K, a.K);
+        if (e >= 0)
+            dot(s.low + i * s.R, s.weights + ((int64_t)e * a.Nw + n + q) * s.R, s.R);
+#pragma unroll
+        for (int p = 0; p < 8; ++p)
+            z[p] = p == q ? sum : z[p];
+    }
+}
+template <bool GATED>
+__device__ __forceinline__ void check8(const ProductArgs &a, const AdapterSide &s, int64_t i, int64_t r, int32_t n, float *z,
+                                       float *up) {
+    if (__builtin_expect(any_nan(z, 8) || (GATED && any_nan(up, 8)), false)) {
+        redo8(a, s, i, r, n, z);
+        if (GATED)
+            redo8(a, s, i, r, n + a.N, up);
+    }
+}
+
+template <class S, bool GATED>
+__global__ __launch_bounds__(S::kThreads) void adapter_product_kernel(ProductArgs a, AdapterSide s, int32_t row_tiles,
+                                                                      int32_t col_tiles, int32_t parts) {
+    __shared__ __attribute__((aligned(1024))) char lds[S::kStages * S::kStageBytes];
+    __shared__ Segment table[S::kJ];
+    Segment EP_LDS *segments = (Segment EP_LDS *)table;
+    __shared__ int32_t row_of[S::kJ], found;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t tiles = (int64_t)row_tiles * col_tiles;
+    int64_t t = tile_of_block(blockIdx.x, tiles * parts);
+    if (t < 0)
+        return;
+    const int32_t part = parts == 1 ? 0 : (int32_t)(t / tiles);
+    t -= part * tiles;
+    int32_t tr, tc;
+    tile_order(t, row_tiles, col_tiles, tr, tc);
+    const int64_t i0 = (int64_t)tr * S::kJ;
+    const int n_rows = a.rows - i0 < S::kJ ? (int)(a.rows - i0) : S::kJ;
+    for (int j = threadIdx.x; j < S::kJ; j += S::kThreads)
+        row_of[j] = j < n_rows ? row_at(s.order, a.rows, i0 + j) : -1;
+    if (wave == 0) {
+        const int n = find_segments<S::kJ>(s, a.rows, i0, n_rows, segments, lane);
+        if (lane == 0)
+            found = n;
+    }
+    __syncthreads();
+    const int count = __builtin_amdgcn_readfirstlane(found);
+
+    const int64_t kb = (int64_t)a.K * 2;
+    constexpr int kOut = GATED ? S::kI / 2 : S::kI;  // output columns of a tile
+    const int32_t n0 = tc * kOut;
+    const int32_t main = a.w ? (int32_t)((kb + kStepBytes - 1) / kStepBytes) : 0;
+    // the weights' row of a tile's column, -1: none
+    const auto column = [&](int row) -> int32_t {
+        const int32_t n = GATED ? n0 + (row >> 4) * 8 + (row & 7) : n0 + row;
+        return n < a.N ? n + (GATED && (row & 8) ? a.N : 0) : -1;
+    };
+    ChainAlong<S::kI, S::kWaves, false> w;
+    ChainAlong<S::kJ, S::kWaves, true> x;
+    w.init(static_cast<const char *>(a.w), (uint32_t)(a.Nw * kb), (int32_t)kb, wave, lane, [&](int row) -> uint32_t {
+        const int32_t n = column(row);
+        return n < 0 ? kNowhere : (uint32_t)(n * kb);
+    });
+    w.chain(main, s, segments, count, s.weights, (uint64_t)s.A * a.Nw * s.R * 2, a.Nw, wave, lane, column);
+    // through an order from x's first row on (x is smaller than 2^31 bytes then)
+    const char *xb = static_cast<const char *>(a.x);
+    x.init(s.order ? xb : xb + i0 * kb, (uint32_t)((s.order ? a.rows : n_rows) * kb), (int32_t)kb, wave, lane,
+           [&](int row) -> uint32_t {
+               if (!s.order)
+                   return (uint32_t)(row * kb);
+               const int32_t r = row_of[row];
+               return r < 0 ? kNowhere : (uint32_t)(r * kb);
+           });
+    x.chain(main, s, segments, count, s.low + i0 * s.R, (uint64_t)n_rows * s.R * 2, 0, wave, lane, [](int row) { return row; });
+
+    int32_t steps = main + (count * (s.R / 8) + 7) / 8;
+    if (parts > 1) {
+        const int32_t per = (steps + parts - 1) / parts, first = part * per;
+        steps = steps - first < per ? steps - first : per;
+        w.skip(first);
+        x.skip(first);
+    }
+    f32x16 acc[S::FI][S::FJ] = {};
+    tile_product<S, Mul::kBf16>(w, x, steps, (char EP_LDS *)lds, wave, lane, acc);
+
+    if (parts > 1) {
+        tile_results<S>(acc, (char EP_LDS *)lds, wave, lane, [&](int row, int col, const float *v) {
+            const int32_t n = n0 + (GATED ? col / 16 * 8 : col);
+            if (row >= n_rows || n >= a.N)
+                return;
+            f32x4 *dst = reinterpret_cast<f32x4 *>(a.partial + ((int64_t)part * a.rows + i0 + row) * a.Nw + n +
+                                                   (GATED && (col & 8) ? a.N : 0));
+            dst[0] = f32x4{v[0], v[1], v[2], v[3]};
+            dst[1] = f32x4{v[4], v[5], v[6], v[7]};
+        });
+        return;
+    }
+    constexpr int kPer = GATED ? 16 : 8;
+    const int32_t n = n0 + first_col<S, kPer>(wave, lane) / (kPer / 8);
+    Columns<false, GATED> columns;
+    if (n < a.N)
+        columns.load(a, 0, n);
+    struct Row {
+        int32_t r;
+        RowExtra<false> x;
+    };
+    tile_rows_out<S, kPer>(
+        acc, (char EP_LDS *)lds, wave, lane,
+        [&](int row) {
+            Row f;
+            f.r = row < n_rows && n < a.N ? row_of[row] : -1;
+            if (f.r >= 0)
+                f.x.load(a, f.r, n);
+            return f;
+        },
+        [&](int row, int, float *v, const Row &f) {
+            if (f.r < 0)
+                return;
+            check8<GATED>(a, s, i0 + row, f.r, n, v, v + kPer / 2);
+            finish8<false, GATED>(a, columns, f.x, f.r, n, v, v + kPer / 2);
+        });
+}
+
+// Adds the parts of a split contraction and runs the epilogue, as the experts' product does: LANES
+// lanes add every LANES-th part of eight neighbouring results each, and are added up in a fixed order.
+template <bool GATED, int LANES>
+__global__ __launch_bounds__(256) void adapter_join_kernel(ProductArgs a, AdapterSide s, int32_t parts, FastDiv groups) {
+    const int lane = threadIdx.x & 63, first = lane / (64 / LANES);
+    const uint32_t at = (blockIdx.x * 4 + (threadIdx.x >> 6)) * (64 / LANES) + lane % (64 / LANES);
+    const uint32_t row = groups.div(at);
+    const int64_t i = row;
+    const int32_t n = (int32_t)(at - row * groups.d) * 8;
+    const int32_t r = i < a.rows ? row_at(s.order, a.rows, i) : -1;
+    float z[8] = {}, up[8] = {};
+    if (r >= 0) {
+        constexpr int kAhead = 4;
+        const int64_t part = a.rows * a.Nw;
+        const float *src = a.partial + i * a.Nw + n;
+        for (int32_t p0 = first; p0 < parts; p0 += LANES * kAhead) {
+            f32x4 v[kAhead][GATED ? 4 : 2];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+                for (int h = 0; h < (GATED ? 4 : 2); ++h) {
+                    v[u][h] = f32x4{};
+                    if (p0 + LANES * u < parts)
+                        v[u][h] = *reinterpret_cast<const f32x4 *>(src + (p0 + LANES * u) * part + (h / 2) * a.N + (h & 1) * 4);
+                }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    z[q] += v[u][q / 4][q % 4];
+                    if (GATED)
+                        up[q] += v[u][(GATED ? 2 : 0) + q / 4][q % 4];
+                }
+        }
+    }
+#pragma unroll
+    for (int d = 64 / LANES; d < 64; d *= 2)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            z[q] += __shfl_xor(z[q], d);
+            if (GATED)
+                up[q] += __shfl_xor(up[q], d);
+        }
+    if (r < 0 || first != 0)
+        return;
+    check8<GATED>(a, s, i, r, n, z, up);
+    Columns<false, GATED> columns;
+    columns.load(a, 0, n);
+    RowExtra<false> x;
+    x.load(a, r, n);
+    finish8<false, GATED>(a, columns, x, r, n, z, up);
+}
+
+// Steps that the adapters add to a tile of `per` rows: its segments to expect.
+int32_t adapter_steps(int64_t rows, int32_t A, int32_t R, int per) {
+    const int64_t some = std::min<int64_t>(std::min<int64_t>(A, per), (int64_t)A * per / std::max<int64_t>(rows, 1) + 1);
+    return (int32_t)((some * R + kStepRows - 1) / kStepRows);
+}
+Plan adapter_plan(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t N, bool base, bool gated) {
+    return make_plan(rows, 1, base ? K : 0, N, false, gated, [&](int per) { return adapter_steps(rows, A, R, per); });
+}
+
+template <class S, bool GATED>
+hipError_t launch_tiles(const ProductArgs &a, const AdapterSide &s, const Plan &p, hipStream_t stream) {
+    if (p.tiles * p.split.parts > kMostTiles)
+        return hipErrorInvalidConfiguration;
+    const hipError_t e = launch_traced("adapter_product", adapter_product_kernel<S, GATED>,
+                                       dim3((unsigned)(p.tiles * p.split.parts + 8)), S::kThreads, stream, a, s,
+                                       (int32_t)(p.tiles / p.cols), p.cols, p.split.parts);
+    if (e != hipSuccess || p.split.parts == 1)
+        return e;
+    const int64_t groups = a.rows * (a.N / 8);
+#define EP_CALL(LANES)                                                                                                     \
+    launch_traced("adapter_product_join", adapter_join_kernel<GATED, LANES>, dim3((unsigned)((groups * LANES + 255) / 256)), \
+                  256, stream, a, s, p.split.parts, fast_div((uint32_t)(a.N / 8)))
+    return p.split.parts <= 4 ? EP_CALL(1) : EP_CALL(8);  // a lane has 4 parts on their way
+#undef EP_CALL
+}
+template <class S>
+hipError_t launch_shape(const ProductArgs &a, const AdapterSide &s, const Plan &p, hipStream_t stream) {
+    return a.act == EP_ACT_SWIGLU ? launch_tiles<S, true>(a, s, p, stream) : launch_tiles<S, false>(a, s, p, stream);
+}
+
+}  // namespace
+
+size_t adapter_product_partial_bytes(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t N, bool base, int32_t act) {
+    if (rows == 0)
+        return 0;
+    const bool gated = act == EP_ACT_SWIGLU;
+    const Plan p = adapter_plan(rows, A, R, K, N, base, gated);
+    return p.split.parts == 1 ? 0 : (size_t)p.split.parts * rows * N * (gated ? 2 : 1) * sizeof(float);
+}
+
+hipError_t launch_adapter_product(const AdapterArgs &a, hipStream_t stream) {
+    if (a.rows == 0)
+        return hipSuccess;
+    const bool gated = a.act == EP_ACT_SWIGLU;
+    ProductArgs p{};
+    p.x = a.x;
+    p.rows = a.rows;
+    p.E = 1;
+    p.w = a.w;
+    p.K = a.K;
+    p.N = a.N;
+    p.Nw = gated ? 2 * a.N : a.N;
+    p.bias = a.bias;
+    p.act = a.act;
+    p.residual = a.residual;
+    p.pre = a.pre;
+    p.y = a.y;
+    p.partial = a.partial;
+    const hipError_t e = launch_adapter_low(
+        {a.x, a.rows, a.order, a.offsets, a.A, a.R, a.K, a.a, a.scale, a.low}, stream);
+    if (e != hipSuccess)
+        return e;
+    const AdapterSide s{a.order, a.offsets, a.A, a.R, static_cast<const uint16_t *>(a.low), static_cast<const uint16_t *>(a.b),
+                        fast_div((uint32_t)a.R), fast_div((uint32_t)(a.R / 8))};
+    const Plan plan = adapter_plan(a.rows, a.A, a.R, a.K, a.N, a.w != nullptr, gated);
+    switch (plan.size) {
+    case Size::kLarge: return launch_shape<Large>(p, s, plan, stream);
+    case Size::kBroad: return launch_shape<Broad>(p, s, plan, stream);
+    case Size::kMedium: return launch_shape<Medium>(p, s, plan, stream);
+    case Size::kSmall: return launch_shape<Small>(p, s, plan, stream);
+    case Size::kWide: return launch_shape<Wide>(p, s, plan, stream);
+    case Size::kFew: return launch_shape<Few>(p, s, plan, stream);
+    default: return launch_shape<Tiny>(p, s, plan, stream);
+    }
+}
+
+}  // namespace ep

@@ -116,6 +116,18 @@ hipError_t launch_traced(const char *name, K kernel, dim3 grid, int threads, hip
 // Compute units; the kernels that loop over their work size their grids by it.
 constexpr int64_t kCus = 256;
 
+// Rows past what the memory-side cache holds are loaded and stored non-temporally.  Measured, us:
+// rmsnorm_grad of 20000 rows of 7168 (1.1 GB) 219 / 196; the forward's at its launcher.
+constexpr int64_t kNormStreamBytes = 256ll << 20;
+
+// Dropout (dropout.h).
+struct DropArgs {
+    const int64_t *rng;  // device: seed, step
+    uint32_t site;
+    uint32_t cut;        // of 65536: values whose 16 random bits are below are dropped
+    float factor;        // of the others
+};
+
 struct NormArgs {
     const u32x4 *x, *residual, *weight;  // residual, weight may be null
     u32x4 *total, *out;                  // may be null
@@ -123,6 +135,7 @@ struct NormArgs {
     int64_t T;
     int32_t H;
     float eps;
+    DropArgs drop;  // of x; rng null: none
 };
 hipError_t launch_rmsnorm(const NormArgs &a, hipStream_t stream);
 
@@ -134,6 +147,8 @@ struct NormGradArgs {
     int64_t T;
     int32_t H;
     float eps;
+    DropArgs drop;     // rng null: none
+    u32x4 *d_residual; // with dropout: the gradient before it (dx the one behind it); either may be null
 };
 int64_t rmsnorm_grad_groups(int64_t T, int32_t H);
 hipError_t launch_rmsnorm_grad(const NormGradArgs &a, hipStream_t stream);
@@ -207,5 +222,58 @@ struct ProductGradArgs {
 };
 size_t product_grad_workspace_bytes(int64_t rows, int32_t E, int32_t K, int32_t N, int32_t act, bool dx, bool dw, bool bias);
 hipError_t launch_product_grad(const ProductGradArgs &a, hipStream_t stream);
+
+// ---- low-rank adapters --------------------------------------------------------------
+hipError_t launch_adapter_rows(const int32_t *row_adapter, int64_t rows, int32_t A, int32_t *order, int32_t *offsets,
+                               hipStream_t stream);
+
+// low[i] = scale[e] x[order[i]] weights[e]^T for place i of adapter e.
+struct LowArgs {
+    const void *x;  // bf16 [rows][K]
+    int64_t rows;
+    const int32_t *order, *offsets;  // null: rows in the adapters' order; one adapter
+    int32_t A, R, K;
+    const void *weights;  // bf16 [A][R][K]
+    const float *scale;   // fp32 [A], null: ones
+    void *low;            // bf16 [rows][R], in the adapters' order
+};
+hipError_t launch_adapter_low(const LowArgs &a, hipStream_t stream);
+
+struct AdapterArgs {
+    const void *x;
+    int64_t rows;
+    const int32_t *order, *offsets;
+    int32_t A, R, K, N;
+    const void *a, *b;
+    const float *scale;
+    const void *w;  // null: the adapters alone
+    const void *bias;
+    int32_t act;
+    const void *residual;
+    void *pre, *low, *y;
+    float *partial;  // workspace of adapter_product_partial_bytes
+};
+size_t adapter_product_partial_bytes(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t N, bool base, int32_t act);
+hipError_t launch_adapter_product(const AdapterArgs &a, hipStream_t stream);
+
+struct AdapterGradArgs {
+    const void *x;
+    int64_t rows;
+    const int32_t *order, *offsets;
+    int32_t A, R, K, N;
+    const void *a, *b, *low;
+    const float *scale;
+    const void *w;
+    int32_t act;
+    const void *pre, *d_y;
+    void *dx, *da, *db;  // may be null
+    void *workspace;     // of adapter_grad_workspace_bytes
+};
+size_t adapter_grad_workspace_bytes(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t N, int32_t act, bool order, bool dx,
+                                    bool da, bool db);
+hipError_t launch_adapter_grad(const AdapterGradArgs &a, hipStream_t stream);
+
+// ---- dropout of a residual addition ---------------------------------------------------
+hipError_t launch_dropout(const void *x, const void *residual, int64_t count, const DropArgs &d, void *out, hipStream_t stream);
 
 }  // namespace ep

@@ -46,19 +46,22 @@ ep_status check_product(const char *who, int64_t rows, int32_t E, int32_t K, int
 
 }  // namespace
 
-extern "C" ep_status ep_rmsnorm(const void *x_dev, const void *residual_dev, const void *weight_dev, int64_t num_tokens,
-                                int32_t hidden, float eps, void *total_dev, void *out_dev, void *rows8_dev,
-                                hipStream_t stream) {
-    const ep_status st = check_norm("ep_rmsnorm", num_tokens, hidden, eps);
+namespace {
+
+// ep_rmsnorm, and with `drop` ep_dropout_rmsnorm.
+ep_status rmsnorm(const char *who, const void *x_dev, const void *residual_dev, const void *weight_dev, int64_t num_tokens,
+                  int32_t hidden, float eps, const ep::DropArgs &drop, void *total_dev, void *out_dev, void *rows8_dev,
+                  hipStream_t stream) {
+    const ep_status st = check_norm(who, num_tokens, hidden, eps);
     if (st != EP_OK)
         return st;
     if (num_tokens > 0 && !total_dev && !out_dev && !rows8_dev)
-        return fail(EP_ERR_INVALID_ARG, "ep_rmsnorm: no output");
+        return fail(EP_ERR_INVALID_ARG, "%s: no output", who);
     if (rows8_dev && hidden % 16 != 0)
-        return fail(EP_ERR_INVALID_ARG, "ep_rmsnorm: 8-bit rows need H %% 16 == 0 (H=%d)", hidden);
+        return fail(EP_ERR_INVALID_ARG, "%s: 8-bit rows need H %% 16 == 0 (H=%d)", who, hidden);
     if (num_tokens > 0 && (!x_dev || !aligned16(x_dev) || !aligned16(residual_dev) || !aligned16(weight_dev) ||
                            !aligned16(total_dev) || !aligned16(out_dev) || !aligned16(rows8_dev)))
-        return fail(EP_ERR_INVALID_ARG, "ep_rmsnorm: x is required, every array 16-byte aligned");
+        return fail(EP_ERR_INVALID_ARG, "%s: x is required, every array 16-byte aligned", who);
     ep::NormArgs a{};
     a.x = static_cast<const ep::u32x4 *>(x_dev);
     a.residual = static_cast<const ep::u32x4 *>(residual_dev);
@@ -69,8 +72,18 @@ extern "C" ep_status ep_rmsnorm(const void *x_dev, const void *residual_dev, con
     a.T = num_tokens;
     a.H = hidden;
     a.eps = eps;
+    a.drop = drop;
     EP_HIP(ep::launch_rmsnorm(a, stream));
     return EP_OK;
+}
+
+}  // namespace
+
+extern "C" ep_status ep_rmsnorm(const void *x_dev, const void *residual_dev, const void *weight_dev, int64_t num_tokens,
+                                int32_t hidden, float eps, void *total_dev, void *out_dev, void *rows8_dev,
+                                hipStream_t stream) {
+    return rmsnorm("ep_rmsnorm", x_dev, residual_dev, weight_dev, num_tokens, hidden, eps, ep::DropArgs{}, total_dev, out_dev,
+                   rows8_dev, stream);
 }
 
 extern "C" ep_status ep_rmsnorm_grad_workspace_bytes(int64_t num_tokens, int32_t hidden, size_t *bytes) {
@@ -83,34 +96,52 @@ extern "C" ep_status ep_rmsnorm_grad_workspace_bytes(int64_t num_tokens, int32_t
     return EP_OK;
 }
 
-extern "C" ep_status ep_rmsnorm_grad(const void *total_dev, const void *weight_dev, const void *d_out_dev,
-                                     const void *d_total_dev, int64_t num_tokens, int32_t hidden, float eps, void *dx_dev,
-                                     float *d_weight, void *workspace, size_t workspace_bytes, hipStream_t stream) {
-    const ep_status st = check_norm("ep_rmsnorm_grad", num_tokens, hidden, eps);
+namespace {
+
+// ep_rmsnorm_grad, and with `drop` ep_dropout_rmsnorm_grad.
+ep_status rmsnorm_grad(const char *who, const void *total_dev, const void *weight_dev, const void *d_out_dev,
+                       const void *d_total_dev, int64_t num_tokens, int32_t hidden, float eps, const ep::DropArgs &drop,
+                       void *dx_dev, void *d_residual_dev, float *d_weight, void *workspace, size_t workspace_bytes,
+                       hipStream_t stream) {
+    const ep_status st = check_norm(who, num_tokens, hidden, eps);
     if (st != EP_OK)
         return st;
-    if (num_tokens > 0 && (!total_dev || !d_out_dev || !dx_dev || !aligned16(total_dev) || !aligned16(weight_dev) ||
-                           !aligned16(d_out_dev) || !aligned16(d_total_dev) || !aligned16(dx_dev)))
-        return fail(EP_ERR_INVALID_ARG, "ep_rmsnorm_grad: total, d_out and dx are required, every array 16-byte aligned");
+    if (num_tokens > 0 && (!total_dev || !d_out_dev || (!dx_dev && !d_residual_dev) || !aligned16(total_dev) ||
+                           !aligned16(weight_dev) || !aligned16(d_out_dev) || !aligned16(d_total_dev) || !aligned16(dx_dev) ||
+                           !aligned16(d_residual_dev)))
+        return fail(EP_ERR_INVALID_ARG, "%s: total, d_out and dx are required, every array 16-byte aligned", who);
+    if (num_tokens > 0 && dx_dev == d_residual_dev)
+        return fail(EP_ERR_INVALID_ARG, "%s: dx and d_residual are one array", who);
     const size_t need = d_weight ? (size_t)ep::rmsnorm_grad_groups(num_tokens, hidden) * hidden * sizeof(float) : 0;
     if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need))
-        return fail(EP_ERR_INVALID_ARG, "ep_rmsnorm_grad: workspace of %zu bytes, need %zu, 16-byte aligned",
+        return fail(EP_ERR_INVALID_ARG, "%s: workspace of %zu bytes, need %zu, 16-byte aligned", who,
                     workspace ? workspace_bytes : (size_t)0, need);
     if (!aligned(d_weight, 4))
-        return fail(EP_ERR_INVALID_ARG, "ep_rmsnorm_grad: d_weight is not 4-byte aligned");
+        return fail(EP_ERR_INVALID_ARG, "%s: d_weight is not 4-byte aligned", who);
     ep::NormGradArgs a{};
     a.total = static_cast<const ep::u32x4 *>(total_dev);
     a.weight = static_cast<const ep::u32x4 *>(weight_dev);
     a.d_out = static_cast<const ep::u32x4 *>(d_out_dev);
     a.d_total = static_cast<const ep::u32x4 *>(d_total_dev);
     a.dx = static_cast<ep::u32x4 *>(dx_dev);
+    a.d_residual = static_cast<ep::u32x4 *>(d_residual_dev);
     a.d_weight = d_weight;
     a.partial = static_cast<float *>(workspace);
     a.T = num_tokens;
     a.H = hidden;
     a.eps = eps;
+    a.drop = drop;
     EP_HIP(ep::launch_rmsnorm_grad(a, stream));
     return EP_OK;
+}
+
+}  // namespace
+
+extern "C" ep_status ep_rmsnorm_grad(const void *total_dev, const void *weight_dev, const void *d_out_dev,
+                                     const void *d_total_dev, int64_t num_tokens, int32_t hidden, float eps, void *dx_dev,
+                                     float *d_weight, void *workspace, size_t workspace_bytes, hipStream_t stream) {
+    return rmsnorm_grad("ep_rmsnorm_grad", total_dev, weight_dev, d_out_dev, d_total_dev, num_tokens, hidden, eps,
+                        ep::DropArgs{}, dx_dev, nullptr, d_weight, workspace, workspace_bytes, stream);
 }
 
 extern "C" ep_status ep_route_workspace_bytes(int64_t num_tokens, int32_t num_experts, size_t *bytes) {
@@ -322,4 +353,57 @@ extern "C" ep_status ep_expert_product_grad(const void *x_dev, int64_t rows, con
     a.workspace = workspace;
     EP_HIP(ep::launch_product_grad(a, stream));
     return EP_OK;
+}
+
+namespace {
+
+ep_status drop_args(const char *who, bool any, double p, const int64_t *rng, uint32_t site, ep::DropArgs *d) {
+    if (!(p >= 0.0 && p <= 1.0))
+        return fail(EP_ERR_INVALID_ARG, "%s: need 0 <= p <= 1 (p=%g)", who, p);
+    if (any && (!rng || !aligned(rng, 8)))
+        return fail(EP_ERR_INVALID_ARG, "%s: rng is required, 8-byte aligned", who);
+    d->rng = rng;
+    d->site = site;
+    d->cut = (uint32_t)std::nearbyint(p * 65536.0);
+    d->factor = d->cut < 65536 ? 65536.f / (float)(65536 - d->cut) : 0.f;
+    return EP_OK;
+}
+
+}  // namespace
+
+extern "C" ep_status ep_dropout(const void *x_dev, const void *residual_dev, int64_t count, double p, const int64_t *rng,
+                                uint32_t site, void *out_dev, hipStream_t stream) {
+    if (count < 0 || count % 8 != 0)
+        return fail(EP_ERR_INVALID_ARG, "ep_dropout: need count a multiple of 8 (count=%lld)", (long long)count);
+    ep::DropArgs d{};
+    const ep_status st = drop_args("ep_dropout", count > 0, p, rng, site, &d);
+    if (st != EP_OK)
+        return st;
+    if (count > 0 && (!x_dev || !out_dev || !aligned16(x_dev) || !aligned16(residual_dev) || !aligned16(out_dev)))
+        return fail(EP_ERR_INVALID_ARG, "ep_dropout: x and out are required, every array 16-byte aligned");
+    EP_HIP(ep::launch_dropout(x_dev, residual_dev, count, d, out_dev, stream));
+    return EP_OK;
+}
+
+extern "C" ep_status ep_dropout_rmsnorm(const void *x_dev, const void *residual_dev, const void *weight_dev,
+                                        int64_t num_tokens, int32_t hidden, float eps, double p, const int64_t *rng,
+                                        uint32_t site, void *total_dev, void *out_dev, void *rows8_dev, hipStream_t stream) {
+    ep::DropArgs d{};
+    const ep_status st = drop_args("ep_dropout_rmsnorm", num_tokens > 0, p, rng, site, &d);
+    if (st != EP_OK)
+        return st;
+    return rmsnorm("ep_dropout_rmsnorm", x_dev, residual_dev, weight_dev, num_tokens, hidden, eps, d, total_dev, out_dev,
+                   rows8_dev, stream);
+}
+
+extern "C" ep_status ep_dropout_rmsnorm_grad(const void *total_dev, const void *weight_dev, const void *d_out_dev,
+                                             const void *d_total_dev, int64_t num_tokens, int32_t hidden, float eps,
+                                             double p, const int64_t *rng, uint32_t site, void *dx_dev, void *d_residual_dev,
+                                             float *d_weight, void *workspace, size_t workspace_bytes, hipStream_t stream) {
+    ep::DropArgs d{};
+    const ep_status st = drop_args("ep_dropout_rmsnorm_grad", num_tokens > 0, p, rng, site, &d);
+    if (st != EP_OK)
+        return st;
+    return rmsnorm_grad("ep_dropout_rmsnorm_grad", total_dev, weight_dev, d_out_dev, d_total_dev, num_tokens, hidden, eps, d,
+                        dx_dev, d_residual_dev, d_weight, workspace, workspace_bytes, stream);
 }

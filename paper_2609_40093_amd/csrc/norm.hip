@@ -3,6 +3,7 @@
 //   forward   s = x + r;  y = s * rstd * w,  rstd = 1 / sqrt(mean(s^2) + eps)
 //   backward  g = d_out * w;  n = s * rstd;  dx = rstd * (g - n mean(g n)) + d_total;
 //             d_weight = sum over tokens of d_out * n
+//   with dropout of x (dropout.h)  s = drop(x) + r, and x's gradient is drop(dx)
 //
 // Both are HBM-bound: every row is read once and held in registers between its reduction and
 // its results.  The forward reduces sum(s^2) and max|s w| in the same step: the row's largest
@@ -11,7 +12,7 @@
 // 7168 with a residual, the sum, bf16 and 8-bit rows: 2.1 GB in 376 us, 5.6 TB/s; the gradient of
 // 5003 rows of 2888: 116 MB in 27 us, 4.3 TB/s; 256 rows of 7168 into 8-bit rows: 5 us, of which 2 are
 // bytes.
-#include "layer.h"
+#include "dropout.h"
 
 namespace ep {
 namespace {
@@ -94,7 +95,7 @@ __device__ __forceinline__ void store_row(T v, T *p, bool nt) {
         *p = v;
 }
 
-template <int WAVES, int V, bool NT>
+template <int WAVES, int V, bool NT, bool DROP>
 __global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_kernel(NormArgs a) {
     constexpr int kRows = block_threads<WAVES>() / (WAVES * 64);
     const int tid = (int)threadIdx.x % (WAVES * 64), sub = (int)threadIdx.x / (WAVES * 64);
@@ -108,6 +109,9 @@ __global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_kernel(NormArg
         if (a.weight && i < vecs)
             wv[v] = a.weight[i];
     }
+    DropKey key;
+    if (DROP)
+        key.load(a.drop);
     int parity = 0;
     for (int64_t row = (int64_t)blockIdx.x * kRows + sub; row < a.T; row += (int64_t)gridDim.x * kRows) {
         const int64_t base = row * vecs;
@@ -128,6 +132,8 @@ __global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_kernel(NormArg
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             unpack8(xv[v], s[v]);
+            if (DROP)
+                drop8(key, (uint64_t)(base + v * (WAVES * 64) + tid), a.drop.cut, a.drop.factor, s[v]);
             if (a.residual) {
                 float r[8];
                 unpack8(rv[v], r);
@@ -224,7 +230,7 @@ __global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_kernel(NormArg
 // gradients stay few.  The next row is on its way while one is reduced where a lane has two
 // vectors of it (5003 rows of 2888: 28.9 / 27.5 us); with four, the registers this takes cost more than it gives
 // (20000 rows of 7168: 196 / 215 us).
-template <int WAVES, int V, bool NT>
+template <int WAVES, int V, bool NT, bool DROP>
 __global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_grad_kernel(NormGradArgs a) {
     constexpr int kRows = block_threads<WAVES>() / (WAVES * 64);
     const int tid = (int)threadIdx.x % (WAVES * 64), sub = (int)threadIdx.x / (WAVES * 64);
@@ -242,6 +248,9 @@ __global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_grad_kernel(No
         for (int q = 0; q < 8; ++q)
             dw[v][q] = 0.f;
     }
+    DropKey key;
+    if (DROP)
+        key.load(a.drop);
     int parity = 0;
     const int64_t stride = (int64_t)gridDim.x * kRows;
     u32x4 sn[V], dn[V], tn[V];
@@ -350,7 +359,16 @@ __global__ __launch_bounds__(block_threads<WAVES>()) void rmsnorm_grad_kernel(No
                 dw[v][q] = fmaf(d[q], n, dw[v][q]);
                 t[q] = fmaf(rms.r, (d[q] * w[q] - n * c) * rms.f, t[q]);
             }
-            store_row(pack8(t), a.dx + base + i, NT);
+            if (!DROP) {
+                store_row(pack8(t), a.dx + base + i, NT);
+                continue;
+            }
+            if (a.d_residual)
+                store_row(pack8(t), a.d_residual + base + i, NT);
+            if (a.dx) {
+                drop8(key, (uint64_t)(base + i), a.drop.cut, a.drop.factor, t);
+                store_row(pack8(t), a.dx + base + i, NT);
+            }
         }
     }
     if (!a.d_weight)
@@ -413,20 +431,18 @@ int64_t row_groups(int64_t T, int waves, int64_t most) {
     return std::min<int64_t>((T + rows - 1) / rows, most);
 }
 
-// Rows past what the memory-side cache holds are loaded and stored non-temporally.  Measured, us:
-// rmsnorm_grad of 20000 rows of 7168 (1.1 GB) 219 / 196; the forward's at its launcher.
-constexpr int64_t kNormStreamBytes = 256ll << 20;
-
 hipError_t launch_grad_rows(const NormGradArgs &a, int64_t groups, hipStream_t stream) {
     const RowGeom g = row_geometry(a.H);
-    const bool nt = a.T * a.H * (a.d_total ? 8 : 6) >= kNormStreamBytes;
-#define EP_CALL(W, V)                                                                                              \
-    (nt ? launch_traced("rmsnorm_grad", rmsnorm_grad_kernel<W, V, true>, dim3((unsigned)groups), block_threads<W>(), \
-                        stream, a)                                                                                 \
-        : launch_traced("rmsnorm_grad", rmsnorm_grad_kernel<W, V, false>, dim3((unsigned)groups), block_threads<W>(), \
-                        stream, a))
+    const bool nt = a.T * a.H * (a.d_total ? 8 : 6) >= kNormStreamBytes, drop = a.drop.rng != nullptr;
+#define EP_LAUNCH(W, V, NT, DROP)                                                                                  \
+    launch_traced(DROP ? "dropout_rmsnorm_grad" : "rmsnorm_grad", rmsnorm_grad_kernel<W, V, NT, DROP>,             \
+                  dim3((unsigned)groups), block_threads<W>(), stream, a)
+#define EP_CALL(W, V)                                                                     \
+    (drop ? (nt ? EP_LAUNCH(W, V, true, true) : EP_LAUNCH(W, V, false, true))             \
+          : (nt ? EP_LAUNCH(W, V, true, false) : EP_LAUNCH(W, V, false, false)))
     EP_ROW_GEOMETRY(g, EP_CALL);
 #undef EP_CALL
+#undef EP_LAUNCH
 }
 
 }  // namespace
@@ -441,12 +457,15 @@ hipError_t launch_rmsnorm(const NormArgs &a, hipStream_t stream) {
     const RowGeom g = row_geometry(a.H);
     const dim3 grid((unsigned)row_groups(a.T, g.waves, 1 << 21));
     const int64_t per = 2 + (a.residual ? 2 : 0) + (a.total ? 2 : 0) + (a.out ? 2 : 0) + (a.rows8 ? 1 : 0);
-    const bool nt = a.T * a.H * per >= kNormStreamBytes;
-#define EP_CALL(W, V)                                                                                        \
-    (nt ? launch_traced("rmsnorm", rmsnorm_kernel<W, V, true>, grid, block_threads<W>(), stream, a)          \
-        : launch_traced("rmsnorm", rmsnorm_kernel<W, V, false>, grid, block_threads<W>(), stream, a))
+    const bool nt = a.T * a.H * per >= kNormStreamBytes, drop = a.drop.rng != nullptr;
+#define EP_LAUNCH(W, V, NT, DROP)                                                                                    \
+    launch_traced(DROP ? "dropout_rmsnorm" : "rmsnorm", rmsnorm_kernel<W, V, NT, DROP>, grid, block_threads<W>(), stream, a)
+#define EP_CALL(W, V)                                                                     \
+    (drop ? (nt ? EP_LAUNCH(W, V, true, true) : EP_LAUNCH(W, V, false, true))             \
+          : (nt ? EP_LAUNCH(W, V, true, false) : EP_LAUNCH(W, V, false, false)))
     EP_ROW_GEOMETRY(g, EP_CALL);
 #undef EP_CALL
+#undef EP_LAUNCH
 }
 
 // Workgroups, and partial rows of the weight gradient.  Two per compute unit: with one, 5003 rows

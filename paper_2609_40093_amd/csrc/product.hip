@@ -14,92 +14,11 @@
 // Bound by the weights' bytes for few rows per expert (2048 rows of 32 experts, K 7168, gated N
 // 2048: 383 us, 1.93 GB, 5.0 TB/s), by the matrix cores and the LDS reads that feed them for many
 // (32768 rows of the same from 8-bit rows: 957 us, 2010 TFLOP/s; 8192 x 8192 x 8192 in bf16 1210).
-#include "product_tile.h"
+#include "product_finish.h"
+#include "product_plan.h"
 
 namespace ep {
 namespace {
-
-// The rest of a call's arguments that the two kernels share.
-struct Split {
-    int32_t parts;  // of the contraction; 1: the tile kernel runs the epilogue
-    int32_t steps;  // of one part
-};
-
-// What eight neighbouring results n..n+7 of every row of expert e share: the scales and the
-// bias of their weight rows (gated: the gates' rows, then the ups').
-template <bool F8, bool GATED>
-struct Columns {
-    float scale[GATED ? 2 : 1][F8 ? 8 : 1], bias[GATED ? 2 : 1][8];
-    __device__ __forceinline__ void load(const ProductArgs &a, int64_t e, int32_t n) {
-#pragma unroll
-        for (int p = 0; p < (GATED ? 2 : 1); ++p) {
-            const int64_t at = e * a.Nw + p * a.N + n;
-            if constexpr (F8)
-#pragma unroll
-                for (int q = 0; q < 8; ++q)
-                    scale[p][q] = a.w_scale[at + q];
-#pragma unroll
-            for (int q = 0; q < 8; ++q)
-                bias[p][q] = 0.f;
-            if (a.bias)
-                unpack8(*reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(a.bias) + at), bias[p]);
-        }
-    }
-    __device__ __forceinline__ void apply(int p, float x_scale, float *z) const {
-#pragma unroll
-        for (int q = 0; q < 8; ++q)
-            z[q] = F8 ? fmaf(z[q], x_scale * scale[p][F8 ? q : 0], bias[p][q]) : z[q] + bias[p][q];
-    }
-};
-// What a row brings besides: its eight residuals and its scale.
-template <bool F8>
-struct RowExtra {
-    u32x4 residual;
-    float scale;
-    __device__ __forceinline__ void load(const ProductArgs &a, int64_t r, int32_t n) {
-        residual = u32x4{0, 0, 0, 0};
-        if (a.residual)
-            residual = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(a.residual) + r * a.N + n);
-        scale = 1.f;
-        if (F8)
-            scale = *reinterpret_cast<const float *>(static_cast<const char *>(a.x) + r * (a.K + EP_ROWS8_EXTRA) + a.K);
-    }
-};
-// The results n..n+7 of row r from their sums (gated: z the gates', up the ups').
-template <bool F8, bool GATED>
-__device__ __forceinline__ void finish8(const ProductArgs &a, const Columns<F8, GATED> &c, const RowExtra<F8> &x, int64_t r,
-                                        int32_t n, float *z, float *up) {
-    c.apply(0, x.scale, z);
-    if constexpr (GATED)
-        c.apply(1, x.scale, up);
-    if (a.pre) {
-        uint16_t *pre = static_cast<uint16_t *>(a.pre) + r * a.Nw + n;
-        *reinterpret_cast<u32x4 *>(pre) = pack8(z);
-        if (GATED)
-            *reinterpret_cast<u32x4 *>(pre + a.N) = pack8(up);
-    }
-    if (GATED) {
-#pragma unroll
-        for (int q = 0; q < 8; ++q)
-            z[q] = z[q] * sigmoid(z[q]) * up[q];
-    } else {
-        activate8(z, a.act);
-    }
-    if (a.residual) {
-        float res[8];
-        unpack8(x.residual, res);
-#pragma unroll
-        for (int q = 0; q < 8; ++q)
-            z[q] += res[q];
-    }
-    if (a.f32) {
-        f32x4 *dst = reinterpret_cast<f32x4 *>(static_cast<float *>(a.y) + r * a.N + n);
-        dst[0] = f32x4{z[0], z[1], z[2], z[3]};
-        dst[1] = f32x4{z[4], z[5], z[6], z[7]};
-    } else {
-        *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.y) + r * a.N + n) = pack8(z);
-    }
-}
 
 template <class S, Mul M, bool GATED>
 __global__ __launch_bounds__(S::kThreads) void product_kernel(ProductArgs a, int32_t col_tiles, Split split) {
@@ -238,90 +157,6 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, Split 
     RowExtra<F8> x;
     x.load(a, r, n);
     finish8<F8, GATED>(a, columns, x, r, n, z, up);
-}
-
-// Besides the sizes of product_tile.h, for many experts of few rows:
-typedef TileShape<256, 128, 4, 2, 2> Wide;   // one workgroup per compute unit (96 KiB of LDS)
-typedef TileShape<256, 64, 4, 2, 3> Few;     // one (120 KiB)
-
-// ---- choice of the tile and of the split, from the sizes the host knows ----------------
-// By the mean rows per expert.  Measured, us (bf16 gated, 32 experts, K 7168, N 2048; then 128
-// experts, K 2048, N 768), Large / Wide / Few / Medium:
-//   mean  24  363 / 338 / 398 / 355    178 / 180 / 180 / 162
-//   mean  64  389 / 427 / 394 / 421    183 / 195 / 203 / 187
-//   mean  96  507 / 431 / 534 / 464    218 / 194 / 221 / 207
-//   mean 160  538 / 548 / 738 / 600    248 / 246 / 287 / 250
-//   mean 256  609 / 721 / 991 / 820
-// Below 80 rows the weights' bytes bound it, and what differs is how evenly the tiles fill the
-// compute units.  With less than 16 rows Tiny gains up to a tenth on Medium (16 experts, K 4096,
-// N 1536, mean 8: 84 / 93).
-//
-// Where that tile gives fewer tiles than compute units (the dense products of a decode step,
-// few experts), the tiles and the parts of the contraction are weighed by an estimate of the time
-// (product_tile.h).  Measured, us, estimate's choice against the larger tile split to
-// fill the chip: 256 rows K 7168 N 256 12 / 15, 500 rows 4096 x 4096 30 / 40, 256 rows 2048 x 2048
-// 12 / 22; against the small tiles alone: 3190 rows of 15 experts 4176 x 1984 120 / 193.
-enum class Size { kLarge, kBroad, kWide, kFew, kMedium, kSmall, kTiny };
-Size tile_size(int64_t rows, int32_t E) {
-    const int64_t mean = rows / E;
-    return mean >= 160 ? Size::kLarge : mean >= 80 ? Size::kWide : mean >= 40 ? Size::kFew : mean >= 16 ? Size::kMedium : Size::kTiny;
-}
-int tile_rows(Size s) {
-    switch (s) {
-    case Size::kLarge: return Large::kJ;
-    case Size::kBroad: return Broad::kJ;
-    case Size::kWide: return Wide::kJ;
-    case Size::kFew: return Few::kJ;
-    case Size::kMedium: return Medium::kJ;
-    case Size::kSmall: return Small::kJ;
-    default: return Tiny::kJ;
-    }
-}
-int tile_cols(Size s, bool gated) {
-    return (s < Size::kMedium ? Large::kI : s == Size::kSmall ? Small::kI : Medium::kI) / (gated ? 2 : 1);
-}
-
-struct Plan {
-    Size size;
-    int64_t tiles;  // at most
-    int32_t cols;
-    Split split;
-};
-Plan make_plan(int64_t rows, int32_t E, int32_t K, int32_t N, bool bits8, bool gated) {
-    const int32_t steps = (int32_t)(((int64_t)K * (bits8 ? 1 : 2) + kStepBytes - 1) / kStepBytes);
-    const auto plan = [&](Size size, int32_t parts) {
-        Plan p;
-        p.size = size;
-        p.cols = (N + tile_cols(size, gated) - 1) / tile_cols(size, gated);
-        p.tiles = row_tiles_most(rows, E, tile_rows(size)) * p.cols;
-        p.split.steps = (steps + parts - 1) / parts;
-        p.split.parts = (steps + p.split.steps - 1) / p.split.steps;
-        return p;
-    };
-    Plan best = plan(tile_size(rows, E), 1);
-    if (best.size == Size::kLarge && broad_rows(rows, E, best.cols))
-        best = plan(Size::kBroad, 1);
-    if (best.tiles >= kCus)
-        return best;
-    double least = 0;
-    bool any = false;
-    for (Size size : {Size::kLarge, Size::kBroad, Size::kMedium, Size::kSmall, Size::kTiny})
-        for (int32_t parts = 1; parts == 1 || steps / parts >= kSplitSteps; parts *= 2) {
-            const Plan p = plan(size, parts);
-            const StepCost cost = size == Size::kLarge    ? kLargeCost
-                                  : size == Size::kBroad  ? kBroadCost
-                                  : size == Size::kMedium ? kMediumCost
-                                  : size == Size::kSmall  ? kSmallCost
-                                                          : kTinyCost;
-            const double t = estimate(cost, row_tiles_likely(rows, E, tile_rows(size)) * p.cols, p.split.parts, p.split.steps,
-                                      rows * N * (gated ? 2 : 1));
-            if (!any || t < least) {
-                any = true;
-                least = t;
-                best = p;
-            }
-        }
-    return best;
 }
 
 template <class S, Mul M, bool GATED>

@@ -14,7 +14,7 @@
 // dz is rounded to bf16 between the kernels, though it is nobody's result: both products multiply
 // bf16, and dz in more bits would double its traffic and their matrix instructions.  It takes
 // the gradients' error from 0.0017 of their 2-norm (their own rounding) to 0.0023.
-#include "product_tile.h"
+#include "product_plan.h"
 
 namespace ep {
 namespace {
@@ -252,39 +252,6 @@ hipError_t launch_dw(const GradTileArgs &a, hipStream_t stream) {
     if (groups > kMostTiles)
         return hipErrorInvalidConfiguration;
     return launch_traced("expert_product_dw", product_dw_kernel<S>, dim3((unsigned)groups), S::kThreads, stream, a, nt, kt);
-}
-
-enum class GradSize { kLarge, kBroad, kMedium, kSmall };
-struct GradTile {
-    GradSize size;
-    int i, j;
-    StepCost cost;
-};
-// An operand read across the contraction makes a step longer, the smaller the tile the more.
-constexpr GradTile kGradTiles[] = {{GradSize::kLarge, Large::kI, Large::kJ, {false, 1.15, 1.90}},
-                                   {GradSize::kBroad, Broad::kI, Broad::kJ, {false, 1.00, 1.48}},
-                                   {GradSize::kMedium, Medium::kI, Medium::kJ, {true, 0.75, 1.10}},
-                                   {GradSize::kSmall, Small::kI, Small::kJ, {true, 0.50, 0.65}}};
-
-// The tile of dx: the large ones where the experts fill them and there is one for every compute
-// unit, else by the estimate of the time.  Measured, us: 300 rows 2048 x 2048, a call's dx and dw,
-// 28 with Medium alone, 21; dx of 4096 rows of four 2048 x 1408 experts 33 with Broad, 46 with
-// Medium; of 574 rows of eight 3168 x 3056 experts 58 with Medium, 88 with Small.
-GradSize plan_dx(int64_t rows, int32_t E, int32_t K, int32_t Nw) {
-    const int64_t large = (K + Large::kI - 1) / Large::kI;
-    if (rows / E >= 160 && row_tiles_most(rows, E, Large::kJ) * large >= kCus)
-        return broad_rows(rows, E, large) ? GradSize::kBroad : GradSize::kLarge;
-    const int32_t steps = (Nw + kStepRows - 1) / kStepRows;
-    GradSize best = GradSize::kMedium;
-    double least = 0;
-    for (const GradTile &g : kGradTiles) {
-        const double t = estimate(g.cost, row_tiles_likely(rows, E, g.j) * ((K + g.i - 1) / g.i), 1, steps, 0);
-        if (least == 0 || t < least) {
-            least = t;
-            best = g.size;
-        }
-    }
-    return best;
 }
 
 // The tile and the parts of dw, from the rows per expert to expect: by the estimate where the large

@@ -1,6 +1,6 @@
 """Python binding of the layer operators (include/ep_layer.h), marshalling only.
 
-Norm, router, experts' products and the gradients run in the library's HIP kernels; outputs
+Norm, router, experts' products, adapters, dropout and the gradients run in the library's HIP kernels; outputs
 and workspaces are torch tensors of the current device.  Without a tensor to write to, a call
 allocates its outputs; with `stream`, allocations belong to that stream.
 
@@ -23,11 +23,14 @@ from ._lib import EP_OUT_BF16, EP_OUT_F32, EP_ROWS8_EXTRA, EP_ROWS_8BIT, EP_ROWS
 from .api import _check, _current_stream, _get_device, _lib_handle, _need, _ptr
 
 __all__ = ["Norm", "rmsnorm", "rmsnorm_grad", "rows8_empty", "rows8_values", "Routing", "route", "route_grad",
-           "combine_grad", "Product", "expert_product", "ProductGrad", "expert_product_grad"]
+           "combine_grad", "Product", "expert_product", "ProductGrad", "expert_product_grad",
+           "AdapterRows", "adapter_rows", "AdapterProduct", "adapter_product", "AdapterGrad", "adapter_product_grad",
+           "dropout", "dropout_rmsnorm", "dropout_rmsnorm_grad"]
 
 _BF16 = (torch.bfloat16,)
 _F32 = (torch.float32,)
 _I32 = (torch.int32,)
+_I64 = (torch.int64,)
 _F8 = (torch.float8_e4m3fn,)
 _NO_STREAM = contextlib.nullcontext()
 
@@ -354,3 +357,199 @@ def expert_product_grad(x: torch.Tensor, w: torch.Tensor, d_y: torch.Tensor, off
         _ptr(x), rows, _ptr(offsets), E, _ptr(w), K, N, code, _ptr(pre), _ptr(d_y), _ptr(got.dx), _ptr(got.dw),
         _ptr(got.dbias), _ptr(ws), n, _current_stream(stream)), "ep_expert_product_grad")
     return got
+
+
+# ------------------------------------------------------------------ low-rank adapters
+
+@dataclass
+class AdapterRows:
+    """A batch's rows by adapter.  order: int32 [rows], none where the rows come by adapter already;
+    offsets: int32 [A + 1], where each adapter's rows begin in that order."""
+    order: Optional[torch.Tensor]
+    offsets: Optional[torch.Tensor]
+
+
+def adapter_rows(row_adapter: torch.Tensor, num_adapters: int, *, out: Optional[AdapterRows] = None,
+                 stream=None) -> AdapterRows:
+    """ep_adapter_rows: the rows sorted by adapter from each row's adapter, int32 [rows] (an id
+    outside [0, num_adapters): none).  Made once for all the projections of a batch."""
+    _need(row_adapter, "row_adapter", _I32, 1)
+    n, dev = row_adapter.shape[0], row_adapter.device
+    if out is None:
+        with _on(stream):
+            out = AdapterRows(torch.empty(n, dtype=torch.int32, device=dev),
+                              torch.empty(max(num_adapters, 0) + 1, dtype=torch.int32, device=dev))
+    else:
+        _optional(_given(out.order, "out.order"), "out.order", _I32, (n,))
+        _optional(_given(out.offsets, "out.offsets"), "out.offsets", _I32, (num_adapters + 1,))
+    _check(_lib_handle().ep_adapter_rows(_ptr(row_adapter), n, num_adapters, _ptr(out.order), _ptr(out.offsets),
+                                         _current_stream(stream)), "ep_adapter_rows")
+    return out
+
+
+@dataclass
+class AdapterProduct:
+    out: torch.Tensor
+    pre: Optional[torch.Tensor]
+    low: Optional[torch.Tensor]
+
+
+def _adapters(x, a, b, rows, w, scale, act):
+    """(rows, A, R, K, weight rows, N) of the adapters' arguments, checked."""
+    _need(x, "x", _BF16, 2)
+    _need(a, "a", _BF16, 3)
+    _need(b, "b", _BF16, 3)
+    (n, K), (A, wide, R) = x.shape, b.shape
+    _shape(a, "a", (A, R, K))
+    if act == "swiglu" and wide % 2:
+        raise ValueError("swiglu needs an even number of weight rows: the gates', then the ups'")
+    _optional(w, "w", _BF16, (wide, K))
+    _optional(scale, "scale", _F32, (A,))
+    if rows.offsets is None:
+        if A != 1:
+            raise ValueError("more than one adapter needs the rows' offsets")
+    else:
+        _optional(rows.offsets, "rows.offsets", _I32, (A + 1,))
+    _optional(rows.order, "rows.order", _I32, (n,))
+    return n, A, R, K, wide, wide // 2 if act == "swiglu" else wide
+
+
+_ALL_ROWS = AdapterRows(None, None)
+
+
+def adapter_product(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, rows: AdapterRows = _ALL_ROWS, *,
+                    w: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                    bias: Optional[torch.Tensor] = None, act: str = "none", residual: Optional[torch.Tensor] = None,
+                    keep_pre: Union[bool, torch.Tensor] = False, keep_low: Union[bool, torch.Tensor] = False,
+                    out: Optional[torch.Tensor] = None, stream=None) -> AdapterProduct:
+    """ep_adapter_product: act(x w^T + scale (x a[i]^T) b[i]^T + bias) + residual, i the row's adapter, if any.
+
+    x bf16 [rows, K]; a bf16 [A, R, K], b bf16 [A, N, R]; w bf16 [N, K], or none for the adapters
+    alone; scale fp32 [A]; bias bf16 [N].  rows: adapter_rows of the batch; AdapterRows(None, offsets) for
+    rows that come by adapter; left out, one adapter has every row.  act: as expert_product (swiglu:
+    w and b with 2N rows).  keep_pre, keep_low: also the values before the activation, and the
+    low-rank values [rows, R], as the gradient reads them.  `out` may be the residual itself."""
+    n, A, R, K, wide, N = _adapters(x, a, b, rows, w, scale, act)
+    _optional(bias, "bias", _BF16, (wide,))
+    _optional(residual, "residual", _BF16, (n, N))
+    code, lib = _act(act), _lib_handle()
+    with _on(stream):
+        got = AdapterProduct(_output(True if out is None else out, "out", torch.bfloat16, (n, N), x.device),
+                             _output(keep_pre, "pre", torch.bfloat16, (n, wide), x.device),
+                             _output(keep_low, "low", torch.bfloat16, (n, R), x.device))
+        size = _bytes("ep_adapter_product_workspace_bytes", n, A, R, K, N, w is not None, code, got.low is not None)
+        ws = _workspace(size, x.device)
+    _check(lib.ep_adapter_product(
+        _ptr(x), n, _ptr(rows.order), _ptr(rows.offsets), A, R, _ptr(a), _ptr(b), _ptr(scale), _ptr(w), K, N, _ptr(bias),
+        code, _ptr(residual), _ptr(got.pre), _ptr(got.low), _ptr(got.out), _ptr(ws), size, _current_stream(stream)),
+        "ep_adapter_product")
+    return got
+
+
+@dataclass
+class AdapterGrad:
+    dx: Optional[torch.Tensor]
+    da: Optional[torch.Tensor]
+    db: Optional[torch.Tensor]
+
+
+def adapter_product_grad(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, low: torch.Tensor, d_y: torch.Tensor,
+                         rows: AdapterRows = _ALL_ROWS, *, w: Optional[torch.Tensor] = None,
+                         scale: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None, act: str = "none",
+                         dx: Union[bool, torch.Tensor] = True, da: Union[bool, torch.Tensor] = True,
+                         db: Union[bool, torch.Tensor] = True, stream=None) -> AdapterGrad:
+    """ep_adapter_product_grad, with w held fast: dx bf16 [rows, K], da like a, db like b.  low, pre:
+    what the forward kept (pre is needed with an activation).  Without w, dx is the adapters' part."""
+    n, A, R, K, wide, N = _adapters(x, a, b, rows, w, scale, act)
+    _optional(_given(low, "low"), "low", _BF16, (n, R))
+    _optional(_given(d_y, "d_y"), "d_y", _BF16, (n, N))
+    code = _act(act)
+    if act != "none" and pre is None:
+        raise ValueError("an activation's gradient needs pre")
+    _optional(pre, "pre", _BF16, (n, wide))
+    lib = _lib_handle()
+    with _on(stream):
+        got = AdapterGrad(_output(dx, "dx", torch.bfloat16, (n, K), x.device),
+                          _output(da, "da", torch.bfloat16, (A, R, K), x.device),
+                          _output(db, "db", torch.bfloat16, (A, wide, R), x.device))
+        size = _bytes("ep_adapter_product_grad_workspace_bytes", n, A, R, K, N, code, rows.order is not None,
+                      (_lib.EP_ADAPTER_DX if got.dx is not None else 0) | (_lib.EP_ADAPTER_DA if got.da is not None else 0)
+                      | (_lib.EP_ADAPTER_DB if got.db is not None else 0))
+        ws = _workspace(size, x.device)
+    _check(lib.ep_adapter_product_grad(
+        _ptr(x), n, _ptr(rows.order), _ptr(rows.offsets), A, R, _ptr(a), _ptr(b), _ptr(scale), _ptr(w), K, N, _ptr(low),
+        code, _ptr(pre), _ptr(d_y), _ptr(got.dx), _ptr(got.da), _ptr(got.db), _ptr(ws), size, _current_stream(stream)),
+        "ep_adapter_product_grad")
+    return got
+
+
+# ---------------------------------------------------------------------------- dropout
+
+def dropout(x: torch.Tensor, p: float, rng: torch.Tensor, *, site: int = 0, residual: Optional[torch.Tensor] = None,
+            out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """ep_dropout: residual + dropout(x), bf16 of any shape with a multiple of 8 values.
+
+    rng: int64 [2] on the device, the seed and the step; site: which of the program's dropouts this is.
+    The same rng and site give the same mask, so the gradient of x is dropout(d_out, p, rng, site=site).
+    `out` may be x or the residual itself."""
+    _need(x, "x", _BF16)
+    _optional(residual, "residual", _BF16, x.shape)
+    _rng(rng, site)
+    with _on(stream):
+        out = _output(True if out is None else out, "out", torch.bfloat16, x.shape, x.device)
+    _check(_lib_handle().ep_dropout(_ptr(x), _ptr(residual), x.numel(), p, _ptr(rng), site, _ptr(out),
+                                    _current_stream(stream)), "ep_dropout")
+    return out
+
+
+def _rng(rng: torch.Tensor, site: int):
+    _optional(_given(rng, "rng"), "rng", _I64, (2,))
+    if not 0 <= site < 1 << 32:
+        raise ValueError(f"site must be a number of 32 bits, not {site}")
+
+
+def dropout_rmsnorm(x: torch.Tensor, p: float, rng: torch.Tensor, weight: Optional[torch.Tensor] = None, *, site: int = 0,
+                    residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                    total: Union[bool, torch.Tensor, None] = None, out: Union[bool, torch.Tensor] = True,
+                    rows8: Union[bool, torch.Tensor] = False, stream=None) -> Norm:
+    """ep_dropout_rmsnorm: rmsnorm of dropout(x) + residual; total = that sum (written where there is a
+    residual, or on request).  The rest as rmsnorm and dropout."""
+    _need(x, "x", _BF16, 2)
+    T, H = x.shape
+    _optional(residual, "residual", _BF16, x.shape)
+    _optional(weight, "weight", _BF16, (H,))
+    _rng(rng, site)
+    with _on(stream):
+        got = Norm(_output(residual is not None if total is None else total, "total", torch.bfloat16, x.shape, x.device),
+                   _output(out, "out", torch.bfloat16, x.shape, x.device),
+                   _output(rows8, "rows8", torch.uint8, (T, H + EP_ROWS8_EXTRA), x.device))
+    _check(_lib_handle().ep_dropout_rmsnorm(_ptr(x), _ptr(residual), _ptr(weight), T, H, eps, p, _ptr(rng), site,
+                                            _ptr(got.total), _ptr(got.out), _ptr(got.rows8), _current_stream(stream)),
+           "ep_dropout_rmsnorm")
+    return got
+
+
+def dropout_rmsnorm_grad(total: torch.Tensor, weight: Optional[torch.Tensor], d_out: torch.Tensor, p: float,
+                         rng: torch.Tensor, *, site: int = 0, d_total: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                         dx: Union[bool, torch.Tensor] = True, d_residual: Union[bool, torch.Tensor] = True,
+                         d_weight: Union[bool, torch.Tensor] = True, stream=None
+                         ) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """ep_dropout_rmsnorm_grad: (dx bf16 [T, H], d_residual bf16 [T, H], d_weight fp32 [H]) at the norm's
+    `total`; each may be left out, but one of the first two is wanted."""
+    _need(total, "total", _BF16, 2)
+    T, H = total.shape
+    _optional(_given(d_out, "d_out"), "d_out", _BF16, total.shape)
+    _optional(d_total, "d_total", _BF16, total.shape)
+    _optional(weight, "weight", _BF16, (H,))
+    _rng(rng, site)
+    lib = _lib_handle()
+    with _on(stream):
+        dx = _output(dx, "dx", torch.bfloat16, total.shape, total.device)
+        d_residual = _output(d_residual, "d_residual", torch.bfloat16, total.shape, total.device)
+        d_weight = _output(d_weight, "d_weight", torch.float32, (H,), total.device)
+        n = _bytes("ep_rmsnorm_grad_workspace_bytes", T, H) if d_weight is not None else 0
+        ws = _workspace(n, total.device)
+    _check(lib.ep_dropout_rmsnorm_grad(_ptr(total), _ptr(weight), _ptr(d_out), _ptr(d_total), T, H, eps, p, _ptr(rng), site,
+                                       _ptr(dx), _ptr(d_residual), _ptr(d_weight), _ptr(ws), n, _current_stream(stream)),
+           "ep_dropout_rmsnorm_grad")
+    return dx, d_residual, d_weight
