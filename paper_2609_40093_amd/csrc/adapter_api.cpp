@@ -27,10 +27,13 @@ ep_status check_sizes(const char *who, int64_t rows, int32_t A, int32_t R, int32
     return EP_OK;
 }
 
-size_t low_bytes(int64_t rows, int32_t R) { return ((size_t)rows * R * 2 + 255) & ~(size_t)255; }
+// What the workspace holds of low: all of it if the caller does not keep it.
+size_t low_bytes(int64_t rows, int32_t R, bool keep_low) {
+    return keep_low || ep::adapter_few(rows) ? 0 : ((size_t)rows * R * 2 + 255) & ~(size_t)255;
+}
 
 size_t product_bytes(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t N, bool base, int32_t act, bool keep_low) {
-    return (keep_low ? 0 : low_bytes(rows, R)) + ep::adapter_product_partial_bytes(rows, A, R, K, N, base, act);
+    return low_bytes(rows, R, keep_low) + ep::adapter_product_partial_bytes(rows, A, R, K, N, base, act);
 }
 
 }  // namespace
@@ -99,9 +102,10 @@ extern "C" ep_status ep_adapter_product(const void *x_dev, int64_t rows, const i
     a.act = act;
     a.residual = residual_dev;
     a.pre = pre_dev;
-    a.low = low_dev ? low_dev : workspace;
     a.y = y_dev;
-    a.partial = reinterpret_cast<float *>(static_cast<char *>(workspace) + (low_dev ? 0 : low_bytes(rows, rank)));
+    const size_t low = low_bytes(rows, rank, low_dev != nullptr);
+    a.low = low ? workspace : low_dev;
+    a.partial = reinterpret_cast<float *>(static_cast<char *>(workspace) + low);
     EP_HIP(ep::launch_adapter_product(a, stream));
     return EP_OK;
 }

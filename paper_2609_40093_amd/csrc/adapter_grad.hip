@@ -1,42 +1,19 @@
 // adapter_grad.hip -- gradients of the adapters' product y = act(x W^T + low b_a^T + bias) + residual, W held:
 //   dz = d_y act'(pre);  v = scale_a dz b_a;  dx = dz W + v a_a;  da_a = v^T x;  db_a = dz^T low.
 //
-// v is made as low is (adapter_low.hip), from b transposed.  dx has the product's form: the contraction
-// over W's rows goes on over the ranks of the tile's adapters (adapter_tile.h).  da and db are
-// contractions over an adapter's rows (product_grad.hip).  Rows go in the adapters' order; where they
-// come in another one, or there is an activation, dz is kept in that order, and so are x's rows for da.
+// v is made as low is (adapter_low.hip).  dx has the product's form: the contraction over W's rows goes on
+// over the ranks of the tile's adapters (adapter_tile.h).  da and db are contractions over an
+// adapter's rows, of a long side (x, dz) that is read once and a short one (v, low): bound by the long
+// side's bytes, so the rows are shared out over workgroups until there is one for every compute unit,
+// and a second kernel adds their fp32 sums in order.  Rows go in the adapters' order, and every kernel
+// gathers its rows of x and d_y through it; only with an activation dz is kept, in that order.
 //
-// v and dz are rounded to bf16 between the kernels: the products multiply bf16.
+// dz is rounded to bf16 between the kernels, v to two bf16 values: the products multiply bf16.
 #include "adapter_tile.h"
 #include "product_plan.h"
 
 namespace ep {
 namespace {
-
-// b [A][N][R] into [A][R][N]: 64 columns n and 64 ranks at a time.
-__global__ __launch_bounds__(256) void adapter_turn_kernel(const uint16_t *b, int32_t N, int32_t R, uint16_t *turned) {
-    __shared__ uint16_t part[64][72];
-    const int32_t n0 = (int32_t)blockIdx.x * 64, r0 = (int32_t)blockIdx.y * 64;
-    const int64_t base = (int64_t)blockIdx.z * N * R;
-    const int width = R - r0 < 64 ? R - r0 : 64, vecs = width / 8;
-    for (int i = threadIdx.x; i < 64 * vecs; i += 256) {
-        const int n = i / vecs, v = i % vecs;
-        if (n0 + n < N)
-            *reinterpret_cast<u32x4 *>(&part[n][v * 8]) =
-                *reinterpret_cast<const u32x4 *>(b + base + (int64_t)(n0 + n) * R + r0 + v * 8);
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < width * 8; i += 256) {
-        const int r = i / 8, n = i % 8 * 8;
-        if (n0 + n >= N)
-            continue;
-        uint32_t o[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            o[q] = part[n + 2 * q][r] | (uint32_t)part[n + 2 * q + 1][r] << 16;
-        *reinterpret_cast<u32x4 *>(turned + base + (int64_t)(r0 + r) * N + n0 + n) = u32x4{o[0], o[1], o[2], o[3]};
-    }
-}
 
 // dz[i] = d_y[r] act'(pre[r]), r = order[i]: eight values per thread.  Without an activation (pre null)
 // it gathers rows.
@@ -82,30 +59,32 @@ struct DxArgs {
     int64_t rows;
     int32_t K, Nw;
     const uint16_t *w, *dz;
+    const int32_t *dz_order;  // dz's rows; null: they are in the adapters' order
     uint16_t *dx;
 };
 
 // The sums of place i, columns k..k+7, of their own terms alone.
 __device__ __forceinline__ void redo8(const DxArgs &a, const AdapterSide &s, int64_t i, int32_t k, float *z) {
-    const int32_t e = adapter_of(s, a.rows, i);
+    const int32_t e = adapter_of(s, a.rows, i), r = row_at(a.dz_order, a.rows, i);
 #pragma unroll
     for (int q = 0; q < 8; ++q)
         z[q] = 0.f;
-    const auto add = [&](const uint16_t *u, const uint16_t *v, int32_t length) {
-#pragma unroll 1
-        for (int32_t n = 0; n < length; ++n) {
-            float g[8];
-            unpack8(*reinterpret_cast<const u32x4 *>(v + (int64_t)n * a.K + k), g);
-            const float f = __uint_as_float((uint32_t)u[n] << 16);
+    const auto add = [&](uint16_t f, const uint16_t *row) {
+        float g[8];
+        unpack8(*reinterpret_cast<const u32x4 *>(row + k), g);
 #pragma unroll
-            for (int q = 0; q < 8; ++q)
-                z[q] = fmaf(f, g[q], z[q]);
-        }
+        for (int q = 0; q < 8; ++q)
+            z[q] = fmaf(__uint_as_float((uint32_t)f << 16), g[q], z[q]);
     };
     if (a.w)
-        add(a.dz + i * a.Nw, a.w, a.Nw);
+#pragma unroll 1
+        for (int32_t n = 0; n < a.Nw; ++n)
+            add(a.dz[(int64_t)r * a.Nw + n], a.w + (int64_t)n * a.K);
     if (e >= 0)
-        add(s.low + i * s.R, s.weights + (int64_t)e * s.R * a.K, s.R);
+#pragma unroll 1
+        for (int32_t j = 0; j < 2 * s.R; ++j)
+            add(s.low[i * s.width + s.chunk_at(j / 8) + j % 8],
+                s.weights + ((int64_t)e * s.R + (j < s.R ? j : j - s.R)) * a.K);
 }
 
 // dx[order[i]][k] = sum_n dz[i][n] w[n][k] + sum_j v[i][j] a_e[j][k]: i = k across the contraction, j = rows.
@@ -114,7 +93,7 @@ __global__ __launch_bounds__(S::kThreads) void adapter_dx_kernel(DxArgs a, Adapt
     __shared__ __attribute__((aligned(1024))) char lds[S::kStages * S::kStageBytes];
     __shared__ Segment table[S::kJ];
     Segment EP_LDS *segments = (Segment EP_LDS *)table;
-    __shared__ int32_t found;
+    __shared__ int32_t row_of[S::kJ], found;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t t = tile_of_block(blockIdx.x, (int64_t)row_tiles * col_tiles);
     if (t < 0)
@@ -123,6 +102,8 @@ __global__ __launch_bounds__(S::kThreads) void adapter_dx_kernel(DxArgs a, Adapt
     tile_order(t, row_tiles, col_tiles, tr, tc);
     const int64_t i0 = (int64_t)tr * S::kJ;
     const int n_rows = a.rows - i0 < S::kJ ? (int)(a.rows - i0) : S::kJ;
+    for (int j = threadIdx.x; j < S::kJ; j += S::kThreads)
+        row_of[j] = j < n_rows ? row_at(s.order, a.rows, i0 + j) : -1;
     if (wave == 0) {
         const int n = find_segments<S::kJ>(s, a.rows, i0, n_rows, segments, lane);
         if (lane == 0)
@@ -133,19 +114,23 @@ __global__ __launch_bounds__(S::kThreads) void adapter_dx_kernel(DxArgs a, Adapt
     const int32_t k0 = tc * S::kI;
     const int32_t main = a.w ? (a.Nw + kStepRows - 1) / kStepRows : 0;
     ChainAcross<S::kI, S::kWaves, S::FI> w;
-    ChainAlong<S::kJ, S::kWaves, true> z;
+    ChainAlong<S::kJ, S::kWaves, LowRows> z;
     w.init(reinterpret_cast<const char *>(a.w), (int64_t)a.K * 2, a.Nw, k0, wave, lane);
-    w.chain(main, s, segments, count, (uint64_t)s.A * s.R * a.K * 2);
+    w.chain(main, s, segments, count, (uint64_t)s.A * s.R * a.K * 2, k0);
     const int64_t zs = (int64_t)a.Nw * 2;
-    z.init(reinterpret_cast<const char *>(a.dz) + i0 * zs, (uint32_t)(n_rows * zs), (int32_t)zs, wave, lane,
-           [&](int row) -> uint32_t { return (uint32_t)(row * zs); });
-    z.chain(main, s, segments, count, s.low + i0 * s.R, (uint64_t)n_rows * s.R * 2, 0, wave, lane, [](int row) { return row; });
+    const char *zb = reinterpret_cast<const char *>(a.dz);
+    z.init(a.dz_order ? zb : zb + i0 * zs, (uint32_t)((a.dz_order ? a.rows : n_rows) * zs), (int32_t)zs, wave, lane,
+           [&](int row) -> uint32_t {
+               const int32_t r = a.dz_order ? row_of[row] : row;
+               return r < 0 ? kNowhere : (uint32_t)(r * zs);
+           });
+    z.chain(main, s, segments, count, s.low + i0 * s.width, (uint64_t)n_rows * s.width * 2, 0, LowRows{});
     f32x16 acc[S::FI][S::FJ] = {};
-    tile_product<S, Mul::kBf16>(w, z, main + (count * (s.R / 8) + 7) / 8, (char EP_LDS *)lds, wave, lane, acc);
+    tile_product<S, Mul::kBf16>(w, z, main + (count * (int32_t)s.chunks.d + 7) / 8, (char EP_LDS *)lds, wave, lane, acc);
     const int32_t k = k0 + first_col<S, 8>(wave, lane);
     tile_rows_out<S, 8>(
         acc, (char EP_LDS *)lds, wave, lane,
-        [&](int row) -> int32_t { return row < n_rows && k < a.K ? row_at(s.order, a.rows, i0 + row) : -1; },
+        [&](int row) -> int32_t { return row < n_rows && k < a.K ? row_of[row] : -1; },
         [&](int row, int, float *v, int32_t r) {
             if (r < 0)
                 return;
@@ -165,22 +150,215 @@ hipError_t launch_dx(const DxArgs &a, const AdapterSide &s, hipStream_t stream) 
                          (int32_t)row_tiles, cols);
 }
 
+// ---- da and db -----------------------------------------------------------------------
+// Rows across the contraction, gathered through an order (null: one after the other).  The next
+// step's entries of the order are on their way while a step's rows are loaded.
+template <int T, int W, int FRAGMENTS>
+struct GatherAcross : AcrossC<T, W, FRAGMENTS> {
+    typedef AcrossC<T, W, FRAGMENTS> First;
+    using First::kLoads;
+    const int32_t *order;
+    int64_t place, last;  // of the order: the next step's first, and the end
+    const char *all;
+    uint32_t size, column;  // bytes of all rows, with an order; the tile's first column
+    int32_t total;
+    int32_t next[kLoads];
+
+    // Places begin .. end - 1 of the n rows, from step `first` on.
+    __device__ __forceinline__ void start(const int32_t *o, const char *rows, int64_t n, int64_t row_bytes, int64_t begin,
+                                          int64_t end, int32_t index0, int32_t first, int wave, int lane) {
+        First::init(rows + (o ? 0 : begin * row_bytes), row_bytes, end - begin, index0, wave, lane);
+        order = o;
+        all = rows;
+        size = (uint32_t)(n * row_bytes);
+        column = (uint32_t)index0;
+        total = (int32_t)n;
+        place = begin + (int64_t)first * kStepRows;
+        last = end;
+        if (o)
+            fetch(wave, lane);
+        else
+            First::skip(first);
+    }
+    __device__ __forceinline__ void fetch(int wave, int lane) {
+#pragma unroll
+        for (int q = 0; q < kLoads; ++q) {
+            const int64_t i = place + First::row_of(q, wave, lane);
+            next[q] = i < last ? order[i] : -1;
+        }
+        place += kStepRows;
+    }
+    __device__ __forceinline__ void begin(bool live) {
+        if (!order) {
+            First::begin(live);
+            return;
+        }
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        First::range = buffer_of(all, live ? size : 0);
+#pragma unroll
+        for (int q = 0; q < kLoads; ++q)
+            First::offset[q] = next[q] >= 0 && next[q] < total ? (uint32_t)next[q] * (uint32_t)First::stride +
+                                                                     First::column_of(q, column, wave, lane)
+                                                               : kNowhere;
+        fetch(wave, lane);
+    }
+    __device__ __forceinline__ void end() {
+        if (!order)
+            First::end();
+    }
+};
+
+struct WeightArgs {
+    const int32_t *order, *offsets;  // order: of the long rows alone; null: they are in the adapters' order
+    int64_t rows;
+    int32_t A, R, L, width;
+    const uint16_t *side, *low;  // [rows][L]; [rows][width]: v in two values (da) or low (db)
+    uint16_t *out;               // da [A][R][L], db [A][L][R]
+    float *partial;              // parts > 1: [parts] of the same
+    int32_t parts;
+};
+
+// da: i = the long side's columns, j = a block of v's ranks, the first values and then the second, which are
+// added up at the end.  db: i = ranks, j = the long side's columns.
+template <class S, bool DA>
+__global__ __launch_bounds__(S::kThreads) void adapter_weight_kernel(WeightArgs a, int32_t long_tiles, int32_t groups) {
+    __shared__ __attribute__((aligned(1024))) char lds[S::kStages * S::kStageBytes];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int64_t t = tile_of_block(blockIdx.x, (int64_t)a.A * a.parts * groups * long_tiles);
+    if (t < 0)
+        return;
+    const int32_t tile = (int32_t)(t % long_tiles);
+    t /= long_tiles;
+    const int32_t group = (int32_t)(t % groups);
+    t /= groups;
+    const int32_t part = (int32_t)(t % a.parts), e = (int32_t)(t / a.parts);
+    int64_t b, end;
+    expert_rows(a.offsets, a.rows, e, b, end);
+    const int32_t all = (int32_t)((end - b + kStepRows - 1) / kStepRows), per = (all + a.parts - 1) / a.parts;
+    const int32_t first = part * per, steps = all - first < per ? all - first : per;  // 0 or less: none
+    constexpr int kLong = DA ? S::kI : S::kJ, kShort = DA ? S::kJ : S::kI;
+    const int32_t l0 = tile * kLong;
+    GatherAcross<kLong, S::kWaves, DA ? S::FI : S::FJ> x;
+    AcrossC<kShort, S::kWaves, DA ? S::FJ : S::FI> v;
+    x.start(a.order, reinterpret_cast<const char *>(a.side), a.rows, (int64_t)a.L * 2, b, end, l0, first, wave, lane);
+    v.init(reinterpret_cast<const char *>(a.low + b * a.width), (int64_t)a.width * 2, end - b, group * kShort, wave, lane);
+    v.skip(first);
+    f32x16 acc[S::FI][S::FJ] = {};
+    // where eight results go: in the weights, counted in values
+    const auto put = [&](int64_t at, const float *o) {
+        if (a.parts == 1) {
+            *reinterpret_cast<u32x4 *>(a.out + at) = pack8(o);
+        } else {
+            f32x4 *dst = reinterpret_cast<f32x4 *>(a.partial + (int64_t)part * a.A * a.R * a.L + at);
+            dst[0] = f32x4{o[0], o[1], o[2], o[3]};
+            dst[1] = f32x4{o[4], o[5], o[6], o[7]};
+        }
+    };
+    if constexpr (DA) {
+        tile_product<S, Mul::kBf16>(x, v, steps, (char EP_LDS *)lds, wave, lane, acc);
+        typedef TileShape<S::kI, S::kJ / 2, S::kWavesI, S::kWavesJ, S::kStages> Half;
+        static_assert(S::kWavesJ == 1, "both values of a rank are one wave's");
+        f32x16 sum[Half::FI][Half::FJ];
+#pragma unroll
+        for (int i = 0; i < Half::FI; ++i)
+#pragma unroll
+            for (int j = 0; j < Half::FJ; ++j)
+                sum[i][j] = acc[i][j] + acc[i][j + Half::FJ];
+        tile_results<Half>(sum, (char EP_LDS *)lds, wave, lane, [&](int row, int col, const float *o) {
+            const int32_t rank = group * (kShort / 2) + row, l = l0 + col;
+            if (rank < a.R && l < a.L)
+                put(((int64_t)e * a.R + rank) * a.L + l, o);
+        });
+    } else {
+        tile_product<S, Mul::kBf16>(v, x, steps, (char EP_LDS *)lds, wave, lane, acc);
+        tile_results<S>(acc, (char EP_LDS *)lds, wave, lane, [&](int row, int col, const float *o) {
+            const int32_t rank = group * kShort + col, l = l0 + row;
+            if (rank < a.R && l < a.L)
+                put(((int64_t)e * a.L + l) * a.R + rank, o);
+        });
+    }
+}
+
+// The parts added up in order: eight values per thread.
+__global__ __launch_bounds__(256) void adapter_weight_join_kernel(const float *partial, int32_t parts, int64_t groups,
+                                                                  uint16_t *out) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= groups)
+        return;
+    float s[8] = {};
+    const f32x4 *src = reinterpret_cast<const f32x4 *>(partial) + i * 2;
+    constexpr int kAhead = 4;
+    for (int32_t p0 = 0; p0 < parts; p0 += kAhead) {
+        f32x4 v[kAhead][2];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                v[u][h] = f32x4{};
+                if (p0 + u < parts)
+                    v[u][h] = src[(p0 + u) * groups * 2 + h];
+            }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                s[q] += v[u][q / 4][q % 4];
+    }
+    reinterpret_cast<u32x4 *>(out)[i] = pack8(s);
+}
+
+typedef TileShape<128, 64, 4, 1, 3> Da32;   // 32 ranks; two workgroups per compute unit each (72, 64 and
+typedef TileShape<128, 128, 4, 1, 2> Da64;  // 64         72 KiB of LDS)
+typedef TileShape<64, 128, 2, 2, 3> Db64;
+
+// Tiles along the long side (x for da, dz for db) and of the ranks, and the parts of the rows.
+struct WeightPlan {
+    int32_t tiles, groups, parts;
+    WeightPlan(int64_t rows, int32_t A, int32_t R, int32_t L, bool da) {
+        const int32_t ranks = da ? 1 << split_log(R) : Db64::kI;
+        tiles = (L + 127) / 128;
+        groups = (R + ranks - 1) / ranks;
+        const int64_t steps = (rows / A + kStepRows - 1) / kStepRows;  // of an adapter, to expect
+        parts = 1;
+        while ((int64_t)A * tiles * groups * parts < 2 * kCus && steps / (parts * 2) >= kSplitSteps)
+            parts *= 2;
+    }
+    size_t bytes(int32_t A, int32_t R, int32_t L) const { return parts > 1 ? (size_t)parts * A * R * L * 4 : 0; }
+};
+
+template <class S, bool DA>
+hipError_t launch_weight(const WeightArgs &a, const WeightPlan &p, hipStream_t stream) {
+    const int64_t blocks = (int64_t)a.A * p.tiles * p.groups * p.parts;
+    if (blocks > kMostTiles)
+        return hipErrorInvalidConfiguration;
+    const hipError_t e = launch_traced(DA ? "adapter_da" : "adapter_db", adapter_weight_kernel<S, DA>,
+                                       dim3((unsigned)(blocks + 8)), S::kThreads, stream, a, p.tiles, p.groups);
+    if (e != hipSuccess || p.parts == 1)
+        return e;
+    const int64_t groups = (int64_t)a.A * a.R * a.L / 8;
+    return launch_traced("adapter_weight_join", adapter_weight_join_kernel, dim3((unsigned)((groups + 255) / 256)), 256,
+                         stream, (const float *)a.partial, p.parts, groups, a.out);
+}
+
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// v [rows][R], b turned [A][R][Nw], dz [rows][Nw] and x's rows [rows][K] in the adapters' order, and the
-// workspace of da's and db's contractions.
+// Rows that are gathered through an order are addressed in 31 bits; larger arrays are copied in order.
+bool too_far(int64_t rows, int64_t length) { return rows * length * 2 > INT32_MAX; }
+
+// v [rows][split_width], dz [rows][Nw] (with an activation, or out of a gather's reach), x's rows [rows][K] (out
+// of its reach), and the parts of da or db.
 struct Workspace {
-    size_t turned = 0, dz = 0, x = 0, sums = 0, bytes = 0;
+    size_t dz = 0, x = 0, sums = 0, bytes = 0;
+    bool own_dz, own_x;
     Workspace(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t N, int32_t act, bool order, bool dx, bool da, bool db) {
         const int64_t Nw = act == EP_ACT_SWIGLU ? 2 * (int64_t)N : N;
-        const bool v = dx || da;
-        turned = v ? align256((size_t)rows * R * 2) : 0;
-        dz = turned + (v ? align256((size_t)A * R * Nw * 2) : 0);
-        x = dz + (order || act != EP_ACT_NONE ? align256((size_t)(rows * Nw * 2)) : 0);
-        sums = x + (order && da ? align256((size_t)rows * K * 2) : 0);
-        const size_t sa = da ? product_grad_workspace_bytes(rows, A, K, R, EP_ACT_NONE, false, true, false) : 0;
-        const size_t sb = db ? product_grad_workspace_bytes(rows, A, R, (int32_t)Nw, EP_ACT_NONE, false, true, false) : 0;
-        bytes = sums + std::max(sa, sb);
+        own_dz = (dx || da || db) && rows > 0 && (act != EP_ACT_NONE || (order && too_far(rows, Nw)));
+        own_x = da && order && too_far(rows, K);
+        dz = dx || da ? align256((size_t)rows * split_width(R) * 2) : 0;
+        x = dz + (own_dz ? align256((size_t)(rows * Nw * 2)) : 0);
+        sums = x + (own_x ? align256((size_t)rows * K * 2) : 0);
+        bytes = sums + std::max(da ? WeightPlan(rows, A, R, K, true).bytes(A, R, K) : 0,
+                                db ? WeightPlan(rows, A, R, (int32_t)Nw, false).bytes(A, R, (int32_t)Nw) : 0);
     }
 };
 
@@ -196,9 +374,10 @@ hipError_t launch_adapter_grad(const AdapterGradArgs &a, hipStream_t stream) {
     const int32_t Nw = gated ? 2 * a.N : a.N;
     const Workspace ws(a.rows, a.A, a.R, a.K, a.N, a.act, a.order != nullptr, a.dx, a.da, a.db);
     char *base = static_cast<char *>(a.workspace);
-    uint16_t *v = reinterpret_cast<uint16_t *>(base), *turned = reinterpret_cast<uint16_t *>(base + ws.turned);
+    uint16_t *v = reinterpret_cast<uint16_t *>(base);
     const uint16_t *dz = static_cast<const uint16_t *>(a.d_y), *x = static_cast<const uint16_t *>(a.x);
-    const auto gather = [&](const uint16_t *pre, const uint16_t *rows, int32_t N, bool two, uint16_t *to) {
+    const int32_t *dz_order = a.order, *x_order = a.order;
+    const auto in_order = [&](const uint16_t *pre, const uint16_t *rows, int32_t N, bool two, uint16_t *to) {
         const dim3 grid((unsigned)((N / 8 + 255) / 256), (unsigned)std::min<int64_t>(a.rows, 1 << 15));
 #define EP_CALL(GATED)                                                                                                 \
     launch_traced("adapter_dz", adapter_dz_kernel<GATED>, grid, 256, stream, a.order, a.rows, N, a.act, pre, rows, to)
@@ -206,28 +385,32 @@ hipError_t launch_adapter_grad(const AdapterGradArgs &a, hipStream_t stream) {
 #undef EP_CALL
     };
     hipError_t e = hipSuccess;
-    if (a.rows > 0 && (a.order || activated)) {
+    if (ws.own_dz) {
         uint16_t *to = reinterpret_cast<uint16_t *>(base + ws.dz);
-        e = gather(activated ? static_cast<const uint16_t *>(a.pre) : nullptr, dz, a.N, gated, to);
+        e = in_order(activated ? static_cast<const uint16_t *>(a.pre) : nullptr, dz, a.N, gated, to);
         if (e != hipSuccess)
             return e;
         dz = to;
+        dz_order = nullptr;
     }
-    if (a.rows > 0 && (a.dx || a.da)) {
-        e = launch_traced("adapter_turn", adapter_turn_kernel,
-                          dim3((unsigned)((Nw + 63) / 64), (unsigned)((a.R + 63) / 64), (unsigned)a.A), 256, stream,
-                          (const uint16_t *)a.b, Nw, a.R, turned);
+    if (ws.own_x) {
+        uint16_t *to = reinterpret_cast<uint16_t *>(base + ws.x);
+        e = in_order(nullptr, x, a.K, false, to);
         if (e != hipSuccess)
             return e;
-        e = launch_adapter_low({dz, a.rows, nullptr, a.offsets, a.A, a.R, Nw, turned, a.scale, v}, stream);
+        x = to;
+        x_order = nullptr;
+    }
+    const int32_t width = split_width(a.R), log = split_log(a.R);
+    if (a.dx || a.da) {
+        e = launch_adapter_low({dz, a.rows, dz_order, a.offsets, a.A, a.R, Nw, a.b, a.scale, v, width, log}, stream);
         if (e != hipSuccess)
             return e;
     }
     if (a.rows > 0 && a.dx) {
-        const DxArgs d{a.rows, a.K, Nw, static_cast<const uint16_t *>(a.w), dz, static_cast<uint16_t *>(a.dx)};
-        const AdapterSide s{a.order, a.offsets, a.A, a.R, v, static_cast<const uint16_t *>(a.a), fast_div((uint32_t)a.R),
-                            fast_div((uint32_t)(a.R / 8))};
-        const GradSize size = plan_dx(a.rows, 1, a.K, a.w ? Nw : a.R);
+        const DxArgs d{a.rows, a.K, Nw, static_cast<const uint16_t *>(a.w), dz, dz_order, static_cast<uint16_t *>(a.dx)};
+        const AdapterSide s = adapter_side(a.order, a.offsets, a.A, a.R, v, width, log, a.a);
+        const GradSize size = plan_dx(a.rows, 1, a.K, a.w ? Nw : 2 * a.R);
         e = size == GradSize::kLarge    ? launch_dx<Large>(d, s, stream)
             : size == GradSize::kBroad  ? launch_dx<Broad>(d, s, stream)
             : size == GradSize::kMedium ? launch_dx<Medium>(d, s, stream)
@@ -235,36 +418,31 @@ hipError_t launch_adapter_grad(const AdapterGradArgs &a, hipStream_t stream) {
         if (e != hipSuccess)
             return e;
     }
-    ProductGradArgs p{};
-    p.rows = a.rows;
-    p.offsets = a.offsets;
-    p.E = a.A;
-    p.act = EP_ACT_NONE;
-    p.workspace = base + ws.sums;
+    WeightArgs p{nullptr, a.offsets, a.rows, a.A, a.R, 0, 0, nullptr, nullptr, nullptr, nullptr, 1};
+    p.partial = reinterpret_cast<float *>(base + ws.sums);
     if (a.da) {
-        if (a.rows > 0 && a.order) {
-            uint16_t *to = reinterpret_cast<uint16_t *>(base + ws.x);
-            e = gather(nullptr, x, a.K, false, to);
-            if (e != hipSuccess)
-                return e;
-            x = to;
-        }
-        p.x = x;
-        p.d_y = v;
-        p.K = a.K;
-        p.N = p.Nw = a.R;
-        p.dw = a.da;
-        e = launch_product_grad(p, stream);
+        const WeightPlan plan(a.rows, a.A, a.R, a.K, true);
+        p.order = x_order;
+        p.L = a.K;
+        p.width = width;
+        p.side = x;
+        p.low = v;
+        p.out = static_cast<uint16_t *>(a.da);
+        p.parts = plan.parts;
+        e = log == 5 ? launch_weight<Da32, true>(p, plan, stream) : launch_weight<Da64, true>(p, plan, stream);
         if (e != hipSuccess)
             return e;
     }
     if (a.db) {
-        p.x = a.low;
-        p.d_y = dz;
-        p.K = a.R;
-        p.N = p.Nw = Nw;
-        p.dw = a.db;
-        e = launch_product_grad(p, stream);
+        const WeightPlan plan(a.rows, a.A, a.R, Nw, false);
+        p.order = dz_order;
+        p.L = Nw;
+        p.width = a.R;
+        p.side = dz;
+        p.low = static_cast<const uint16_t *>(a.low);
+        p.out = static_cast<uint16_t *>(a.db);
+        p.parts = plan.parts;
+        e = launch_weight<Db64, false>(p, plan, stream);
     }
     return e;
 }

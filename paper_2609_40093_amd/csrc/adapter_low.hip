@@ -1,118 +1,226 @@
-// adapter_low.hip -- the low-rank values of the adapters' rows: low[i] = scale_a x[order[i]] a_a^T, rounded
-// to bf16 (the products that read them multiply bf16).  Rows without an adapter get zeros.  Its second
-// use is the gradient's v = scale_a dz b_a, from b transposed.
+// adapter_low.hip -- the low-rank values of the adapters' rows:
+//   low[i] = scale_a x[order[i]] a_a^T    in bf16, which the product multiplies (the forward);
+//   v[i]   = scale_a dz[order[i]] b_a     as the sum of two bf16 values (the gradient, see below).
+// Rows without an adapter get zeros.
 //
-// Bound by the rows' bytes, or for few rows by the adapters'.  A workgroup takes the rows of one
-// adapter, 16 or 32 at a time, and up to 64 ranks; its waves share out the contraction, 64 values
-// (whole cache lines) at a time, straight from memory into the operands of 16x16 matrix
-// instructions, and are added up through LDS in a fixed order.
+// Bound by the rows' bytes, or for few rows by the adapters'.  Many rows go through the MFMA tile
+// (product_tile.h), ranks by rows of one adapter, its LDS stages as deep as they fit, since what bounds it
+// are loads in flight.  Few rows go straight from memory into the operands of 16x16 matrix instructions:
+// the 16 waves of a workgroup share out the contraction, 64 values (whole cache lines) at a time with
+// every load of a wave on its way at once, and are added up through LDS in a fixed order.
+//
+// v is nobody's result, and what it loses goes into dx and da on top of what dz and they themselves lose
+// to bf16: da's error is 0.0029 of its 2-norm with v in one bf16 value, 0.0024 with the rest of that in a
+// second one, which costs the ranks' part of the contractions twice.
 #include "adapter_tile.h"
 
 namespace ep {
 namespace {
 
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+// Zeros for the rows without an adapter, before the first one's rows and behind the last one's: the
+// workgroups past the adapters' row tiles take `per` of them each.
+__device__ __forceinline__ void clear_rows(const LowArgs &a, int per, int threads, int lane) {
+    if (!a.offsets)
+        return;
+    const int64_t z = (int64_t)blockIdx.x - count_row_tiles(a.offsets, a.rows, a.A, per, lane);
+    const int64_t before = clamp_row(a.offsets[0], a.rows), behind = clamp_row(a.offsets[a.A], a.rows);
+    const int vecs = a.width / 8;
+    for (int i = threadIdx.x; i < per * vecs; i += threads) {
+        const int64_t p = z * per + i / vecs;
+        const int64_t row = p < before ? p : behind + (p - before);
+        if (z >= 0 && row < a.rows)
+            *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.low) + row * a.width + i % vecs * 8) = u32x4{0, 0, 0, 0};
+    }
+}
 
-// FQ fragments of 16 ranks, FR of 16 rows.
-template <int FQ, int FR, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void adapter_low_kernel(LowArgs a) {
-    constexpr int kRows = FR * 16, kRanks = FQ * 16;
-    __shared__ f32x4 sums[WAVES][FQ * FR][64];
+// ---- few rows ------------------------------------------------------------------------
+constexpr int kFewWaves = 16, kFewRows = 16, kFewRanks = 16;
+
+__global__ __launch_bounds__(kFewWaves * 64) void adapter_low_few_kernel(LowArgs a) {
+    __shared__ f32x4 sums[kFewWaves][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int rank0 = (int)blockIdx.y * kRanks;
-    const RowTile rt = find_row_tile(a.offsets, a.rows, a.A, kRows, (int32_t)blockIdx.x, lane);
-    uint16_t *low = static_cast<uint16_t *>(a.low);
-    if (rt.e < 0) {  // rows without an adapter: before the first one's and behind the last one's
-        if (!a.offsets)
-            return;
-        const int64_t z = (int64_t)blockIdx.x - count_row_tiles(a.offsets, a.rows, a.A, kRows, lane);
-        const int64_t before = clamp_row(a.offsets[0], a.rows), behind = clamp_row(a.offsets[a.A], a.rows);
-        const int width = a.R - rank0 < kRanks ? a.R - rank0 : kRanks;
-        for (int i = threadIdx.x; i < kRows * (width / 8); i += WAVES * 64) {
-            const int64_t p = z * kRows + i / (width / 8);
-            const int64_t row = p < before ? p : behind + (p - before);
-            if (z >= 0 && row < a.rows)
-                *reinterpret_cast<u32x4 *>(low + row * a.R + rank0 + i % (width / 8) * 8) = u32x4{0, 0, 0, 0};
-        }
+    const int rank0 = (int)blockIdx.y * kFewRanks;
+    const RowTile rt = find_row_tile(a.offsets, a.rows, a.A, kFewRows, (int32_t)blockIdx.x, lane);
+    if (rt.e < 0) {
+        if (blockIdx.y == 0)
+            clear_rows(a, kFewRows, kFewWaves * 64, lane);
         return;
     }
     const int g = lane / 16;  // which 16 bytes of a fragment's 64 this lane takes
-    const uint16_t *xr[FR], *ar[FQ];
-    bool has_x[FR], has_a[FQ];
-#pragma unroll
-    for (int f = 0; f < FR; ++f) {
-        const int row = f * 16 + lane % 16;
-        const int32_t r = row < rt.n ? row_at(a.order, a.rows, rt.row0 + row) : -1;
-        has_x[f] = r >= 0;
-        xr[f] = static_cast<const uint16_t *>(a.x) + (has_x[f] ? (int64_t)r * a.K : 0);
-    }
-#pragma unroll
-    for (int f = 0; f < FQ; ++f) {
-        const int rank = rank0 + f * 16 + lane % 16;
-        has_a[f] = rank < a.R;
-        ar[f] = static_cast<const uint16_t *>(a.weights) + ((int64_t)rt.e * a.R + (has_a[f] ? rank : 0)) * a.K;
-    }
-    f32x4 acc[FQ][FR] = {};
-    constexpr int kAhead = 2;
-    for (int32_t k0 = wave * 64; k0 < a.K; k0 += WAVES * 64 * kAhead) {
-        u32x4 xv[kAhead][2][FR], av[kAhead][2][FQ];
+    const int rank = rank0 + lane % 16;
+    const bool has_a = rank < a.R;
+    const uint16_t *ar = static_cast<const uint16_t *>(a.weights) + ((int64_t)rt.e * a.R + (has_a ? rank : 0)) * a.K;
+    const int32_t r = lane % 16 < rt.n ? row_at(a.order, a.rows, rt.row0 + lane % 16) : -1;
+    const uint16_t *xr = static_cast<const uint16_t *>(a.x) + (r >= 0 ? (int64_t)r * a.K : 0);
+    f32x4 acc = {};
+    constexpr int kAhead = 4;
+    for (int32_t k0 = wave * 64; k0 < a.K; k0 += kFewWaves * 64 * kAhead) {
+        u32x4 xv[kAhead][2], av[kAhead][2];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int32_t k = k0 + u * WAVES * 64 + h * 32 + g * 8;
-                const bool in = k < a.K;
+                const int32_t k = k0 + u * kFewWaves * 64 + h * 32 + g * 8;
+                av[u][h] = u32x4{0, 0, 0, 0};
+                if (k < a.K && has_a)
+                    av[u][h] = *reinterpret_cast<const u32x4 *>(ar + k);
+            }
 #pragma unroll
-                for (int f = 0; f < FR; ++f) {
-                    xv[u][h][f] = u32x4{0, 0, 0, 0};
-                    if (in && has_x[f])
-                        xv[u][h][f] = *reinterpret_cast<const u32x4 *>(xr[f] + k);
-                }
+        for (int u = 0; u < kAhead; ++u)
 #pragma unroll
-                for (int f = 0; f < FQ; ++f) {
-                    av[u][h][f] = u32x4{0, 0, 0, 0};
-                    if (in && has_a[f])
-                        av[u][h][f] = *reinterpret_cast<const u32x4 *>(ar[f] + k);
-                }
+            for (int h = 0; h < 2; ++h) {
+                const int32_t k = k0 + u * kFewWaves * 64 + h * 32 + g * 8;
+                xv[u][h] = u32x4{0, 0, 0, 0};
+                if (k < a.K && r >= 0)
+                    xv[u][h] = *reinterpret_cast<const u32x4 *>(xr + k);
             }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int q = 0; q < FQ; ++q)
-#pragma unroll
-                    for (int f = 0; f < FR; ++f)
-                        acc[q][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, av[u][h][q]),
-                                                                            __builtin_bit_cast(bf16x8, xv[u][h][f]),
-                                                                            acc[q][f], 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, av[u][h]),
+                                                              __builtin_bit_cast(bf16x8, xv[u][h]), acc, 0, 0, 0);
     }
-#pragma unroll
-    for (int q = 0; q < FQ; ++q)
-#pragma unroll
-        for (int f = 0; f < FR; ++f)
-            sums[wave][q * FR + f][lane] = acc[q][f];
+    sums[wave][lane] = acc;
     __syncthreads();
+    if (threadIdx.x >= 64)
+        return;
     const float scale = a.scale ? a.scale[rt.e] : 1.f;
-    for (int i = threadIdx.x; i < FQ * FR * 64; i += WAVES * 64) {
-        const int at = i / 64, l = i % 64;  // a lane holds four ranks of one row
-        f32x4 s = sums[0][at][l];
+    f32x4 s = sums[0][lane];
 #pragma unroll
-        for (int v = 1; v < WAVES; ++v)
-            s += sums[v][at][l];
-        const int rank = rank0 + at / FR * 16 + l / 16 * 4, row = at % FR * 16 + l % 16;
-        if (row < rt.n && rank < a.R)
-            *reinterpret_cast<uint64_t *>(low + (rt.row0 + row) * a.R + rank) =
-                bf16_pair(s[0] * scale, s[1] * scale) | (uint64_t)bf16_pair(s[2] * scale, s[3] * scale) << 32;
-    }
+    for (int v = 1; v < kFewWaves; ++v)
+        s += sums[v][lane];
+    const int q = rank0 + lane / 16 * 4, row = lane % 16;  // a lane holds four ranks of one row
+    if (row < rt.n && q < a.R)
+        *reinterpret_cast<uint64_t *>(static_cast<uint16_t *>(a.low) + (rt.row0 + row) * a.width + q) =
+            bf16_pair(s[0] * scale, s[1] * scale) | (uint64_t)bf16_pair(s[2] * scale, s[3] * scale) << 32;
 }
 
-template <int FQ, int FR, int WAVES>
+// ---- many rows -----------------------------------------------------------------------
+// An operand of which a group has `own` steps; the ones behind bring zeros.  (They lie past the
+// contraction's end, where the operand's own range check does not hold.)
+template <class Op>
+struct Part : Op {
+    int32_t own;
+    __device__ __forceinline__ void part(int32_t first, int32_t steps) {
+        Op::skip(first);
+        own = steps;
+    }
+    __device__ __forceinline__ void begin(bool live) {
+        Op::begin(live && own > 0);
+        --own;
+    }
+};
+
+// A workgroup's GROUPS groups of waves take every GROUPS-th part of the contraction each, with LDS stages of
+// their own, and are added up in order.  (A step of so small a tile takes 0.5 us whatever it holds,
+// which is how long its loads, its two barriers and its LDS reads take one after the other: 8192 rows of
+// 4096, 16 ranks, with one group per workgroup 36 us, 61 where the rows come from HBM.)
+// ACROSS: the weights are [A][K][R] and v is written, else [A][R][K] and low.
+template <class S, int GROUPS, bool ACROSS>
+__global__ __launch_bounds__(S::kThreads * GROUPS) void adapter_low_kernel(LowArgs a) {
+    constexpr int kGroupBytes = S::kStages * S::kStageBytes;
+    __shared__ __attribute__((aligned(1024))) char lds[GROUPS * kGroupBytes];
+    __shared__ int32_t row_of[S::kJ];
+    const int lane = threadIdx.x & 63, all_waves = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int group = all_waves / S::kWaves, wave = all_waves % S::kWaves;
+    const int rank0 = (int)blockIdx.y * S::kI;
+    const RowTile rt = find_row_tile(a.offsets, a.rows, a.A, S::kJ, (int32_t)blockIdx.x, lane);
+    if (rt.e < 0) {
+        if (blockIdx.y == 0)
+            clear_rows(a, S::kJ, S::kThreads * GROUPS, lane);
+        return;
+    }
+    for (int j = threadIdx.x; j < S::kJ; j += S::kThreads * GROUPS)
+        row_of[j] = j < rt.n ? row_at(a.order, a.rows, rt.row0 + j) : -1;
+    __syncthreads();
+    const int64_t kb = (int64_t)a.K * 2;
+    const char *weights = static_cast<const char *>(a.weights) + (int64_t)rt.e * a.R * kb;
+    const char *xb = static_cast<const char *>(a.x);
+    char EP_LDS *own = (char EP_LDS *)lds + group * kGroupBytes;
+    Part<AlongC<S::kJ, S::kWaves>> x;
+    // through an order from x's first row on (x is smaller than 2^31 bytes then)
+    x.init(a.order ? xb : xb + rt.row0 * kb, (uint32_t)((a.order ? a.rows : rt.n) * kb), (int32_t)kb, wave, lane,
+           [&](int row) -> uint32_t {
+               const int32_t r = a.order ? row_of[row] : row;
+               return r < 0 ? kNowhere : (uint32_t)(r * kb);
+           });
+    f32x16 acc[S::FI][S::FJ] = {};
+    // every group the same number of steps, for the barriers
+    const int32_t all = (a.K + kStepRows - 1) / kStepRows, steps = (all + GROUPS - 1) / GROUPS;
+    const int32_t first = group * steps < all ? group * steps : all, mine = all - first < steps ? all - first : steps;
+    x.part(first, mine);
+    if constexpr (ACROSS) {
+        Part<AcrossC<S::kI, S::kWaves, S::FI>> w;
+        w.init(weights, (int64_t)a.R * 2, a.K, rank0, wave, lane);
+        w.part(first, mine);
+        tile_product<S, Mul::kBf16>(w, x, steps, own, wave, lane, acc);
+    } else {
+        Part<AlongC<S::kI, S::kWaves>> w;
+        w.init(weights, (uint32_t)(a.R * kb), (int32_t)kb, wave, lane,
+               [&](int row) -> uint32_t { return rank0 + row < a.R ? (uint32_t)((rank0 + row) * kb) : kNowhere; });
+        w.part(first, mine);
+        tile_product<S, Mul::kBf16>(w, x, steps, own, wave, lane, acc);
+    }
+    if constexpr (GROUPS > 1) {
+        static_assert(S::kWaves * S::FI * S::FJ * 4096 <= kGroupBytes, "a group's sums fit its stages");
+        f32x16 EP_LDS *sums = reinterpret_cast<f32x16 EP_LDS *>(own);
+        if (group > 0)
+#pragma unroll
+            for (int i = 0; i < S::FI; ++i)
+#pragma unroll
+                for (int j = 0; j < S::FJ; ++j)
+                    sums[((wave * S::FI + i) * S::FJ + j) * 64 + lane] = acc[i][j];
+        __syncthreads();
+        if (group > 0)
+            return;
+#pragma unroll
+        for (int g = 1; g < GROUPS; ++g)
+#pragma unroll
+            for (int i = 0; i < S::FI; ++i)
+#pragma unroll
+                for (int j = 0; j < S::FJ; ++j)
+                    acc[i][j] += sums[g * (kGroupBytes / 64) + ((wave * S::FI + i) * S::FJ + j) * 64 + lane];
+    }
+    const float scale = a.scale ? a.scale[rt.e] : 1.f;
+    tile_results<S>(acc, own, wave, lane, [&](int row, int col, const float *v) {
+        const int rank = rank0 + col;
+        if (row >= rt.n || rank >= a.R)
+            return;
+        float o[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            o[q] = v[q] * scale;
+        const u32x4 high = pack8(o);
+        uint16_t *dst = static_cast<uint16_t *>(a.low) + (rt.row0 + row) * a.width;
+        if constexpr (!ACROSS) {
+            *reinterpret_cast<u32x4 *>(dst + rank) = high;
+        } else {
+            float h[8];
+            unpack8(high, h);
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                o[q] -= h[q];
+            const int at = rank + (rank >> a.log << a.log);
+            *reinterpret_cast<u32x4 *>(dst + at) = high;
+            *reinterpret_cast<u32x4 *>(dst + at + (1 << a.log)) = pack8(o);
+        }
+    });
+}
+
+// 32, 64 and 128 ranks.  With up to one tile per compute unit, one workgroup of as many groups as its LDS
+// holds (144, 128 and 144 KiB), else two of half as many.
+typedef TileShape<32, 64, 1, 2, 3> Low32;
+typedef TileShape<64, 64, 2, 2, 2> Low64;
+typedef TileShape<128, 64, 4, 2, 3> Low128;
+
+template <class S, int GROUPS, bool ACROSS>
 hipError_t launch_shape(const LowArgs &a, hipStream_t stream) {
-    // every row is one of an adapter or one of none: two tiles more than an adapter more would give
-    const int64_t tiles = row_tiles_most(a.rows, a.A + 2, FR * 16);
-    return launch_traced("adapter_low", adapter_low_kernel<FQ, FR, WAVES>,
-                         dim3((unsigned)tiles, (unsigned)((a.R + FQ * 16 - 1) / (FQ * 16))), WAVES * 64, stream, a);
+    // every row is one of an adapter or one of none, which make up to two more tiles than an adapter would
+    const dim3 grid((unsigned)row_tiles_most(a.rows, a.A + 2, S::kJ), (unsigned)((a.R + S::kI - 1) / S::kI));
+    if (row_tiles_likely(a.rows, a.A, S::kJ) * grid.y <= kCus)
+        return launch_traced("adapter_low", adapter_low_kernel<S, GROUPS, ACROSS>, grid, S::kThreads * GROUPS, stream, a);
+    return launch_traced("adapter_low", adapter_low_kernel<S, GROUPS / 2, ACROSS>, grid, S::kThreads * GROUPS / 2, stream, a);
 }
 
 }  // namespace
@@ -120,12 +228,17 @@ hipError_t launch_shape(const LowArgs &a, hipStream_t stream) {
 hipError_t launch_adapter_low(const LowArgs &a, hipStream_t stream) {
     if (a.rows == 0)
         return hipSuccess;
-    const bool few = a.rows / a.A < 24 || a.rows < 2048;
-    if (a.R <= 16)
-        return few ? launch_shape<1, 1, 16>(a, stream) : launch_shape<1, 2, 8>(a, stream);
-    if (a.R <= 32)
-        return few ? launch_shape<2, 1, 16>(a, stream) : launch_shape<2, 2, 8>(a, stream);
-    return few ? launch_shape<4, 1, 16>(a, stream) : launch_shape<4, 2, 8>(a, stream);
+    if (a.log)
+        return a.R <= 64 ? launch_shape<Low64, 4, true>(a, stream) : launch_shape<Low128, 2, true>(a, stream);
+    const bool far = a.order && a.rows * a.K * 2 > INT32_MAX;  // rows that a tile cannot address
+    if (far || a.rows / a.A < 24 || a.rows < 2048)
+        return launch_traced("adapter_low", adapter_low_few_kernel,
+                             dim3((unsigned)row_tiles_most(a.rows, a.A + 2, kFewRows),
+                                  (unsigned)((a.R + kFewRanks - 1) / kFewRanks)),
+                             kFewWaves * 64, stream, a);
+    return a.R <= 32   ? launch_shape<Low32, 4, false>(a, stream)
+           : a.R <= 64 ? launch_shape<Low64, 4, false>(a, stream)
+                       : launch_shape<Low128, 2, false>(a, stream);
 }
 
 }  // namespace ep

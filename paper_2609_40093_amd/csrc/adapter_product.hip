@@ -49,6 +49,16 @@ __device__ __forceinline__ void check8(const ProductArgs &a, const AdapterSide &
     }
 }
 
+// The weights' row of a tile's row, -1: none (gated: 8 gate rows beside their 8 up rows, as in the experts' product).
+template <bool GATED>
+struct WeightRow {
+    int32_t n0, N;
+    __device__ __forceinline__ int32_t operator()(int row) const {
+        const int32_t n = GATED ? n0 + (row >> 4) * 8 + (row & 7) : n0 + row;
+        return n < N ? n + (GATED && (row & 8) ? N : 0) : -1;
+    }
+};
+
 template <class S, bool GATED>
 __global__ __launch_bounds__(S::kThreads) void adapter_product_kernel(ProductArgs a, AdapterSide s, int32_t row_tiles,
                                                                       int32_t col_tiles, int32_t parts) {
@@ -81,18 +91,14 @@ __global__ __launch_bounds__(S::kThreads) void adapter_product_kernel(ProductArg
     constexpr int kOut = GATED ? S::kI / 2 : S::kI;  // output columns of a tile
     const int32_t n0 = tc * kOut;
     const int32_t main = a.w ? (int32_t)((kb + kStepBytes - 1) / kStepBytes) : 0;
-    // the weights' row of a tile's column, -1: none
-    const auto column = [&](int row) -> int32_t {
-        const int32_t n = GATED ? n0 + (row >> 4) * 8 + (row & 7) : n0 + row;
-        return n < a.N ? n + (GATED && (row & 8) ? a.N : 0) : -1;
-    };
-    ChainAlong<S::kI, S::kWaves, false> w;
-    ChainAlong<S::kJ, S::kWaves, true> x;
+    const WeightRow<GATED> column{n0, a.N};
+    ChainAlong<S::kI, S::kWaves, WeightRow<GATED>> w;
+    ChainAlong<S::kJ, S::kWaves, LowRows> x;
     w.init(static_cast<const char *>(a.w), (uint32_t)(a.Nw * kb), (int32_t)kb, wave, lane, [&](int row) -> uint32_t {
         const int32_t n = column(row);
         return n < 0 ? kNowhere : (uint32_t)(n * kb);
     });
-    w.chain(main, s, segments, count, s.weights, (uint64_t)s.A * a.Nw * s.R * 2, a.Nw, wave, lane, column);
+    w.chain(main, s, segments, count, s.weights, (uint64_t)s.A * a.Nw * s.R * 2, a.Nw, column);
     // through an order from x's first row on (x is smaller than 2^31 bytes then)
     const char *xb = static_cast<const char *>(a.x);
     x.init(s.order ? xb : xb + i0 * kb, (uint32_t)((s.order ? a.rows : n_rows) * kb), (int32_t)kb, wave, lane,
@@ -102,7 +108,7 @@ __global__ __launch_bounds__(S::kThreads) void adapter_product_kernel(ProductArg
                const int32_t r = row_of[row];
                return r < 0 ? kNowhere : (uint32_t)(r * kb);
            });
-    x.chain(main, s, segments, count, s.low + i0 * s.R, (uint64_t)n_rows * s.R * 2, 0, wave, lane, [](int row) { return row; });
+    x.chain(main, s, segments, count, s.low + i0 * s.R, (uint64_t)n_rows * s.R * 2, 0, LowRows{});
 
     int32_t steps = main + (count * (s.R / 8) + 7) / 8;
     if (parts > 1) {
@@ -240,6 +246,8 @@ hipError_t launch_shape(const ProductArgs &a, const AdapterSide &s, const Plan &
 size_t adapter_product_partial_bytes(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t N, bool base, int32_t act) {
     if (rows == 0)
         return 0;
+    if (adapter_few(rows))
+        return adapter_few_bytes(rows, R, K, N, base, act);
     const bool gated = act == EP_ACT_SWIGLU;
     const Plan p = adapter_plan(rows, A, R, K, N, base, gated);
     return p.split.parts == 1 ? 0 : (size_t)p.split.parts * rows * N * (gated ? 2 : 1) * sizeof(float);
@@ -248,6 +256,8 @@ size_t adapter_product_partial_bytes(int64_t rows, int32_t A, int32_t R, int32_t
 hipError_t launch_adapter_product(const AdapterArgs &a, hipStream_t stream) {
     if (a.rows == 0)
         return hipSuccess;
+    if (adapter_few(a.rows))
+        return launch_adapter_few(a, stream);
     const bool gated = a.act == EP_ACT_SWIGLU;
     ProductArgs p{};
     p.x = a.x;
@@ -264,11 +274,10 @@ hipError_t launch_adapter_product(const AdapterArgs &a, hipStream_t stream) {
     p.y = a.y;
     p.partial = a.partial;
     const hipError_t e = launch_adapter_low(
-        {a.x, a.rows, a.order, a.offsets, a.A, a.R, a.K, a.a, a.scale, a.low}, stream);
+        {a.x, a.rows, a.order, a.offsets, a.A, a.R, a.K, a.a, a.scale, a.low, a.R, 0}, stream);
     if (e != hipSuccess)
         return e;
-    const AdapterSide s{a.order, a.offsets, a.A, a.R, static_cast<const uint16_t *>(a.low), static_cast<const uint16_t *>(a.b),
-                        fast_div((uint32_t)a.R), fast_div((uint32_t)(a.R / 8))};
+    const AdapterSide s = adapter_side(a.order, a.offsets, a.A, a.R, a.low, a.R, 0, a.b);
     const Plan plan = adapter_plan(a.rows, a.A, a.R, a.K, a.N, a.w != nullptr, gated);
     switch (plan.size) {
     case Size::kLarge: return launch_shape<Large>(p, s, plan, stream);

@@ -3,7 +3,8 @@
 //
 // Rows are taken in the adapters' order (row i of the order is row order[i] of x and y), so the rows
 // that an adapter has in a tile are a segment of it.  The second part is as long as the segments'
-// ranks together: its places are (segment, rank), rank fastest.  The row operand holds zeros at the
+// ranks together: its places are (segment, rank), rank fastest; where low is kept as two values each, a segment has the
+// ranks twice.  The row operand holds zeros at the
 // places of the segments that a row is not in, and the column operand the weights of the place's
 // adapter, so one accumulator adds up both parts; 64 places are one step whoever's they are: four
 // adapters of rank 16 cost what one of rank 64 costs.  (A step per adapter would take 64 steps
@@ -23,10 +24,33 @@ struct AdapterSide {
     const int32_t *order;    // null: the rows come in the adapters' order
     const int32_t *offsets;  // null: one adapter with every row
     int32_t A, R;
-    const uint16_t *low;     // [rows][R], in the adapters' order
+    const uint16_t *low;     // [rows][width], in the adapters' order
     const uint16_t *weights; // b [A][Nw][R] of the product, a [A][R][K] of its gradient
-    FastDiv places, chunks;  // by R and R / 8
+    int32_t width, log;      // log2 of LowArgs's block, 0: none; with one a segment has 2 R places
+    FastDiv places, chunks;  // by a segment's places, and by an eighth of them
+
+    // Where the eight values at chunk `in` of a segment lie in a row of low.
+    __device__ __forceinline__ int32_t chunk_at(int32_t in) const {
+        int32_t j = in * 8;
+        if (!log)
+            return j;
+        const int32_t second = j >= R ? 1 : 0;
+        j -= second ? R : 0;
+        return j + (((j >> log) + second) << log);
+    }
 };
+inline AdapterSide adapter_side(const int32_t *order, const int32_t *offsets, int32_t A, int32_t R, const void *low,
+                                int32_t width, int32_t log, const void *weights) {
+    const uint32_t places = (uint32_t)R * (log ? 2 : 1);
+    return {order, offsets, A, R, static_cast<const uint16_t *>(low), static_cast<const uint16_t *>(weights), width, log,
+            fast_div(places), fast_div(places / 8)};
+}
+// The layout of v: blocks of 32 ranks (up to 32 ranks) or 64, the first values of a block, then the second.
+inline int32_t split_log(int32_t R) { return R <= 32 ? 5 : 6; }
+inline int32_t split_width(int32_t R) {
+    const int32_t block = 1 << split_log(R);
+    return (R + block - 1) / block * block * 2;
+}
 
 // The segments of rows i0 .. i0 + n - 1, in the adapters' order; at most PER (more only where offsets
 // decrease).  One wave calls it.
@@ -56,38 +80,37 @@ __device__ __forceinline__ int32_t row_at(const int32_t *order, int64_t rows, in
     return r >= 0 && r < rows ? r : -1;
 }
 
-// Rows along the contraction (AlongC), then the second part: LOW: the rows' low-rank values, else the
-// weights b of each column.
-template <int T, int W, bool LOW>
+// Rows along the contraction (AlongC), then the second part: the rows' low-rank values (Index: LowRows), else
+// the weights b of each column, whose row Index gives for a tile's row (-1: none).  The second
+// part's offsets take the place of the first one's, which are not needed any more.
+struct LowRows {};
+template <int T, int W, typename Index>
 struct ChainAlong : AlongC<T, W> {
     typedef AlongC<T, W> First;
     using First::kLoads;
+    static constexpr bool kChained = true;
+    static constexpr bool LOW = std::is_same<Index, LowRows>::value;
     int32_t first;        // steps of the first part left
     int32_t chunk, most;  // 16-byte chunks of the second part: the next step's first, and all
     const Segment EP_LDS *segments;
-    FastDiv per;          // chunks of a segment
+    const AdapterSide *side;
     const char *base2;
     uint32_t size2;
-    uint32_t row_bytes;   // of a row of the second part
-    uint32_t adapter_bytes;
-    uint32_t now[kLoads];
-    int32_t index[kLoads];  // LOW: the tile's row; else the weights' row, -1: none
+    uint32_t adapter_rows;  // of the weights
+    Index index;
 
-    template <typename F>
-    __device__ __forceinline__ void chain(int32_t steps, const AdapterSide &s, const Segment EP_LDS *at, int count, const void *base,
-                                          uint64_t size, int64_t adapter_rows, int wave, int lane, F index_of) {
+    // steps: of the first part.  base, size: of the second one's array.
+    __device__ __forceinline__ void chain(int32_t steps, const AdapterSide &s, const Segment EP_LDS *at, int count,
+                                          const void *base, uint64_t size, int64_t rows, Index index_of) {
         first = steps;
         chunk = 0;
-        most = count * (s.R / 8);
+        most = count * (int32_t)s.chunks.d;
         segments = at;
-        per = s.chunks;
+        side = &s;
         base2 = static_cast<const char *>(base);
         size2 = (uint32_t)size;
-        row_bytes = (uint32_t)s.R * 2;
-        adapter_bytes = (uint32_t)(adapter_rows * row_bytes);
-#pragma unroll
-        for (int q = 0; q < kLoads; ++q)
-            index[q] = index_of(First::load_number(wave, q) * 8 + lane / 8);
+        adapter_rows = (uint32_t)rows;
+        index = index_of;
     }
     __device__ __forceinline__ void skip(int32_t steps) {
         const int32_t n = steps < first ? steps : first;
@@ -97,32 +120,32 @@ struct ChainAlong : AlongC<T, W> {
         chunk += (steps - n) * 8;
     }
     __device__ __forceinline__ void begin(bool live) {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         if (first > 0) {
             First::begin(live);
-#pragma unroll
-            for (int q = 0; q < kLoads; ++q) {
-                const int row = First::load_number(wave, q) * 8 + lane / 8;
-                now[q] = First::swizzle(row, lane % 8) * 16 < First::bytes ? First::offset[q] : kNowhere;
-            }
             return;
         }
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         First::range = buffer_of(base2, live ? size2 : 0);
+        First::bytes = kStepBytes;  // every chunk of the step is looked up
 #pragma unroll
         for (int q = 0; q < kLoads; ++q) {
             const int row = First::load_number(wave, q) * 8 + lane / 8;
             const int32_t c = chunk + First::swizzle(row, lane % 8);
-            now[q] = kNowhere;
+            uint32_t o = kNowhere;
             if (live && c < most) {
-                const uint32_t at = per.div((uint32_t)c), in = (uint32_t)c - at * per.d;
+                const uint32_t at = side->chunks.div((uint32_t)c), in = (uint32_t)c - at * side->chunks.d;
                 const Segment s = segments[at];
-                if (LOW ? index[q] >= (s[1] & 0xffff) && index[q] < s[1] >> 16 : index[q] >= 0)
-                    now[q] = (LOW ? 0u : (uint32_t)s[0] * adapter_bytes) + (uint32_t)index[q] * row_bytes + in * 16;
+                if constexpr (LOW) {
+                    if (row >= (s[1] & 0xffff) && row < s[1] >> 16)
+                        o = (uint32_t)(row * side->width + side->chunk_at((int32_t)in)) * 2;
+                } else {
+                    const int32_t n = index(row);
+                    if (n >= 0)
+                        o = (((uint32_t)s[0] * adapter_rows + (uint32_t)n) * (uint32_t)side->R + in * 8) * 2;
+                }
             }
+            First::offset[q] = o;
         }
-    }
-    __device__ __forceinline__ void load(int q, char EP_LDS *lds, int wave, int) {
-        load_to_lds(First::range, now[q], lds + First::load_number(wave, q) * 1024);
     }
     __device__ __forceinline__ void end() {
         if (first > 0) {
@@ -139,47 +162,43 @@ template <int T, int W, int FRAGMENTS>
 struct ChainAcross : AcrossC<T, W, FRAGMENTS> {
     typedef AcrossC<T, W, FRAGMENTS> First;
     using First::kLoads;
+    static constexpr bool kChained = true;
     int32_t first;        // steps of the first part left
     int32_t place, most;  // places of the second part: the next step's first, and all
     const Segment EP_LDS *segments;
-    FastDiv per;          // places of a segment
-    const char *base2;
-    uint32_t size2;
-    uint32_t now[kLoads];
+    const AdapterSide *side;
+    uint32_t size2, column;  // column: the tile's first
 
-    __device__ __forceinline__ void chain(int32_t steps, const AdapterSide &s, const Segment EP_LDS *at, int count, uint64_t size) {
+    __device__ __forceinline__ void chain(int32_t steps, const AdapterSide &s, const Segment EP_LDS *at, int count, uint64_t size,
+                                          int32_t index0) {
         first = steps;
         place = 0;
-        most = count * s.R;
+        most = count * (int32_t)s.places.d;
         segments = at;
-        per = s.places;
-        base2 = reinterpret_cast<const char *>(s.weights);
+        side = &s;
         size2 = (uint32_t)size;
+        column = (uint32_t)index0;
     }
     __device__ __forceinline__ void begin(bool live) {
         if (first > 0) {
             First::begin(live);
-#pragma unroll
-            for (int q = 0; q < kLoads; ++q)
-                now[q] = First::offset[q];
             return;
         }
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        First::range = buffer_of(base2, live ? size2 : 0);
-        const uint32_t row_bytes = (uint32_t)First::stride;
+        First::range = buffer_of(reinterpret_cast<const char *>(side->weights), live ? size2 : 0);
 #pragma unroll
         for (int q = 0; q < kLoads; ++q) {
-            const int row = (First::load_number(wave, q) * 1024 + lane * 16) / (2 * T);
+            const int row = First::row_of(q, wave, lane);
             const int32_t p = place + row;
-            now[q] = kNowhere;
+            uint32_t o = kNowhere;
             if (live && p < most) {
-                const uint32_t at = per.div((uint32_t)p), in = (uint32_t)p - at * per.d;
-                now[q] = ((uint32_t)segments[at][0] * per.d + in) * row_bytes + (First::offset[q] - (uint32_t)row * row_bytes);
+                const uint32_t at = side->places.div((uint32_t)p), ranks = (uint32_t)side->R;
+                uint32_t in = (uint32_t)p - at * side->places.d;
+                in -= in >= ranks ? ranks : 0;
+                o = ((uint32_t)segments[at][0] * ranks + in) * (uint32_t)First::stride + First::column_of(q, column, wave, lane);
             }
+            First::offset[q] = o;
         }
-    }
-    __device__ __forceinline__ void load(int q, char EP_LDS *lds, int wave, int) {
-        load_to_lds(First::range, now[q], lds + First::load_number(wave, q) * 1024);
     }
     __device__ __forceinline__ void end() {
         if (first > 0) {

@@ -227,15 +227,16 @@ hipError_t launch_product_grad(const ProductGradArgs &a, hipStream_t stream);
 hipError_t launch_adapter_rows(const int32_t *row_adapter, int64_t rows, int32_t A, int32_t *order, int32_t *offsets,
                                hipStream_t stream);
 
-// low[i] = scale[e] x[order[i]] weights[e]^T for place i of adapter e.
+// The adapters' low-rank values (adapter_low.hip).
 struct LowArgs {
-    const void *x;  // bf16 [rows][K]
+    const void *x;  // bf16 [rows][K]; with an order and a log smaller than 2^31 bytes
     int64_t rows;
     const int32_t *order, *offsets;  // null: rows in the adapters' order; one adapter
     int32_t A, R, K;
-    const void *weights;  // bf16 [A][R][K]
+    const void *weights;  // bf16 [A][R][K]; with a log [A][K][R]
     const float *scale;   // fp32 [A], null: ones
-    void *low;            // bf16 [rows][R], in the adapters' order
+    void *low;            // bf16 [rows][width], in the adapters' order
+    int32_t width, log;   // log 0: R values.  Else each as two, 2^log of the first and then of the second
 };
 hipError_t launch_adapter_low(const LowArgs &a, hipStream_t stream);
 
@@ -253,6 +254,10 @@ struct AdapterArgs {
     void *pre, *low, *y;
     float *partial;  // workspace of adapter_product_partial_bytes
 };
+// The low-rank values are the workspace's business (low may be null) where adapter_few, else the caller's.
+bool adapter_few(int64_t rows);
+size_t adapter_few_bytes(int64_t rows, int32_t R, int32_t K, int32_t N, bool base, int32_t act);
+hipError_t launch_adapter_few(const AdapterArgs &a, hipStream_t stream);
 size_t adapter_product_partial_bytes(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t N, bool base, int32_t act);
 hipError_t launch_adapter_product(const AdapterArgs &a, hipStream_t stream);
 

@@ -23,6 +23,8 @@
 
 #include "ep_layer.h"
 
+#include <type_traits>
+
 namespace ep {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -62,6 +64,7 @@ constexpr int loads_per_wave() {
 template <int T, int W>
 struct AlongC {
     static constexpr int kLoads = loads_per_wave<T, W>();
+    static constexpr bool kChained = false;
     const char *base;
     uint32_t left;    // bytes from base to the end of the operand
     int32_t bytes;    // bytes of the contraction left
@@ -120,6 +123,7 @@ struct AlongC {
 template <int T, int W, int FRAGMENTS>
 struct AcrossC {
     static constexpr int kLoads = loads_per_wave<T, W>();
+    static constexpr bool kChained = false;
     static constexpr int kChunks = T / 16;  // 32-byte chunks of a row
     const char *base;
     int64_t stride;  // bytes of a row
@@ -139,11 +143,17 @@ struct AcrossC {
         stride = row_bytes;
         rows = n;
 #pragma unroll
-        for (int q = 0; q < kLoads; ++q) {
-            const int p = load_number(wave, q) * 1024 + lane * 16;
-            const int row = p / (2 * T), chunk = p % (2 * T) / 32, half = p / 16 % 2;
-            offset[q] = (uint32_t)(row * stride + index0 * 2 + (chunk ^ key(row)) * 32 + half * 16);
-        }
+        for (int q = 0; q < kLoads; ++q)
+            offset[q] = (uint32_t)(row_of(q, wave, lane) * stride) + column_of(q, (uint32_t)index0, wave, lane);
+    }
+    // Load q of a step: the row of the step that this lane brings, and its byte within the row.
+    __device__ __forceinline__ static int row_of(int q, int wave, int lane) {
+        return (load_number(wave, q) * 1024 + lane * 16) / (2 * T);
+    }
+    __device__ __forceinline__ static uint32_t column_of(int q, uint32_t index0, int wave, int lane) {
+        const int p = load_number(wave, q) * 1024 + lane * 16;
+        const int row = p / (2 * T), chunk = p % (2 * T) / 32, half = p / 16 % 2;
+        return index0 * 2 + (uint32_t)((chunk ^ key(row)) * 32 + half * 16);
     }
     __device__ __forceinline__ void skip(int32_t steps) {
         base += (int64_t)steps * kStepRows * stride;
@@ -277,6 +287,26 @@ __device__ __forceinline__ void wait_and_meet() {
 }
 constexpr int kAnyLoads = 63;  // no wait for loads
 
+// An operand may be chained (kChained: adapter_tile.h): its contraction goes on into a second part of
+// another form behind the `first` steps left of the plain one, and both operands of a tile are.
+// The steps that load the plain part have a loop of their own, without the second one's registers.
+template <bool PLAIN, class Op>
+__device__ __forceinline__ void begin_loads(Op &o, bool live) {
+    if constexpr (PLAIN && Op::kChained)
+        o.First::begin(live);
+    else
+        o.begin(live);
+}
+template <bool PLAIN, class Op>
+__device__ __forceinline__ void end_loads(Op &o) {
+    if constexpr (PLAIN && Op::kChained) {
+        o.First::end();
+        --o.first;
+    } else {
+        o.end();
+    }
+}
+
 // Runs `steps` steps of the contraction into acc.  Step t's place in LDS is t % STAGES.
 //
 // A wave enters step t with its first half in registers.  Between the matrix instructions of
@@ -321,12 +351,14 @@ __device__ __forceinline__ void tile_product(OpA &a, OpB &b, int32_t steps, char
     for (int r = 0; r < kReads; ++r)
         read_fragment<S>(first, r, a, b, lds, 0);
     int place = 0;
-    for (int32_t t = 0; t < steps; ++t) {
+    // Step t; PLAIN: the loads it issues are of operands in their plain form.
+    const auto step = [&](int32_t t, auto plain) {
+        constexpr bool PLAIN = decltype(plain)::value;
         char EP_LDS *here = lds + place * S::kStageBytes;
         place = place + 1 == S::kStages ? 0 : place + 1;
         const char EP_LDS *next = lds + place * S::kStageBytes;
-        a.begin(t + S::kStages < steps);
-        b.begin(t + S::kStages < steps);
+        begin_loads<PLAIN>(a, t + S::kStages < steps);
+        begin_loads<PLAIN>(b, t + S::kStages < steps);
         const auto behind = [&](int m) {
 #pragma unroll
             for (int r = 0; r < kReads; ++r)
@@ -347,9 +379,15 @@ __device__ __forceinline__ void tile_product(OpA &a, OpB &b, int32_t steps, char
         };
         multiply<S, M>(first, acc, behind);
         multiply<S, M>(second, acc, [&](int m) { behind(kMuls + m); });
-        a.end();
-        b.end();
-    }
+        end_loads<PLAIN>(a);
+        end_loads<PLAIN>(b);
+    };
+    int32_t t = 0;
+    if constexpr (OpA::kChained)  // as long as both operands' loads are of their first part
+        for (; t < steps && a.first > 0; ++t)
+            step(t, std::true_type{});
+    for (; t < steps; ++t)
+        step(t, std::integral_constant<bool, !OpA::kChained>{});
     // every load has landed and every read is done before the kernel uses the LDS again
     wait_and_meet<0, true>();
 }

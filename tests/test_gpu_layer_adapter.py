@@ -271,3 +271,13 @@ def test_binding_refusals():
             ep.adapter_rows(s["ids"], A)
     with pytest.raises(ValueError):
         ep.adapter_rows(s["ids"], 3, out=ep.AdapterRows(None, rows.offsets))
+
+
+@pytest.mark.parametrize("R", [16, 40, 72])
+@pytest.mark.parametrize("K", [8, 72, 200, 264, 328])
+def test_short_contractions_of_single_rows(K, R):
+    """Tiles of one row, whose contraction has fewer steps than a workgroup has groups of waves for them."""
+    say(f"adapter_product tiles of one row K={K} R={R}")
+    s = ar.make(ar.packed_ids([65] * 40, 1), 40, R, K, 136, K)
+    ar.check(s, packed=True)
+    ar.check_grad(ar.make(ar.packed_ids([65] * 40, 1), 40, R, 136, K, K), packed=True)
