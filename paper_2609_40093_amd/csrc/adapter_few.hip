@@ -19,6 +19,7 @@ namespace {
 
 constexpr int kRows = 16, kRanks = 16, kAhead = 6;  // kAhead: 64-value pieces of the contraction of a wave
 constexpr int kPiece = 64, kPartPieces = 4 * kAhead;
+constexpr int kPartsAhead = 8;  // parts of a sum on their way at once
 
 // What the two kernels share.
 struct FewArgs {
@@ -80,6 +81,12 @@ __device__ __forceinline__ void low_part(const FewArgs &f, int32_t block, f32x4 
     const int q = rank0 + g * 4, row = lane % 16;  // a lane holds four ranks of one row
     if (row < rt.n && q < f.R)
         *reinterpret_cast<f32x4 *>(f.low_parts + ((int64_t)part * f.p.rows + rt.row0 + row) * f.R + q) = s;
+}
+
+// The low-rank parts alone, with next to no LDS: all workgroups at once.
+__global__ __launch_bounds__(256) void adapter_few_low_kernel(FewArgs f) {
+    __shared__ f32x4 sums[256];
+    low_part(f, (int32_t)blockIdx.x, (f32x4 EP_LDS *)sums, threadIdx.x & 63, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
 }
 
 template <class S, bool GATED>
@@ -165,9 +172,23 @@ __global__ __launch_bounds__(64) void adapter_few_join_kernel(FewArgs f) {
     for (int u = 0; u < 2; ++u) {
         n[u] = n0 + g * 4 + (GATED ? 0 : u * 16);
         mine[u] = r >= 0 && n[u] < a.N;
-        if (mine[u])
-            for (int32_t p = 0; p < f.parts; ++p)
-                acc[u] += *reinterpret_cast<const f32x4 *>(a.partial + ((int64_t)p * a.rows + r) * a.Nw + n[u] + (GATED && u ? a.N : 0));
+    }
+    const float *sums = a.partial + (int64_t)(r < 0 ? 0 : r) * a.Nw;
+    for (int32_t p0 = 0; p0 < f.parts; p0 += kPartsAhead) {
+        f32x4 v[kPartsAhead][2];
+#pragma unroll
+        for (int p = 0; p < kPartsAhead; ++p)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                v[p][u] = f32x4{};
+                if (mine[u] && p0 + p < f.parts)
+                    v[p][u] = *reinterpret_cast<const f32x4 *>(sums + (p0 + p) * a.rows * a.Nw + n[u] + (GATED && u ? a.N : 0));
+            }
+#pragma unroll
+        for (int p = 0; p < kPartsAhead; ++p)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                acc[u] += v[p][u];
     }
     // this row's adapter, and its low-rank values
     int32_t e = -1;
@@ -182,42 +203,63 @@ __global__ __launch_bounds__(64) void adapter_few_join_kernel(FewArgs f) {
     for (int q = 0; q < STEPS; ++q) {
         const int32_t rank = q * 32 + g * 8;
         f32x4 v[2] = {};
-        if (e >= 0 && rank < f.R)
-            for (int32_t p = 0; p < f.low_count; ++p) {
-                const f32x4 *src = reinterpret_cast<const f32x4 *>(f.low_parts + ((int64_t)p * a.rows + i0 + j) * f.R + rank);
-                v[0] += src[0];
-                v[1] += src[1];
+        for (int32_t p0 = 0; p0 < f.low_count; p0 += kPartsAhead) {
+            f32x4 t[kPartsAhead][2];
+#pragma unroll
+            for (int p = 0; p < kPartsAhead; ++p) {
+                t[p][0] = t[p][1] = f32x4{};
+                if (e >= 0 && rank < f.R && p0 + p < f.low_count) {
+                    const f32x4 *src =
+                        reinterpret_cast<const f32x4 *>(f.low_parts + ((int64_t)(p0 + p) * a.rows + i0 + j) * f.R + rank);
+                    t[p][0] = src[0];
+                    t[p][1] = src[1];
+                }
             }
+#pragma unroll
+            for (int p = 0; p < kPartsAhead; ++p) {
+                v[0] += t[p][0];
+                v[1] += t[p][1];
+            }
+        }
         const u32x4 b = {bf16_pair(v[0][0] * scale, v[0][1] * scale), bf16_pair(v[0][2] * scale, v[0][3] * scale),
                          bf16_pair(v[1][0] * scale, v[1][1] * scale), bf16_pair(v[1][2] * scale, v[1][3] * scale)};
         low[q] = __builtin_bit_cast(bf16x8, b);
         if (f.low && blockIdx.x == 0 && j < n_rows && rank < f.R)
             *reinterpret_cast<u32x4 *>(f.low + (i0 + j) * f.R + rank) = b;
     }
-    for (int s = 0; s < count; ++s) {
-        const Segment t = segments[s];
-        const bool has = j >= (t[1] & 0xffff) && j < t[1] >> 16;
-        const uint16_t *b = f.b + (int64_t)t[0] * a.Nw * f.R;
-        u32x4 w[2][STEPS];
+    constexpr int kSegments = STEPS == 1 ? 8 : STEPS == 2 ? 4 : STEPS == 4 ? 2 : 1;  // whose weights are on their way at once
+    for (int s0 = 0; s0 < count; s0 += kSegments) {
+        u32x4 w[kSegments][2][STEPS];
+        bool has[kSegments];
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int s = 0; s < kSegments; ++s) {
+            const bool some = s0 + s < count;
+            const Segment t = segments[some ? s0 + s : s0];
+            has[s] = some && j >= (t[1] & 0xffff) && j < t[1] >> 16;
+            const uint16_t *b = f.b + (int64_t)t[0] * a.Nw * f.R;
 #pragma unroll
-            for (int q = 0; q < STEPS; ++q) {
-                const int32_t rank = q * 32 + g * 8;
-                w[u][q] = u32x4{0, 0, 0, 0};
-                if (row_of_b(u) < a.N && rank < f.R)
-                    w[u][q] = *reinterpret_cast<const u32x4 *>(b + (int64_t)(row_of_b(u) + (GATED && u ? a.N : 0)) * f.R + rank);
-            }
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            f32x4 z = {};
-#pragma unroll
-            for (int q = 0; q < STEPS; ++q)
-                z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[u][q]), low[q], z, 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                acc[u][i] += has ? z[i] : 0.f;
+                for (int q = 0; q < STEPS; ++q) {
+                    const int32_t rank = q * 32 + g * 8;
+                    w[s][u][q] = u32x4{0, 0, 0, 0};
+                    if (some && row_of_b(u) < a.N && rank < f.R)
+                        w[s][u][q] =
+                            *reinterpret_cast<const u32x4 *>(b + (int64_t)(row_of_b(u) + (GATED && u ? a.N : 0)) * f.R + rank);
+                }
         }
+#pragma unroll
+        for (int s = 0; s < kSegments; ++s)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                f32x4 z = {};
+#pragma unroll
+                for (int q = 0; q < STEPS; ++q)
+                    z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[s][u][q]), low[q], z, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    acc[u][i] += has[s] ? z[i] : 0.f;
+            }
     }
     float z[8];
 #pragma unroll
@@ -286,10 +328,17 @@ int32_t low_parts(int32_t K) { return (K + kPartPieces * kPiece - 1) / (kPartPie
 template <class S, bool GATED>
 hipError_t launch_first(const FewArgs &f, hipStream_t stream) {
     const int64_t blocks = (int64_t)f.low_tiles * f.rank_tiles * f.low_count;
-    const int64_t tiles = f.parts ? (int64_t)f.row_tiles * f.col_tiles * f.parts + 8 : 0;
+    const int64_t tiles = (int64_t)f.row_tiles * f.col_tiles * f.parts + 8;
     if (blocks + tiles > kMostTiles)
         return hipErrorInvalidConfiguration;
     return launch_traced("adapter_few", adapter_few_kernel<S, GATED>, dim3((unsigned)(blocks + tiles)), S::kThreads, stream, f);
+}
+
+hipError_t launch_low(const FewArgs &f, hipStream_t stream) {
+    const int64_t blocks = (int64_t)f.low_tiles * f.rank_tiles * f.low_count;
+    if (blocks > kMostTiles)
+        return hipErrorInvalidConfiguration;
+    return launch_traced("adapter_few_low", adapter_few_low_kernel, dim3((unsigned)blocks), 256, stream, f);
 }
 
 template <bool GATED>
@@ -348,7 +397,8 @@ hipError_t launch_adapter_few(const AdapterArgs &a, hipStream_t stream) {
         f.col_tiles = base.col_tiles;
     }
 #define EP_CALL(S) (gated ? launch_first<S, true>(f, stream) : launch_first<S, false>(f, stream))
-    const hipError_t e = size == Size::kMedium ? EP_CALL(Medium) : size == Size::kSmall ? EP_CALL(Small) : EP_CALL(Tiny);
+    const hipError_t e = !a.w ? launch_low(f, stream)
+                         : size == Size::kMedium ? EP_CALL(Medium) : size == Size::kSmall ? EP_CALL(Small) : EP_CALL(Tiny);
 #undef EP_CALL
     if (e != hipSuccess)
         return e;

@@ -215,22 +215,21 @@ struct WeightArgs {
     const uint16_t *side, *low;  // [rows][L]; [rows][width]: v in two values (da) or low (db)
     uint16_t *out;               // da [A][R][L], db [A][L][R]
     float *partial;              // parts > 1: [parts] of the same
-    int32_t parts;
+    int32_t tiles, groups, parts;  // along L, of the ranks, of an adapter's rows
+    int32_t blocks;              // workgroups, a multiple of 8; 0: not wanted
 };
 
 // da: i = the long side's columns, j = a block of v's ranks, the first values and then the second, which are
 // added up at the end.  db: i = ranks, j = the long side's columns.
 template <class S, bool DA>
-__global__ __launch_bounds__(S::kThreads) void adapter_weight_kernel(WeightArgs a, int32_t long_tiles, int32_t groups) {
-    __shared__ __attribute__((aligned(1024))) char lds[S::kStages * S::kStageBytes];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    int64_t t = tile_of_block(blockIdx.x, (int64_t)a.A * a.parts * groups * long_tiles);
+__device__ __forceinline__ void weight_tile(const WeightArgs &a, int32_t block, char EP_LDS *lds, int lane, int wave) {
+    int64_t t = tile_of_block(block, (int64_t)a.A * a.parts * a.groups * a.tiles);
     if (t < 0)
         return;
-    const int32_t tile = (int32_t)(t % long_tiles);
-    t /= long_tiles;
-    const int32_t group = (int32_t)(t % groups);
-    t /= groups;
+    const int32_t tile = (int32_t)(t % a.tiles);
+    t /= a.tiles;
+    const int32_t group = (int32_t)(t % a.groups);
+    t /= a.groups;
     const int32_t part = (int32_t)(t % a.parts), e = (int32_t)(t / a.parts);
     int64_t b, end;
     expert_rows(a.offsets, a.rows, e, b, end);
@@ -255,7 +254,7 @@ __global__ __launch_bounds__(S::kThreads) void adapter_weight_kernel(WeightArgs 
         }
     };
     if constexpr (DA) {
-        tile_product<S, Mul::kBf16>(x, v, steps, (char EP_LDS *)lds, wave, lane, acc);
+        tile_product<S, Mul::kBf16>(x, v, steps, lds, wave, lane, acc);
         typedef TileShape<S::kI, S::kJ / 2, S::kWavesI, S::kWavesJ, S::kStages> Half;
         static_assert(S::kWavesJ == 1, "both values of a rank are one wave's");
         f32x16 sum[Half::FI][Half::FJ];
@@ -264,14 +263,14 @@ __global__ __launch_bounds__(S::kThreads) void adapter_weight_kernel(WeightArgs 
 #pragma unroll
             for (int j = 0; j < Half::FJ; ++j)
                 sum[i][j] = acc[i][j] + acc[i][j + Half::FJ];
-        tile_results<Half>(sum, (char EP_LDS *)lds, wave, lane, [&](int row, int col, const float *o) {
+        tile_results<Half>(sum, lds, wave, lane, [&](int row, int col, const float *o) {
             const int32_t rank = group * (kShort / 2) + row, l = l0 + col;
             if (rank < a.R && l < a.L)
                 put(((int64_t)e * a.R + rank) * a.L + l, o);
         });
     } else {
-        tile_product<S, Mul::kBf16>(v, x, steps, (char EP_LDS *)lds, wave, lane, acc);
-        tile_results<S>(acc, (char EP_LDS *)lds, wave, lane, [&](int row, int col, const float *o) {
+        tile_product<S, Mul::kBf16>(v, x, steps, lds, wave, lane, acc);
+        tile_results<S>(acc, lds, wave, lane, [&](int row, int col, const float *o) {
             const int32_t rank = group * kShort + col, l = l0 + row;
             if (rank < a.R && l < a.L)
                 put(((int64_t)e * a.L + l) * a.R + rank, o);
@@ -279,10 +278,33 @@ __global__ __launch_bounds__(S::kThreads) void adapter_weight_kernel(WeightArgs 
     }
 }
 
-// The parts added up in order: eight values per thread.
-__global__ __launch_bounds__(256) void adapter_weight_join_kernel(const float *partial, int32_t parts, int64_t groups,
-                                                                  uint16_t *out) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+// Both in one launch: neither fills the chip for long, and they do not need each other.
+template <class SA, class SB>
+__global__ __launch_bounds__(SA::kThreads) void adapter_weights_kernel(WeightArgs da, WeightArgs db) {
+    static_assert(SA::kThreads == SB::kThreads, "");
+    constexpr int kA = SA::kStages * SA::kStageBytes, kB = SB::kStages * SB::kStageBytes;
+    __shared__ __attribute__((aligned(1024))) char lds[kA > kB ? kA : kB];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if ((int32_t)blockIdx.x < da.blocks)
+        weight_tile<SA, true>(da, (int32_t)blockIdx.x, (char EP_LDS *)lds, lane, wave);
+    else
+        weight_tile<SB, false>(db, (int32_t)blockIdx.x - da.blocks, (char EP_LDS *)lds, lane, wave);
+}
+
+// The parts added up in order: eight values per thread, da's and then db's.
+struct JoinArgs {
+    const float *partial;
+    int32_t parts;  // 1: nothing to do
+    int64_t groups;
+    uint16_t *out;
+};
+__global__ __launch_bounds__(256) void adapter_weights_join_kernel(JoinArgs da, JoinArgs db) {
+    int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const bool second = i >= da.groups;
+    i -= second ? da.groups : 0;
+    const float *partial = second ? db.partial : da.partial;
+    const int32_t parts = second ? db.parts : da.parts;
+    const int64_t groups = second ? db.groups : da.groups;
     if (i >= groups)
         return;
     float s[8] = {};
@@ -304,7 +326,7 @@ __global__ __launch_bounds__(256) void adapter_weight_join_kernel(const float *p
             for (int q = 0; q < 8; ++q)
                 s[q] += v[u][q / 4][q % 4];
     }
-    reinterpret_cast<u32x4 *>(out)[i] = pack8(s);
+    reinterpret_cast<u32x4 *>(second ? db.out : da.out)[i] = pack8(s);
 }
 
 typedef TileShape<128, 64, 4, 1, 3> Da32;   // 32 ranks; two workgroups per compute unit each (72, 64 and
@@ -326,18 +348,26 @@ struct WeightPlan {
     size_t bytes(int32_t A, int32_t R, int32_t L) const { return parts > 1 ? (size_t)parts * A * R * L * 4 : 0; }
 };
 
-template <class S, bool DA>
-hipError_t launch_weight(const WeightArgs &a, const WeightPlan &p, hipStream_t stream) {
-    const int64_t blocks = (int64_t)a.A * p.tiles * p.groups * p.parts;
-    if (blocks > kMostTiles)
-        return hipErrorInvalidConfiguration;
-    const hipError_t e = launch_traced(DA ? "adapter_da" : "adapter_db", adapter_weight_kernel<S, DA>,
-                                       dim3((unsigned)(blocks + 8)), S::kThreads, stream, a, p.tiles, p.groups);
-    if (e != hipSuccess || p.parts == 1)
+void set_plan(WeightArgs &a, const WeightPlan &p) {
+    a.tiles = p.tiles;
+    a.groups = p.groups;
+    a.parts = p.parts;
+    a.blocks = (int32_t)(((int64_t)a.A * p.tiles * p.groups * p.parts + 15) / 8 * 8);
+}
+JoinArgs join_args(const WeightArgs &a) {
+    return {a.partial, a.parts, a.blocks && a.parts > 1 ? (int64_t)a.A * a.R * a.L / 8 : 0, a.out};
+}
+
+hipError_t launch_weights(const WeightArgs &da, const WeightArgs &db, int32_t log, hipStream_t stream) {
+    const dim3 grid((unsigned)(da.blocks + db.blocks));
+    const hipError_t e =
+        log == 5 ? launch_traced("adapter_weights", adapter_weights_kernel<Da32, Db64>, grid, Db64::kThreads, stream, da, db)
+                 : launch_traced("adapter_weights", adapter_weights_kernel<Da64, Db64>, grid, Db64::kThreads, stream, da, db);
+    const JoinArgs ja = join_args(da), jb = join_args(db);
+    if (e != hipSuccess || ja.groups + jb.groups == 0)
         return e;
-    const int64_t groups = (int64_t)a.A * a.R * a.L / 8;
-    return launch_traced("adapter_weight_join", adapter_weight_join_kernel, dim3((unsigned)((groups + 255) / 256)), 256,
-                         stream, (const float *)a.partial, p.parts, groups, a.out);
+    return launch_traced("adapter_weights_join", adapter_weights_join_kernel,
+                         dim3((unsigned)((ja.groups + jb.groups + 255) / 256)), 256, stream, ja, jb);
 }
 
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -346,9 +376,9 @@ size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 bool too_far(int64_t rows, int64_t length) { return rows * length * 2 > INT32_MAX; }
 
 // v [rows][split_width], dz [rows][Nw] (with an activation, or out of a gather's reach), x's rows [rows][K] (out
-// of its reach), and the parts of da or db.
+// of its reach), and the parts of da and of db.
 struct Workspace {
-    size_t dz = 0, x = 0, sums = 0, bytes = 0;
+    size_t dz = 0, x = 0, da_sums = 0, db_sums = 0, bytes = 0;
     bool own_dz, own_x;
     Workspace(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t N, int32_t act, bool order, bool dx, bool da, bool db) {
         const int64_t Nw = act == EP_ACT_SWIGLU ? 2 * (int64_t)N : N;
@@ -356,9 +386,9 @@ struct Workspace {
         own_x = da && order && too_far(rows, K);
         dz = dx || da ? align256((size_t)rows * split_width(R) * 2) : 0;
         x = dz + (own_dz ? align256((size_t)(rows * Nw * 2)) : 0);
-        sums = x + (own_x ? align256((size_t)rows * K * 2) : 0);
-        bytes = sums + std::max(da ? WeightPlan(rows, A, R, K, true).bytes(A, R, K) : 0,
-                                db ? WeightPlan(rows, A, R, (int32_t)Nw, false).bytes(A, R, (int32_t)Nw) : 0);
+        da_sums = x + (own_x ? align256((size_t)rows * K * 2) : 0);
+        db_sums = da_sums + (da ? align256(WeightPlan(rows, A, R, K, true).bytes(A, R, K)) : 0);
+        bytes = db_sums + (db ? WeightPlan(rows, A, R, (int32_t)Nw, false).bytes(A, R, (int32_t)Nw) : 0);
     }
 };
 
@@ -418,33 +448,18 @@ hipError_t launch_adapter_grad(const AdapterGradArgs &a, hipStream_t stream) {
         if (e != hipSuccess)
             return e;
     }
-    WeightArgs p{nullptr, a.offsets, a.rows, a.A, a.R, 0, 0, nullptr, nullptr, nullptr, nullptr, 1};
-    p.partial = reinterpret_cast<float *>(base + ws.sums);
+    WeightArgs da{}, db{};
     if (a.da) {
-        const WeightPlan plan(a.rows, a.A, a.R, a.K, true);
-        p.order = x_order;
-        p.L = a.K;
-        p.width = width;
-        p.side = x;
-        p.low = v;
-        p.out = static_cast<uint16_t *>(a.da);
-        p.parts = plan.parts;
-        e = log == 5 ? launch_weight<Da32, true>(p, plan, stream) : launch_weight<Da64, true>(p, plan, stream);
-        if (e != hipSuccess)
-            return e;
+        da = {x_order, a.offsets, a.rows, a.A, a.R, a.K, width, x, v, static_cast<uint16_t *>(a.da),
+              reinterpret_cast<float *>(base + ws.da_sums), 0, 0, 0, 0};
+        set_plan(da, WeightPlan(a.rows, a.A, a.R, a.K, true));
     }
     if (a.db) {
-        const WeightPlan plan(a.rows, a.A, a.R, Nw, false);
-        p.order = dz_order;
-        p.L = Nw;
-        p.width = a.R;
-        p.side = dz;
-        p.low = static_cast<const uint16_t *>(a.low);
-        p.out = static_cast<uint16_t *>(a.db);
-        p.parts = plan.parts;
-        e = launch_weight<Db64, false>(p, plan, stream);
+        db = {dz_order, a.offsets, a.rows, a.A, a.R, Nw, a.R, dz, static_cast<const uint16_t *>(a.low),
+              static_cast<uint16_t *>(a.db), reinterpret_cast<float *>(base + ws.db_sums), 0, 0, 0, 0};
+        set_plan(db, WeightPlan(a.rows, a.A, a.R, Nw, false));
     }
-    return e;
+    return da.blocks + db.blocks ? launch_weights(da, db, log, stream) : e;
 }
 
 }  // namespace ep
