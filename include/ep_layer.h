@@ -211,14 +211,14 @@ ep_status ep_expert_product_grad(const void *x_dev, int64_t rows, const int32_t 
 ep_status ep_adapter_rows(const int32_t *row_adapter, int64_t rows, int32_t num_adapters, int32_t *order,
                           int32_t *offsets, hipStream_t stream);
 
-/* Bytes of workspace ep_adapter_product needs: with_w and keep_low say whether w and low are given. */
+/* Bytes of workspace ep_adapter_product needs; with_w says whether w is given. */
 ep_status ep_adapter_product_workspace_bytes(int64_t rows, int32_t num_adapters, int32_t rank, int32_t in_length,
-                                             int32_t out_length, int32_t with_w, ep_activation act, int32_t keep_low,
+                                             int32_t out_length, int32_t with_w, ep_activation act,
                                              size_t *bytes /* host out */);
 
 /* A projection with the low-rank adapters of its rows.  Place i of the adapters' order is row
  * r = order[i], of adapter a if offsets[a] <= i < offsets[a+1]:
- *   low[i] = bf16(scale[a] * x[r] A_a^T), zeros without an adapter
+ *   low[i] = scale[a] * x[r] A_a^T, zeros without an adapter
  *   z = x[r] W^T + low[i] B_a^T (+ bias);  y[r] = act(z) (+ residual[r])
  *   x        bf16 [rows][K]
  *   order    device int32 [rows], a permutation of the rows; NULL: the rows come in the adapters' order
@@ -231,10 +231,9 @@ ep_status ep_adapter_product_workspace_bytes(int64_t rows, int32_t num_adapters,
  *            of rows before their dropout) that comes as the residual
  *   bias     bf16 [Nw] or NULL;  residual  bf16 [rows][N] or NULL, may be y itself
  *   pre      bf16 [rows][Nw] or NULL: z, which the gradient of an activation needs
- *   low      bf16 [rows][R] or NULL (kept in the workspace then), in the adapters' order, as the
- *            gradient reads it
+ *   low      bf16 [rows][R] or NULL: low, in the adapters' order, as the gradient reads it
  *   y        bf16 [rows][N]
- * An adapter's infinities and NaN reach its own rows only.
+ * For its product with B low is held in 16 bits of mantissa.  An adapter's infinities and NaN reach its own rows only.
  * Requires 0 <= rows < 2^31, 1 <= A <= EP_ADAPTER_MAX, R a multiple of 8 up to EP_ADAPTER_MAX_RANK, K and N
  * positive multiples of 8, K and Nw <= EP_PRODUCT_MAX_LENGTH; w, a and b, and x with an order and w,
  * smaller than 2^31 bytes. */
@@ -253,7 +252,7 @@ ep_status ep_adapter_product_grad_workspace_bytes(int64_t rows, int32_t num_adap
                                                   int32_t results, size_t *bytes /* host out */);
 
 /* Gradient of ep_adapter_product with w held fast:
- *   dz = d_y * act'(pre);  v[i] = bf16(scale[a] * dz[r] B_a)
+ *   dz = d_y * act'(pre);  v[i] = scale[a] * dz[r] B_a
  *   dx[r] = dz[r] W + v[i] A_a;  da_a = sum v[i]^T x[r];  db_a = sum dz[r]^T low[i]
  * (the residual's gradient is d_y itself; w's, where it is trained too, ep_expert_product_grad's of one expert)
  *   x, order, offsets, a, b, scale, w  as in the forward (w NULL: dx of the adapters alone)
@@ -261,7 +260,8 @@ ep_status ep_adapter_product_grad_workspace_bytes(int64_t rows, int32_t num_adap
  *   pre     bf16 [rows][Nw] as the forward wrote it; NULL with EP_ACT_NONE
  *   d_y     bf16 [rows][N]
  *   dx      bf16 [rows][K] or NULL;  da  bf16 [A][R][K] or NULL;  db  bf16 [A][Nw][R] or NULL
- * dz and v are rounded to bf16 for the products.  An adapter without rows gets zeros in da and db.
+ * dz is rounded to bf16 for the products, v held in 16 bits of mantissa.  An adapter without rows gets
+ * zeros in da and db.
  * Requires what the forward requires, but that x may have any size. */
 ep_status ep_adapter_product_grad(const void *x_dev, int64_t rows, const int32_t *order, const int32_t *offsets,
                                   int32_t num_adapters, int32_t rank, const void *a_dev, const void *b_dev,

@@ -27,15 +27,6 @@ ep_status check_sizes(const char *who, int64_t rows, int32_t A, int32_t R, int32
     return EP_OK;
 }
 
-// What the workspace holds of low: all of it if the caller does not keep it.
-size_t low_bytes(int64_t rows, int32_t R, bool keep_low) {
-    return keep_low || ep::adapter_few(rows) ? 0 : ((size_t)rows * R * 2 + 255) & ~(size_t)255;
-}
-
-size_t product_bytes(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t N, bool base, int32_t act, bool keep_low) {
-    return low_bytes(rows, R, keep_low) + ep::adapter_product_partial_bytes(rows, A, R, K, N, base, act);
-}
-
 }  // namespace
 
 extern "C" ep_status ep_adapter_rows(const int32_t *row_adapter, int64_t rows, int32_t num_adapters, int32_t *order,
@@ -51,14 +42,14 @@ extern "C" ep_status ep_adapter_rows(const int32_t *row_adapter, int64_t rows, i
 
 extern "C" ep_status ep_adapter_product_workspace_bytes(int64_t rows, int32_t num_adapters, int32_t rank, int32_t in_length,
                                                         int32_t out_length, int32_t with_w, ep_activation act,
-                                                        int32_t keep_low, size_t *bytes) {
+                                                        size_t *bytes) {
     const ep_status st =
         check_sizes("ep_adapter_product_workspace_bytes", rows, num_adapters, rank, in_length, out_length, act);
     if (st != EP_OK)
         return st;
     if (!bytes)
         return fail(EP_ERR_INVALID_ARG, "ep_adapter_product_workspace_bytes: bytes is NULL");
-    *bytes = product_bytes(rows, num_adapters, rank, in_length, out_length, with_w != 0, act, keep_low != 0);
+    *bytes = ep::adapter_product_workspace_bytes(rows, num_adapters, rank, in_length, out_length, with_w != 0, act);
     return EP_OK;
 }
 
@@ -81,7 +72,7 @@ extern "C" ep_status ep_adapter_product(const void *x_dev, int64_t rows, const i
         return fail(EP_ERR_INVALID_ARG,
                     "ep_adapter_product: x, a, b and y are required, every array 16-byte aligned (order, offsets, scale 4)");
     const size_t need =
-        product_bytes(rows, num_adapters, rank, in_length, out_length, w_dev != nullptr, act, low_dev != nullptr);
+        ep::adapter_product_workspace_bytes(rows, num_adapters, rank, in_length, out_length, w_dev != nullptr, act);
     if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need))
         return fail(EP_ERR_INVALID_ARG, "ep_adapter_product: workspace of %zu bytes, need %zu, 16-byte aligned",
                     workspace ? workspace_bytes : (size_t)0, need);
@@ -102,10 +93,9 @@ extern "C" ep_status ep_adapter_product(const void *x_dev, int64_t rows, const i
     a.act = act;
     a.residual = residual_dev;
     a.pre = pre_dev;
+    a.low = low_dev;
     a.y = y_dev;
-    const size_t low = low_bytes(rows, rank, low_dev != nullptr);
-    a.low = low ? workspace : low_dev;
-    a.partial = reinterpret_cast<float *>(static_cast<char *>(workspace) + low);
+    a.workspace = workspace;
     EP_HIP(ep::launch_adapter_product(a, stream));
     return EP_OK;
 }

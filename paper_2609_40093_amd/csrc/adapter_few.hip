@@ -1,8 +1,8 @@
 // adapter_few.hip -- the adapters' product for few rows (a decode step), in two kernels:
 //   the first  makes parts of x W^T (tiles of product_tile.h, rows as they come) and parts of
 //              x[order] a_a^T, side by side in one launch, since neither needs the other;
-//   the second adds the parts up, in order, rounds the low-rank values to bf16, adds their products with b and
-//              runs the epilogue.
+//   the second adds the parts up, in order, makes two bf16 values of each low-rank one (adapter_low.hip),
+//              adds their products with b and runs the epilogue.
 // Bound by the latencies of dependent loads and by the bytes of W, a and b.
 //
 // The low-rank parts: a workgroup takes 16 rows of one adapter, 16 ranks and a part of the contraction
@@ -197,7 +197,7 @@ __global__ __launch_bounds__(64) void adapter_few_join_kernel(FewArgs f) {
         if (j >= (t[1] & 0xffff) && j < t[1] >> 16)
             e = t[0];
     }
-    bf16x8 low[STEPS];
+    bf16x8 low[STEPS], rest[STEPS];
     const float scale = e >= 0 && f.scale ? f.scale[e] : 1.f;
 #pragma unroll
     for (int q = 0; q < STEPS; ++q) {
@@ -221,9 +221,15 @@ __global__ __launch_bounds__(64) void adapter_few_join_kernel(FewArgs f) {
                 v[1] += t[p][1];
             }
         }
-        const u32x4 b = {bf16_pair(v[0][0] * scale, v[0][1] * scale), bf16_pair(v[0][2] * scale, v[0][3] * scale),
-                         bf16_pair(v[1][0] * scale, v[1][1] * scale), bf16_pair(v[1][2] * scale, v[1][3] * scale)};
+        u32x4 b, c;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float lo = v[i / 2][i % 2 * 2] * scale, hi = v[i / 2][i % 2 * 2 + 1] * scale;
+            b[i] = bf16_pair(lo, hi);
+            c[i] = bf16_pair(rest_of(lo, bf16_lo(b[i])), rest_of(hi, bf16_hi(b[i])));
+        }
         low[q] = __builtin_bit_cast(bf16x8, b);
+        rest[q] = __builtin_bit_cast(bf16x8, c);
         if (f.low && blockIdx.x == 0 && j < n_rows && rank < f.R)
             *reinterpret_cast<u32x4 *>(f.low + (i0 + j) * f.R + rank) = b;
     }
@@ -254,8 +260,11 @@ __global__ __launch_bounds__(64) void adapter_few_join_kernel(FewArgs f) {
             for (int u = 0; u < 2; ++u) {
                 f32x4 z = {};
 #pragma unroll
-                for (int q = 0; q < STEPS; ++q)
-                    z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[s][u][q]), low[q], z, 0, 0, 0);
+                for (int q = 0; q < STEPS; ++q) {
+                    const bf16x8 b = __builtin_bit_cast(bf16x8, w[s][u][q]);
+                    z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, low[q], z, 0, 0, 0);
+                    z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, rest[q], z, 0, 0, 0);
+                }
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     acc[u][i] += has[s] ? z[i] : 0.f;
@@ -386,8 +395,8 @@ hipError_t launch_adapter_few(const AdapterArgs &a, hipStream_t stream) {
     f.low_count = low_parts(a.K);
     f.low_tiles = (int32_t)row_tiles_most(a.rows, a.A, kRows);
     f.rank_tiles = (a.R + kRanks - 1) / kRanks;
-    f.low_parts = a.partial;
-    f.p.partial = a.partial + (size_t)f.low_count * a.rows * a.R;
+    f.low_parts = static_cast<float *>(a.workspace);
+    f.p.partial = f.low_parts + (size_t)f.low_count * a.rows * a.R;
     Size size = Size::kSmall;
     if (a.w) {
         const Base base = plan_base(a.rows, a.K, a.N, gated);

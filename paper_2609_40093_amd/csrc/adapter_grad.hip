@@ -83,8 +83,7 @@ __device__ __forceinline__ void redo8(const DxArgs &a, const AdapterSide &s, int
     if (e >= 0)
 #pragma unroll 1
         for (int32_t j = 0; j < 2 * s.R; ++j)
-            add(s.low[i * s.width + s.chunk_at(j / 8) + j % 8],
-                s.weights + ((int64_t)e * s.R + (j < s.R ? j : j - s.R)) * a.K);
+            add(s.low[i * s.width + s.value_at(j)], s.weights + ((int64_t)e * s.R + s.rank_of(j)) * a.K);
 }
 
 // dx[order[i]][k] = sum_n dz[i][n] w[n][k] + sum_j v[i][j] a_e[j][k]: i = k across the contraction, j = rows.
@@ -433,7 +432,7 @@ hipError_t launch_adapter_grad(const AdapterGradArgs &a, hipStream_t stream) {
     }
     const int32_t width = split_width(a.R), log = split_log(a.R);
     if (a.dx || a.da) {
-        e = launch_adapter_low({dz, a.rows, dz_order, a.offsets, a.A, a.R, Nw, a.b, a.scale, v, width, log}, stream);
+        e = launch_adapter_low({dz, a.rows, dz_order, a.offsets, a.A, a.R, Nw, a.b, true, a.scale, nullptr, v, width, log}, stream);
         if (e != hipSuccess)
             return e;
     }

@@ -1,17 +1,18 @@
 // adapter_low.hip -- the low-rank values of the adapters' rows:
-//   low[i] = scale_a x[order[i]] a_a^T    in bf16, which the product multiplies (the forward);
-//   v[i]   = scale_a dz[order[i]] b_a     as the sum of two bf16 values (the gradient, see below).
-// Rows without an adapter get zeros.
+//   scale_a x[order[i]] a_a^T of the forward, scale_a dz[order[i]] b_a of the gradient,
+// as the sum of two bf16 values each for the products that read them, and for the forward also as the one
+// bf16 value that a caller keeps.  Rows without an adapter get zeros.
 //
 // Bound by the rows' bytes, or for few rows by the adapters'.  Many rows go through the MFMA tile
-// (product_tile.h), ranks by rows of one adapter, its LDS stages as deep as they fit, since what bounds it
-// are loads in flight.  Few rows go straight from memory into the operands of 16x16 matrix instructions:
-// the 16 waves of a workgroup share out the contraction, 64 values (whole cache lines) at a time with
-// every load of a wave on its way at once, and are added up through LDS in a fixed order.
+// (product_tile.h), ranks by rows of one adapter.  Few rows go straight from memory into the operands of
+// 16x16 matrix instructions: the 16 waves of a workgroup share out the contraction, 64 values (whole
+// cache lines) at a time with every load of a wave on its way at once, and are added up through LDS in
+// a fixed order.
 //
-// v is nobody's result, and what it loses goes into dx and da on top of what dz and they themselves lose
-// to bf16: da's error is 0.0029 of its 2-norm with v in one bf16 value, 0.0024 with the rest of that in a
-// second one, which costs the ranks' part of the contractions twice.
+// The products multiply bf16, and in one bf16 value each the low-rank values lose as much as the results
+// do: a gated product's error is 0.0025 of its 2-norm that way and 0.0017, its own rounding, with the
+// rest of each value in a second one; da's 0.0029 and 0.0023.  It takes the ranks' part of the contractions
+// twice, a step or two of a hundred.
 #include "adapter_tile.h"
 
 namespace ep {
@@ -28,9 +29,37 @@ __device__ __forceinline__ void clear_rows(const LowArgs &a, int per, int thread
     for (int i = threadIdx.x; i < per * vecs; i += threads) {
         const int64_t p = z * per + i / vecs;
         const int64_t row = p < before ? p : behind + (p - before);
-        if (z >= 0 && row < a.rows)
-            *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.low) + row * a.width + i % vecs * 8) = u32x4{0, 0, 0, 0};
+        const int at = i % vecs * 8;
+        if (z < 0 || row >= a.rows)
+            continue;
+        *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.split) + row * a.width + at) = u32x4{0, 0, 0, 0};
+        if (a.low && at < a.R)
+            *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.low) + row * a.R + at) = u32x4{0, 0, 0, 0};
     }
+}
+
+// N neighbouring values (4 or 8) from rank on of a row: N / 2 words per array.
+template <int N>
+__device__ __forceinline__ void put_values(const LowArgs &a, int64_t row, int rank, const float *v) {
+    uint32_t high[N / 2], rest[N / 2];
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+        high[i] = bf16_pair(v[2 * i], v[2 * i + 1]);
+        rest[i] = bf16_pair(rest_of(v[2 * i], bf16_lo(high[i])), rest_of(v[2 * i + 1], bf16_hi(high[i])));
+    }
+    typedef uint32_t words __attribute__((ext_vector_type(N / 2)));
+    const auto put = [](void *to, int64_t at, const uint32_t *w) {
+        words o;
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i)
+            o[i] = w[i];
+        *reinterpret_cast<words *>(static_cast<uint16_t *>(to) + at) = o;
+    };
+    const int64_t at = row * a.width + rank + (rank >> a.log << a.log);
+    put(a.split, at, high);
+    put(a.split, at + (1 << a.log), rest);
+    if (a.low)
+        put(a.low, row * a.R + rank, high);
 }
 
 // ---- few rows ------------------------------------------------------------------------
@@ -91,9 +120,10 @@ __global__ __launch_bounds__(kFewWaves * 64) void adapter_low_few_kernel(LowArgs
     for (int v = 1; v < kFewWaves; ++v)
         s += sums[v][lane];
     const int q = rank0 + lane / 16 * 4, row = lane % 16;  // a lane holds four ranks of one row
-    if (row < rt.n && q < a.R)
-        *reinterpret_cast<uint64_t *>(static_cast<uint16_t *>(a.low) + (rt.row0 + row) * a.width + q) =
-            bf16_pair(s[0] * scale, s[1] * scale) | (uint64_t)bf16_pair(s[2] * scale, s[3] * scale) << 32;
+    if (row < rt.n && q < a.R) {
+        const float o[4] = {s[0] * scale, s[1] * scale, s[2] * scale, s[3] * scale};
+        put_values<4>(a, rt.row0 + row, q, o);
+    }
 }
 
 // ---- many rows -----------------------------------------------------------------------
@@ -116,7 +146,7 @@ struct Part : Op {
 // their own, and are added up in order.  (A step of so small a tile takes 0.5 us whatever it holds,
 // which is how long its loads, its two barriers and its LDS reads take one after the other: 8192 rows of
 // 4096, 16 ranks, with one group per workgroup 36 us, 61 where the rows come from HBM.)
-// ACROSS: the weights are [A][K][R] and v is written, else [A][R][K] and low.
+// ACROSS: the weights are [A][K][R], else [A][R][K].
 template <class S, int GROUPS, bool ACROSS>
 __global__ __launch_bounds__(S::kThreads * GROUPS) void adapter_low_kernel(LowArgs a) {
     constexpr int kGroupBytes = S::kStages * S::kStageBytes;
@@ -191,20 +221,7 @@ __global__ __launch_bounds__(S::kThreads * GROUPS) void adapter_low_kernel(LowAr
 #pragma unroll
         for (int q = 0; q < 8; ++q)
             o[q] = v[q] * scale;
-        const u32x4 high = pack8(o);
-        uint16_t *dst = static_cast<uint16_t *>(a.low) + (rt.row0 + row) * a.width;
-        if constexpr (!ACROSS) {
-            *reinterpret_cast<u32x4 *>(dst + rank) = high;
-        } else {
-            float h[8];
-            unpack8(high, h);
-#pragma unroll
-            for (int q = 0; q < 8; ++q)
-                o[q] -= h[q];
-            const int at = rank + (rank >> a.log << a.log);
-            *reinterpret_cast<u32x4 *>(dst + at) = high;
-            *reinterpret_cast<u32x4 *>(dst + at + (1 << a.log)) = pack8(o);
-        }
+        put_values<8>(a, rt.row0 + row, rank, o);
     });
 }
 
@@ -228,7 +245,7 @@ hipError_t launch_shape(const LowArgs &a, hipStream_t stream) {
 hipError_t launch_adapter_low(const LowArgs &a, hipStream_t stream) {
     if (a.rows == 0)
         return hipSuccess;
-    if (a.log)
+    if (a.across)
         return a.R <= 64 ? launch_shape<Low64, 4, true>(a, stream) : launch_shape<Low128, 2, true>(a, stream);
     const bool far = a.order && a.rows * a.K * 2 > INT32_MAX;  // rows that a tile cannot address
     if (far || a.rows / a.A < 24 || a.rows < 2048)

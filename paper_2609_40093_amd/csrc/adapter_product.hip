@@ -4,7 +4,7 @@
 // The low-rank values low = scale_a x a_a^T come from adapter_low.hip.  Rows go in the adapters'
 // order: a tile gathers its rows of x through it and leaves its results through it.  The
 // contraction over K goes on over the ranks of the adapters that the tile's rows have
-// (adapter_tile.h), so the adapters cost the tile (segments * R) / 64 steps, and y is written
+// (adapter_tile.h), so the adapters cost the tile (segments * 2 R) / 64 steps, and y is written
 // once.  Without W the contraction begins with the ranks.
 #include "adapter_tile.h"
 #include "product_finish.h"
@@ -19,21 +19,23 @@ __device__ __forceinline__ void redo8(const ProductArgs &a, const AdapterSide &s
 #pragma unroll 1
     for (int q = 0; q < 8; ++q) {
         float sum = 0.f;
-        const auto dot = [&](const uint16_t *u, const uint16_t *v, int32_t length) {
-#pragma unroll 1
-            for (int32_t k = 0; k < length; k += 8) {
-                float f[8], g[8];
-                unpack8(*reinterpret_cast<const u32x4 *>(u + k), f);
-                unpack8(*reinterpret_cast<const u32x4 *>(v + k), g);
+        const auto dot8 = [&](const uint16_t *u, const uint16_t *v) {
+            float f[8], g[8];
+            unpack8(*reinterpret_cast<const u32x4 *>(u), f);
+            unpack8(*reinterpret_cast<const u32x4 *>(v), g);
 #pragma unroll
-                for (int p = 0; p < 8; ++p)
-                    sum = fmaf(f[p], g[p], sum);
-            }
+            for (int p = 0; p < 8; ++p)
+                sum = fmaf(f[p], g[p], sum);
         };
         if (a.w)
-            dot(static_cast<const uint16_t *>(a.x) + r * a.K, static_cast<const uint16_t *>(a.w) + (int64_t)(n + q) * a.K, a.K);
+#pragma unroll 1
+            for (int32_t k = 0; k < a.K; k += 8)
+                dot8(static_cast<const uint16_t *>(a.x) + r * a.K + k,
+                     static_cast<const uint16_t *>(a.w) + (int64_t)(n + q) * a.K + k);
         if (e >= 0)
-            dot(s.low + i * s.R, s.weights + ((int64_t)e * a.Nw + n + q) * s.R, s.R);
+#pragma unroll 1
+            for (int32_t j = 0; j < 2 * s.R; j += 8)
+                dot8(s.low + i * s.width + s.value_at(j), s.weights + ((int64_t)e * a.Nw + n + q) * s.R + s.rank_of(j));
 #pragma unroll
         for (int p = 0; p < 8; ++p)
             z[p] = p == q ? sum : z[p];
@@ -108,9 +110,9 @@ __global__ __launch_bounds__(S::kThreads) void adapter_product_kernel(ProductArg
                const int32_t r = row_of[row];
                return r < 0 ? kNowhere : (uint32_t)(r * kb);
            });
-    x.chain(main, s, segments, count, s.low + i0 * s.R, (uint64_t)n_rows * s.R * 2, 0, LowRows{});
+    x.chain(main, s, segments, count, s.low + i0 * s.width, (uint64_t)n_rows * s.width * 2, 0, LowRows{});
 
-    int32_t steps = main + (count * (s.R / 8) + 7) / 8;
+    int32_t steps = main + (count * (int32_t)s.chunks.d + 7) / 8;
     if (parts > 1) {
         const int32_t per = (steps + parts - 1) / parts, first = part * per;
         steps = steps - first < per ? steps - first : per;
@@ -214,7 +216,7 @@ __global__ __launch_bounds__(256) void adapter_join_kernel(ProductArgs a, Adapte
 // Steps that the adapters add to a tile of `per` rows: its segments to expect.
 int32_t adapter_steps(int64_t rows, int32_t A, int32_t R, int per) {
     const int64_t some = std::min<int64_t>(std::min<int64_t>(A, per), (int64_t)A * per / std::max<int64_t>(rows, 1) + 1);
-    return (int32_t)((some * R + kStepRows - 1) / kStepRows);
+    return (int32_t)((some * 2 * R + kStepRows - 1) / kStepRows);
 }
 Plan adapter_plan(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t N, bool base, bool gated) {
     return make_plan(rows, 1, base ? K : 0, N, false, gated, [&](int per) { return adapter_steps(rows, A, R, per); });
@@ -241,16 +243,20 @@ hipError_t launch_shape(const ProductArgs &a, const AdapterSide &s, const Plan &
     return a.act == EP_ACT_SWIGLU ? launch_tiles<S, true>(a, s, p, stream) : launch_tiles<S, false>(a, s, p, stream);
 }
 
+// The split low-rank values, then the parts' sums.
+size_t split_bytes(int64_t rows, int32_t R) { return ((size_t)rows * split_width(R) * 2 + 255) & ~(size_t)255; }
+
 }  // namespace
 
-size_t adapter_product_partial_bytes(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t N, bool base, int32_t act) {
+size_t adapter_product_workspace_bytes(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t N, bool base, int32_t act) {
     if (rows == 0)
         return 0;
     if (adapter_few(rows))
         return adapter_few_bytes(rows, R, K, N, base, act);
     const bool gated = act == EP_ACT_SWIGLU;
     const Plan p = adapter_plan(rows, A, R, K, N, base, gated);
-    return p.split.parts == 1 ? 0 : (size_t)p.split.parts * rows * N * (gated ? 2 : 1) * sizeof(float);
+    return split_bytes(rows, R) +
+           (p.split.parts == 1 ? 0 : (size_t)p.split.parts * rows * N * (gated ? 2 : 1) * sizeof(float));
 }
 
 hipError_t launch_adapter_product(const AdapterArgs &a, hipStream_t stream) {
@@ -272,12 +278,13 @@ hipError_t launch_adapter_product(const AdapterArgs &a, hipStream_t stream) {
     p.residual = a.residual;
     p.pre = a.pre;
     p.y = a.y;
-    p.partial = a.partial;
+    p.partial = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + split_bytes(a.rows, a.R));
+    const int32_t width = split_width(a.R), log = split_log(a.R);
     const hipError_t e = launch_adapter_low(
-        {a.x, a.rows, a.order, a.offsets, a.A, a.R, a.K, a.a, a.scale, a.low, a.R, 0}, stream);
+        {a.x, a.rows, a.order, a.offsets, a.A, a.R, a.K, a.a, false, a.scale, a.low, a.workspace, width, log}, stream);
     if (e != hipSuccess)
         return e;
-    const AdapterSide s = adapter_side(a.order, a.offsets, a.A, a.R, a.low, a.R, 0, a.b);
+    const AdapterSide s = adapter_side(a.order, a.offsets, a.A, a.R, a.workspace, width, log, a.b);
     const Plan plan = adapter_plan(a.rows, a.A, a.R, a.K, a.N, a.w != nullptr, gated);
     switch (plan.size) {
     case Size::kLarge: return launch_shape<Large>(p, s, plan, stream);

@@ -7,8 +7,7 @@
 // ranks twice.  The row operand holds zeros at the
 // places of the segments that a row is not in, and the column operand the weights of the place's
 // adapter, so one accumulator adds up both parts; 64 places are one step whoever's they are: four
-// adapters of rank 16 cost what one of rank 64 costs.  (A step per adapter would take 64 steps
-// more for 64 rows with an adapter each; of rank 16 it is 16.)
+// adapters of rank 8 cost what one of rank 32 costs.
 //
 // Zeros times another adapter's infinities or NaN are NaN, which the epilogues look for (redo below).
 #pragma once
@@ -24,28 +23,30 @@ struct AdapterSide {
     const int32_t *order;    // null: the rows come in the adapters' order
     const int32_t *offsets;  // null: one adapter with every row
     int32_t A, R;
-    const uint16_t *low;     // [rows][width], in the adapters' order
+    const uint16_t *low;     // LowArgs's split [rows][width], in the adapters' order
     const uint16_t *weights; // b [A][Nw][R] of the product, a [A][R][K] of its gradient
-    int32_t width, log;      // log2 of LowArgs's block, 0: none; with one a segment has 2 R places
-    FastDiv places, chunks;  // by a segment's places, and by an eighth of them
+    int32_t width, log;
+    FastDiv places, chunks;  // by a segment's 2 R places, and by an eighth of them
 
-    // Where the eight values at chunk `in` of a segment lie in a row of low.
-    __device__ __forceinline__ int32_t chunk_at(int32_t in) const {
-        int32_t j = in * 8;
-        if (!log)
-            return j;
-        const int32_t second = j >= R ? 1 : 0;
-        j -= second ? R : 0;
-        return j + (((j >> log) + second) << log);
+    // A segment's places are its ranks with the first values, then its ranks with the second.  The rank of
+    // place j, and where the value lies in a row of low.
+    __device__ __forceinline__ int32_t rank_of(int32_t j) const { return j >= R ? j - R : j; }
+    __device__ __forceinline__ int32_t value_at(int32_t j) const {
+        const int32_t rank = rank_of(j);
+        return rank + (((rank >> log) + (j >= R ? 1 : 0)) << log);
     }
 };
 inline AdapterSide adapter_side(const int32_t *order, const int32_t *offsets, int32_t A, int32_t R, const void *low,
                                 int32_t width, int32_t log, const void *weights) {
-    const uint32_t places = (uint32_t)R * (log ? 2 : 1);
     return {order, offsets, A, R, static_cast<const uint16_t *>(low), static_cast<const uint16_t *>(weights), width, log,
-            fast_div(places), fast_div(places / 8)};
+            fast_div((uint32_t)R * 2), fast_div((uint32_t)R / 4)};
 }
-// The layout of v: blocks of 32 ranks (up to 32 ranks) or 64, the first values of a block, then the second.
+// The second bf16 value of v, of which the first is `first`; none of infinities and NaN.
+__device__ __forceinline__ float rest_of(float v, float first) {
+    const float d = v - first;
+    return d - d == 0.f ? d : 0.f;
+}
+// The layout of split: blocks of 32 ranks (up to 32 ranks) or 64, the first values of a block, then the second.
 inline int32_t split_log(int32_t R) { return R <= 32 ? 5 : 6; }
 inline int32_t split_width(int32_t R) {
     const int32_t block = 1 << split_log(R);
@@ -137,11 +138,12 @@ struct ChainAlong : AlongC<T, W> {
                 const Segment s = segments[at];
                 if constexpr (LOW) {
                     if (row >= (s[1] & 0xffff) && row < s[1] >> 16)
-                        o = (uint32_t)(row * side->width + side->chunk_at((int32_t)in)) * 2;
+                        o = (uint32_t)(row * side->width + side->value_at((int32_t)in * 8)) * 2;
                 } else {
                     const int32_t n = index(row);
                     if (n >= 0)
-                        o = (((uint32_t)s[0] * adapter_rows + (uint32_t)n) * (uint32_t)side->R + in * 8) * 2;
+                        o = (((uint32_t)s[0] * adapter_rows + (uint32_t)n) * (uint32_t)side->R +
+                             (uint32_t)side->rank_of((int32_t)in * 8)) * 2;
                 }
             }
             First::offset[q] = o;
@@ -192,10 +194,10 @@ struct ChainAcross : AcrossC<T, W, FRAGMENTS> {
             const int32_t p = place + row;
             uint32_t o = kNowhere;
             if (live && p < most) {
-                const uint32_t at = side->places.div((uint32_t)p), ranks = (uint32_t)side->R;
-                uint32_t in = (uint32_t)p - at * side->places.d;
-                in -= in >= ranks ? ranks : 0;
-                o = ((uint32_t)segments[at][0] * ranks + in) * (uint32_t)First::stride + First::column_of(q, column, wave, lane);
+                const uint32_t at = side->places.div((uint32_t)p);
+                const uint32_t rank = (uint32_t)side->rank_of((int32_t)((uint32_t)p - at * side->places.d));
+                o = ((uint32_t)segments[at][0] * (uint32_t)side->R + rank) * (uint32_t)First::stride +
+                    First::column_of(q, column, wave, lane);
             }
             First::offset[q] = o;
         }

@@ -229,14 +229,16 @@ hipError_t launch_adapter_rows(const int32_t *row_adapter, int64_t rows, int32_t
 
 // The adapters' low-rank values (adapter_low.hip).
 struct LowArgs {
-    const void *x;  // bf16 [rows][K]; with an order and a log smaller than 2^31 bytes
+    const void *x;  // bf16 [rows][K]; with an order and `across` smaller than 2^31 bytes
     int64_t rows;
     const int32_t *order, *offsets;  // null: rows in the adapters' order; one adapter
     int32_t A, R, K;
-    const void *weights;  // bf16 [A][R][K]; with a log [A][K][R]
+    const void *weights;  // bf16 [A][R][K]; `across`: [A][K][R]
+    bool across;
     const float *scale;   // fp32 [A], null: ones
-    void *low;            // bf16 [rows][width], in the adapters' order
-    int32_t width, log;   // log 0: R values.  Else each as two, 2^log of the first and then of the second
+    void *low;            // bf16 [rows][R], in the adapters' order; may be null
+    void *split;          // bf16 [rows][width], each value as two: 2^log of the first, then of the second
+    int32_t width, log;
 };
 hipError_t launch_adapter_low(const LowArgs &a, hipStream_t stream);
 
@@ -252,14 +254,14 @@ struct AdapterArgs {
     int32_t act;
     const void *residual;
     void *pre, *low, *y;
-    float *partial;  // workspace of adapter_product_partial_bytes
+    void *workspace;  // of adapter_product_workspace_bytes
 };
-// The low-rank values are the workspace's business (low may be null) where adapter_few, else the caller's.
+size_t adapter_product_workspace_bytes(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t N, bool base, int32_t act);
+hipError_t launch_adapter_product(const AdapterArgs &a, hipStream_t stream);
+// The same for few rows (adapter_few.hip).
 bool adapter_few(int64_t rows);
 size_t adapter_few_bytes(int64_t rows, int32_t R, int32_t K, int32_t N, bool base, int32_t act);
 hipError_t launch_adapter_few(const AdapterArgs &a, hipStream_t stream);
-size_t adapter_product_partial_bytes(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t N, bool base, int32_t act);
-hipError_t launch_adapter_product(const AdapterArgs &a, hipStream_t stream);
 
 struct AdapterGradArgs {
     const void *x;

@@ -437,7 +437,7 @@ def adapter_product(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, rows: Ada
         got = AdapterProduct(_output(True if out is None else out, "out", torch.bfloat16, (n, N), x.device),
                              _output(keep_pre, "pre", torch.bfloat16, (n, wide), x.device),
                              _output(keep_low, "low", torch.bfloat16, (n, R), x.device))
-        size = _bytes("ep_adapter_product_workspace_bytes", n, A, R, K, N, w is not None, code, got.low is not None)
+        size = _bytes("ep_adapter_product_workspace_bytes", n, A, R, K, N, w is not None, code)
         ws = _workspace(size, x.device)
     _check(lib.ep_adapter_product(
         _ptr(x), n, _ptr(rows.order), _ptr(rows.offsets), A, R, _ptr(a), _ptr(b), _ptr(scale), _ptr(w), K, N, _ptr(bias),

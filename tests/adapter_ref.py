@@ -2,13 +2,15 @@
 
 Bounds: products of bf16 values are exact in fp32; a sum of n terms in any order, each addition rounded
 or truncated, is within (n + 8) 2^-23 of the sum of magnitudes (8 more for the scale, the bias, the
-residual and the join of partial sums).  low and v are rounded to bf16 (2^-8 of them); the
-products' references take low as the call kept it.  An activation stretches an error by at most 1.2
+residual and the join of partial sums).  The low that a call keeps is rounded to bf16 (2^-8 of it); the low
+and the v that are multiplied are the sum of two such values (2^-16).  An activation stretches an error by at most 1.2
 (layer_ref.act_error); the gradient's dz is rounded to bf16 and its slope is within 2^-17."""
 import torch
 
 import layer_ref as ref
 import paper_2609_40093_amd as ep
+
+TWO = ref.BF16 ** 2    # what the sum of two bf16 values leaves of a number
 
 
 def make(ids, A, R, K, N, seed, act="none", base=True, bias=False, residual=False, scaled=True):
@@ -70,16 +72,18 @@ def check(s, packed=False, keep=True, **more):
     by = scales(s, of)
     off = size * by * (K + 8) * ref.U23
     ref.within(low, want * by, off + ref.BF16 * (want.abs() * by + off), "low")
-    part, size = by_adapter(low.double(), of, s["b"].double().transpose(1, 2))
-    z, all_sizes = torch.zeros_like(part), torch.zeros_like(part)
-    z[order], all_sizes[order] = part, size
+    b = s["b"].double().transpose(1, 2)
+    part, size = by_adapter(want * by, of, b)
+    part_off, _ = by_adapter(off + TWO * (want.abs() * by + off), of, b.abs())
+    z, all_sizes, z_off = torch.zeros_like(part), torch.zeros_like(part), torch.zeros_like(part)
+    z[order], all_sizes[order], z_off[order] = part, size, part_off
     if s["w"] is not None:
         z += x @ s["w"].double().t()
         all_sizes += x.abs() @ s["w"].double().abs().t()
     if s["bias"] is not None:
         z += s["bias"].double()
         all_sizes += s["bias"].double().abs()
-    off = all_sizes * (K + R + 8) * ref.U23
+    off = z_off + (all_sizes + z_off) * (K + 2 * R + 8) * ref.U23
     if keep:
         ref.within(pre, z, off + ref.BF16 * (z.abs() + off), "pre")
     y, dy = ref.act(z, s["act"]), ref.act_error(z, off, s["act"])
@@ -116,11 +120,11 @@ def check_grad(s, packed=False, seed=5, **more):
     v, size = by_adapter(dz, of, b)
     v_off = by * (by_adapter(off, of, b.abs())[0] + size * (wide + 8) * ref.U23)
     v = v * by
-    v_off = v_off + ref.BF16 * (v.abs() + v_off)
+    v_off = v_off + TWO * (v.abs() + v_off)
     if got.dx is not None:
         dx, size = by_adapter(v, of, a)
         dx_off = by_adapter(v_off, of, a.abs())[0]
-        terms = R
+        terms = 2 * R
         if s["w"] is not None:
             w = s["w"].double()
             dx, size, dx_off, terms = dx + dz @ w, size + dz.abs() @ w.abs(), dx_off + off @ w.abs(), terms + wide
@@ -131,7 +135,7 @@ def check_grad(s, packed=False, seed=5, **more):
         n = int(at.sum())
         if got.da is not None:
             want = v[at].t() @ x[at]
-            o = v_off[at].t() @ x[at].abs() + (v[at].abs() + v_off[at]).t() @ x[at].abs() * (n + 8) * ref.U23
+            o = v_off[at].t() @ x[at].abs() + (v[at].abs() + v_off[at]).t() @ x[at].abs() * (2 * n + 8) * ref.U23
             ref.within(got.da[e], want, o + ref.BF16 * (want.abs() + o), f"da {e}")
         if got.db is not None:
             u = low.double()[at]

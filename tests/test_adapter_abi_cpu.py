@@ -54,17 +54,17 @@ def test_product(lib, bad):
 def test_product_workspace(lib):
     n = ctypes.c_size_t()
 
-    def size(rows=64, A=8, R=16, K=7168, N=2048, w=1, act=0, keep=0):
-        assert lib.ep_adapter_product_workspace_bytes(rows, A, R, K, N, w, act, keep, ctypes.byref(n)) == _lib.EP_OK
+    def size(rows=64, A=8, R=16, K=7168, N=2048, w=1, act=0):
+        assert lib.ep_adapter_product_workspace_bytes(rows, A, R, K, N, w, act, ctypes.byref(n)) == _lib.EP_OK
         return n.value
 
-    assert size() >= size(keep=1) + 64 * 16 * 2
-    assert size(rows=0) == 0 and size(rows=100000, keep=1) == 0
+    assert size() > size(w=0) > 0
+    assert size(rows=0) == 0 and size(rows=100000) >= 100000 * 32 * 2
     for bad in SIZES:
         a = {"rows": 4, "A": 2, "R": 16, "K": 64, "N": 32, "act": 0, **bad}
-        refused(lib, lib.ep_adapter_product_workspace_bytes(a["rows"], a["A"], a["R"], a["K"], a["N"], 1, a["act"], 0,
+        refused(lib, lib.ep_adapter_product_workspace_bytes(a["rows"], a["A"], a["R"], a["K"], a["N"], 1, a["act"],
                                                             ctypes.byref(n)), "ep_adapter_product_workspace_bytes")
-    refused(lib, lib.ep_adapter_product_workspace_bytes(4, 2, 16, 64, 32, 1, 0, 0, None), "bytes is NULL")
+    refused(lib, lib.ep_adapter_product_workspace_bytes(4, 2, 16, 64, 32, 1, 0, None), "bytes is NULL")
 
 
 def grad(lib, x=D, rows=4, order=None, off=D, A=2, R=16, a=D, b=D, scale=None, w=D, K=64, N=32, low=D, act=0, pre=None, d=D,
