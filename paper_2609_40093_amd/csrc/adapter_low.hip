@@ -3,8 +3,8 @@
 // as the sum of two bf16 values each for the products that read them, and for the forward also as the one
 // bf16 value that a caller keeps.  Rows without an adapter get zeros.
 //
-// Bound by the rows' bytes, or for few rows by the adapters'.  Many rows go through the MFMA tile
-// (product_tile.h), ranks by rows of one adapter.  Few rows go straight from memory into the operands of
+// Bound by the rows' bytes, or for few rows by the adapters'.  Many rows go through LDS, with more than
+// 32 ranks and in the gradient through the MFMA tile (product_tile.h).  Few rows go straight from memory into the operands of
 // 16x16 matrix instructions: the 16 waves of a workgroup share out the contraction, 64 values (whole
 // cache lines) at a time with every load of a wave on its way at once, and are added up through LDS in
 // a fixed order.
@@ -18,17 +18,21 @@
 namespace ep {
 namespace {
 
-// Zeros for the rows without an adapter, before the first one's rows and behind the last one's: the
-// workgroups past the adapters' row tiles take `per` of them each.
-__device__ __forceinline__ void clear_rows(const LowArgs &a, int per, int threads, int lane) {
-    if (!a.offsets)
-        return;
-    const int64_t z = (int64_t)blockIdx.x - count_row_tiles(a.offsets, a.rows, a.A, per, lane);
-    const int64_t before = clamp_row(a.offsets[0], a.rows), behind = clamp_row(a.offsets[a.A], a.rows);
+// The rows without an adapter: before the first one's rows and behind the last one's.
+struct Others {
+    int64_t before, behind, count;
+    __device__ __forceinline__ explicit Others(const LowArgs &a) {
+        before = a.offsets ? clamp_row(a.offsets[0], a.rows) : 0;
+        behind = a.offsets ? clamp_row(a.offsets[a.A], a.rows) : a.rows;
+        count = before + a.rows - behind;
+    }
+};
+// Zeros for the `per` of them from number z on.
+__device__ __forceinline__ void clear_rows(const LowArgs &a, const Others &o, int64_t z, int per, int threads) {
     const int vecs = a.width / 8;
     for (int i = threadIdx.x; i < per * vecs; i += threads) {
-        const int64_t p = z * per + i / vecs;
-        const int64_t row = p < before ? p : behind + (p - before);
+        const int64_t p = z + i / vecs;
+        const int64_t row = p < o.before ? p : o.behind + (p - o.before);
         const int at = i % vecs * 8;
         if (z < 0 || row >= a.rows)
             continue;
@@ -36,6 +40,19 @@ __device__ __forceinline__ void clear_rows(const LowArgs &a, int per, int thread
         if (a.low && at < a.R)
             *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.low) + row * a.R + at) = u32x4{0, 0, 0, 0};
     }
+}
+// Row tile number `block` of all, the adapters' and then those of the rows without one, in contiguous
+// ranges per XCD: an adapter's weights then stay in one or two of the eight L2s.  e < 0: nothing to multiply.
+template <int PER>
+__device__ __forceinline__ RowTile low_tile(const LowArgs &a, int32_t block, int threads, bool clears, int lane) {
+    const int32_t tiles = count_row_tiles(a.offsets, a.rows, a.A, PER, lane);
+    const Others o(a);
+    const int64_t t = tile_of_block(block, tiles + (o.count + PER - 1) / PER);
+    if (t < tiles)
+        return t < 0 ? RowTile{-1, 0, 0} : find_row_tile(a.offsets, a.rows, a.A, PER, (int32_t)t, lane);
+    if (clears)
+        clear_rows(a, o, (t - tiles) * PER, PER, threads);
+    return {-1, 0, 0};
 }
 
 // N neighbouring values (4 or 8) from rank on of a row: N / 2 words per array.
@@ -69,12 +86,9 @@ __global__ __launch_bounds__(kFewWaves * 64) void adapter_low_few_kernel(LowArgs
     __shared__ f32x4 sums[kFewWaves][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rank0 = (int)blockIdx.y * kFewRanks;
-    const RowTile rt = find_row_tile(a.offsets, a.rows, a.A, kFewRows, (int32_t)blockIdx.x, lane);
-    if (rt.e < 0) {
-        if (blockIdx.y == 0)
-            clear_rows(a, kFewRows, kFewWaves * 64, lane);
+    const RowTile rt = low_tile<kFewRows>(a, (int32_t)blockIdx.x, kFewWaves * 64, blockIdx.y == 0, lane);
+    if (rt.e < 0)
         return;
-    }
     const int g = lane / 16;  // which 16 bytes of a fragment's 64 this lane takes
     const int rank = rank0 + lane % 16;
     const bool has_a = rank < a.R;
@@ -126,7 +140,123 @@ __global__ __launch_bounds__(kFewWaves * 64) void adapter_low_few_kernel(LowArgs
     }
 }
 
-// ---- many rows -----------------------------------------------------------------------
+// ---- many rows, up to 32 ranks -----------------------------------------------------------
+// A wave takes 32 rows of one adapter and every WAVES-th step of 64 values of the contraction; the waves
+// of a workgroup are added up at the end.  The rows go to LDS (their fragments are whole cache lines
+// there), the weights, which no other wave of the workgroup needs, into registers.  No wave waits for another:
+// each has kDeep steps on their way, and as loads return in order, as many of the weights' as of the
+// rows'.  (3440 rows of 6656, 8 ranks: 15 us, as a tile of product_tile.h 21 to 27.  With 64 ranks the
+// weights' loads, which touch a cache line per rank, take longer than the tile's: 16379 rows of 7168 132 us, 78.)
+constexpr int kDeep = 5, kDeepRows = 32;
+
+template <int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void adapter_low_rows_kernel(LowArgs a) {
+    typedef AlongC<kDeepRows, 1> Rows;
+    constexpr int kStage = kDeepRows * kStepBytes, kLoads = Rows::kLoads + 4;
+    static_assert((kDeep - 1) * kLoads < 64 && 4096 <= kDeep * kStage, "");
+    __shared__ __attribute__((aligned(1024))) char lds[WAVES * kDeep * kStage];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const RowTile rt = low_tile<kDeepRows>(a, (int32_t)blockIdx.x, WAVES * 64, blockIdx.y == 0, lane);
+    if (rt.e < 0)
+        return;
+    const int64_t kb = (int64_t)a.K * 2;
+    char EP_LDS *own = (char EP_LDS *)lds + wave * kDeep * kStage;
+    const char *xb = static_cast<const char *>(a.x);
+    Rows x;
+    // through an order from x's first row on (x is smaller than 2^31 bytes then)
+    x.init(a.order ? xb : xb + rt.row0 * kb, (uint32_t)((a.order ? a.rows : rt.n) * kb), (int32_t)kb, 0, lane,
+           [&](int row) -> uint32_t {
+               if (row >= rt.n)
+                   return kNowhere;
+               const int32_t r = a.order ? row_at(a.order, a.rows, rt.row0 + row) : row;
+               return r < 0 ? kNowhere : (uint32_t)(r * kb);
+           });
+    x.aim(0, lane);
+    const __amdgpu_buffer_rsrc_t weights =
+        buffer_of(static_cast<const char *>(a.weights) + (int64_t)rt.e * a.R * kb, (uint32_t)(a.R * kb));
+    const int64_t end = lane % 32 < a.R ? kb : 0;  // of this lane's rank
+    const uint32_t at = (uint32_t)(lane % 32 * kb);
+    const int32_t all = (a.K + kStepRows - 1) / kStepRows;
+    const int32_t steps = all > wave ? (all - wave + WAVES - 1) / WAVES : 0;
+    int32_t next = 0;  // the step whose loads are issued next
+    int32_t byte = (wave * kStepRows + lane / 32 * 8) * 2;  // of the contraction
+    if (wave > 0)
+        x.skip(wave);
+    u32x4 w[kDeep][4];
+    const auto load = [&](int place) {
+        const bool live = next < steps;
+        x.begin(live);
+#pragma unroll
+        for (int q = 0; q < Rows::kLoads; ++q)
+            x.load(q, own + place * kStage, 0, lane);
+        x.skip(WAVES);
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            const uint32_t o = live && byte + h * 32 < end ? at + (uint32_t)(byte + h * 32) : kNowhere;
+            w[place][h] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(weights, (int)o, 0, 0));
+        }
+        byte += WAVES * kStepBytes;
+        ++next;
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    f32x16 acc = {};
+#pragma unroll
+    for (int p = 0; p < kDeep - 1; ++p)
+        load(p);
+    for (int32_t t = 0; t < steps; t += kDeep) {
+#pragma unroll
+        for (int p = 0; p < kDeep; ++p) {
+            load((p + kDeep - 1) % kDeep);
+            asm volatile("" ::: "memory");
+            constexpr int kFlying = (kDeep - 1) * kLoads;  // this step has landed, the others are on their way
+            __builtin_amdgcn_s_waitcnt((kFlying & 15) | 7 << 4 | 15 << 8 | kFlying >> 4 << 14);
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                const bf16x8 r = __builtin_bit_cast(bf16x8, x.read(own + p * kStage, 0, h));
+                acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w[p][h]), r, acc, 0, 0, 0);
+            }
+            // the fragments are read before the place is loaded again
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(15 | 7 << 4 | 0 << 8 | 3 << 14);
+            asm volatile("" ::: "memory");
+        }
+    }
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0 | 7 << 4 | 0 << 8);  // loads past the end have landed, too
+    asm volatile("" ::: "memory");
+    // four neighbouring ranks of one row per lane and quarter
+    f32x4 EP_LDS *sums = reinterpret_cast<f32x4 EP_LDS *>(own);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        sums[q * 64 + lane] = f32x4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
+    __syncthreads();
+    const float scale = a.scale ? a.scale[rt.e] : 1.f;
+    const f32x4 EP_LDS *first = (const f32x4 EP_LDS *)(char EP_LDS *)lds;
+    for (int i = threadIdx.x; i < 256; i += WAVES * 64) {
+        f32x4 s = first[i];
+#pragma unroll
+        for (int v = 1; v < WAVES; ++v)
+            s += first[v * (kDeep * kStage / 16) + i];
+        const int l = i % 64, row = l % 32, rank = i / 64 * 8 + l / 32 * 4;
+        if (row >= rt.n || rank >= a.R)
+            continue;
+        const float o[4] = {s[0] * scale, s[1] * scale, s[2] * scale, s[3] * scale};
+        put_values<4>(a, rt.row0 + row, rank, o);
+    }
+}
+
+// As many waves per workgroup as fill the compute units' LDS: six per compute unit of 20 KiB each.
+hipError_t launch_rows(const LowArgs &a, hipStream_t stream) {
+    // every row is one of an adapter or one of none, which make up to two more tiles than an adapter would
+    const dim3 grid((unsigned)row_tiles_most(a.rows, a.A + 2, kDeepRows) + 8);
+    const double tiles = row_tiles_likely(a.rows, a.A, kDeepRows);
+#define EP_CALL(W) launch_traced("adapter_low", adapter_low_rows_kernel<W>, grid, W * 64, stream, a)
+    return tiles <= kCus ? EP_CALL(6) : tiles <= 2 * kCus ? EP_CALL(3) : EP_CALL(2);
+#undef EP_CALL
+}
+
+// ---- many rows, more ranks or weights across the contraction ------------------------------
 // An operand of which a group has `own` steps; the ones behind bring zeros.  (They lie past the
 // contraction's end, where the operand's own range check does not hold.)
 template <class Op>
@@ -155,12 +285,9 @@ __global__ __launch_bounds__(S::kThreads * GROUPS) void adapter_low_kernel(LowAr
     const int lane = threadIdx.x & 63, all_waves = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int group = all_waves / S::kWaves, wave = all_waves % S::kWaves;
     const int rank0 = (int)blockIdx.y * S::kI;
-    const RowTile rt = find_row_tile(a.offsets, a.rows, a.A, S::kJ, (int32_t)blockIdx.x, lane);
-    if (rt.e < 0) {
-        if (blockIdx.y == 0)
-            clear_rows(a, S::kJ, S::kThreads * GROUPS, lane);
+    const RowTile rt = low_tile<S::kJ>(a, (int32_t)blockIdx.x, S::kThreads * GROUPS, blockIdx.y == 0, lane);
+    if (rt.e < 0)
         return;
-    }
     for (int j = threadIdx.x; j < S::kJ; j += S::kThreads * GROUPS)
         row_of[j] = j < rt.n ? row_at(a.order, a.rows, rt.row0 + j) : -1;
     __syncthreads();
@@ -225,19 +352,21 @@ __global__ __launch_bounds__(S::kThreads * GROUPS) void adapter_low_kernel(LowAr
     });
 }
 
-// 32, 64 and 128 ranks.  With up to one tile per compute unit, one workgroup of as many groups as its LDS
-// holds (144, 128 and 144 KiB), else two of half as many.
-typedef TileShape<32, 64, 1, 2, 3> Low32;
+// 64 ranks by 32 rows, or by 64 where those are more than the compute units: one workgroup of four groups per
+// compute unit (144 and 128 KiB of LDS), and with more tiles still two of two groups.
+typedef TileShape<64, 32, 2, 1, 3> Low32;
 typedef TileShape<64, 64, 2, 2, 2> Low64;
-typedef TileShape<128, 64, 4, 2, 3> Low128;
 
-template <class S, int GROUPS, bool ACROSS>
-hipError_t launch_shape(const LowArgs &a, hipStream_t stream) {
-    // every row is one of an adapter or one of none, which make up to two more tiles than an adapter would
-    const dim3 grid((unsigned)row_tiles_most(a.rows, a.A + 2, S::kJ), (unsigned)((a.R + S::kI - 1) / S::kI));
-    if (row_tiles_likely(a.rows, a.A, S::kJ) * grid.y <= kCus)
-        return launch_traced("adapter_low", adapter_low_kernel<S, GROUPS, ACROSS>, grid, S::kThreads * GROUPS, stream, a);
-    return launch_traced("adapter_low", adapter_low_kernel<S, GROUPS / 2, ACROSS>, grid, S::kThreads * GROUPS / 2, stream, a);
+template <bool ACROSS>
+hipError_t launch_tiles(const LowArgs &a, hipStream_t stream) {
+    const auto grid = [&](int per) {
+        return dim3((unsigned)row_tiles_most(a.rows, a.A + 2, per) + 8, (unsigned)((a.R + 63) / 64));
+    };
+    const auto tiles = [&](int per) { return row_tiles_likely(a.rows, a.A, per) * ((a.R + 63) / 64); };
+#define EP_CALL(S, G) \
+    launch_traced("adapter_low", adapter_low_kernel<S, G, ACROSS>, grid(S::kJ), S::kThreads * G, stream, a)
+    return tiles(Low32::kJ) <= kCus ? EP_CALL(Low32, 4) : tiles(Low64::kJ) <= kCus ? EP_CALL(Low64, 4) : EP_CALL(Low64, 2);
+#undef EP_CALL
 }
 
 }  // namespace
@@ -246,16 +375,14 @@ hipError_t launch_adapter_low(const LowArgs &a, hipStream_t stream) {
     if (a.rows == 0)
         return hipSuccess;
     if (a.across)
-        return a.R <= 64 ? launch_shape<Low64, 4, true>(a, stream) : launch_shape<Low128, 2, true>(a, stream);
+        return launch_tiles<true>(a, stream);
     const bool far = a.order && a.rows * a.K * 2 > INT32_MAX;  // rows that a tile cannot address
     if (far || a.rows / a.A < 24 || a.rows < 2048)
         return launch_traced("adapter_low", adapter_low_few_kernel,
-                             dim3((unsigned)row_tiles_most(a.rows, a.A + 2, kFewRows),
+                             dim3((unsigned)row_tiles_most(a.rows, a.A + 2, kFewRows) + 8,
                                   (unsigned)((a.R + kFewRanks - 1) / kFewRanks)),
                              kFewWaves * 64, stream, a);
-    return a.R <= 32   ? launch_shape<Low32, 4, false>(a, stream)
-           : a.R <= 64 ? launch_shape<Low64, 4, false>(a, stream)
-                       : launch_shape<Low128, 2, false>(a, stream);
+    return a.R <= 32 ? launch_rows(a, stream) : launch_tiles<false>(a, stream);
 }
 
 }  // namespace ep
