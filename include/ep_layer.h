@@ -243,13 +243,14 @@ ep_status ep_adapter_product(const void *x_dev, int64_t rows, const int32_t *ord
                              ep_activation act, const void *residual_dev, void *pre_dev, void *low_dev, void *y_dev,
                              void *workspace, size_t workspace_bytes, hipStream_t stream);
 
-/* Bytes of workspace ep_adapter_product_grad needs for the results named (EP_ADAPTER_DX, _DA, _DB). */
+/* Bytes of workspace ep_adapter_product_grad needs for the results named (EP_ADAPTER_DX, _DA, _DB); with_w and
+ * with_order say whether w and an order are given. */
 #define EP_ADAPTER_DX 1
 #define EP_ADAPTER_DA 2
 #define EP_ADAPTER_DB 4
 ep_status ep_adapter_product_grad_workspace_bytes(int64_t rows, int32_t num_adapters, int32_t rank, int32_t in_length,
-                                                  int32_t out_length, ep_activation act, int32_t with_order,
-                                                  int32_t results, size_t *bytes /* host out */);
+                                                  int32_t out_length, int32_t with_w, ep_activation act,
+                                                  int32_t with_order, int32_t results, size_t *bytes /* host out */);
 
 /* Gradient of ep_adapter_product with w held fast:
  *   dz = d_y * act'(pre);  v[i] = scale[a] * dz[r] B_a

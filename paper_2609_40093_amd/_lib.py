@@ -115,7 +115,7 @@ SIGNATURES = {
                                                    ctypes.POINTER(c_size)]),
     "ep_adapter_product": (c_i32, [c_vp, c_i64, c_vp, c_vp, c_i32, c_i32, c_vp, c_vp, c_vp, c_vp, c_i32, c_i32, c_vp,
                                    c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, c_size, c_vp]),
-    "ep_adapter_product_grad_workspace_bytes": (c_i32, [c_i64, c_i32, c_i32, c_i32, c_i32, c_i32, c_i32, c_i32,
+    "ep_adapter_product_grad_workspace_bytes": (c_i32, [c_i64, c_i32, c_i32, c_i32, c_i32, c_i32, c_i32, c_i32, c_i32,
                                                         ctypes.POINTER(c_size)]),
     "ep_adapter_product_grad": (c_i32, [c_vp, c_i64, c_vp, c_vp, c_i32, c_i32, c_vp, c_vp, c_vp, c_vp, c_i32, c_i32, c_vp,
                                         c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_size, c_vp]),

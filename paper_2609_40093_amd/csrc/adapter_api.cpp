@@ -101,8 +101,9 @@ extern "C" ep_status ep_adapter_product(const void *x_dev, int64_t rows, const i
 }
 
 extern "C" ep_status ep_adapter_product_grad_workspace_bytes(int64_t rows, int32_t num_adapters, int32_t rank,
-                                                             int32_t in_length, int32_t out_length, ep_activation act,
-                                                             int32_t with_order, int32_t results, size_t *bytes) {
+                                                             int32_t in_length, int32_t out_length, int32_t with_w,
+                                                             ep_activation act, int32_t with_order, int32_t results,
+                                                             size_t *bytes) {
     const char *who = "ep_adapter_product_grad_workspace_bytes";
     const ep_status st = check_sizes(who, rows, num_adapters, rank, in_length, out_length, act);
     if (st != EP_OK)
@@ -111,7 +112,7 @@ extern "C" ep_status ep_adapter_product_grad_workspace_bytes(int64_t rows, int32
         return fail(EP_ERR_INVALID_ARG, "%s: bytes is NULL", who);
     if (results < 0 || results > (EP_ADAPTER_DX | EP_ADAPTER_DA | EP_ADAPTER_DB))
         return fail(EP_ERR_INVALID_ARG, "%s: unknown results %d", who, results);
-    *bytes = ep::adapter_grad_workspace_bytes(rows, num_adapters, rank, in_length, out_length, act, with_order != 0,
+    *bytes = ep::adapter_grad_workspace_bytes(rows, num_adapters, rank, in_length, out_length, act, with_w != 0, with_order != 0,
                                               (results & EP_ADAPTER_DX) != 0, (results & EP_ADAPTER_DA) != 0,
                                               (results & EP_ADAPTER_DB) != 0);
     return EP_OK;
@@ -140,7 +141,7 @@ extern "C" ep_status ep_adapter_product_grad(const void *x_dev, int64_t rows, co
         !aligned4(order) || !aligned4(offsets) || !aligned4(scale))
         return fail(EP_ERR_INVALID_ARG, "%s: an array is not 16-byte aligned (order, offsets, scale: 4)", who);
     const size_t need = ep::adapter_grad_workspace_bytes(rows, num_adapters, rank, in_length, out_length, act,
-                                                         order != nullptr, dx_dev != nullptr, da_dev != nullptr,
+                                                         w_dev != nullptr, order != nullptr, dx_dev != nullptr, da_dev != nullptr,
                                                          db_dev != nullptr);
     if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need))
         return fail(EP_ERR_INVALID_ARG, "%s: workspace of %zu bytes, need %zu, 16-byte aligned", who,

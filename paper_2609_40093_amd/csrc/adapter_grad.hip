@@ -61,6 +61,8 @@ struct DxArgs {
     const uint16_t *w, *dz;
     const int32_t *dz_order;  // dz's rows; null: they are in the adapters' order
     uint16_t *dx;
+    float *partial;  // parts > 1: [parts][rows][K], in the adapters' order
+    int32_t row_tiles, col_tiles, parts;
 };
 
 // The sums of place i, columns k..k+7, of their own terms alone.
@@ -88,17 +90,20 @@ __device__ __forceinline__ void redo8(const DxArgs &a, const AdapterSide &s, int
 
 // dx[order[i]][k] = sum_n dz[i][n] w[n][k] + sum_j v[i][j] a_e[j][k]: i = k across the contraction, j = rows.
 template <class S>
-__global__ __launch_bounds__(S::kThreads) void adapter_dx_kernel(DxArgs a, AdapterSide s, int32_t row_tiles, int32_t col_tiles) {
+__global__ __launch_bounds__(S::kThreads) void adapter_dx_kernel(DxArgs a, AdapterSide s) {
     __shared__ __attribute__((aligned(1024))) char lds[S::kStages * S::kStageBytes];
     __shared__ Segment table[S::kJ];
     Segment EP_LDS *segments = (Segment EP_LDS *)table;
     __shared__ int32_t row_of[S::kJ], found;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t t = tile_of_block(blockIdx.x, (int64_t)row_tiles * col_tiles);
+    const int64_t tiles = (int64_t)a.row_tiles * a.col_tiles;
+    int64_t t = tile_of_block(blockIdx.x, tiles * a.parts);
     if (t < 0)
         return;
+    const int32_t part = a.parts == 1 ? 0 : (int32_t)(t / tiles);
+    t -= part * tiles;
     int32_t tr, tc;
-    tile_order(t, row_tiles, col_tiles, tr, tc);
+    tile_order(t, a.row_tiles, a.col_tiles, tr, tc);
     const int64_t i0 = (int64_t)tr * S::kJ;
     const int n_rows = a.rows - i0 < S::kJ ? (int)(a.rows - i0) : S::kJ;
     for (int j = threadIdx.x; j < S::kJ; j += S::kThreads)
@@ -124,8 +129,25 @@ __global__ __launch_bounds__(S::kThreads) void adapter_dx_kernel(DxArgs a, Adapt
                return r < 0 ? kNowhere : (uint32_t)(r * zs);
            });
     z.chain(main, s, segments, count, s.low + i0 * s.width, (uint64_t)n_rows * s.width * 2, 0, LowRows{});
+    int32_t steps = main + (count * (int32_t)s.chunks.d + 7) / 8;
+    if (a.parts > 1) {
+        const int32_t per = (steps + a.parts - 1) / a.parts, first = part * per;
+        steps = steps - first < per ? steps - first : per;  // 0 or less: none
+        w.skip(first);
+        z.skip(first);
+    }
     f32x16 acc[S::FI][S::FJ] = {};
-    tile_product<S, Mul::kBf16>(w, z, main + (count * (int32_t)s.chunks.d + 7) / 8, (char EP_LDS *)lds, wave, lane, acc);
+    tile_product<S, Mul::kBf16>(w, z, steps, (char EP_LDS *)lds, wave, lane, acc);
+    if (a.parts > 1) {
+        tile_results<S>(acc, (char EP_LDS *)lds, wave, lane, [&](int row, int col, const float *v) {
+            if (row >= n_rows || k0 + col >= a.K)
+                return;
+            f32x4 *dst = reinterpret_cast<f32x4 *>(a.partial + ((int64_t)part * a.rows + i0 + row) * a.K + k0 + col);
+            dst[0] = f32x4{v[0], v[1], v[2], v[3]};
+            dst[1] = f32x4{v[4], v[5], v[6], v[7]};
+        });
+        return;
+    }
     const int32_t k = k0 + first_col<S, 8>(wave, lane);
     tile_rows_out<S, 8>(
         acc, (char EP_LDS *)lds, wave, lane,
@@ -139,14 +161,84 @@ __global__ __launch_bounds__(S::kThreads) void adapter_dx_kernel(DxArgs a, Adapt
         });
 }
 
+// dx from its parts, added in order: eight values per thread.
+__global__ __launch_bounds__(256) void adapter_dx_join_kernel(DxArgs a, AdapterSide s, FastDiv groups) {
+    const uint32_t at = blockIdx.x * 256 + threadIdx.x, row = groups.div(at);
+    const int64_t i = row;
+    const int32_t k = (int32_t)(at - row * groups.d) * 8;
+    const int32_t r = i < a.rows ? row_at(s.order, a.rows, i) : -1;
+    if (r < 0)
+        return;
+    float z[8] = {};
+    const float *src = a.partial + i * a.K + k;
+    constexpr int kAhead = 4;
+    for (int32_t p0 = 0; p0 < a.parts; p0 += kAhead) {
+        f32x4 v[kAhead][2];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                v[u][h] = f32x4{};
+                if (p0 + u < a.parts)
+                    v[u][h] = *reinterpret_cast<const f32x4 *>(src + (p0 + u) * a.rows * a.K + h * 4);
+            }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                z[q] += v[u][q / 4][q % 4];
+    }
+    if (__builtin_expect(any_nan(z, 8), false))
+        redo8(a, s, i, k, z);
+    *reinterpret_cast<u32x4 *>(a.dx + (int64_t)r * a.K + k) = pack8(z);
+}
+
+// The tile of dx and the parts of its contraction, by the estimate of the time.
+enum class DxSize { kLarge, kBroad, kMedium, kSmall, kTiny };
+struct DxTile {
+    DxSize size;
+    int i, j;
+    StepCost cost;
+};
+constexpr DxTile kDxTiles[] = {{DxSize::kLarge, Large::kI, Large::kJ, kGradTiles[0].cost},
+                               {DxSize::kBroad, Broad::kI, Broad::kJ, kGradTiles[1].cost},
+                               {DxSize::kMedium, Medium::kI, Medium::kJ, kGradTiles[2].cost},
+                               {DxSize::kSmall, Small::kI, Small::kJ, kGradTiles[3].cost},
+                               {DxSize::kTiny, TinyRows::kI, TinyRows::kJ, {true, 0.50, 0.65}}};
+struct DxPlan {
+    DxSize size;
+    int32_t row_tiles, col_tiles, parts;
+};
+DxPlan plan_adapter_dx(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t main) {
+    DxPlan best{};
+    double least = 0;
+    for (const DxTile &g : kDxTiles) {
+        const int32_t steps = main + adapter_steps(rows, A, R, g.j);
+        const int32_t row_tiles = (int32_t)((rows + g.j - 1) / g.j), col_tiles = (K + g.i - 1) / g.i;
+        for (int32_t parts = 1; parts == 1 || steps / parts >= kSplitSteps; parts *= 2) {
+            const double t = estimate(g.cost, (double)row_tiles * col_tiles, parts, (steps + parts - 1) / parts, rows * K);
+            if (least == 0 || t < least) {
+                least = t;
+                best = {g.size, row_tiles, col_tiles, parts};
+            }
+        }
+    }
+    return best;
+}
+int32_t main_steps(bool base, int32_t Nw) { return base ? (Nw + kStepRows - 1) / kStepRows : 0; }
+
 template <class S>
 hipError_t launch_dx(const DxArgs &a, const AdapterSide &s, hipStream_t stream) {
-    const int32_t cols = (a.K + S::kI - 1) / S::kI;
-    const int64_t row_tiles = (a.rows + S::kJ - 1) / S::kJ;
-    if (row_tiles * cols > kMostTiles)
+    const int64_t tiles = (int64_t)a.row_tiles * a.col_tiles * a.parts;
+    if (tiles > kMostTiles)
         return hipErrorInvalidConfiguration;
-    return launch_traced("adapter_dx", adapter_dx_kernel<S>, dim3((unsigned)(row_tiles * cols + 8)), S::kThreads, stream, a, s,
-                         (int32_t)row_tiles, cols);
+    const hipError_t e =
+        launch_traced("adapter_dx", adapter_dx_kernel<S>, dim3((unsigned)(tiles + 8)), S::kThreads, stream, a, s);
+    if (e != hipSuccess || a.parts == 1)
+        return e;
+    const int64_t groups = a.rows * (a.K / 8);
+    return launch_traced("adapter_dx_join", adapter_dx_join_kernel, dim3((unsigned)((groups + 255) / 256)), 256, stream, a, s,
+                         fast_div((uint32_t)(a.K / 8)));
 }
 
 // ---- da and db -----------------------------------------------------------------------
@@ -375,17 +467,20 @@ size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 bool too_far(int64_t rows, int64_t length) { return rows * length * 2 > INT32_MAX; }
 
 // v [rows][split_width], dz [rows][Nw] (with an activation, or out of a gather's reach), x's rows [rows][K] (out
-// of its reach), and the parts of da and of db.
+// of its reach), and the parts of dx, of da and of db.
 struct Workspace {
-    size_t dz = 0, x = 0, da_sums = 0, db_sums = 0, bytes = 0;
+    size_t dz = 0, x = 0, dx_sums = 0, da_sums = 0, db_sums = 0, bytes = 0;
     bool own_dz, own_x;
-    Workspace(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t N, int32_t act, bool order, bool dx, bool da, bool db) {
+    Workspace(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t N, int32_t act, bool base, bool order, bool dx, bool da,
+              bool db) {
         const int64_t Nw = act == EP_ACT_SWIGLU ? 2 * (int64_t)N : N;
         own_dz = (dx || da || db) && rows > 0 && (act != EP_ACT_NONE || (order && too_far(rows, Nw)));
         own_x = da && order && too_far(rows, K);
         dz = dx || da ? align256((size_t)rows * split_width(R) * 2) : 0;
         x = dz + (own_dz ? align256((size_t)(rows * Nw * 2)) : 0);
-        da_sums = x + (own_x ? align256((size_t)rows * K * 2) : 0);
+        dx_sums = x + (own_x ? align256((size_t)rows * K * 2) : 0);
+        const int32_t parts = dx && rows > 0 ? plan_adapter_dx(rows, A, R, K, main_steps(base, (int32_t)Nw)).parts : 1;
+        da_sums = dx_sums + (parts > 1 ? align256((size_t)parts * rows * K * 4) : 0);
         db_sums = da_sums + (da ? align256(WeightPlan(rows, A, R, K, true).bytes(A, R, K)) : 0);
         bytes = db_sums + (db ? WeightPlan(rows, A, R, (int32_t)Nw, false).bytes(A, R, (int32_t)Nw) : 0);
     }
@@ -393,15 +488,15 @@ struct Workspace {
 
 }  // namespace
 
-size_t adapter_grad_workspace_bytes(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t N, int32_t act, bool order, bool dx,
-                                    bool da, bool db) {
-    return Workspace(rows, A, R, K, N, act, order, dx, da, db).bytes;
+size_t adapter_grad_workspace_bytes(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t N, int32_t act, bool base, bool order,
+                                    bool dx, bool da, bool db) {
+    return Workspace(rows, A, R, K, N, act, base, order, dx, da, db).bytes;
 }
 
 hipError_t launch_adapter_grad(const AdapterGradArgs &a, hipStream_t stream) {
     const bool gated = a.act == EP_ACT_SWIGLU, activated = a.act != EP_ACT_NONE;
     const int32_t Nw = gated ? 2 * a.N : a.N;
-    const Workspace ws(a.rows, a.A, a.R, a.K, a.N, a.act, a.order != nullptr, a.dx, a.da, a.db);
+    const Workspace ws(a.rows, a.A, a.R, a.K, a.N, a.act, a.w != nullptr, a.order != nullptr, a.dx, a.da, a.db);
     char *base = static_cast<char *>(a.workspace);
     uint16_t *v = reinterpret_cast<uint16_t *>(base);
     const uint16_t *dz = static_cast<const uint16_t *>(a.d_y), *x = static_cast<const uint16_t *>(a.x);
@@ -437,13 +532,15 @@ hipError_t launch_adapter_grad(const AdapterGradArgs &a, hipStream_t stream) {
             return e;
     }
     if (a.rows > 0 && a.dx) {
-        const DxArgs d{a.rows, a.K, Nw, static_cast<const uint16_t *>(a.w), dz, dz_order, static_cast<uint16_t *>(a.dx)};
+        const DxPlan plan = plan_adapter_dx(a.rows, a.A, a.R, a.K, main_steps(a.w != nullptr, Nw));
+        const DxArgs d{a.rows, a.K, Nw, static_cast<const uint16_t *>(a.w), dz, dz_order, static_cast<uint16_t *>(a.dx),
+                       reinterpret_cast<float *>(base + ws.dx_sums), plan.row_tiles, plan.col_tiles, plan.parts};
         const AdapterSide s = adapter_side(a.order, a.offsets, a.A, a.R, v, width, log, a.a);
-        const GradSize size = plan_dx(a.rows, 1, a.K, a.w ? Nw : 2 * a.R);
-        e = size == GradSize::kLarge    ? launch_dx<Large>(d, s, stream)
-            : size == GradSize::kBroad  ? launch_dx<Broad>(d, s, stream)
-            : size == GradSize::kMedium ? launch_dx<Medium>(d, s, stream)
-                                        : launch_dx<Small>(d, s, stream);
+        e = plan.size == DxSize::kLarge    ? launch_dx<Large>(d, s, stream)
+            : plan.size == DxSize::kBroad  ? launch_dx<Broad>(d, s, stream)
+            : plan.size == DxSize::kMedium ? launch_dx<Medium>(d, s, stream)
+            : plan.size == DxSize::kSmall  ? launch_dx<Small>(d, s, stream)
+                                           : launch_dx<TinyRows>(d, s, stream);
         if (e != hipSuccess)
             return e;
     }

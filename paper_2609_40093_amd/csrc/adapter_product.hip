@@ -213,11 +213,6 @@ __global__ __launch_bounds__(256) void adapter_join_kernel(ProductArgs a, Adapte
     finish8<false, GATED>(a, columns, x, r, n, z, up);
 }
 
-// Steps that the adapters add to a tile of `per` rows: its segments to expect.
-int32_t adapter_steps(int64_t rows, int32_t A, int32_t R, int per) {
-    const int64_t some = std::min<int64_t>(std::min<int64_t>(A, per), (int64_t)A * per / std::max<int64_t>(rows, 1) + 1);
-    return (int32_t)((some * 2 * R + kStepRows - 1) / kStepRows);
-}
 Plan adapter_plan(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t N, bool base, bool gated) {
     return make_plan(rows, 1, base ? K : 0, N, false, gated, [&](int per) { return adapter_steps(rows, A, R, per); });
 }
@@ -293,7 +288,7 @@ hipError_t launch_adapter_product(const AdapterArgs &a, hipStream_t stream) {
     case Size::kSmall: return launch_shape<Small>(p, s, plan, stream);
     case Size::kWide: return launch_shape<Wide>(p, s, plan, stream);
     case Size::kFew: return launch_shape<Few>(p, s, plan, stream);
-    default: return launch_shape<Tiny>(p, s, plan, stream);
+    default: return launch_shape<TinyRows>(p, s, plan, stream);
     }
 }
 

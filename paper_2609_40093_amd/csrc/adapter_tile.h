@@ -41,6 +41,14 @@ inline AdapterSide adapter_side(const int32_t *order, const int32_t *offsets, in
     return {order, offsets, A, R, static_cast<const uint16_t *>(low), static_cast<const uint16_t *>(weights), width, log,
             fast_div((uint32_t)R * 2), fast_div((uint32_t)R / 4)};
 }
+// Steps that the adapters add to a tile of `per` rows: its segments to expect.
+inline int32_t adapter_steps(int64_t rows, int32_t A, int32_t R, int per) {
+    const int64_t some = std::min<int64_t>(std::min<int64_t>(A, per), (int64_t)A * per / std::max<int64_t>(rows, 1) + 1);
+    return (int32_t)((some * 2 * R + kStepRows - 1) / kStepRows);
+}
+// Tiny (product_tile.h) with a stage less, so that two workgroups and their tables fit a compute unit.
+typedef TileShape<128, 32, 4, 1, 3> TinyRows;
+
 // The second bf16 value of v, of which the first is `first`; none of infinities and NaN.
 __device__ __forceinline__ float rest_of(float v, float first) {
     const float d = v - first;
@@ -180,6 +188,13 @@ struct ChainAcross : AcrossC<T, W, FRAGMENTS> {
         side = &s;
         size2 = (uint32_t)size;
         column = (uint32_t)index0;
+    }
+    __device__ __forceinline__ void skip(int32_t steps) {
+        const int32_t n = steps < first ? steps : first;
+        if (n > 0)
+            First::skip(n);
+        first -= n;
+        place += (steps - n) * kStepRows;
     }
     __device__ __forceinline__ void begin(bool live) {
         if (first > 0) {

@@ -276,8 +276,8 @@ struct AdapterGradArgs {
     void *dx, *da, *db;  // may be null
     void *workspace;     // of adapter_grad_workspace_bytes
 };
-size_t adapter_grad_workspace_bytes(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t N, int32_t act, bool order, bool dx,
-                                    bool da, bool db);
+size_t adapter_grad_workspace_bytes(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t N, int32_t act, bool base, bool order,
+                                    bool dx, bool da, bool db);
 hipError_t launch_adapter_grad(const AdapterGradArgs &a, hipStream_t stream);
 
 // ---- dropout of a residual addition ---------------------------------------------------

@@ -472,7 +472,7 @@ def adapter_product_grad(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, low:
         got = AdapterGrad(_output(dx, "dx", torch.bfloat16, (n, K), x.device),
                           _output(da, "da", torch.bfloat16, (A, R, K), x.device),
                           _output(db, "db", torch.bfloat16, (A, wide, R), x.device))
-        size = _bytes("ep_adapter_product_grad_workspace_bytes", n, A, R, K, N, code, rows.order is not None,
+        size = _bytes("ep_adapter_product_grad_workspace_bytes", n, A, R, K, N, w is not None, code, rows.order is not None,
                       (_lib.EP_ADAPTER_DX if got.dx is not None else 0) | (_lib.EP_ADAPTER_DA if got.da is not None else 0)
                       | (_lib.EP_ADAPTER_DB if got.db is not None else 0))
         ws = _workspace(size, x.device)

@@ -85,7 +85,7 @@ def test_grad_workspace(lib):
     n = ctypes.c_size_t()
 
     def size(results, act=0, order=0, rows=4096):
-        assert lib.ep_adapter_product_grad_workspace_bytes(rows, 8, 16, 1024, 512, act, order, results, ctypes.byref(n)) == 0
+        assert lib.ep_adapter_product_grad_workspace_bytes(rows, 8, 16, 1024, 512, 1, act, order, results, ctypes.byref(n)) == 0
         return n.value
 
     every = _lib.EP_ADAPTER_DX | _lib.EP_ADAPTER_DA | _lib.EP_ADAPTER_DB
@@ -93,11 +93,11 @@ def test_grad_workspace(lib):
     assert size(1, act=2) >= size(1) + 4096 * 512 * 2  # dz
     for bad in SIZES:
         a = {"rows": 4, "A": 2, "R": 16, "K": 64, "N": 32, "act": 0, **bad}
-        refused(lib, lib.ep_adapter_product_grad_workspace_bytes(a["rows"], a["A"], a["R"], a["K"], a["N"], a["act"], 0, 7,
-                                                                 ctypes.byref(n)), "ep_adapter_product_grad_workspace_bytes")
+        refused(lib, lib.ep_adapter_product_grad_workspace_bytes(a["rows"], a["A"], a["R"], a["K"], a["N"], 1, a["act"],
+                                                                 0, 7, ctypes.byref(n)), "ep_adapter_product_grad_workspace_bytes")
     for results in (-1, 8):
-        refused(lib, lib.ep_adapter_product_grad_workspace_bytes(4, 2, 16, 64, 32, 0, 0, results, ctypes.byref(n)), "results")
-    refused(lib, lib.ep_adapter_product_grad_workspace_bytes(4, 2, 16, 64, 32, 0, 0, 7, None), "bytes is NULL")
+        refused(lib, lib.ep_adapter_product_grad_workspace_bytes(4, 2, 16, 64, 32, 1, 0, 0, results, ctypes.byref(n)), "results")
+    refused(lib, lib.ep_adapter_product_grad_workspace_bytes(4, 2, 16, 64, 32, 1, 0, 0, 7, None), "bytes is NULL")
 
 
 def dropout(lib, x=D, r=None, count=64, p=0.1, rng=D, out=D):
