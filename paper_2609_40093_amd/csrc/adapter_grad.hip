@@ -91,10 +91,9 @@ __device__ __forceinline__ void redo8(const DxArgs &a, const AdapterSide &s, int
 // dx[order[i]][k] = sum_n dz[i][n] w[n][k] + sum_j v[i][j] a_e[j][k]: i = k across the contraction, j = rows.
 template <class S>
 __global__ __launch_bounds__(S::kThreads) void adapter_dx_kernel(DxArgs a, AdapterSide s) {
-    __shared__ __attribute__((aligned(1024))) char lds[S::kStages * S::kStageBytes];
-    __shared__ Segment table[S::kJ];
-    Segment EP_LDS *segments = (Segment EP_LDS *)table;
-    __shared__ int32_t row_of[S::kJ], found;
+    __shared__ __attribute__((aligned(1024))) char lds[TileLds<S>::kBytes];
+    const TileLds<S> tile{(char EP_LDS *)lds};
+    const int32_t EP_LDS *row_of = tile.row_of();
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t tiles = (int64_t)a.row_tiles * a.col_tiles;
     int64_t t = tile_of_block(blockIdx.x, tiles * a.parts);
@@ -106,21 +105,13 @@ __global__ __launch_bounds__(S::kThreads) void adapter_dx_kernel(DxArgs a, Adapt
     tile_order(t, a.row_tiles, a.col_tiles, tr, tc);
     const int64_t i0 = (int64_t)tr * S::kJ;
     const int n_rows = a.rows - i0 < S::kJ ? (int)(a.rows - i0) : S::kJ;
-    for (int j = threadIdx.x; j < S::kJ; j += S::kThreads)
-        row_of[j] = j < n_rows ? row_at(s.order, a.rows, i0 + j) : -1;
-    if (wave == 0) {
-        const int n = find_segments<S::kJ>(s, a.rows, i0, n_rows, segments, lane);
-        if (lane == 0)
-            found = n;
-    }
-    __syncthreads();
-    const int count = __builtin_amdgcn_readfirstlane(found);
+    const int count = tile.fill(s, a.rows, i0, n_rows, wave, lane);
     const int32_t k0 = tc * S::kI;
     const int32_t main = a.w ? (a.Nw + kStepRows - 1) / kStepRows : 0;
     ChainAcross<S::kI, S::kWaves, S::FI> w;
     ChainAlong<S::kJ, S::kWaves, LowRows> z;
     w.init(reinterpret_cast<const char *>(a.w), (int64_t)a.K * 2, a.Nw, k0, wave, lane);
-    w.chain(main, s, segments, count, (uint64_t)s.A * s.R * a.K * 2, k0);
+    w.chain(main, s, tile.segments(), count, (uint64_t)s.A * s.R * a.K * 2, k0);
     const int64_t zs = (int64_t)a.Nw * 2;
     const char *zb = reinterpret_cast<const char *>(a.dz);
     z.init(a.dz_order ? zb : zb + i0 * zs, (uint32_t)((a.dz_order ? a.rows : n_rows) * zs), (int32_t)zs, wave, lane,
@@ -128,7 +119,7 @@ __global__ __launch_bounds__(S::kThreads) void adapter_dx_kernel(DxArgs a, Adapt
                const int32_t r = a.dz_order ? row_of[row] : row;
                return r < 0 ? kNowhere : (uint32_t)(r * zs);
            });
-    z.chain(main, s, segments, count, s.low + i0 * s.width, (uint64_t)n_rows * s.width * 2, 0, LowRows{});
+    z.chain(main, s, tile.segments(), count, s.low + i0 * s.width, (uint64_t)n_rows * s.width * 2, 0, LowRows{});
     int32_t steps = main + (count * (int32_t)s.chunks.d + 7) / 8;
     if (a.parts > 1) {
         const int32_t per = (steps + a.parts - 1) / a.parts, first = part * per;

@@ -174,7 +174,7 @@ __global__ __launch_bounds__(WAVES * 64) void adapter_low_rows_kernel(LowArgs a)
     x.aim(0, lane);
     const __amdgpu_buffer_rsrc_t weights =
         buffer_of(static_cast<const char *>(a.weights) + (int64_t)rt.e * a.R * kb, (uint32_t)(a.R * kb));
-    const int64_t end = lane % 32 < a.R ? kb : 0;  // of this lane's rank
+    const int32_t end = lane % 32 < a.R ? (int32_t)kb : 0;  // of this lane's rank
     const uint32_t at = (uint32_t)(lane % 32 * kb);
     const int32_t all = (a.K + kStepRows - 1) / kStepRows;
     const int32_t steps = all > wave ? (all - wave + WAVES - 1) / WAVES : 0;
@@ -190,9 +190,10 @@ __global__ __launch_bounds__(WAVES * 64) void adapter_low_rows_kernel(LowArgs a)
         for (int q = 0; q < Rows::kLoads; ++q)
             x.load(q, own + place * kStage, 0, lane);
         x.skip(WAVES);
+        const int32_t until = live ? end : 0;
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
-            const uint32_t o = live && byte + h * 32 < end ? at + (uint32_t)(byte + h * 32) : kNowhere;
+            const uint32_t o = byte + h * 32 < until ? at + (uint32_t)(byte + h * 32) : kNowhere;
             w[place][h] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(weights, (int)o, 0, 0));
         }
         byte += WAVES * kStepBytes;
@@ -280,8 +281,8 @@ struct Part : Op {
 template <class S, int GROUPS, bool ACROSS>
 __global__ __launch_bounds__(S::kThreads * GROUPS) void adapter_low_kernel(LowArgs a) {
     constexpr int kGroupBytes = S::kStages * S::kStageBytes;
-    __shared__ __attribute__((aligned(1024))) char lds[GROUPS * kGroupBytes];
-    __shared__ int32_t row_of[S::kJ];
+    __shared__ __attribute__((aligned(1024))) char lds[GROUPS * kGroupBytes + S::kJ * 4];  // one array: see TileLds
+    int32_t EP_LDS *row_of = (int32_t EP_LDS *)((char EP_LDS *)lds + GROUPS * kGroupBytes);
     const int lane = threadIdx.x & 63, all_waves = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int group = all_waves / S::kWaves, wave = all_waves % S::kWaves;
     const int rank0 = (int)blockIdx.y * S::kI;

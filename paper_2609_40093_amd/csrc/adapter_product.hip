@@ -64,10 +64,9 @@ struct WeightRow {
 template <class S, bool GATED>
 __global__ __launch_bounds__(S::kThreads) void adapter_product_kernel(ProductArgs a, AdapterSide s, int32_t row_tiles,
                                                                       int32_t col_tiles, int32_t parts) {
-    __shared__ __attribute__((aligned(1024))) char lds[S::kStages * S::kStageBytes];
-    __shared__ Segment table[S::kJ];
-    Segment EP_LDS *segments = (Segment EP_LDS *)table;
-    __shared__ int32_t row_of[S::kJ], found;
+    __shared__ __attribute__((aligned(1024))) char lds[TileLds<S>::kBytes];
+    const TileLds<S> tile{(char EP_LDS *)lds};
+    const int32_t EP_LDS *row_of = tile.row_of();
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t tiles = (int64_t)row_tiles * col_tiles;
     int64_t t = tile_of_block(blockIdx.x, tiles * parts);
@@ -79,15 +78,7 @@ __global__ __launch_bounds__(S::kThreads) void adapter_product_kernel(ProductArg
     tile_order(t, row_tiles, col_tiles, tr, tc);
     const int64_t i0 = (int64_t)tr * S::kJ;
     const int n_rows = a.rows - i0 < S::kJ ? (int)(a.rows - i0) : S::kJ;
-    for (int j = threadIdx.x; j < S::kJ; j += S::kThreads)
-        row_of[j] = j < n_rows ? row_at(s.order, a.rows, i0 + j) : -1;
-    if (wave == 0) {
-        const int n = find_segments<S::kJ>(s, a.rows, i0, n_rows, segments, lane);
-        if (lane == 0)
-            found = n;
-    }
-    __syncthreads();
-    const int count = __builtin_amdgcn_readfirstlane(found);
+    const int count = tile.fill(s, a.rows, i0, n_rows, wave, lane);
 
     const int64_t kb = (int64_t)a.K * 2;
     constexpr int kOut = GATED ? S::kI / 2 : S::kI;  // output columns of a tile
@@ -100,7 +91,7 @@ __global__ __launch_bounds__(S::kThreads) void adapter_product_kernel(ProductArg
         const int32_t n = column(row);
         return n < 0 ? kNowhere : (uint32_t)(n * kb);
     });
-    w.chain(main, s, segments, count, s.weights, (uint64_t)s.A * a.Nw * s.R * 2, a.Nw, column);
+    w.chain(main, s, tile.segments(), count, s.weights, (uint64_t)s.A * a.Nw * s.R * 2, a.Nw, column);
     // through an order from x's first row on (x is smaller than 2^31 bytes then)
     const char *xb = static_cast<const char *>(a.x);
     x.init(s.order ? xb : xb + i0 * kb, (uint32_t)((s.order ? a.rows : n_rows) * kb), (int32_t)kb, wave, lane,
@@ -110,7 +101,7 @@ __global__ __launch_bounds__(S::kThreads) void adapter_product_kernel(ProductArg
                const int32_t r = row_of[row];
                return r < 0 ? kNowhere : (uint32_t)(r * kb);
            });
-    x.chain(main, s, segments, count, s.low + i0 * s.width, (uint64_t)n_rows * s.width * 2, 0, LowRows{});
+    x.chain(main, s, tile.segments(), count, s.low + i0 * s.width, (uint64_t)n_rows * s.width * 2, 0, LowRows{});
 
     int32_t steps = main + (count * (int32_t)s.chunks.d + 7) / 8;
     if (parts > 1) {

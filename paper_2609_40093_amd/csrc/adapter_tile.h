@@ -89,6 +89,32 @@ __device__ __forceinline__ int32_t row_at(const int32_t *order, int64_t rows, in
     return r >= 0 && r < rows ? r : -1;
 }
 
+// LDS of a tile with chained operands, in one array: the stages, the segments, each row's place in memory
+// and the number of segments.  (With several __shared__ variables the compiler tells their accesses apart, and then
+// waits for every load into LDS before it reads there: the loads of a step no longer run under the step
+// before, and 16379 rows of 7168 by 4096 take 871 us instead of 772.)
+template <class S>
+struct TileLds {
+    static constexpr int kTable = S::kStages * S::kStageBytes, kRows = kTable + S::kJ * 8, kFound = kRows + S::kJ * 4;
+    static constexpr int kBytes = kFound + 16;
+    char EP_LDS *stages;
+    __device__ __forceinline__ Segment EP_LDS *segments() const { return (Segment EP_LDS *)(stages + kTable); }
+    __device__ __forceinline__ int32_t EP_LDS *row_of() const { return (int32_t EP_LDS *)(stages + kRows); }
+    // Fills the tables for rows i0 .. i0 + n - 1 and gives the number of segments.
+    __device__ __forceinline__ int fill(const AdapterSide &s, int64_t rows, int64_t i0, int n, int wave, int lane) const {
+        for (int j = threadIdx.x; j < S::kJ; j += S::kThreads)
+            row_of()[j] = j < n ? row_at(s.order, rows, i0 + j) : -1;
+        int32_t EP_LDS *found = (int32_t EP_LDS *)(stages + kFound);
+        if (wave == 0) {
+            const int count = find_segments<S::kJ>(s, rows, i0, n, segments(), lane);
+            if (lane == 0)
+                *found = count;
+        }
+        __syncthreads();
+        return __builtin_amdgcn_readfirstlane(*found);
+    }
+};
+
 // Rows along the contraction (AlongC), then the second part: the rows' low-rank values (Index: LowRows), else
 // the weights b of each column, whose row Index gives for a tile's row (-1: none).  The second
 // part's offsets take the place of the first one's, which are not needed any more.

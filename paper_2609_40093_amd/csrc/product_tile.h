@@ -119,6 +119,14 @@ struct AlongC {
     }
 };
 
+// The transposing LDS load.  The restricted pointer, once inlined, gives the load alias information, as a
+// plain load's type does; without any the compiler waits before it for every load into LDS, also those
+// that have one and a half steps to land.  (8192 rows of two 4096 x 4096 experts: dx 282 us instead of 249,
+// dw 232 instead of 218.)
+__device__ __forceinline__ s16x4 read_transposed(const s16x4 EP_LDS *__restrict__ p) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16(const_cast<s16x4 EP_LDS *>(p));
+}
+
 // A bf16 operand with rows across c: T indexes per row, loaded by W waves.
 template <int T, int W, int FRAGMENTS>
 struct AcrossC {
@@ -183,8 +191,8 @@ struct AcrossC {
     }
     __device__ __forceinline__ i32x4 read(const char EP_LDS *lds, int k, int h) const {
         const char EP_LDS *p = lds + at[k] + h * 16 * (2 * T);
-        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 EP_LDS *)p);
-        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 EP_LDS *)(p + 4 * (2 * T)));
+        const s16x4 a = read_transposed((const s16x4 EP_LDS *)p);
+        const s16x4 b = read_transposed((const s16x4 EP_LDS *)(p + 4 * (2 * T)));
         return __builtin_bit_cast(i32x4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };
