@@ -41,18 +41,28 @@ __device__ __forceinline__ void clear_rows(const LowArgs &a, const Others &o, in
             *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.low) + row * a.R + at) = u32x4{0, 0, 0, 0};
     }
 }
-// Row tile number `block` of all, the adapters' and then those of the rows without one, in contiguous
-// ranges per XCD: an adapter's weights then stay in one or two of the eight L2s.  e < 0: nothing to multiply.
-template <int PER>
-__device__ __forceinline__ RowTile low_tile(const LowArgs &a, int32_t block, int threads, bool clears, int lane) {
-    const int32_t tiles = count_row_tiles(a.offsets, a.rows, a.A, PER, lane);
+// The tile of `per` rows of one adapter, and of `cols` its column `col`, that the workgroup takes; e < 0: none.  Each
+// XCD takes a contiguous eighth of the tiles, so that an adapter's weights stay in one or two of the eight L2s; the
+// workgroups left over clear the rows without an adapter.  (Dealt out together with those, the adapters'
+// tiles leave an XCD idle and come twice to compute units of others: 8192 rows of 4096, a quarter without, 38 us
+// instead of 26.)
+__device__ __forceinline__ RowTile low_tile(const LowArgs &a, int32_t per, int32_t cols, int32_t &col, int threads, int lane) {
+    const int32_t block = (int32_t)blockIdx.x;
+    const int32_t tiles = count_row_tiles(a.offsets, a.rows, a.A, per, lane) * cols;
+    const int32_t t = (int32_t)tile_of_block(block, tiles);
+    if (t >= 0) {
+        col = t % cols;
+        return find_row_tile(a.offsets, a.rows, a.A, per, t / cols, lane);
+    }
+    const int32_t spare = block - (tiles + 7) / 8 * 8;
     const Others o(a);
-    const int64_t t = tile_of_block(block, tiles + (o.count + PER - 1) / PER);
-    if (t < tiles)
-        return t < 0 ? RowTile{-1, 0, 0} : find_row_tile(a.offsets, a.rows, a.A, PER, (int32_t)t, lane);
-    if (clears)
-        clear_rows(a, o, (t - tiles) * PER, PER, threads);
+    if (spare >= 0 && spare < (o.count + per - 1) / per)
+        clear_rows(a, o, (int64_t)spare * per, per, threads);
     return {-1, 0, 0};
+}
+// All tiles, the rows without an adapter being one more adapter's, in whole eighths.
+dim3 low_grid(const LowArgs &a, int per, int cols) {
+    return dim3((unsigned)((row_tiles_most(a.rows, a.A + 1, per) * cols + 7) / 8 * 8 + 8));
 }
 
 // N neighbouring values (4 or 8) from rank on of a row: N / 2 words per array.
@@ -85,10 +95,11 @@ constexpr int kFewWaves = 16, kFewRows = 16, kFewRanks = 16;
 __global__ __launch_bounds__(kFewWaves * 64) void adapter_low_few_kernel(LowArgs a) {
     __shared__ f32x4 sums[kFewWaves][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int rank0 = (int)blockIdx.y * kFewRanks;
-    const RowTile rt = low_tile<kFewRows>(a, (int32_t)blockIdx.x, kFewWaves * 64, blockIdx.y == 0, lane);
+    int32_t col;
+    const RowTile rt = low_tile(a, kFewRows, (a.R + kFewRanks - 1) / kFewRanks, col, kFewWaves * 64, lane);
     if (rt.e < 0)
         return;
+    const int rank0 = col * kFewRanks;
     const int g = lane / 16;  // which 16 bytes of a fragment's 64 this lane takes
     const int rank = rank0 + lane % 16;
     const bool has_a = rank < a.R;
@@ -146,7 +157,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void adapter_low_few_kernel(LowArgs
 // there), the weights, which no other wave of the workgroup needs, into registers.  No wave waits for another:
 // each has kDeep steps on their way, and as loads return in order, as many of the weights' as of the
 // rows'.  (3440 rows of 6656, 8 ranks: 15 us, as a tile of product_tile.h 21 to 27.  With 64 ranks the
-// weights' loads, which touch a cache line per rank, take longer than the tile's: 16379 rows of 7168 132 us, 78.)
+// weights' loads, which touch a cache line per rank, take longer than the tile's: 16379 rows of 7168 132 us, 103.)
 constexpr int kDeep = 5, kDeepRows = 32;
 
 template <int WAVES>
@@ -156,7 +167,8 @@ __global__ __launch_bounds__(WAVES * 64) void adapter_low_rows_kernel(LowArgs a)
     static_assert((kDeep - 1) * kLoads < 64 && 4096 <= kDeep * kStage, "");
     __shared__ __attribute__((aligned(1024))) char lds[WAVES * kDeep * kStage];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const RowTile rt = low_tile<kDeepRows>(a, (int32_t)blockIdx.x, WAVES * 64, blockIdx.y == 0, lane);
+    int32_t col;
+    const RowTile rt = low_tile(a, kDeepRows, 1, col, WAVES * 64, lane);
     if (rt.e < 0)
         return;
     const int64_t kb = (int64_t)a.K * 2;
@@ -249,54 +261,33 @@ __global__ __launch_bounds__(WAVES * 64) void adapter_low_rows_kernel(LowArgs a)
 
 // As many waves per workgroup as fill the compute units' LDS: six per compute unit of 20 KiB each.
 hipError_t launch_rows(const LowArgs &a, hipStream_t stream) {
-    // every row is one of an adapter or one of none, which make up to two more tiles than an adapter would
-    const dim3 grid((unsigned)row_tiles_most(a.rows, a.A + 2, kDeepRows) + 8);
-    const double tiles = row_tiles_likely(a.rows, a.A, kDeepRows);
+    const dim3 grid = low_grid(a, kDeepRows, 1);
+    const int64_t tiles = a.rows / kDeepRows + a.A;
 #define EP_CALL(W) launch_traced("adapter_low", adapter_low_rows_kernel<W>, grid, W * 64, stream, a)
     return tiles <= kCus ? EP_CALL(6) : tiles <= 2 * kCus ? EP_CALL(3) : EP_CALL(2);
 #undef EP_CALL
 }
 
 // ---- many rows, more ranks or weights across the contraction ------------------------------
-// An operand of which a group has `own` steps; the ones behind bring zeros.  (They lie past the
-// contraction's end, where the operand's own range check does not hold.)
-template <class Op>
-struct Part : Op {
-    int32_t own;
-    __device__ __forceinline__ void part(int32_t first, int32_t steps) {
-        Op::skip(first);
-        own = steps;
-    }
-    __device__ __forceinline__ void begin(bool live) {
-        Op::begin(live && own > 0);
-        --own;
-    }
-};
-
-// A workgroup's GROUPS groups of waves take every GROUPS-th part of the contraction each, with LDS stages of
-// their own, and are added up in order.  (A step of so small a tile takes 0.5 us whatever it holds,
-// which is how long its loads, its two barriers and its LDS reads take one after the other: 8192 rows of
-// 4096, 16 ranks, with one group per workgroup 36 us, 61 where the rows come from HBM.)
 // ACROSS: the weights are [A][K][R], else [A][R][K].
-template <class S, int GROUPS, bool ACROSS>
-__global__ __launch_bounds__(S::kThreads * GROUPS) void adapter_low_kernel(LowArgs a) {
-    constexpr int kGroupBytes = S::kStages * S::kStageBytes;
-    __shared__ __attribute__((aligned(1024))) char lds[GROUPS * kGroupBytes + S::kJ * 4];  // one array: see TileLds
-    int32_t EP_LDS *row_of = (int32_t EP_LDS *)((char EP_LDS *)lds + GROUPS * kGroupBytes);
-    const int lane = threadIdx.x & 63, all_waves = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int group = all_waves / S::kWaves, wave = all_waves % S::kWaves;
-    const int rank0 = (int)blockIdx.y * S::kI;
-    const RowTile rt = low_tile<S::kJ>(a, (int32_t)blockIdx.x, S::kThreads * GROUPS, blockIdx.y == 0, lane);
+template <class S, bool ACROSS>
+__global__ __launch_bounds__(S::kThreads) void adapter_low_kernel(LowArgs a, int32_t per) {
+    constexpr int kBytes = S::kStages * S::kStageBytes;
+    __shared__ __attribute__((aligned(1024))) char lds[kBytes + S::kJ * 4];  // one array: see TileLds
+    int32_t EP_LDS *row_of = (int32_t EP_LDS *)((char EP_LDS *)lds + kBytes);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int32_t col;
+    const RowTile rt = low_tile(a, per, (a.R + S::kI - 1) / S::kI, col, S::kThreads, lane);
     if (rt.e < 0)
         return;
-    for (int j = threadIdx.x; j < S::kJ; j += S::kThreads * GROUPS)
+    const int rank0 = col * S::kI;
+    for (int j = threadIdx.x; j < S::kJ; j += S::kThreads)
         row_of[j] = j < rt.n ? row_at(a.order, a.rows, rt.row0 + j) : -1;
     __syncthreads();
     const int64_t kb = (int64_t)a.K * 2;
     const char *weights = static_cast<const char *>(a.weights) + (int64_t)rt.e * a.R * kb;
     const char *xb = static_cast<const char *>(a.x);
-    char EP_LDS *own = (char EP_LDS *)lds + group * kGroupBytes;
-    Part<AlongC<S::kJ, S::kWaves>> x;
+    AlongC<S::kJ, S::kWaves> x;
     // through an order from x's first row on (x is smaller than 2^31 bytes then)
     x.init(a.order ? xb : xb + rt.row0 * kb, (uint32_t)((a.order ? a.rows : rt.n) * kb), (int32_t)kb, wave, lane,
            [&](int row) -> uint32_t {
@@ -304,44 +295,19 @@ __global__ __launch_bounds__(S::kThreads * GROUPS) void adapter_low_kernel(LowAr
                return r < 0 ? kNowhere : (uint32_t)(r * kb);
            });
     f32x16 acc[S::FI][S::FJ] = {};
-    // every group the same number of steps, for the barriers
-    const int32_t all = (a.K + kStepRows - 1) / kStepRows, steps = (all + GROUPS - 1) / GROUPS;
-    const int32_t first = group * steps < all ? group * steps : all, mine = all - first < steps ? all - first : steps;
-    x.part(first, mine);
+    const int32_t steps = (a.K + kStepRows - 1) / kStepRows;
     if constexpr (ACROSS) {
-        Part<AcrossC<S::kI, S::kWaves, S::FI>> w;
+        AcrossC<S::kI, S::kWaves, S::FI> w;
         w.init(weights, (int64_t)a.R * 2, a.K, rank0, wave, lane);
-        w.part(first, mine);
-        tile_product<S, Mul::kBf16>(w, x, steps, own, wave, lane, acc);
+        tile_product<S, Mul::kBf16>(w, x, steps, (char EP_LDS *)lds, wave, lane, acc);
     } else {
-        Part<AlongC<S::kI, S::kWaves>> w;
+        AlongC<S::kI, S::kWaves> w;
         w.init(weights, (uint32_t)(a.R * kb), (int32_t)kb, wave, lane,
                [&](int row) -> uint32_t { return rank0 + row < a.R ? (uint32_t)((rank0 + row) * kb) : kNowhere; });
-        w.part(first, mine);
-        tile_product<S, Mul::kBf16>(w, x, steps, own, wave, lane, acc);
-    }
-    if constexpr (GROUPS > 1) {
-        static_assert(S::kWaves * S::FI * S::FJ * 4096 <= kGroupBytes, "a group's sums fit its stages");
-        f32x16 EP_LDS *sums = reinterpret_cast<f32x16 EP_LDS *>(own);
-        if (group > 0)
-#pragma unroll
-            for (int i = 0; i < S::FI; ++i)
-#pragma unroll
-                for (int j = 0; j < S::FJ; ++j)
-                    sums[((wave * S::FI + i) * S::FJ + j) * 64 + lane] = acc[i][j];
-        __syncthreads();
-        if (group > 0)
-            return;
-#pragma unroll
-        for (int g = 1; g < GROUPS; ++g)
-#pragma unroll
-            for (int i = 0; i < S::FI; ++i)
-#pragma unroll
-                for (int j = 0; j < S::FJ; ++j)
-                    acc[i][j] += sums[g * (kGroupBytes / 64) + ((wave * S::FI + i) * S::FJ + j) * 64 + lane];
+        tile_product<S, Mul::kBf16>(w, x, steps, (char EP_LDS *)lds, wave, lane, acc);
     }
     const float scale = a.scale ? a.scale[rt.e] : 1.f;
-    tile_results<S>(acc, own, wave, lane, [&](int row, int col, const float *v) {
+    tile_results<S>(acc, (char EP_LDS *)lds, wave, lane, [&](int row, int col, const float *v) {
         const int rank = rank0 + col;
         if (row >= rt.n || rank >= a.R)
             return;
@@ -353,20 +319,28 @@ __global__ __launch_bounds__(S::kThreads * GROUPS) void adapter_low_kernel(LowAr
     });
 }
 
-// 64 ranks by 32 rows, or by 64 where those are more than the compute units: one workgroup of four groups per
-// compute unit (144 and 128 KiB of LDS), and with more tiles still two of two groups.
-typedef TileShape<64, 32, 2, 1, 3> Low32;
-typedef TileShape<64, 64, 2, 2, 2> Low64;
+// 64 ranks by `per` rows, as many as leave every compute unit a tile (and with more than 128 every one of them
+// two, three and so on): a tile takes as long as its loads, and a compute unit that has one tile more than the others takes
+// all that time more.  In the smallest shape that holds them, of which two workgroups fit a compute unit's LDS.
+// (16379 rows of 7168, eight adapters, in tiles of 64 rows, which are 260: 127 us, 103 in tiles of 128.)
+typedef TileShape<64, 32, 2, 1, 5> Low32;
+typedef TileShape<64, 64, 2, 2, 3> Low64;
+typedef TileShape<64, 128, 2, 4, 3> Low128;
+
+int tile_rows(int64_t rows, int32_t A, int32_t cols) {
+    const int64_t partly = A > 1 ? (int64_t)A * cols : 0;  // every adapter's last tile may be nearly empty
+    const int64_t turns = (rows * cols / Low128::kJ + partly + kCus) / kCus;
+    const int64_t whole = turns * kCus - partly;
+    return std::clamp((int)((rows * cols + whole - 1) / whole + 7) / 8 * 8, Low32::kJ, Low128::kJ);
+}
 
 template <bool ACROSS>
 hipError_t launch_tiles(const LowArgs &a, hipStream_t stream) {
-    const auto grid = [&](int per) {
-        return dim3((unsigned)row_tiles_most(a.rows, a.A + 2, per) + 8, (unsigned)((a.R + 63) / 64));
-    };
-    const auto tiles = [&](int per) { return row_tiles_likely(a.rows, a.A, per) * ((a.R + 63) / 64); };
-#define EP_CALL(S, G) \
-    launch_traced("adapter_low", adapter_low_kernel<S, G, ACROSS>, grid(S::kJ), S::kThreads * G, stream, a)
-    return tiles(Low32::kJ) <= kCus ? EP_CALL(Low32, 4) : tiles(Low64::kJ) <= kCus ? EP_CALL(Low64, 4) : EP_CALL(Low64, 2);
+    const int32_t cols = (a.R + 63) / 64;
+    const int per = tile_rows(a.rows, a.A, cols);
+    const dim3 grid = low_grid(a, per, cols);
+#define EP_CALL(S) launch_traced("adapter_low", adapter_low_kernel<S, ACROSS>, grid, S::kThreads, stream, a, per)
+    return per <= Low32::kJ ? EP_CALL(Low32) : per <= Low64::kJ ? EP_CALL(Low64) : EP_CALL(Low128);
 #undef EP_CALL
 }
 
@@ -380,9 +354,7 @@ hipError_t launch_adapter_low(const LowArgs &a, hipStream_t stream) {
     const bool far = a.order && a.rows * a.K * 2 > INT32_MAX;  // rows that a tile cannot address
     if (far || a.rows / a.A < 24 || a.rows < 2048)
         return launch_traced("adapter_low", adapter_low_few_kernel,
-                             dim3((unsigned)row_tiles_most(a.rows, a.A + 2, kFewRows) + 8,
-                                  (unsigned)((a.R + kFewRanks - 1) / kFewRanks)),
-                             kFewWaves * 64, stream, a);
+                             low_grid(a, kFewRows, (a.R + kFewRanks - 1) / kFewRanks), kFewWaves * 64, stream, a);
     return a.R <= 32 ? launch_rows(a, stream) : launch_tiles<false>(a, stream);
 }
 

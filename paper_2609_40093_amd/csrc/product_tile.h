@@ -57,6 +57,7 @@ __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, uint32_t o
 // there are waves is loaded by several waves alike, so that every wave counts the same.
 template <int T, int W>
 constexpr int loads_per_wave() {
+    static_assert(T / 8 % W == 0 || W % (T / 8) == 0, "every wave loads as much");
     return T / 8 > W ? T / 8 / W : 1;
 }
 
@@ -487,7 +488,7 @@ __device__ __forceinline__ int32_t count_row_tiles(const int32_t *offsets, int64
         if (e0 + lane < E) {
             int64_t b, t;
             expert_rows(offsets, rows, e0 + lane, b, t);
-            n = (int32_t)((t - b + per - 1) / per);
+            n = (int32_t)((uint32_t)(t - b + per - 1) / (uint32_t)per);
         }
         total += __builtin_amdgcn_readlane(wave_inclusive_scan(n), 63);
     }
@@ -501,7 +502,7 @@ __device__ __forceinline__ RowTile find_row_tile(const int32_t *offsets, int64_t
         int64_t b = 0, t = 0;
         if (e0 + lane < E)
             expert_rows(offsets, rows, e0 + lane, b, t);
-        const int32_t n = (int32_t)((t - b + per - 1) / per);
+        const int32_t n = (int32_t)((uint32_t)(t - b + per - 1) / (uint32_t)per);
         const int32_t incl = wave_inclusive_scan(n);
         const uint64_t past = __ballot(before + incl > idx);
         if (past) {
