@@ -361,10 +361,13 @@ hipError_t launch_join(const FewArgs &f, hipStream_t stream) {
 
 }  // namespace
 
-// Measured, us, this way and by adapter_product.hip: 523 rows of 50 adapters, rank 64, 512 x 2048 20 / 43, 1041 rows
-// 3584 x 1536 45 / 58, 2195 rows 5520 x 512 63 / 80, 1460 rows 2560 x 2048 75 / 74, 3192 rows 1568 x 1248 51 / 50,
-// 4673 rows gated 1056 x 448 44 / 36, 3096 rows 512 x 3080 69 / 42.
-bool adapter_few(int64_t rows, int32_t N, int32_t act) { return rows * N * (act == EP_ACT_SWIGLU ? 2 : 1) <= 2300000; }
+// Measured, us, this way and by adapter_product.hip: 337 rows of 50 adapters, gated, 1024 x 2640 24 / 30, 998 rows
+// 4568 x 1056 36 / 43, 1172 rows 1536 x 2952 38 / 36, 3429 rows 3496 x 376 41 / 42, 3696 rows 6328 x 496 78 / 68, 2965
+// rows 1664 x 1576 52 / 41; without W 2491 rows 3320 x 800 16 / 20, 5600 rows 3616 x 696 33 / 32, 9340 rows 4096 x 512
+// 49 / 32.  (A row costs about as much as 256 results do: its low-rank values in parts.)
+bool adapter_few(int64_t rows, int32_t N, bool base, int32_t act) {
+    return rows * ((act == EP_ACT_SWIGLU ? 2 : 1) * (int64_t)N + 256) <= (base ? 2300000 : 4000000);
+}
 
 size_t adapter_few_bytes(int64_t rows, int32_t R, int32_t K, int32_t N, bool base, int32_t act) {
     const bool gated = act == EP_ACT_SWIGLU;
