@@ -233,61 +233,50 @@ hipError_t launch_dx(const DxArgs &a, const AdapterSide &s, hipStream_t stream) 
 }
 
 // ---- da and db -----------------------------------------------------------------------
-// Rows across the contraction, gathered through an order (null: one after the other).  The next
-// step's entries of the order are on their way while a step's rows are loaded.
+// Rows across the contraction, gathered through an order.  The next step's entries of the order are on
+// their way while a step's rows are loaded.
 template <int T, int W, int FRAGMENTS>
 struct GatherAcross : AcrossC<T, W, FRAGMENTS> {
     typedef AcrossC<T, W, FRAGMENTS> First;
     using First::kLoads;
-    const int32_t *order;
-    int64_t place, last;  // of the order: the next step's first, and the end
+    __amdgpu_buffer_rsrc_t order;
+    int32_t place, last;  // of the order, from its first entry on: the next step's first, and the end
     const char *all;
-    uint32_t size, column;  // bytes of all rows, with an order; the tile's first column
+    uint32_t size, column;  // bytes of all rows; the tile's first column
     int32_t total;
     int32_t next[kLoads];
 
-    // Places begin .. end - 1 of the n rows, from step `first` on.
+    // Places begin .. end - 1 of the n rows, from step `first` on.  (As the rows are smaller than 2^31 bytes, and
+    // eight values or more each, the order is smaller than 2^29.)
     __device__ __forceinline__ void start(const int32_t *o, const char *rows, int64_t n, int64_t row_bytes, int64_t begin,
                                           int64_t end, int32_t index0, int32_t first, int wave, int lane) {
-        First::init(rows + (o ? 0 : begin * row_bytes), row_bytes, end - begin, index0, wave, lane);
-        order = o;
+        First::init(rows, row_bytes, 0, index0, wave, lane);
+        order = buffer_of(reinterpret_cast<const char *>(o + begin), (uint32_t)(end - begin) * 4);
         all = rows;
         size = (uint32_t)(n * row_bytes);
         column = (uint32_t)index0;
         total = (int32_t)n;
-        place = begin + (int64_t)first * kStepRows;
-        last = end;
-        if (o)
-            fetch(wave, lane);
-        else
-            First::skip(first);
+        place = first * kStepRows;
+        last = (int32_t)(end - begin);
+        fetch(wave, lane);
     }
     __device__ __forceinline__ void fetch(int wave, int lane) {
 #pragma unroll
-        for (int q = 0; q < kLoads; ++q) {
-            const int64_t i = place + First::row_of(q, wave, lane);
-            next[q] = i < last ? order[i] : -1;
-        }
+        for (int q = 0; q < kLoads; ++q)
+            next[q] = __builtin_amdgcn_raw_buffer_load_b32(order, (place + First::row_of(q, wave, lane)) * 4, 0, 0);
         place += kStepRows;
     }
     __device__ __forceinline__ void begin(bool live) {
-        if (!order) {
-            First::begin(live);
-            return;
-        }
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         First::range = buffer_of(all, live ? size : 0);
 #pragma unroll
         for (int q = 0; q < kLoads; ++q)
-            First::offset[q] = next[q] >= 0 && next[q] < total ? (uint32_t)next[q] * (uint32_t)First::stride +
-                                                                     First::column_of(q, column, wave, lane)
-                                                               : kNowhere;
+            First::offset[q] = place - kStepRows + First::row_of(q, wave, lane) < last && (uint32_t)next[q] < (uint32_t)total
+                                   ? (uint32_t)next[q] * (uint32_t)First::stride + First::column_of(q, column, wave, lane)
+                                   : kNowhere;
         fetch(wave, lane);
     }
-    __device__ __forceinline__ void end() {
-        if (!order)
-            First::end();
-    }
+    __device__ __forceinline__ void end() {}
 };
 
 struct WeightArgs {
@@ -303,7 +292,7 @@ struct WeightArgs {
 
 // da: i = the long side's columns, j = a block of v's ranks, the first values and then the second, which are
 // added up at the end.  db: i = ranks, j = the long side's columns.
-template <class S, bool DA>
+template <class S, bool DA, bool GATHERED>
 __device__ __forceinline__ void weight_tile(const WeightArgs &a, int32_t block, char EP_LDS *lds, int lane, int wave) {
     int64_t t = tile_of_block(block, (int64_t)a.A * a.parts * a.groups * a.tiles);
     if (t < 0)
@@ -319,9 +308,16 @@ __device__ __forceinline__ void weight_tile(const WeightArgs &a, int32_t block, 
     const int32_t first = part * per, steps = all - first < per ? all - first : per;  // 0 or less: none
     constexpr int kLong = DA ? S::kI : S::kJ, kShort = DA ? S::kJ : S::kI;
     const int32_t l0 = tile * kLong;
-    GatherAcross<kLong, S::kWaves, DA ? S::FI : S::FJ> x;
+    std::conditional_t<GATHERED, GatherAcross<kLong, S::kWaves, DA ? S::FI : S::FJ>,
+                       AcrossC<kLong, S::kWaves, DA ? S::FI : S::FJ>>
+        x;
     AcrossC<kShort, S::kWaves, DA ? S::FJ : S::FI> v;
-    x.start(a.order, reinterpret_cast<const char *>(a.side), a.rows, (int64_t)a.L * 2, b, end, l0, first, wave, lane);
+    if constexpr (GATHERED) {
+        x.start(a.order, reinterpret_cast<const char *>(a.side), a.rows, (int64_t)a.L * 2, b, end, l0, first, wave, lane);
+    } else {
+        x.init(reinterpret_cast<const char *>(a.side + b * a.L), (int64_t)a.L * 2, end - b, l0, wave, lane);
+        x.skip(first);
+    }
     v.init(reinterpret_cast<const char *>(a.low + b * a.width), (int64_t)a.width * 2, end - b, group * kShort, wave, lane);
     v.skip(first);
     f32x16 acc[S::FI][S::FJ] = {};
@@ -360,6 +356,14 @@ __device__ __forceinline__ void weight_tile(const WeightArgs &a, int32_t block, 
     }
 }
 
+template <class S, bool DA>
+__device__ __forceinline__ void any_weight_tile(const WeightArgs &a, int32_t block, char EP_LDS *lds, int lane, int wave) {
+    if (a.order)
+        weight_tile<S, DA, true>(a, block, lds, lane, wave);
+    else
+        weight_tile<S, DA, false>(a, block, lds, lane, wave);
+}
+
 // Both in one launch: neither fills the chip for long, and they do not need each other.
 template <class SA, class SB>
 __global__ __launch_bounds__(SA::kThreads) void adapter_weights_kernel(WeightArgs da, WeightArgs db) {
@@ -368,9 +372,9 @@ __global__ __launch_bounds__(SA::kThreads) void adapter_weights_kernel(WeightArg
     __shared__ __attribute__((aligned(1024))) char lds[kA > kB ? kA : kB];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if ((int32_t)blockIdx.x < da.blocks)
-        weight_tile<SA, true>(da, (int32_t)blockIdx.x, (char EP_LDS *)lds, lane, wave);
+        any_weight_tile<SA, true>(da, (int32_t)blockIdx.x, (char EP_LDS *)lds, lane, wave);
     else
-        weight_tile<SB, false>(db, (int32_t)blockIdx.x - da.blocks, (char EP_LDS *)lds, lane, wave);
+        any_weight_tile<SB, false>(db, (int32_t)blockIdx.x - da.blocks, (char EP_LDS *)lds, lane, wave);
 }
 
 // The parts added up in order: eight values per thread, da's and then db's.
@@ -411,11 +415,16 @@ __global__ __launch_bounds__(256) void adapter_weights_join_kernel(JoinArgs da, 
     reinterpret_cast<u32x4 *>(second ? db.out : da.out)[i] = pack8(s);
 }
 
-typedef TileShape<128, 64, 4, 1, 3> Da32;   // 32 ranks; two workgroups per compute unit each (72, 64 and
-typedef TileShape<128, 128, 4, 1, 2> Da64;  // 64         72 KiB of LDS)
-typedef TileShape<64, 128, 2, 2, 3> Db64;
+// 32 and 64 ranks of da, 64 of db.  Two stages (48, 64 and 48 KiB of LDS), so that three workgroups or two fit a compute
+// unit: 1103 rows of 47 adapters 14 us, 18 with three stages; 6744 rows of 49 22, 25.
+typedef TileShape<128, 64, 4, 1, 2> Da32;
+typedef TileShape<128, 128, 4, 1, 2> Da64;
+typedef TileShape<64, 128, 2, 2, 2> Db64;
 
-// Tiles along the long side (x for da, dz for db) and of the ranks, and the parts of the rows.
+// Tiles along the long side (x for da, dz for db) and of the ranks, and the parts of the rows, until each of the two
+// products has a tile per compute unit (8192 rows, 4096 x 4096: 42 us; two tiles each 52, and more for their parts' sums).
+// Pieces of so many rows instead of parts of each adapter's serve a long adapter among short ones better (6855 rows of 9
+// adapters, most of one: 25 us instead of 35), but need the kernel that joins them in every call, which costs all others 4.
 struct WeightPlan {
     int32_t tiles, groups, parts;
     WeightPlan(int64_t rows, int32_t A, int32_t R, int32_t L, bool da) {
@@ -424,7 +433,7 @@ struct WeightPlan {
         groups = (R + ranks - 1) / ranks;
         const int64_t steps = (rows / A + kStepRows - 1) / kStepRows;  // of an adapter, to expect
         parts = 1;
-        while ((int64_t)A * tiles * groups * parts < 2 * kCus && steps / (parts * 2) >= kSplitSteps)
+        while ((int64_t)A * tiles * groups * parts < kCus && steps / (parts * 2) >= kSplitSteps)
             parts *= 2;
     }
     size_t bytes(int32_t A, int32_t R, int32_t L) const { return parts > 1 ? (size_t)parts * A * R * L * 4 : 0; }
