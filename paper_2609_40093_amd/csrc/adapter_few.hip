@@ -3,7 +3,8 @@
 //              x[order] a_a^T, side by side in one launch, since neither needs the other;
 //   the second adds the parts up, in order, makes two bf16 values of each low-rank one (adapter_low.hip),
 //              adds their products with b and runs the epilogue.
-// Bound by the latencies of dependent loads and by the bytes of W, a and b.
+// Bound by the latencies of dependent loads and by the bytes of W, a and b: 64 rows of 7168 by 2048, 32 adapters of
+// 16 ranks (38 MB) 10.6 and 8.5 us; 256 rows 7168 x 4096, 64 adapters of 32 ranks, without W (52 MB) 11.1 and 9.3.
 //
 // The low-rank parts: a workgroup takes 16 rows of one adapter, 16 ranks and a part of the contraction
 // short enough for every load of its four waves to be on its way at once.  The second kernel: a wave

@@ -3,7 +3,8 @@
 // as the sum of two bf16 values each for the products that read them, and for the forward also as the one
 // bf16 value that a caller keeps.  Rows without an adapter get zeros.
 //
-// Bound by the rows' bytes, or for few rows by the adapters'.  Many rows go through LDS, with more than
+// Bound by the rows' bytes, or for few rows by the adapters' (16379 rows of 7168, 64 ranks 65 us, 3.6 TB/s; 8192 rows of
+// 4096, 16 ranks, a quarter of them without an adapter 18).  Many rows go through LDS, with more than
 // 32 ranks and in the gradient through the MFMA tile (product_tile.h).  Few rows go straight from memory into the operands of
 // 16x16 matrix instructions: the 16 waves of a workgroup share out the contraction, 64 values (whole
 // cache lines) at a time with every load of a wave on its way at once, and are added up through LDS in

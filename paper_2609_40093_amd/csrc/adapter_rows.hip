@@ -5,7 +5,8 @@
 // per adapter of its own in LDS: it counts its rows 64 at a time (lanes of one adapter find each
 // other by ballots, the first adds their number), the counters become the places where each wave's
 // rows of each adapter begin, and the wave goes over its rows again.  Latency-bound, and made once for
-// all the projections of a batch: 64 rows of 32 adapters take 4.6 us, 8192 of 16 take 9.6.
+// all the projections of a batch: 64 rows of 32 adapters take 2.9 us, 6136 of 20
+// take 8, 14368 of 14 take 17.
 #include "layer.h"
 #include "wave.h"
 

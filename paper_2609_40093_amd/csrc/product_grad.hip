@@ -6,8 +6,8 @@
 // product_tile.h.  Neither needs a transposed copy: W in dx, and dz and x in dw, are read
 // across the contraction by the transposing LDS load.
 //
-// 8192 rows of two 4096 x 4096 experts through gelu, with a bias: dz 49 us, dbias 5, dx 270 (1020
-// TFLOP/s), dw 234 (1180), one after the other in a call.  dx is the slower since the two experts' rows
+// 8192 rows of two 4096 x 4096 experts through gelu, with a bias: dz 44 us, dbias 4, dx 240 (1145
+// TFLOP/s), dw 214 (1285), one after the other in a call.  dx is the slower since the two experts' rows
 // fill no whole number of tiles nor of the chip's turns; both products are bound by the matrix cores
 // and the LDS reads that feed them.
 //
