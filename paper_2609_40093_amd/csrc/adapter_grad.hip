@@ -65,12 +65,24 @@ struct DxArgs {
     const int32_t *dz_order;  // dz's rows; null: they are in the adapters' order
     uint16_t *dx;
     float *partial;  // parts > 1: [parts][rows][K], in the adapters' order
-    int32_t row_tiles, col_tiles, parts;
+    int32_t row_tiles, col_tiles, parts, tile_rows;
 };
 
-// The sums of place i, columns k..k+7, of their own terms alone.
-__device__ __forceinline__ void redo8(const DxArgs &a, const AdapterSide &s, int64_t i, int32_t k, float *z) {
+// The sums of place i, columns k..k+7, of their own terms alone, if others of the tile, whose first place is
+// i0, could have made them NaN.
+__device__ __forceinline__ void redo8(const DxArgs &a, const AdapterSide &s, int64_t i0, int tile_rows, int64_t i, int32_t k,
+                                      float *z) {
     const int32_t e = adapter_of(s, a.rows, i), r = row_at(a.dz_order, a.rows, i);
+    const auto broken = [&](int32_t other) {
+        const uint16_t *w = s.weights + (int64_t)other * s.R * a.K + k;
+#pragma unroll 1
+        for (int32_t j = 0; j < s.R; ++j, w += a.K)
+            if (any_not_finite(*reinterpret_cast<const u32x4 *>(w)))
+                return true;
+        return false;
+    };
+    if (!others_broken(s, a.rows, i0, tile_rows, e, broken))
+        return;
 #pragma unroll
     for (int q = 0; q < 8; ++q)
         z[q] = 0.f;
@@ -150,7 +162,7 @@ __global__ __launch_bounds__(S::kThreads) void adapter_dx_kernel(DxArgs a, Adapt
             if (r < 0)
                 return;
             if (__builtin_expect(any_nan(v, 8), false))
-                redo8(a, s, i0 + row, k, v);
+                redo8(a, s, i0, S::kJ, i0 + row, k, v);
             *reinterpret_cast<u32x4 *>(a.dx + (int64_t)r * a.K + k) = pack8(v);
         });
 }
@@ -183,7 +195,7 @@ __global__ __launch_bounds__(256) void adapter_dx_join_kernel(DxArgs a, AdapterS
                 z[q] += v[u][q / 4][q % 4];
     }
     if (__builtin_expect(any_nan(z, 8), false))
-        redo8(a, s, i, k, z);
+        redo8(a, s, i - i % a.tile_rows, a.tile_rows, i, k, z);
     *reinterpret_cast<u32x4 *>(a.dx + (int64_t)r * a.K + k) = pack8(z);
 }
 
@@ -204,7 +216,7 @@ constexpr DxTile kDxTiles[] = {{DxSize::kLarge, Large::kI, Large::kJ, kGradTiles
                                {DxSize::kTiny, TinyRows::kI, TinyRows::kJ, {true, 0.42, 0.60}}};
 struct DxPlan {
     DxSize size;
-    int32_t row_tiles, col_tiles, parts;
+    int32_t row_tiles, col_tiles, parts, tile_rows;
 };
 DxPlan plan_adapter_dx(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t main) {
     DxPlan best{};
@@ -216,7 +228,7 @@ DxPlan plan_adapter_dx(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t ma
             const double t = estimate(g.cost, (double)row_tiles * col_tiles, parts, (steps + parts - 1) / parts, rows * K);
             if (least == 0 || t < least) {
                 least = t;
-                best = {g.size, row_tiles, col_tiles, parts};
+                best = {g.size, row_tiles, col_tiles, parts, g.j};
             }
         }
     }
@@ -540,7 +552,7 @@ hipError_t launch_adapter_grad(const AdapterGradArgs &a, hipStream_t stream) {
     if (a.rows > 0 && a.dx) {
         const DxPlan plan = plan_adapter_dx(a.rows, a.A, a.R, a.K, main_steps(a.w != nullptr, Nw));
         const DxArgs d{a.rows, a.K, Nw, static_cast<const uint16_t *>(a.w), dz, dz_order, static_cast<uint16_t *>(a.dx),
-                       reinterpret_cast<float *>(base + ws.dx_sums), plan.row_tiles, plan.col_tiles, plan.parts};
+                       reinterpret_cast<float *>(base + ws.dx_sums), plan.row_tiles, plan.col_tiles, plan.parts, plan.tile_rows};
         const AdapterSide s = adapter_side(a.order, a.offsets, a.A, a.R, v, width, log, a.a);
         e = plan.size == DxSize::kLarge    ? launch_dx<Large>(d, s, stream)
             : plan.size == DxSize::kBroad  ? launch_dx<Broad>(d, s, stream)

@@ -17,9 +17,21 @@
 namespace ep {
 namespace {
 
-// The sums of place i (row r), columns n..n+7, of their own terms alone.
-__device__ __forceinline__ void redo8(const ProductArgs &a, const AdapterSide &s, int64_t i, int64_t r, int32_t n, float *z) {
+// The sums of place i (row r), columns n..n+7, of their own terms alone, if others of the tile, whose first
+// place is i0, could have made them NaN.
+__device__ __forceinline__ void redo8(const ProductArgs &a, const AdapterSide &s, int64_t i0, int tile_rows, int64_t i, int64_t r,
+                                      int32_t n, float *z) {
     const int32_t e = adapter_of(s, a.rows, i);
+    const auto broken = [&](int32_t other) {
+        const u32x4 *b = reinterpret_cast<const u32x4 *>(s.weights + ((int64_t)other * a.Nw + n) * s.R);
+#pragma unroll 1
+        for (int32_t j = 0; j < s.R; ++j)  // eight columns of R / 8 vectors, one after the other
+            if (any_not_finite(b[j]))
+                return true;
+        return false;
+    };
+    if (!others_broken(s, a.rows, i0, tile_rows, e, broken))
+        return;
 #pragma unroll 1
     for (int q = 0; q < 8; ++q) {
         float sum = 0.f;
@@ -46,12 +58,12 @@ __device__ __forceinline__ void redo8(const ProductArgs &a, const AdapterSide &s
     }
 }
 template <bool GATED>
-__device__ __forceinline__ void check8(const ProductArgs &a, const AdapterSide &s, int64_t i, int64_t r, int32_t n, float *z,
-                                       float *up) {
+__device__ __forceinline__ void check8(const ProductArgs &a, const AdapterSide &s, int64_t i0, int tile_rows, int64_t i,
+                                       int64_t r, int32_t n, float *z, float *up) {
     if (__builtin_expect(any_nan(z, 8) || (GATED && any_nan(up, 8)), false)) {
-        redo8(a, s, i, r, n, z);
+        redo8(a, s, i0, tile_rows, i, r, n, z);
         if (GATED)
-            redo8(a, s, i, r, n + a.N, up);
+            redo8(a, s, i0, tile_rows, i, r, n + a.N, up);
     }
 }
 
@@ -150,7 +162,7 @@ __global__ __launch_bounds__(S::kThreads) void adapter_product_kernel(ProductArg
         [&](int row, int, float *v, const Row &f) {
             if (f.r < 0)
                 return;
-            check8<GATED>(a, s, i0 + row, f.r, n, v, v + kPer / 2);
+            check8<GATED>(a, s, i0, S::kJ, i0 + row, f.r, n, v, v + kPer / 2);
             finish8<false, GATED>(a, columns, f.x, f.r, n, v, v + kPer / 2);
         });
 }
@@ -158,7 +170,8 @@ __global__ __launch_bounds__(S::kThreads) void adapter_product_kernel(ProductArg
 // Adds the parts of a split contraction and runs the epilogue, as the experts' product does: LANES
 // lanes add every LANES-th part of eight neighbouring results each, and are added up in a fixed order.
 template <bool GATED, int LANES>
-__global__ __launch_bounds__(256) void adapter_join_kernel(ProductArgs a, AdapterSide s, int32_t parts, FastDiv groups) {
+__global__ __launch_bounds__(256) void adapter_join_kernel(ProductArgs a, AdapterSide s, int32_t parts, int32_t tile_rows,
+                                                          FastDiv groups) {
     const int lane = threadIdx.x & 63, first = lane / (64 / LANES);
     const uint32_t at = (blockIdx.x * 4 + (threadIdx.x >> 6)) * (64 / LANES) + lane % (64 / LANES);
     const uint32_t row = groups.div(at);
@@ -200,7 +213,7 @@ __global__ __launch_bounds__(256) void adapter_join_kernel(ProductArgs a, Adapte
         }
     if (r < 0 || first != 0)
         return;
-    check8<GATED>(a, s, i, r, n, z, up);
+    check8<GATED>(a, s, i - i % tile_rows, tile_rows, i, r, n, z, up);
     Columns<false, GATED> columns;
     columns.load(a, 0, n);
     RowExtra<false> x;
@@ -224,7 +237,7 @@ hipError_t launch_tiles(const ProductArgs &a, const AdapterSide &s, const Plan &
     const int64_t groups = a.rows * (a.N / 8);
 #define EP_CALL(LANES)                                                                                                     \
     launch_traced("adapter_product_join", adapter_join_kernel<GATED, LANES>, dim3((unsigned)((groups * LANES + 255) / 256)), \
-                  256, stream, a, s, p.split.parts, fast_div((uint32_t)(a.N / 8)))
+                  256, stream, a, s, p.split.parts, S::kJ, fast_div((uint32_t)(a.N / 8)))
     return p.split.parts <= 4 ? EP_CALL(1) : EP_CALL(8);  // a lane has 4 parts on their way
 #undef EP_CALL
 }

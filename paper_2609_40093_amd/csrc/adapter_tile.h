@@ -255,18 +255,25 @@ struct ChainAcross : AcrossC<T, W, FRAGMENTS> {
 
 // ---- results that are NaN ------------------------------------------------------------
 // A tile adds zeros times the weights of the other adapters in it, which is NaN where those are
-// infinite or NaN.  Results that come out NaN are therefore summed again of their own terms alone,
-// one after the other: slow, for broken weights and for rows that are NaN anyway.
+// infinite or NaN.  Where results come out NaN and another adapter of the tile has such weights, they are summed again
+// of their own terms alone, one after the other.  (That is slow, so rows that are NaN by themselves, as a padded
+// batch may have them, are not: with 4096 such rows among 8192 of 4096 x 4096 the product took 36 ms, now 266 us.)
 __device__ __forceinline__ bool any_nan(const float *v, int n) {
     float s = 0.f;
     for (int i = 0; i < n; ++i)
         s += v[i];
     return s != s;
 }
-// The adapter that row i of the order has, -1: none.
-__device__ __forceinline__ int32_t adapter_of(const AdapterSide &s, int64_t rows, int64_t i) {
-    if (!s.offsets)
-        return 0;
+// Whether one of eight bf16 values is infinite or NaN.
+__device__ __forceinline__ bool any_not_finite(u32x4 v) {
+    bool any = false;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        any = any || (v[q] & 0x7f80u) == 0x7f80u || (v[q] & 0x7f800000u) == 0x7f800000u;
+    return any;
+}
+// The last adapter that begins at place i of the order or before, else the first.
+__device__ __forceinline__ int32_t last_before(const AdapterSide &s, int64_t rows, int64_t i) {
     int32_t a = 0, hi = s.A;
     while (hi - a > 1) {
         const int32_t mid = (a + hi) / 2;
@@ -275,6 +282,28 @@ __device__ __forceinline__ int32_t adapter_of(const AdapterSide &s, int64_t rows
         else
             hi = mid;
     }
+    return a;
+}
+// Whether an adapter with rows among places i0 .. i0 + n - 1, but not e, is broken(a).
+template <typename F>
+__device__ __forceinline__ bool others_broken(const AdapterSide &s, int64_t rows, int64_t i0, int n, int32_t e, F broken) {
+    if (!s.offsets)
+        return false;
+#pragma unroll 1
+    for (int32_t a = last_before(s, rows, i0); a < s.A; ++a) {
+        const int64_t begin = clamp_row(s.offsets[a], rows), end = clamp_row(s.offsets[a + 1], rows);
+        if (begin >= i0 + n)
+            break;
+        if (a != e && end > begin && end > i0 && broken(a))
+            return true;
+    }
+    return false;
+}
+// The adapter that row i of the order has, -1: none.
+__device__ __forceinline__ int32_t adapter_of(const AdapterSide &s, int64_t rows, int64_t i) {
+    if (!s.offsets)
+        return 0;
+    const int32_t a = last_before(s, rows, i);
     return i >= clamp_row(s.offsets[a], rows) && i < clamp_row(s.offsets[a + 1], rows) ? a : -1;
 }
 

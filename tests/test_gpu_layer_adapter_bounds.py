@@ -155,3 +155,36 @@ def test_an_order_over_more_than_2_gib():
         ref.within(a, b.double(), 4 * ref.BF16 * b.double().abs() + 2.0 ** -8 * float(b.double().abs().mean()), what)
     with pytest.raises(ep.EPError):
         ep.adapter_product(x, s["a"], s["b"], by, w=torch.zeros((16, K), dtype=torch.bfloat16, device="cuda"))
+
+
+# few results; one pass over the contraction; the contraction in parts
+@pytest.mark.parametrize("rows,K,N", [(300, 264, 136), (5000, 136, 1032), (2600, 6000, 1032), (4500, 5632, 1024)])
+@pytest.mark.parametrize("act", ["none", "swiglu"])
+def test_broken_rows_and_adapters_of_every_path(rows, K, N, act):
+    """NaN rows (a padded batch's) and adapters with infinities: the other rows keep their values."""
+    say(f"adapters: NaN rows and broken adapters rows={rows} K={K} N={N} {act}")
+    A, R = 6, 16
+    s = ar.make(ar.random_ids(rows, A, rows), A, R, K, N, rows, act)
+    by, wide = ar.rows_of(s), s["b"].shape[1]
+    d, low = ref.normal((rows, N), ref.gen(1)), ref.normal((rows, R), ref.gen(2))
+    pre = None if act == "none" else ref.normal((rows, wide), ref.gen(3))
+    more = {"w": s["w"], "scale": s["scale"], "act": act}
+    clean = ep.adapter_product(s["x"], s["a"], s["b"], by, **more).out
+    dx = ep.adapter_product_grad(s["x"], s["a"], s["b"], low, d, by, pre=pre, **more).dx
+    none = s["ids"] < 0
+    s["x"][none], d[none] = float("nan"), float("nan")
+    whole = ~none
+    got = ep.adapter_product(s["x"], s["a"], s["b"], by, **more).out
+    grad = ep.adapter_product_grad(s["x"], s["a"], s["b"], low, d, by, pre=pre, **more)
+    assert torch.equal(got[whole], clean[whole]) and torch.equal(grad.dx[whole], dx[whole])
+    assert torch.isnan(got[none]).all() and torch.isnan(grad.dx[none]).all()
+    assert torch.isfinite(grad.da).all() and torch.isfinite(grad.db).all()
+    a, b = s["a"].clone(), s["b"].clone()
+    a[2, 1], b[4, :, 3] = float("inf"), float("nan")
+    got = ep.adapter_product(s["x"], a, b, by, **more).out
+    grad = ep.adapter_product_grad(s["x"], a, b, low, d, by, pre=pre, **more)
+    assert torch.isnan(got[none | (s["ids"] == 4)]).all() and torch.isnan(grad.dx[none | (s["ids"] == 4)]).all()
+    for bad, what, want in ((got, "y", clean), (grad.dx, "dx", dx)):
+        whole = ~none & (s["ids"] != 2) & (s["ids"] != 4)
+        # summed again in another order: the result's rounding, and sums of up to 6000 terms of about 1 / sqrt(6000)
+        ref.within(bad[whole], want[whole].double(), want[whole].double().abs() * 2 * ref.BF16 + 1e-2, what)
