@@ -353,9 +353,12 @@ hipError_t launch_adapter_low(const LowArgs &a, hipStream_t stream) {
     if (a.across)
         return launch_tiles<true>(a, stream);
     const bool far = a.order && a.rows * a.K * 2 > INT32_MAX;  // rows that a tile cannot address
-    if (far || a.rows / a.A < 24 || a.rows < 2048)
-        return launch_traced("adapter_low", adapter_low_few_kernel,
-                             low_grid(a, kFewRows, (a.R + kFewRanks - 1) / kFewRanks), kFewWaves * 64, stream, a);
+    // Few rows: at most a workgroup of theirs per compute unit.  Measured, us, that way and by tiles, of 512 and 5000
+    // values a row: 3000 rows of 20 adapters, 16 ranks (198 workgroups) 4.2 10.7 / 6.8 14.0, 5000 (322) 6.4 19.8 / 6.9 14.8;
+    // 450 rows, 64 ranks (152) 4.2 9.7 / 5.3 18.6, 2000 (540) 8.1 25.2 / 5.1 18.8; 1500 rows of 300, 64 ranks 28 61 / 9.8 65.
+    const int32_t cols = (a.R + kFewRanks - 1) / kFewRanks;
+    if (far || row_tiles_likely(a.rows, a.A, kFewRows) * cols <= kCus)
+        return launch_traced("adapter_low", adapter_low_few_kernel, low_grid(a, kFewRows, cols), kFewWaves * 64, stream, a);
     return a.R <= 32 ? launch_rows(a, stream) : launch_tiles<false>(a, stream);
 }
 
