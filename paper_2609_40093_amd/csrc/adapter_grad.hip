@@ -124,7 +124,7 @@ __global__ __launch_bounds__(S::kThreads) void adapter_dx_kernel(DxArgs a, Adapt
     const int32_t k0 = tc * S::kI;
     const int32_t main = a.w ? (a.Nw + kStepRows - 1) / kStepRows : 0;
     ChainAcross<S::kI, S::kWaves, S::FI> w;
-    ChainAlong<S::kJ, S::kWaves, LowRows> z;
+    ChainAlong<S::kJ, S::kWaves, LowRows<true>> z;
     w.init(reinterpret_cast<const char *>(a.w), (int64_t)a.K * 2, a.Nw, k0, wave, lane);
     w.chain(main, s, tile.segments(), count, (uint64_t)s.A * s.R * a.K * 2, k0);
     const int64_t zs = (int64_t)a.Nw * 2;
@@ -134,7 +134,7 @@ __global__ __launch_bounds__(S::kThreads) void adapter_dx_kernel(DxArgs a, Adapt
                const int32_t r = a.dz_order ? row_of[row] : row;
                return r < 0 ? kNowhere : (uint32_t)(r * zs);
            });
-    z.chain(main, s, tile.segments(), count, s.low + i0 * s.width, (uint64_t)n_rows * s.width * 2, 0, LowRows{});
+    z.chain(main, s, tile.segments(), count, s.low + i0 * s.width, (uint64_t)n_rows * s.width * 2, 0, LowRows<true>{});
     int32_t steps = main + (count * (int32_t)s.chunks.d + 7) / 8;
     if (a.parts > 1) {
         const int32_t per = (steps + a.parts - 1) / a.parts, first = part * per;

@@ -70,6 +70,7 @@ __device__ __forceinline__ void check8(const ProductArgs &a, const AdapterSide &
 // The weights' row of a tile's row, -1: none (gated: 8 gate rows beside their 8 up rows, as in the experts' product).
 template <bool GATED>
 struct WeightRow {
+    static constexpr bool kLow = false, kSkips = false;
     int32_t n0, N;
     __device__ __forceinline__ int32_t operator()(int row) const {
         const int32_t n = GATED ? n0 + (row >> 4) * 8 + (row & 7) : n0 + row;
@@ -102,7 +103,7 @@ __global__ __launch_bounds__(S::kThreads) void adapter_product_kernel(ProductArg
     const int32_t main = a.w ? (int32_t)((kb + kStepBytes - 1) / kStepBytes) : 0;
     const WeightRow<GATED> column{n0, a.N};
     ChainAlong<S::kI, S::kWaves, WeightRow<GATED>> w;
-    ChainAlong<S::kJ, S::kWaves, LowRows> x;
+    ChainAlong<S::kJ, S::kWaves, LowRows<false>> x;
     w.init(static_cast<const char *>(a.w), (uint32_t)(a.Nw * kb), (int32_t)kb, wave, lane, [&](int row) -> uint32_t {
         const int32_t n = column(row);
         return n < 0 ? kNowhere : (uint32_t)(n * kb);
@@ -117,7 +118,7 @@ __global__ __launch_bounds__(S::kThreads) void adapter_product_kernel(ProductArg
                const int32_t r = row_of[row];
                return r < 0 ? kNowhere : (uint32_t)(r * kb);
            });
-    x.chain(main, s, tile.segments(), count, s.low + i0 * s.width, (uint64_t)n_rows * s.width * 2, 0, LowRows{});
+    x.chain(main, s, tile.segments(), count, s.low + i0 * s.width, (uint64_t)n_rows * s.width * 2, 0, LowRows<false>{});
 
     int32_t steps = main + (count * (int32_t)s.chunks.d + 7) / 8;
     if (parts > 1) {

@@ -115,16 +115,31 @@ struct TileLds {
     }
 };
 
+// This lane's number, in the large tiles unknown to the compiler anew in every step: what the second part's steps make
+// of it is not kept in registers through the first part's, where those tiles have none to spare.
+template <int T>
+__device__ __forceinline__ int lane_of_step() {
+    int lane = threadIdx.x & 63;
+    if (T >= 256)
+        asm volatile("" : "+v"(lane));
+    return lane;
+}
+
 // Rows along the contraction (AlongC), then the second part: the rows' low-rank values (Index: LowRows), else
 // the weights b of each column, whose row Index gives for a tile's row (-1: none).  The second
 // part's offsets take the place of the first one's, which are not needed any more.
-struct LowRows {};
+// SKIPS: branches round places that none of a wave's lanes has, where the gradient's tiles gain from them (762 rows of 21
+// adapters 36 us, 37.5 without); the product's do without (7393 rows of 62 adapters, 64 ranks 117 us, 129 with them).
+template <bool SKIPS>
+struct LowRows {
+    static constexpr bool kLow = true, kSkips = SKIPS;
+};
 template <int T, int W, typename Index>
 struct ChainAlong : AlongC<T, W> {
     typedef AlongC<T, W> First;
     using First::kLoads;
     static constexpr bool kChained = true;
-    static constexpr bool LOW = std::is_same<Index, LowRows>::value;
+    static constexpr bool LOW = Index::kLow;
     int32_t first;        // steps of the first part left
     int32_t chunk, most;  // 16-byte chunks of the second part: the next step's first, and all
     const Segment EP_LDS *segments;
@@ -159,28 +174,57 @@ struct ChainAlong : AlongC<T, W> {
             First::begin(live);
             return;
         }
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        const int lane = lane_of_step<T>(), wave = threadIdx.x >> 6;
         First::range = buffer_of(base2, live ? size2 : 0);
         First::bytes = kStepBytes;  // every chunk of the step is looked up
+        if constexpr (Index::kSkips) {
 #pragma unroll
-        for (int q = 0; q < kLoads; ++q) {
-            const int row = First::load_number(wave, q) * 8 + lane / 8;
-            const int32_t c = chunk + First::swizzle(row, lane % 8);
-            uint32_t o = kNowhere;
-            if (live && c < most) {
-                const uint32_t at = side->chunks.div((uint32_t)c), in = (uint32_t)c - at * side->chunks.d;
-                const Segment s = segments[at];
-                if constexpr (LOW) {
+            for (int q = 0; q < kLoads; ++q) {
+                const int row = First::load_number(wave, q) * 8 + lane / 8;
+                const int32_t c = chunk + First::swizzle(row, lane % 8);
+                uint32_t o = kNowhere;
+                if (live && c < most) {
+                    const uint32_t at = side->chunks.div((uint32_t)c), in = (uint32_t)c - at * side->chunks.d;
+                    const Segment s = segments[at];
                     if (row >= (s[1] & 0xffff) && row < s[1] >> 16)
                         o = (uint32_t)(row * side->width + side->value_at((int32_t)in * 8)) * 2;
-                } else {
-                    const int32_t n = index(row);
-                    if (n >= 0)
-                        o = (((uint32_t)s[0] * adapter_rows + (uint32_t)n) * (uint32_t)side->R +
-                             (uint32_t)side->rank_of((int32_t)in * 8)) * 2;
                 }
+                First::offset[q] = o;
             }
-            First::offset[q] = o;
+            return;
+        }
+        // A lane's rows are of two kinds, by which chunk they bring: rows of even and of odd load numbers.
+        bool has[2];
+        Segment of[2];
+        uint32_t place[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int32_t c = chunk + First::swizzle(h * 8 + lane / 8, lane % 8);
+            has[h] = live && c < most;
+            const uint32_t at = has[h] ? side->chunks.div((uint32_t)c) : 0;
+            of[h] = segments[at];
+            place[h] = ((uint32_t)c - at * side->chunks.d) * 8;
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            place[h] = (LOW ? (uint32_t)side->value_at((int32_t)place[h])
+                            : (uint32_t)of[h][0] * adapter_rows * (uint32_t)side->R + (uint32_t)side->rank_of((int32_t)place[h])) *
+                       2;
+        const uint32_t row_bytes = (uint32_t)(LOW ? side->width : side->R) * 2;
+#pragma unroll
+        for (int q = 0; q < kLoads; ++q) {
+            const int number = First::load_number(wave, q), row = number * 8 + lane / 8;
+            const bool odd = number & 1;
+            const int32_t rows = odd ? of[1][1] : of[0][1];
+            bool here = odd ? has[1] : has[0];
+            int32_t n = row;
+            if constexpr (LOW) {
+                here = here && row >= (rows & 0xffff) && row < rows >> 16;
+            } else {
+                n = index(row);
+                here = here && n >= 0;
+            }
+            First::offset[q] = here ? (uint32_t)n * row_bytes + (odd ? place[1] : place[0]) : kNowhere;
         }
     }
     __device__ __forceinline__ void end() {
@@ -227,7 +271,7 @@ struct ChainAcross : AcrossC<T, W, FRAGMENTS> {
             First::begin(live);
             return;
         }
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        const int lane = lane_of_step<T>(), wave = threadIdx.x >> 6;
         First::range = buffer_of(reinterpret_cast<const char *>(side->weights), live ? size2 : 0);
 #pragma unroll
         for (int q = 0; q < kLoads; ++q) {
