@@ -66,6 +66,10 @@ extern "C" ep_status ep_adapter_product(const void *x_dev, int64_t rows, const i
         return fail(EP_ERR_INVALID_ARG, "ep_adapter_product: more than one adapter needs offsets");
     if (order && w_dev && rows * in_length * 2 > INT32_MAX)
         return fail(EP_ERR_INVALID_ARG, "ep_adapter_product: with an order and w, x must be smaller than 2^31 bytes");
+    if (order && rows * in_length * 2 > INT32_MAX && rows * ((rank + 15) / 16) > EP_ADAPTER_MAX_GATHERED)
+        return fail(EP_ERR_INVALID_ARG, "ep_adapter_product: with an order over x of 2^31 bytes and more, rows * ceil(rank / 16) "
+                                        "must be at most %d (rows=%lld R=%d)",
+                    EP_ADAPTER_MAX_GATHERED, (long long)rows, rank);
     if (rows > 0 && (!x_dev || !a_dev || !b_dev || !y_dev || !aligned16(x_dev) || !aligned16(a_dev) || !aligned16(b_dev) ||
                      !aligned16(y_dev) || !aligned16(w_dev) || !aligned16(bias_dev) || !aligned16(residual_dev) ||
                      !aligned16(pre_dev) || !aligned16(low_dev) || !aligned4(order) || !aligned4(offsets) || !aligned4(scale)))

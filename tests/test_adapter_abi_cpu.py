@@ -46,7 +46,8 @@ def product(lib, x=D, rows=4, order=None, off=D, A=2, R=16, a=D, b=D, scale=None
 @pytest.mark.parametrize("bad", SIZES + [
     dict(off=None), dict(x=None), dict(a=None), dict(b=None), dict(y=None), dict(x=ODD), dict(a=ODD), dict(b=ODD), dict(w=ODD),
     dict(y=ODD), dict(bias=ODD), dict(res=ODD), dict(pre=ODD), dict(low=ODD), dict(order=ODD4), dict(off=ODD4), dict(scale=ODD4),
-    dict(ws=None), dict(ws=ODD), dict(n=16), dict(order=D, rows=1 << 24, K=64)])
+    dict(ws=None), dict(ws=ODD), dict(n=16), dict(order=D, rows=1 << 24, K=64),
+    dict(order=D, w=None, rows=(1 << 25) + 1), dict(order=D, w=None, rows=1 << 24, R=40, K=72)])
 def test_product(lib, bad):
     refused(lib, product(lib, **bad), "ep_adapter_product")
 
