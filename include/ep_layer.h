@@ -234,7 +234,8 @@ ep_status ep_adapter_product_workspace_bytes(int64_t rows, int32_t num_adapters,
  *   pre      bf16 [rows][Nw] or NULL: z, which the gradient of an activation needs
  *   low      bf16 [rows][R] or NULL: low, in the adapters' order, as the gradient reads it
  *   y        bf16 [rows][N]
- * For its product with B low is held in 16 bits of mantissa.  An adapter's infinities and NaN reach its own rows only.
+ * For its product with B low is held in 16 bits of mantissa.  An adapter's infinities and NaN reach its own rows only,
+ * there as the formula has them.
  * Requires 0 <= rows < 2^31, 1 <= A <= EP_ADAPTER_MAX, R a multiple of 8 up to EP_ADAPTER_MAX_RANK, K and N
  * positive multiples of 8, K and Nw <= EP_PRODUCT_MAX_LENGTH; w, a and b, and x with an order and w,
  * smaller than 2^31 bytes; with an order over a larger x, rows * ceil(R / 16) <= EP_ADAPTER_MAX_GATHERED. */

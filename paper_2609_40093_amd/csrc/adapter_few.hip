@@ -222,17 +222,18 @@ __global__ __launch_bounds__(64) void adapter_few_join_kernel(FewArgs f) {
                 v[1] += t[p][1];
             }
         }
-        u32x4 b, c;
+        u32x4 b, c, kept;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float lo = v[i / 2][i % 2 * 2] * scale, hi = v[i / 2][i % 2 * 2 + 1] * scale;
-            b[i] = bf16_pair(lo, hi);
-            c[i] = bf16_pair(rest_of(lo, bf16_lo(b[i])), rest_of(hi, bf16_hi(b[i])));
+            b[i] = first_pair(lo, hi);
+            c[i] = rest_pair(lo, hi);
+            kept[i] = bf16_pair(lo, hi);
         }
         low[q] = __builtin_bit_cast(bf16x8, b);
         rest[q] = __builtin_bit_cast(bf16x8, c);
         if (f.low && blockIdx.x == 0 && j < n_rows && rank < f.R)
-            *reinterpret_cast<u32x4 *>(f.low + (i0 + j) * f.R + rank) = b;
+            *reinterpret_cast<u32x4 *>(f.low + (i0 + j) * f.R + rank) = kept;
     }
     constexpr int kSegments = STEPS == 1 ? 8 : STEPS == 2 ? 4 : STEPS == 4 ? 2 : 1;  // whose weights are on their way at once
     for (int s0 = 0; s0 < count; s0 += kSegments) {

@@ -69,11 +69,12 @@ dim3 low_grid(const LowArgs &a, int per, int cols) {
 // N neighbouring values (4 or 8) from rank on of a row: N / 2 words per array.
 template <int N>
 __device__ __forceinline__ void put_values(const LowArgs &a, int64_t row, int rank, const float *v) {
-    uint32_t high[N / 2], rest[N / 2];
+    uint32_t first[N / 2], rest[N / 2], kept[N / 2];
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) {
-        high[i] = bf16_pair(v[2 * i], v[2 * i + 1]);
-        rest[i] = bf16_pair(rest_of(v[2 * i], bf16_lo(high[i])), rest_of(v[2 * i + 1], bf16_hi(high[i])));
+        first[i] = first_pair(v[2 * i], v[2 * i + 1]);
+        rest[i] = rest_pair(v[2 * i], v[2 * i + 1]);
+        kept[i] = bf16_pair(v[2 * i], v[2 * i + 1]);
     }
     typedef uint32_t words __attribute__((ext_vector_type(N / 2)));
     const auto put = [](void *to, int64_t at, const uint32_t *w) {
@@ -84,10 +85,10 @@ __device__ __forceinline__ void put_values(const LowArgs &a, int64_t row, int ra
         *reinterpret_cast<words *>(static_cast<uint16_t *>(to) + at) = o;
     };
     const int64_t at = row * a.width + rank + (rank >> a.log << a.log);
-    put(a.split, at, high);
+    put(a.split, at, first);
     put(a.split, at + (1 << a.log), rest);
     if (a.low)
-        put(a.low, row * a.R + rank, high);
+        put(a.low, row * a.R + rank, kept);
 }
 
 // ---- few rows ------------------------------------------------------------------------

@@ -49,11 +49,23 @@ inline int32_t adapter_steps(int64_t rows, int32_t A, int32_t R, int per) {
 // Tiny (product_tile.h) with a stage less, so that two workgroups and their tables fit a compute unit.
 typedef TileShape<128, 32, 4, 1, 3> TinyRows;
 
-// The second bf16 value of v, of which the first is `first`; none of infinities and NaN.
-__device__ __forceinline__ float rest_of(float v, float first) {
-    const float d = v - first;
-    return d - d == 0.f ? d : 0.f;
+// A low-rank value v as the sum of two bf16 values: the largest one that lies before v on the way from zero, and the rest
+// of v, which the caller rounds.  Their sum is v itself where bf16 holds v, else within 2^-16 of it, or 2^-133, bf16's
+// smallest number.  Both have v's sign, and neither is zero where |v| is above 2^-133: so with an infinite
+// weight w the products' first w + rest w is v w.  (Rounding the first to nearest would be within 2^-17, but leaves a rest that
+// is zero or of the other sign, and infinite weights NaN.)
+// Zeros, infinities and NaN are both values.  (Told by their bits: v may be a product, and v - v contracted with it.)
+__device__ __forceinline__ bool splits(float v) {
+    return v != 0.f && (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u;
 }
+__device__ __forceinline__ float first_of(float v) {
+    return splits(v) ? __uint_as_float((__float_as_uint(v) - 1u) & 0xffff0000u) : v;
+}
+__device__ __forceinline__ float rest_of(float v) {
+    return splits(v) ? copysignf(fmaxf(fabsf(v - first_of(v)), 0x1p-133f), v) : v;
+}
+__device__ __forceinline__ uint32_t first_pair(float lo, float hi) { return bf16_pair(first_of(lo), first_of(hi)); }
+__device__ __forceinline__ uint32_t rest_pair(float lo, float hi) { return bf16_pair(rest_of(lo), rest_of(hi)); }
 // The layout of split: blocks of 32 ranks (up to 32 ranks) or 64, the first values of a block, then the second.
 inline int32_t split_log(int32_t R) { return R <= 32 ? 5 : 6; }
 inline int32_t split_width(int32_t R) {
