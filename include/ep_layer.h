@@ -50,6 +50,7 @@ extern "C" {
 #define EP_ADAPTER_MAX 2047     /* most adapters of a call */
 #define EP_ADAPTER_MAX_RANK 256
 #define EP_ADAPTER_MAX_GATHERED 33554432 /* see ep_adapter_product */
+#define EP_ADAPTER_MAX_ROWS 1071644672   /* 2^30 - 2^21: see ep_adapter_product */
 
 typedef enum {
     EP_ROWS_BF16 = 0,
@@ -236,8 +237,8 @@ ep_status ep_adapter_product_workspace_bytes(int64_t rows, int32_t num_adapters,
  *   y        bf16 [rows][N]
  * For its product with B low is held in 16 bits of mantissa.  An adapter's infinities and NaN reach its own rows only,
  * there as the formula has them.
- * Requires 0 <= rows < 2^31, 1 <= A <= EP_ADAPTER_MAX, R a multiple of 8 up to EP_ADAPTER_MAX_RANK, K and N
- * positive multiples of 8, K and Nw <= EP_PRODUCT_MAX_LENGTH; w, a and b, and x with an order and w,
+ * Requires 0 <= rows, rows * ceil(R / 64) <= EP_ADAPTER_MAX_ROWS, 1 <= A <= EP_ADAPTER_MAX, R a multiple of 8 up to
+ * EP_ADAPTER_MAX_RANK, K and N positive multiples of 8, K and Nw <= EP_PRODUCT_MAX_LENGTH; w, a and b, and x with an order and w,
  * smaller than 2^31 bytes; with an order over a larger x, rows * ceil(R / 16) <= EP_ADAPTER_MAX_GATHERED. */
 ep_status ep_adapter_product(const void *x_dev, int64_t rows, const int32_t *order, const int32_t *offsets,
                              int32_t num_adapters, int32_t rank, const void *a_dev, const void *b_dev, const float *scale,

@@ -22,6 +22,12 @@ ep_status check_sizes(const char *who, int64_t rows, int32_t A, int32_t R, int32
                     "%s: need 0 <= rows < 2^31, 1 <= A <= %d, the rank a multiple of 8 up to %d, K and N positive multiples "
                     "of 8, K and the weight rows at most %d (rows=%lld A=%d R=%d K=%d N=%d)",
                     who, EP_ADAPTER_MAX, EP_ADAPTER_MAX_RANK, EP_PRODUCT_MAX_LENGTH, (long long)rows, A, R, K, N);
+    // A launch has fewer than 2^32 threads.  The low-rank pass takes the most: 4 per row and 64 ranks (128 for 32 rows, 512 for
+    // 128), and the 2^21 rows less than 2^30 leave room for each adapter's last tile.  The products take 2 to 4 per row and
+    // column of tiles; with more than two columns so many rows would be results of 2^39 bytes.
+    if (rows * ((R + 63) / 64) > EP_ADAPTER_MAX_ROWS)
+        return fail(EP_ERR_INVALID_ARG, "%s: rows * ceil(rank / 64) must be at most %d (rows=%lld R=%d)", who,
+                    EP_ADAPTER_MAX_ROWS, (long long)rows, R);
     if (Nw * K * 2 > INT32_MAX || (int64_t)A * R * K * 2 > INT32_MAX || A * R * Nw * 2 > INT32_MAX)
         return fail(EP_ERR_INVALID_ARG, "%s: w, a or b takes 2^31 bytes or more", who);
     return EP_OK;
