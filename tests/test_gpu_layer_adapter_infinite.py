@@ -42,8 +42,9 @@ def forward(s):
     return low, z if s["w"] is None else z + x @ s["w"].double().t()
 
 
-# few results, with and without W; one pass over the contraction; the contraction in parts
-SIZES = [(70, 264, 136, True), (300, 136, 264, False), (5000, 136, 1032, True), (5000, 72, 1032, False), (4500, 5632, 1024, True)]
+# few results, with and without W; one pass over the contraction; the contraction in two parts, gated too, and in eight
+SIZES = [(70, 264, 136, True), (300, 136, 264, False), (5000, 136, 1032, True), (5000, 72, 1032, False), (4500, 5632, 1024, True),
+         (141, 1736, 8432, True), (5883, 5576, 144, True)]
 
 
 @pytest.mark.parametrize("rows,K,N,base", SIZES)
