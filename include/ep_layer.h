@@ -258,7 +258,8 @@ ep_status ep_adapter_product_grad_workspace_bytes(int64_t rows, int32_t num_adap
 /* Gradient of ep_adapter_product with w held fast:
  *   dz = d_y * act'(pre);  v[i] = scale[a] * dz[r] B_a
  *   dx[r] = dz[r] W + v[i] A_a;  da_a = sum v[i]^T x[r];  db_a = sum dz[r]^T low[i]
- * (the residual's gradient is d_y itself; w's, where it is trained too, ep_expert_product_grad's of one expert)
+ * (the residual's gradient is d_y itself; those of a bias and of a w that are trained too come from
+ * ep_expert_product_grad of one expert, offsets NULL, with the same pre and d_y: dbias, for which x and w may be NULL, and dw)
  *   x, order, offsets, a, b, scale, w  as in the forward (w NULL: dx of the adapters alone)
  *   low     bf16 [rows][R] as the forward wrote it (for db)
  *   pre     bf16 [rows][Nw] as the forward wrote it; NULL with EP_ACT_NONE

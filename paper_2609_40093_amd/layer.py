@@ -459,7 +459,9 @@ def adapter_product_grad(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, low:
                          dx: Union[bool, torch.Tensor] = True, da: Union[bool, torch.Tensor] = True,
                          db: Union[bool, torch.Tensor] = True, stream=None) -> AdapterGrad:
     """ep_adapter_product_grad, with w held fast: dx bf16 [rows, K], da like a, db like b.  low, pre:
-    what the forward kept (pre is needed with an activation).  Without w, dx is the adapters' part."""
+    what the forward kept (pre is needed with an activation).  Without w, dx is the adapters' part.  A trained
+    bias's gradient: expert_product_grad(x, w[None], d_y, pre=pre, act=act, dx=False, dw=False, with_bias=True).dbias[0]
+    (and w's: its dw)."""
     n, A, R, K, wide, N = _adapters(x, a, b, rows, w, scale, act)
     _optional(_given(low, "low"), "low", _BF16, (n, R))
     _optional(_given(d_y, "d_y"), "d_y", _BF16, (n, N))
