@@ -363,12 +363,22 @@ hipError_t launch_join(const FewArgs &f, hipStream_t stream) {
 
 }  // namespace
 
-// Measured, us, this way and by adapter_product.hip: 337 rows of 50 adapters, gated, 1024 x 2640 24 / 30, 998 rows
-// 4568 x 1056 36 / 43, 1172 rows 1536 x 2952 38 / 36, 3429 rows 3496 x 376 41 / 42, 3696 rows 6328 x 496 78 / 68, 2965
-// rows 1664 x 1576 52 / 41; without W 2491 rows 3320 x 800 16 / 20, 5600 rows 3616 x 696 33 / 32, 9340 rows 4096 x 512
-// 49 / 32.  (A row costs about as much as 256 results do: its low-rank values in parts.)
-bool adapter_few(int64_t rows, int32_t N, bool base, int32_t act) {
-    return rows * ((act == EP_ACT_SWIGLU ? 2 : 1) * (int64_t)N + 256) <= (base ? 2300000 : 4000000);
+// Few results, and few low-rank values: this way reads the rows once per 16 ranks, and the parts of their low-rank values once per
+// 32 columns, half of that from the L2, at 5.5 TB/s; the pass of adapter_low.hip that it saves takes 3 us and 1.6 ns for each value of
+// the contraction.  Measured, us, this way and by adapter_product.hip, with 8 adapters unless said:
+//   16 ranks   449 rows 7168 x 1024 27 / 38, 1707 rows 53 / 58; 502 rows 7168 x 4096 51 / 59; 6828 rows 7168 x 64 49 / 43;
+//              without W 873 rows 7168 x 4096 21 / 27, 2968 rows 7168 x 1024 25 / 27, 11875 rows 1024 x 64 14 / 16
+//   64 ranks   449 rows 7168 x 1024 34 / 40, 1707 rows 74 / 69; without W 781 rows 7168 x 1024 24 / 25, 1875 rows 42 / 36,
+//              7500 rows 7168 x 64 98 / 36; 700 adapters 300 rows 7168 x 2048 71 / 87
+//   256 ranks  132 rows 7168 x 4096 54 / 55, 1796 rows 7168 x 64 124 / 49, 1707 rows 7168 x 1024 172 / 75;
+//              without W 229 rows 7168 x 4096 43 / 47, 11875 rows 16384 x 64 1269 / 214
+// Past the first limit the tiles of x W^T are the faster: 2965 rows 1664 x 1576 52 / 41, without W 9340 rows 4096 x 512 49 / 32.
+bool adapter_few(int64_t rows, int32_t R, int32_t K, int32_t N, bool base, int32_t act) {
+    const int64_t Nw = (act == EP_ACT_SWIGLU ? 2 : 1) * (int64_t)N;
+    if (rows * (Nw + 256) > (base ? 2300000 : 4000000))
+        return false;
+    const int64_t rank_tiles = (R + kRanks - 1) / kRanks;
+    return rows * (K * 2 * rank_tiles + (int64_t)low_parts(K) * R * 4 * Nw / 64) <= 16000000 + 9000 * (int64_t)K;
 }
 
 size_t adapter_few_bytes(int64_t rows, int32_t R, int32_t K, int32_t N, bool base, int32_t act) {

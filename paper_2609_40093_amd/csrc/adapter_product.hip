@@ -255,7 +255,7 @@ size_t split_bytes(int64_t rows, int32_t R) { return ((size_t)rows * split_width
 size_t adapter_product_workspace_bytes(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t N, bool base, int32_t act) {
     if (rows == 0)
         return 0;
-    if (adapter_few(rows, N, base, act))
+    if (adapter_few(rows, R, K, N, base, act))
         return adapter_few_bytes(rows, R, K, N, base, act);
     const bool gated = act == EP_ACT_SWIGLU;
     const Plan p = adapter_plan(rows, A, R, K, N, base, gated);
@@ -266,7 +266,7 @@ size_t adapter_product_workspace_bytes(int64_t rows, int32_t A, int32_t R, int32
 hipError_t launch_adapter_product(const AdapterArgs &a, hipStream_t stream) {
     if (a.rows == 0)
         return hipSuccess;
-    if (adapter_few(a.rows, a.N, a.w != nullptr, a.act))
+    if (adapter_few(a.rows, a.R, a.K, a.N, a.w != nullptr, a.act))
         return launch_adapter_few(a, stream);
     const bool gated = a.act == EP_ACT_SWIGLU;
     ProductArgs p{};

@@ -259,7 +259,7 @@ struct AdapterArgs {
 size_t adapter_product_workspace_bytes(int64_t rows, int32_t A, int32_t R, int32_t K, int32_t N, bool base, int32_t act);
 hipError_t launch_adapter_product(const AdapterArgs &a, hipStream_t stream);
 // The same for few results (adapter_few.hip).
-bool adapter_few(int64_t rows, int32_t N, bool base, int32_t act);
+bool adapter_few(int64_t rows, int32_t R, int32_t K, int32_t N, bool base, int32_t act);
 size_t adapter_few_bytes(int64_t rows, int32_t R, int32_t K, int32_t N, bool base, int32_t act);
 hipError_t launch_adapter_few(const AdapterArgs &a, hipStream_t stream);
 

@@ -54,6 +54,17 @@ def test_the_limit(act, base):
     check(ar.make(ar.random_ids(rows + 1, 5, 1), 5, 16, 136, N, 1, act, base))
 
 
+@pytest.mark.parametrize("base", [True, False])
+@pytest.mark.parametrize("R,K,N,rows", [(256, 1448, 72, 611), (64, 7168, 64, 1373), (128, 264, 1032, 1472)])
+def test_the_limit_of_low_rank_values(R, K, N, rows, base):
+    """The same where the low-rank values' bytes set it."""
+    say(f"adapter_product round rows={rows} R={R} K={K} N={N} base={base}")
+    few = kernels(lambda: ar.check(ar.make(ar.random_ids(rows, 5, 1), 5, R, K, N, 1, base=base)))[1]
+    assert few and few <= FEW, few
+    ran = kernels(lambda: ar.check(ar.make(ar.random_ids(rows + 1, 5, 1), 5, R, K, N, 1, base=base)))[1]
+    assert {"adapter_low", "adapter_product"} <= ran and not ran & FEW, ran
+
+
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("base", [True, False])
 def test_epilogues(act, base):
