@@ -239,3 +239,44 @@ def test_gradient_shapes(rows, A, R, K, N, base, dx, da, db):
                 assert ran == want, ran
             else:
                 assert ran - {"adapter_dx_join"} == want, ran
+
+
+@pytest.mark.parametrize("rows,first,none,base", [(90, 17, 5, True), (300, 40, 0, False), (5000, 700, 31, True), (9000, 300, 0, False)])
+@pytest.mark.parametrize("ordered", [False, True])
+def test_rows_before_the_first_adapter(rows, first, none, base, ordered):
+    """offsets[0] above 0: the places before it have no adapter, as those behind offsets[A].  Whole numbers: every sum is exact."""
+    say(f"adapter_product: {first} rows before the first adapter of {rows}, W={base} ordered={ordered}")
+    A, R, K, N = 4, 24, 136, 264
+    g = ref.gen(rows)
+
+    def whole(shape, most):
+        return torch.randint(-most, most + 1, shape, device="cuda", generator=g).bfloat16()
+
+    x, d = whole((rows, K), 50), whole((rows, N), 50)
+    a, b, w = whole((A, R, K), 1), whole((A, N, R), 1), whole((N, K), 1) if base else None
+    inner = torch.randint(0, A, (rows - first - none,), device="cuda", generator=g).sort()[0]
+    of = torch.cat([inner.new_full((first,), A), inner, inner.new_full((none,), A)])
+    offsets = torch.searchsorted(inner, torch.arange(A + 1, device="cuda")) + first
+    order = torch.randperm(rows, device="cuda", generator=g) if ordered else torch.arange(rows, device="cuda")
+    by = ep.AdapterRows(order.int() if ordered else None, offsets.int())
+    out, pre = torch.full((rows, N), 7.0, dtype=torch.bfloat16, device="cuda"), True
+    got = ep.adapter_product(x, a, b, by, w=w, out=out, keep_pre=pre, keep_low=True)
+    low = ar.by_adapter(x.double()[order], of, a.double().transpose(1, 2))[0]
+    z = torch.zeros((rows, N), dtype=torch.float64, device="cuda")
+    z[order] = ar.by_adapter(low, of, b.double().transpose(1, 2))[0]
+    if base:
+        z += x.double() @ w.double().t()
+    assert torch.equal(got.low, low.bfloat16()) and torch.equal(got.out, z.bfloat16()) and torch.equal(got.pre, z.bfloat16())
+    grad = ep.adapter_product_grad(x, a, b, got.low, d, by, w=w)
+    v = ar.by_adapter(d.double()[order], of, b.double())[0]
+    dx = torch.zeros((rows, K), dtype=torch.float64, device="cuda")
+    dx[order] = ar.by_adapter(v, of, a.double())[0]
+    if base:
+        dx += d.double() @ w.double()
+    assert torch.equal(grad.dx, dx.bfloat16())
+    for e in range(A):
+        at = of == e
+        for have, long, short, what in ((grad.da[e].t(), x, v, "da"), (grad.db[e], d, got.low.double(), "db")):
+            want = long.double()[order][at].t() @ short[at]
+            off = long.double()[order][at].abs().t() @ short[at].abs() * (2 * rows + 8) * ref.U23  # past 2^24 sums are rounded
+            ref.within(have, want, off + ref.BF16 * (want.abs() + off), f"{what} {e}")
