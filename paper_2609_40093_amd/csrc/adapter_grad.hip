@@ -440,9 +440,10 @@ typedef TileShape<128, 128, 4, 1, 2> Da64;
 typedef TileShape<64, 128, 2, 2, 2> Db64;
 
 // Tiles along the long side (x for da, dz for db) and of the ranks, and the parts of the rows, until each of the two
-// products has a tile per compute unit (8192 rows, 4096 x 4096: 42 us; two tiles each 52, and more for their parts' sums).
-// Pieces of so many rows instead of parts of each adapter's serve a long adapter among short ones better (6855 rows of 9
-// adapters, most of one: 25 us instead of 35), but need the kernel that joins them in every call, which costs all others 4.
+// products has a tile per compute unit (8192 rows, 4096 x 4096, 64 ranks, from the memory-side cache: 24 us and 4 for the
+// parts' sums; two tiles each 29 and 6).  A long adapter among short ones has no more parts than they have (6855 rows of 9
+// adapters, 2888 x 1448, 16 ranks: 14 us, 39 with four fifths of the rows one adapter's): pieces of so many rows instead would
+// need the kernel that joins them in every call, 4 us.
 struct WeightPlan {
     int32_t tiles, groups, parts;
     WeightPlan(int64_t rows, int32_t A, int32_t R, int32_t L, bool da) {
