@@ -372,7 +372,8 @@ hipError_t launch_join(const FewArgs &f, hipStream_t stream) {
 //              7500 rows 7168 x 64 98 / 36; 700 adapters 300 rows 7168 x 2048 71 / 87
 //   256 ranks  132 rows 7168 x 4096 54 / 55, 1796 rows 7168 x 64 124 / 49, 1707 rows 7168 x 1024 172 / 75;
 //              without W 229 rows 7168 x 4096 43 / 47, 11875 rows 16384 x 64 1269 / 214
-// Past the first limit the tiles of x W^T are the faster: 2965 rows 1664 x 1576 52 / 41, without W 9340 rows 4096 x 512 49 / 32.
+// Past the first limit the other way is the faster: 2965 rows 1664 x 1576, 16 ranks 47 / 38, 2400 rows 4096 x 1576 69 / 51;
+// without W 9340 rows 4096 x 512, 16 ranks 35 / 34, 32 ranks 52 / 39.
 bool adapter_few(int64_t rows, int32_t R, int32_t K, int32_t N, bool base, int32_t act) {
     const int64_t Nw = (act == EP_ACT_SWIGLU ? 2 : 1) * (int64_t)N;
     if (rows * (Nw + 256) > (base ? 2300000 : 4000000))
